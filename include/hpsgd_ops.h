@@ -1,0 +1,116 @@
+/*
+ * libhpsgd, operators: what a program that trains or runs a language model needs beside the
+ * replica update and the merge of hpsgd.h: the optimizer step over many tensors.
+ * (The HPSGD paper has no counterpart for any of them.)
+ *
+ * Conventions (in addition to those of hpsgd.h)
+ *   - The operators need no hpsgd_init and keep no state: every buffer is the caller's, and work
+ *     is enqueued on the stream that is given (a cudaStream_t; NULL = the default stream) and on
+ *     no other.  They allocate nothing and wait for nothing, so they can be captured in a graph.
+ *   - Structs and arrays of structs are HOST memory, read during the call; the pointers in them
+ *     are DEVICE pointers.
+ *   - Arguments are checked before anything is enqueued.  A size of zero is legal and does nothing
+ *     unless the call says otherwise.
+ *   - Every reduction has a fixed order: the same inputs give the same bits.
+ *   - Sums, moments and statistics are held in binary32 or wider whatever the stored types.
+ *
+ * The 8-bit block format.  128 consecutive values share one power of two.  A value is an E4M3 code
+ * (1 sign, 4 exponent and 3 mantissa bits, largest magnitude 448, no infinity) times 2^e, where e is
+ * the smallest integer >= -127 with 448 * 2^e >= the largest finite magnitude of the block; the scale
+ * is stored as the byte e + 127 (E8M0).  The codes have an exponent of their own, so the relative
+ * precision does not depend on where in its octave the scale lies: a power of two loses nothing
+ * against an arbitrary factor, multiplying by it is exact, and values can be moved to blocks along the
+ * other axis without being rounded again (except where they fall below the smallest code).  Values
+ * that are not finite become the NaN code 0x7F and do not count for the scale.
+ */
+#ifndef HPSGD_OPS_H_
+#define HPSGD_OPS_H_
+
+#include "hpsgd.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ------------------------------------------------------------------------------------
+ * AdamW over many tensors.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * One tensor of a step.  Element pointers need the alignment of their element; where the addresses
+ * of param, grad and copy are multiples of 32 bytes (16 for bf16) and those of the moments of 32 bytes
+ * (8 for 8-bit codes) the wide accesses are used, for that tensor alone.
+ *   param         n values of the call's param_dtype, updated in place
+ *   grad          n values of the call's grad_dtype
+ *   m, v          state_bits 32: n floats each.  state_bits 8: n codes each; v holds the SQUARE ROOT of
+ *                 the second moment.  All zero (codes and scales too) is the state before the first step.
+ *   m_scale, v_scale   state_bits 8 only: ceil(n / 128) scale bytes each, block b covering the elements
+ *                 [128 b, 128 b + 128)
+ *   copy          n bf16 values that receive the new parameters rounded to nearest even (the copy a
+ *                 bf16 forward pass reads), or NULL.  Only with param_dtype HPSGD_F32.
+ *   weight_decay  decoupled decay of this tensor, >= 0
+ *   rng_offset    position of the tensor's first element in the step's sequence of random bits: give
+ *                 tensors of one step disjoint ranges [rng_offset, rng_offset + n)
+ */
+typedef struct hpsgd_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+    void* copy;
+    int64_t n;
+    uint64_t rng_offset;
+    double weight_decay;
+} hpsgd_adamw_tensor;
+
+/*
+ * One AdamW step of every tensor, in as few launches as the table takes (one up to 360 tensors):
+ *     g = grad * c                                    c = *grad_scale, 1 if NULL
+ *     m = beta1 m + (1 - beta1) g
+ *     v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in binary32; the factors that do not depend on the element are computed in binary64 and rounded once.
+ *
+ * If grad_scale points to a value that is not finite (hpsgd_grad_norm writes one when the norm is not)
+ * the call changes nothing: a step whose gradients overflowed is skipped without the host having to look.
+ *
+ * state_bits 8: the moments are read from and written to the 8-bit block format, m as it is and v as
+ * r = sqrt(v), which halves the range that the codes have to span.  The parameter is stepped with the new
+ * moments before they are rounded.  Rounding is stochastic, with 16 random bits for each: to nearest, an
+ * average with beta2 = 0.999 that moves by 0.1 % a step would never leave a code whose neighbours are 6 to
+ * 12 % away.  m goes to one of its two neighbours so that the expected value is m, r so that the expected
+ * SQUARE is v; a positive v is never rounded to 0, which would leave eps alone to divide by.
+ * param_dtype HPSGD_BF16: the new parameter is rounded stochastically to bf16 too, for the same reason.
+ *
+ * The 32 random bits x of element i (position q = rng_offset + i, all in uint32 arithmetic):
+ *     key = mix(mix(mix(seed + M3) ^ step) + M4)      mix and M1..M4 as for hpsgd_gen_grads (64 bits)
+ *     x = ((uint32)q ^ (uint32)key) * N1;  x ^= x >> 15;  x = (x + (uint32)(key >> 32) + (uint32)(q >> 32) * N3) * N2
+ *     x ^= x >> 14;  x *= N3;  x ^= x >> 16           N1..N3 = frac(sqrt 2, 3, 5) * 2^32 with the low bit set
+ * the upper 16 are m's, the lower 16 r's, and the upper 16 of x * N2 a bf16 parameter's.
+ *
+ * beta1, beta2 in [0, 1), eps > 0, lr >= 0, step >= 1 (the first step is 1).
+ */
+int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param_dtype, int grad_dtype, int state_bits,
+                     double lr, double beta1, double beta2, double eps, int64_t step, uint64_t seed,
+                     const float* grad_scale, void* stream);
+
+/*
+ * Global norm of the gradients of a table (only grad and n are read) and what clips it:
+ *     out[0] = sqrt(sum over all tensors of grad^2)
+ *     out[1] = max_norm / out[0] if out[0] > max_norm, else 1; NaN if the norm is not finite
+ * Squares are added in binary32 eight at a time, those sums in binary64.  max_norm > 0; infinity is legal
+ * (the norm alone).  `workspace`: HPSGD_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned, filled with
+ * zeros before its first use; every call leaves it ready for the next.  Calls that share a workspace have to
+ * be ordered on one stream.  Without tensors out is {0, 1}.
+ */
+#define HPSGD_GRAD_NORM_WORKSPACE 65536
+int hpsgd_grad_norm(const hpsgd_adamw_tensor* tensors, int n_tensors, int grad_dtype, double max_norm,
+                    void* workspace, float* out, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* HPSGD_OPS_H_ */

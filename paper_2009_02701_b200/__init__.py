@@ -5,3 +5,5 @@ the first call does, and that call fails loudly if the library has not been buil
 """
 from . import binding   # noqa: F401
 from .binding import *  # noqa: F401,F403
+from . import ops       # noqa: F401
+from .ops import *      # noqa: F401,F403

@@ -105,7 +105,8 @@ def load():
             raise ImportError("%s is missing: build it with paper_2009_02701_b200.build.build(); "
                               "there is no non-CUDA implementation" % LIB_PATH)
         lib = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        from .ops import SIGNATURES as OPS_SIGNATURES
+        for name, (res, args) in {**SIGNATURES, **OPS_SIGNATURES}.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
         _lib = lib

@@ -3,6 +3,21 @@
 // kernel launches in hpsgd_schedule.cuh, the device code in hpsgd_kernels.cuh.
 #include "hpsgd_schedule.cuh"
 
+namespace hpsgd {
+
+int report(int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+void count_launches(int n) { g.launches += n; }
+
+}  // namespace hpsgd
+
 // =============================================================================== C ABI
 extern "C" {
 

@@ -1,0 +1,156 @@
+// What the operators share: the 8-bit block format, wide loads and stores, argument and device checks.
+#pragma once
+
+#include "../../include/hpsgd_ops.h"
+
+#include <cmath>
+#include <cuda_bf16.h>
+
+#include "hpsgd_internal.h"
+
+namespace hpsgd {
+namespace ops {
+
+#define OPS_CUDA(expr)                                                                             \
+    do {                                                                                           \
+        cudaError_t e_ = (expr);                                                                   \
+        if (e_ != cudaSuccess) {                                                                   \
+            cudaGetLastError();                                                                    \
+            return report(HPSGD_E_CUDA, "%s failed: %s", #expr, cudaGetErrorString(e_));           \
+        }                                                                                          \
+    } while (0)
+
+#define OPS_TRY(expr)            \
+    do {                         \
+        int rc_ = (expr);        \
+        if (rc_) return rc_;     \
+    } while (0)
+
+// SM count of the current device, after checking that the kernels can run on it.
+HPSGD_HIDDEN int device_sms(int* sms);
+
+// What a kernel launch just did, as a status.
+inline int launched(const char* what)
+{
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return report(HPSGD_E_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
+    count_launches(1);
+    return HPSGD_OK;
+}
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// ---------------------------------------------------------------------------- the 8-bit block format
+constexpr int kBlock = 128;
+
+// Exponent byte e + 127 of a block whose largest finite magnitude is `top`: 448 = 1.75 * 2^8, so with
+// top = 1.f * 2^k the exponent is k - 8, or k - 7 where 1.f > 1.75.
+__device__ __forceinline__ int scale_byte(float top)
+{
+    const uint32_t b = __float_as_uint(top);
+    const int k = (int)(b >> 23);                               // k + 127; 0 for subnormal values, whose scale is 2^-127 anyway
+    return max(0, k - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0));
+}
+
+// 2^(byte - 127) and 2^(127 - byte), exactly; bytes up to 247 (those of finite blocks) keep both normal
+// but for 2^-127 itself.
+__device__ __forceinline__ float scale_value(int byte)
+{
+    return __uint_as_float(byte > 0 ? (uint32_t)byte << 23 : 0x400000u);
+}
+__device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+// The bits of an E4M3 code without its sign are the top of a binary32 that is 2^120 times smaller (exponent
+// biases 7 and 127), subnormal codes included: a shift and one exact multiplication convert either way.
+__device__ __forceinline__ float e4m3_magnitude(uint32_t code) { return __fmul_rn(__uint_as_float(code << 20), 0x1p120f); }
+__device__ __forceinline__ float e4m3_value(uint32_t code)
+{
+    const float x = __uint_as_float(__float_as_uint(e4m3_magnitude(code & 0x7Fu)) | (code & 0x80u) << 24);
+    return (code & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : x;
+}
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
+__device__ __forceinline__ float finite_magnitude(float x) { return finite(x) ? fabsf(x) : 0.f; }
+
+// ---------------------------------------------------------------------------- eight consecutive values
+struct f8 {
+    float v[8];
+};
+
+__device__ __forceinline__ void widen_pair(uint32_t u, float& lo, float& hi)
+{
+    lo = __uint_as_float(u << 16);
+    hi = __uint_as_float(u & 0xFFFF0000u);
+}
+
+__device__ __forceinline__ f8 load8(const float* p)
+{
+    f8 x;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(x.v[0]), "=f"(x.v[1]), "=f"(x.v[2]), "=f"(x.v[3]), "=f"(x.v[4]), "=f"(x.v[5]), "=f"(x.v[6]), "=f"(x.v[7])
+                 : "l"(p));
+    return x;
+}
+
+__device__ __forceinline__ void store8(float* p, const f8& x)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]),
+                 "f"(x.v[3]), "f"(x.v[4]), "f"(x.v[5]), "f"(x.v[6]), "f"(x.v[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ f8 load8(const __nv_bfloat16* p)
+{
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    f8 x;
+    widen_pair(u.x, x.v[0], x.v[1]);
+    widen_pair(u.y, x.v[2], x.v[3]);
+    widen_pair(u.z, x.v[4], x.v[5]);
+    widen_pair(u.w, x.v[6], x.v[7]);
+    return x;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t u;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+    return u;
+}
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const f8& x)
+{
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x.v[0], x.v[1]), pack_bf16(x.v[2], x.v[3]),
+                                              pack_bf16(x.v[4], x.v[5]), pack_bf16(x.v[6], x.v[7]));
+}
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// Eight values from p, or the first `left` of them (zeros behind) where p is not aligned for the wide access or
+// the tensor ends inside the eight.
+template <typename T>
+__device__ __forceinline__ f8 load_some(const T* p, bool wide, int left)
+{
+    if (wide) return load8(p);
+    f8 x;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x.v[q] = q < left ? load1(p + q) : 0.f;
+    return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int left)
+{
+    if (wide) {
+        store8(p, x);
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < left) store1(p + q, x.v[q]);
+}
+
+}  // namespace ops
+}  // namespace hpsgd

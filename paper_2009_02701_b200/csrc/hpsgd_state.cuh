@@ -4,6 +4,7 @@
 #pragma once
 
 #include "../../include/hpsgd.h"
+#include "hpsgd_internal.h"
 
 #include <algorithm>
 #include <cstdarg>

@@ -1,0 +1,65 @@
+"""ctypes binding of the operators of ``libhpsgd.so`` (``include/hpsgd_ops.h``): same names as the C ABI, argument
+marshalling only.  What a call needs every time (a table of tensors, an argument block) is built once by a ``make_*``
+function and passed again and again; the buffers it names have to stay alive, which the returned object sees to.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import binding as _b
+from .binding import _ci, _f64, _i64, _ptr, _stream, _u64, _vp
+
+__all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm"]
+
+HPSGD_GRAD_NORM_WORKSPACE = 65536
+
+
+class hpsgd_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", _vp), ("grad", _vp), ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp), ("copy", _vp),
+                ("n", _i64), ("rng_offset", _u64), ("weight_decay", _f64)]
+
+
+SIGNATURES = {
+    "hpsgd_adamw_step": (_ci, [_vp, _ci, _ci, _ci, _ci, _f64, _f64, _f64, _f64, _i64, _u64, _vp, _vp]),
+    "hpsgd_grad_norm": (_ci, [_vp, _ci, _ci, _f64, _vp, _vp, _vp]),
+}
+
+
+# ---- AdamW over many tensors -----------------------------------------------------------
+class AdamWTable:
+    """The tensors of a step (see make_adamw_table)."""
+
+    def __init__(self, rows, param_dtype, grad_dtype, state_bits):
+        self.array = (hpsgd_adamw_tensor * len(rows))()
+        self.address = ctypes.addressof(self.array)
+        self.count, self.param_dtype, self.grad_dtype, self.state_bits = len(rows), int(param_dtype), int(grad_dtype), int(state_bits)
+        self.keep = rows
+
+
+def make_adamw_table(rows, param_dtype, grad_dtype, state_bits):
+    """A table for hpsgd_adamw_step / hpsgd_grad_norm from dicts with the fields of ``hpsgd_adamw_tensor`` (tensors or addresses;
+    what is left out is NULL or 0).  ``rng_offset`` left out: the tensors follow one another in the order given."""
+    table = AdamWTable(list(rows), param_dtype, grad_dtype, state_bits)
+    names = {f[0] for f in hpsgd_adamw_tensor._fields_}
+    at = 0
+    for item, row in zip(table.array, table.keep):
+        unknown = set(row) - names
+        if unknown:
+            raise TypeError("not a field of hpsgd_adamw_tensor: %s" % sorted(unknown))
+        for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy"):
+            setattr(item, name, _ptr(row.get(name)))
+        item.n = int(row["n"])
+        item.weight_decay = float(row.get("weight_decay", 0.0))
+        item.rng_offset = int(row.get("rng_offset", at))
+        at = item.rng_offset + item.n
+    return table
+
+
+def hpsgd_adamw_step(table, lr, beta1, beta2, eps, step, seed=0, grad_scale=None, stream=None):
+    return _b._check(_b.load().hpsgd_adamw_step(table.address, table.count, table.param_dtype, table.grad_dtype, table.state_bits,
+                                                lr, beta1, beta2, eps, step, seed, _ptr(grad_scale), _stream(stream)))
+
+
+def hpsgd_grad_norm(table, max_norm, workspace, out, stream=None):
+    return _b._check(_b.load().hpsgd_grad_norm(table.address, table.count, table.grad_dtype, max_norm, _ptr(workspace), _ptr(out),
+                                               _stream(stream)))

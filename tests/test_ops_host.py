@@ -1,0 +1,108 @@
+"""The operators' refusals: every bad argument is an error code before any GPU work, so all of it runs without a device.
+Also the header of the operators: plain C, and what it declares is what is bound and exported."""
+import ctypes
+import math
+import os
+import re
+import subprocess
+
+import pytest
+
+import paper_2009_02701_b200 as hp
+from paper_2009_02701_b200 import binding, build, ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "hpsgd_ops.h")
+A = 1 << 20            # an address that is aligned for everything; nothing is ever read from it
+
+
+def refused(code, call, *args, **kw):
+    with pytest.raises(hp.HpsgdError) as err:
+        call(*args, **kw)
+    assert err.value.code == code, str(err.value)
+
+
+def test_header_declares_what_is_bound_and_exported():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(hpsgd_[a-z_0-9]+)\s*\(", text)))
+    lib = ctypes.CDLL(build.build())
+    assert names == sorted(ops.SIGNATURES) and all(hasattr(lib, n) for n in names)
+    assert not set(names) & set(binding.SIGNATURES)
+
+
+def test_header_is_plain_c(tmp_path):
+    src = tmp_path / "use.c"
+    src.write_text('#include "hpsgd_ops.h"\nint probe(void) { hpsgd_adamw_tensor t = {0}; return (int)sizeof t + HPSGD_GRAD_NORM_WORKSPACE + (int)t.n; }\n')
+    inc = os.path.join(ROOT, "include")
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-fsyntax-only", "-I", inc, str(src)], check=True)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-fsyntax-only", "-x", "c++", "-I", inc, str(src)], check=True)
+
+
+def sizeof_in_c(tmp_path, expr):
+    src = tmp_path / "size.c"
+    src.write_text('#include <stdio.h>\n#include "hpsgd_ops.h"\nint main(void) { printf("%%d", (int)sizeof(%s)); return 0; }\n' % expr)
+    exe = tmp_path / "size"
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(exe), str(src)], check=True)
+    return int(subprocess.run([str(exe)], capture_output=True, check=True).stdout)
+
+
+def test_structs_have_the_header_s_size(tmp_path):
+    for name in [n for n in dir(ops) if isinstance(getattr(ops, n), type) and issubclass(getattr(ops, n), ctypes.Structure)]:
+        assert sizeof_in_c(tmp_path, name) == ctypes.sizeof(getattr(ops, name)), name
+
+
+# ---------------------------------------------------------------------------------------------- AdamW
+ROW = dict(param=A, grad=A, m=A, v=A, n=100)
+HY = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+
+
+def table(bits=32, pd=hp.HPSGD_F32, gd=hp.HPSGD_F32, **change):
+    return hp.make_adamw_table([{**ROW, **({"m_scale": A, "v_scale": A} if bits == 8 else {}), **change}], pd, gd, bits)
+
+
+@pytest.mark.parametrize("change", [dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
+                                    dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1e-8), dict(eps=1e-60), dict(eps=math.nan), dict(step=0),
+                                    dict(step=-5), dict(grad_scale=A + 2)], ids=str)
+def test_adamw_refuses_hyperparameters(change):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(), **{**HY, **change})
+
+
+@pytest.mark.parametrize("change", [dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(n=-1), dict(weight_decay=-0.1),
+                                    dict(weight_decay=math.nan), dict(param=A + 2), dict(grad=A + 1), dict(m=A + 2), dict(v=A + 1), dict(copy=A + 1)], ids=str)
+def test_adamw_refuses_tensors(change):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(**change), **HY)
+
+
+def test_adamw_refuses_forms():
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(bits=16), **HY)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(pd=7), **HY)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(gd=7), **HY)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(bits=8, m_scale=None), **HY)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(bits=8, v_scale=None), **HY)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_adamw_step, table(pd=hp.HPSGD_BF16, copy=A), **HY)
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_adamw_step, table(n=(1 << 40) + 1), **HY)
+    with pytest.raises(TypeError):
+        hp.make_adamw_table([{**ROW, "weights": A}], 0, 0, 32)
+    lib = hp.load()
+    assert lib.hpsgd_adamw_step(None, 1, 0, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 1, 0, None, None) == hp.HPSGD_E_BADARG
+    assert lib.hpsgd_adamw_step(None, -1, 0, 0, 32, 1e-3, 0.9, 0.999, 1e-8, 1, 0, None, None) == hp.HPSGD_E_BADARG
+    assert "n_tensors" in hp.last_error()
+
+
+@pytest.mark.parametrize("args", [(0.0, A, A), (-1.0, A, A), (math.nan, A, A), (1.0, None, A), (1.0, A + 8, A), (1.0, A, None), (1.0, A, A + 2)], ids=str)
+def test_norm_refuses(args):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_grad_norm, table(), *args)
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_grad_norm, table(grad=None), 1.0, A, A)
+
+
+def test_no_fallback_without_a_device():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a CUDA device is present")
+    refused(hp.HPSGD_E_CUDA, hp.hpsgd_adamw_step, table(), **HY)
+    refused(hp.HPSGD_E_CUDA, hp.hpsgd_grad_norm, table(), 1.0, A, A)
+
+
+def test_tables_number_their_random_bits():
+    t = hp.make_adamw_table([dict(ROW, n=5), dict(ROW, n=7), dict(ROW, n=1, rng_offset=1 << 40), dict(ROW, n=2)], 0, 0, 32)
+    assert [x.rng_offset for x in t.array] == [0, 5, 1 << 40, (1 << 40) + 1]
