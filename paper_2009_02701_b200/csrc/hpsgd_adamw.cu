@@ -8,6 +8,7 @@
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
+#include <cuda_fp16.h>
 
 namespace hpsgd {
 namespace ops {
@@ -74,64 +75,91 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t q, uint32_t key0, uint3
     return x ^ x >> 16;
 }
 
-struct Codes8 {
-    uint32_t c[8];
-};
-
-__device__ __forceinline__ Codes8 load_codes(const uint8_t* p, bool wide, int left)
+// Eight codes, as stored.
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, bool wide, int left)
 {
-    Codes8 x;
-    if (wide) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
+    if (wide) return *reinterpret_cast<const uint2*>(p);
+    uint2 u = make_uint2(0u, 0u);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            x.c[q] = u.x >> 8 * q & 0xFFu;
-            x.c[q + 4] = u.y >> 8 * q & 0xFFu;
-        }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) x.c[q] = q < left ? p[q] : 0u;
+    for (int q = 0; q < 4; ++q) {
+        if (q < left) u.x |= (uint32_t)p[q] << 8 * q;
+        if (q + 4 < left) u.y |= (uint32_t)p[q + 4] << 8 * q;
     }
+    return u;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t* p, uint2 u, bool wide, int left)
+{
+    if (wide) {
+        *reinterpret_cast<uint2*>(p) = u;
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < left) p[q] = (uint8_t)((q < 4 ? u.x : u.y) >> 8 * (q & 3));
+}
+
+// Two codes (the low 16 bits) to two values: the conversion goes through f16, which holds every E4M3 value and its NaN.
+__device__ __forceinline__ void decode_pair(uint32_t two, float& lo, float& hi)
+{
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    lo = f.x;
+    hi = f.y;
+}
+
+__device__ __forceinline__ f8 decode8(uint2 u)
+{
+    f8 x;
+    decode_pair(u.x, x.v[0], x.v[1]);
+    decode_pair(u.x >> 16, x.v[2], x.v[3]);
+    decode_pair(u.y, x.v[4], x.v[5]);
+    decode_pair(u.y >> 16, x.v[6], x.v[7]);
     return x;
 }
 
-__device__ __forceinline__ void store_codes(uint8_t* p, const Codes8& x, bool wide, int left)
+// What multiplies a value of a block with scale 2^(byte - 127) so that the value's E4M3 code comes to stand in bits 20..26 of
+// its binary32 pattern: 2^(127 - byte - 120), in one factor as long as that is a normal number.  Blocks above 2^6 * 448, whose
+// factor is not, first have their values multiplied by the rest (`excess`).
+__device__ __forceinline__ float code_factor(int byte) { return __uint_as_float((uint32_t)(max(254 - 120 - byte, 1)) << 23); }
+__device__ __forceinline__ bool has_excess(int byte) { return byte > 133; }
+__device__ __forceinline__ float excess(int byte) { return __uint_as_float((uint32_t)(127 - (byte - 133)) << 23); }
+
+// One of the two codes around |x|, such that the expected value is |x|; `x` is already multiplied by its block's code factor.
+// 16 random bits, centred, are added below the last bit that is kept, and the carry decides.  An exact code stays.
+// The code comes back in the top byte, sign included.
+__device__ __forceinline__ uint32_t round_first(float x, uint32_t rnd)
 {
-    if (wide) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(x.c[0] | x.c[1] << 8 | x.c[2] << 16 | x.c[3] << 24,
-                                                  x.c[4] | x.c[5] << 8 | x.c[6] << 16 | x.c[7] << 24);
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < left) p[q] = (uint8_t)x.c[q];
-    }
+    const uint32_t b = __float_as_uint(fabsf(x)) + ((rnd >> 12 & 0xFFFF0u) | 8u);
+    return (b << 4 & 0x7F000000u) | (__float_as_uint(x) & 0x80000000u);
 }
 
-// Largest value over the 16 lanes that hold one 128-element block.
-__device__ __forceinline__ float block_top(float x)
+// One of the two codes a <= x < b, such that the expected square is x^2: b with probability (x^2 - a^2) / (b^2 - a^2), so where
+// x^2 > a^2 + u (b^2 - a^2).  0 only for 0.  `t` is x multiplied by its block's code factor.  The code comes back in the top byte.
+__device__ __forceinline__ uint32_t round_second(float t, uint32_t rnd)
 {
-#pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
-    return x;
+    const uint32_t ab = __float_as_uint(t) & 0xFFF00000u;
+    const float x = __fmul_rn(t, 0x1p120f);
+    const float a = __fmul_rn(__uint_as_float(ab), 0x1p120f), b = __fmul_rn(__uint_as_float(ab + 0x100000u), 0x1p120f);
+    const float u1 = __uint_as_float(0x3F800040u | (rnd << 7 & 0x7FFF80u));          // 1 + u, u = (16 bits + 0.5) / 2^16
+    const float d = __fmul_rn(__fsub_rn(b, a), __fadd_rn(b, a));
+    const bool up = __fmul_rn(__fsub_rn(x, a), __fadd_rn(x, a)) > __fmul_rn(__fsub_rn(u1, 1.f), d);
+    const uint32_t c = (up ? ab + 0x100000u : ab) << 4;
+    return max(c, t > 0.f ? 0x1000000u : 0u);
 }
 
-// One of the two codes around |x| (x already divided by its block's scale), such that the expected value is |x|: 16 random
-// bits, centred, are added below the last bit that is kept, and the carry decides.  An exact code stays.
-__device__ __forceinline__ uint32_t round_first(float x, uint32_t r16)
+// Four codes from their top bytes.
+__device__ __forceinline__ uint32_t gather_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    const uint32_t b = __float_as_uint(__fmul_rn(fabsf(x), 0x1p-120f));
-    return (b + (r16 * 16u + 8u)) >> 20 | (__float_as_uint(x) >> 31) << 7;
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
-// One of the two codes a <= x < b, such that the expected square is x^2: b with probability (x^2 - a^2) / (b^2 - a^2).
-// 0 only for 0.
-__device__ __forceinline__ uint32_t round_second(float x, uint32_t r16)
+__device__ __forceinline__ float root_approx(float x)
 {
-    const uint32_t c = __float_as_uint(__fmul_rn(x, 0x1p-120f)) >> 20;
-    const float a = e4m3_magnitude(c), b = e4m3_magnitude(c + 1);
-    const float u = __fmul_rn(__fadd_rn((float)r16, 0.5f), 0x1p-16f);
-    const bool up = __fmul_rn(u, __fmul_rn(__fsub_rn(b, a), __fadd_rn(b, a))) < __fmul_rn(__fsub_rn(x, a), __fadd_rn(x, a));
-    return max(c + (up ? 1u : 0u), x > 0.f ? 1u : 0u);
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // ---------------------------------------------------------------------------- the step
@@ -154,35 +182,39 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     f8 p = load_some(pp, wide, left);
     f8 g = load_some(static_cast<const G*>(it.g) + at, wide, left);
     f8 m, v;
-    Codes8 mc, vc;
-    int mb = 0, vb = 0;
     if constexpr (B8) {
-        mc = load_codes(static_cast<const uint8_t*>(it.m) + at, wide, left);
-        vc = load_codes(static_cast<const uint8_t*>(it.v) + at, wide, left);
+        const uint2 mc = load_codes(static_cast<const uint8_t*>(it.m) + at, wide, left);
+        const uint2 vc = load_codes(static_cast<const uint8_t*>(it.v) + at, wide, left);
+        int mb = 0, vb = 0;
         if (left > 0) {
             mb = it.ms[at / kBlock];
             vb = it.vs[at / kBlock];
         }
         const float sm = scale_value(mb), sv = scale_value(vb);
+        m = decode8(mc);
+        v = decode8(vc);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            m.v[q] = __fmul_rn(e4m3_value(mc.c[q]), sm);
-            const float r = __fmul_rn(e4m3_value(vc.c[q]), sv);
-            v.v[q] = __fmul_rn(r, r);
+            m.v[q] = __fmul_rn(m.v[q], sm);
+            v.v[q] = __fmul_rn(v.v[q], sv);
+            v.v[q] = __fmul_rn(v.v[q], v.v[q]);
         }
     } else {
         m = load_some(static_cast<const float*>(it.m) + at, wide, left);
         v = load_some(static_cast<const float*>(it.v) + at, wide, left);
     }
 
+    // With 32-bit moments HBM is what bounds the kernel, and root and quotient are correctly rounded; with 8-bit moments
+    // instructions are, and they are the hardware's approximations (2 units in the last place, of a step that is added to p).
     f8 r;                                          // sqrt(v), which the step divides by and the 8-bit form keeps
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
         const float gq = __fmul_rn(g.v[q], c);
-        m.v[q] = __fmaf_rn(hy.beta1, m.v[q], __fmul_rn(hy.rest1, gq));
-        v.v[q] = __fmaf_rn(hy.beta2, v.v[q], __fmul_rn(hy.rest2, __fmul_rn(gq, gq)));
-        r.v[q] = __fsqrt_rn(v.v[q]);
-        const float step = __fdiv_rn(m.v[q], __fmaf_rn(r.v[q], hy.root, hy.eps));
+        m.v[q] = __fadd_rn(__fmul_rn(hy.beta1, m.v[q]), __fmul_rn(hy.rest1, gq));
+        v.v[q] = __fadd_rn(__fmul_rn(hy.beta2, v.v[q]), __fmul_rn(hy.rest2, __fmul_rn(gq, gq)));
+        r.v[q] = B8 ? root_approx(v.v[q]) : __fsqrt_rn(v.v[q]);
+        const float below = __fmaf_rn(r.v[q], hy.root, hy.eps);
+        const float step = B8 ? __fdividef(m.v[q], below) : __fdiv_rn(m.v[q], below);
         p.v[q] = __fmaf_rn(-hy.rate, step, __fmul_rn(p.v[q], it.keep));
     }
 
@@ -190,10 +222,13 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     constexpr bool kPB = sizeof(P) == 2;
     if constexpr (B8 || kPB) {
         const uint64_t q0 = it.rng + (uint64_t)at;
+        const uint32_t low = (uint32_t)q0, key1 = hy.key1 + (uint32_t)(q0 >> 32) * kN3;
+        if (low <= 0xFFFFFFF8u) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const uint64_t pos = q0 + q;
-            rnd[q] = random_bits((uint32_t)pos, hy.key0, hy.key1 + (uint32_t)(pos >> 32) * kN3);
+            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, key1);
+        } else {                                   // the position's upper half changes within the eight
+#pragma unroll
+            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, low + q < low ? key1 + kN3 : key1);
         }
     }
     if constexpr (kPB) {
@@ -207,24 +242,53 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     if (it.copy) store_some(it.copy + at, p, wide, left);
 
     if constexpr (B8) {
-        float tm = 0.f, tr = 0.f;
+        // Largest magnitudes of the block, as bit patterns: what is not finite comes out on top of every number.  Elements
+        // behind the end of the tensor are zeros here (all their inputs are).
+        uint32_t tm = 0, tr = 0;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            if (q < left) {
-                tm = fmaxf(tm, finite_magnitude(m.v[q]));
-                tr = fmaxf(tr, finite_magnitude(r.v[q]));
+            tm = max(tm, __float_as_uint(fabsf(m.v[q])));
+            tr = max(tr, __float_as_uint(fabsf(r.v[q])));
+        }
+        const uint32_t half = threadIdx.x & 16 ? 0xFFFF0000u : 0xFFFFu;       // the 16 lanes that hold the block
+        uint32_t bm = __reduce_max_sync(half, tm), br = __reduce_max_sync(half, tr);
+        const bool odd = max(bm, br) >= 0x7F800000u;
+        if (odd) {                                 // rare: the scale is that of the finite values
+            tm = tr = 0;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                tm = max(tm, __float_as_uint(finite_magnitude(m.v[q])));
+                tr = max(tr, __float_as_uint(finite_magnitude(r.v[q])));
+            }
+            bm = __reduce_max_sync(half, tm);
+            br = __reduce_max_sync(half, tr);
+        }
+        const int mb = scale_byte(__uint_as_float(bm)), vb = scale_byte(__uint_as_float(br));
+        f8 sm = m, sr = r;
+        if (has_excess(mb) || has_excess(vb)) {
+            const float em = has_excess(mb) ? excess(mb) : 1.f, er = has_excess(vb) ? excess(vb) : 1.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                sm.v[q] = __fmul_rn(sm.v[q], em);
+                sr.v[q] = __fmul_rn(sr.v[q], er);
             }
         }
-        mb = scale_byte(block_top(tm));
-        vb = scale_byte(block_top(tr));
-        const float im = scale_inverse(mb), iv = scale_inverse(vb);
+        const float fm = code_factor(mb), fr = code_factor(vb);
+        uint32_t cm[8], cr[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            mc.c[q] = finite(m.v[q]) ? round_first(__fmul_rn(m.v[q], im), rnd[q] >> 16) : 0x7Fu;
-            vc.c[q] = finite(r.v[q]) ? round_second(__fmul_rn(r.v[q], iv), rnd[q] & 0xFFFFu) : 0x7Fu;
+            cm[q] = round_first(__fmul_rn(sm.v[q], fm), rnd[q]);
+            cr[q] = round_second(__fmul_rn(sr.v[q], fr), rnd[q]);
         }
-        store_codes(static_cast<uint8_t*>(it.m) + at, mc, wide, left);
-        store_codes(static_cast<uint8_t*>(it.v) + at, vc, wide, left);
+        if (odd) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (!finite(m.v[q])) cm[q] = 0x7F000000u;
+                if (!finite(r.v[q])) cr[q] = 0x7F000000u;
+            }
+        }
+        store_codes(static_cast<uint8_t*>(it.m) + at, make_uint2(gather_codes(cm[0], cm[1], cm[2], cm[3]), gather_codes(cm[4], cm[5], cm[6], cm[7])), wide, left);
+        store_codes(static_cast<uint8_t*>(it.v) + at, make_uint2(gather_codes(cr[0], cr[1], cr[2], cr[3]), gather_codes(cr[4], cr[5], cr[6], cr[7])), wide, left);
         if (left > 0 && (threadIdx.x & 15) == 0) {
             it.ms[at / kBlock] = (uint8_t)mb;
             it.vs[at / kBlock] = (uint8_t)vb;
