@@ -90,7 +90,7 @@ typedef struct hpsgd_adamw_tensor {
  *     x ^= x >> 14;  x *= N3;  x ^= x >> 16           N1..N3 = frac(sqrt 2, 3, 5) * 2^32 with the low bit set
  * the upper 16 are m's, the lower 16 r's, and the upper 16 of x * N2 a bf16 parameter's.
  *
- * beta1, beta2 in [0, 1), eps > 0, lr >= 0, step >= 1 (the first step is 1).
+ * beta1, beta2 in [0, 1), eps >= 2^-126, lr >= 0, step >= 1 (the first step is 1).
  */
 int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param_dtype, int grad_dtype, int state_bits,
                      double lr, double beta1, double beta2, double eps, int64_t step, uint64_t seed,

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kAdamThreads = 128;
 constexpr int kChunk = kAdamThreads * 8;       // elements a block handles: eight 8-bit blocks
+constexpr int kSpanChunks = 4;
 constexpr int kMaxItems = 360;                 // what 32764 bytes of kernel parameters hold
 
 // Constants of the element's random bits: frac(sqrt 2, 3, 5) * 2^32 with the low bit set.
@@ -50,6 +51,7 @@ struct Hyper {
     float eps;
     uint32_t key0, key1;
     const float* scale;
+    int span;                                  // elements per block
 };
 
 // The tensor that a chunk belongs to: the last whose first chunk is not behind it.
@@ -65,11 +67,12 @@ __device__ __forceinline__ int find_item(const Table<CAP>& t, uint32_t chunk)
     return lo;
 }
 
-__device__ __forceinline__ uint32_t random_bits(uint32_t q, uint32_t key0, uint32_t key1)
+// `turn`: the second key (with the position's upper half) times N2, which the second product then only adds.
+__device__ __forceinline__ uint32_t random_bits(uint32_t q, uint32_t key0, uint32_t turn)
 {
     uint32_t x = (q ^ key0) * kN1;
     x ^= x >> 15;
-    x = (x + key1) * kN2;
+    x = x * kN2 + turn;
     x ^= x >> 14;
     x *= kN3;
     return x ^ x >> 16;
@@ -99,203 +102,371 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 u, bool wide, int 
         if (q < left) p[q] = (uint8_t)((q < 4 ? u.x : u.y) >> 8 * (q & 3));
 }
 
+// ---------------------------------------------------------------------------- two values at a time
+// The packed binary32 instructions round each half as the scalar ones do and take one issue slot for two results.
+typedef unsigned long long pair;
+
+__device__ __forceinline__ pair make_pair(float lo, float hi)
+{
+    pair x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
+    return x;
+}
+__device__ __forceinline__ void split(pair x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ pair mul2(pair a, pair b)
+{
+    pair x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ pair add2(pair a, pair b)
+{
+    pair x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ pair fma2(pair a, pair b, pair c)
+{
+    pair x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ pair both(float x) { return make_pair(x, x); }
+
+struct p4 {
+    pair v[4];
+};
+
+__device__ __forceinline__ p4 to_pairs(const f8& x)
+{
+    p4 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y.v[q] = make_pair(x.v[2 * q], x.v[2 * q + 1]);
+    return y;
+}
+__device__ __forceinline__ f8 to_values(const p4& x)
+{
+    f8 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) split(x.v[q], y.v[2 * q], y.v[2 * q + 1]);
+    return y;
+}
+
+// ---------------------------------------------------------------------------- codes
 // Two codes (the low 16 bits) to two values: the conversion goes through f16, which holds every E4M3 value and its NaN.
-__device__ __forceinline__ void decode_pair(uint32_t two, float& lo, float& hi)
+__device__ __forceinline__ pair decode_pair(uint32_t two)
 {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    lo = f.x;
-    hi = f.y;
+    return make_pair(f.x, f.y);
 }
 
-__device__ __forceinline__ f8 decode8(uint2 u)
+__device__ __forceinline__ p4 decode8(uint2 u)
 {
-    f8 x;
-    decode_pair(u.x, x.v[0], x.v[1]);
-    decode_pair(u.x >> 16, x.v[2], x.v[3]);
-    decode_pair(u.y, x.v[4], x.v[5]);
-    decode_pair(u.y >> 16, x.v[6], x.v[7]);
+    p4 x;
+    x.v[0] = decode_pair(u.x);
+    x.v[1] = decode_pair(u.x >> 16);
+    x.v[2] = decode_pair(u.y);
+    x.v[3] = decode_pair(u.y >> 16);
     return x;
 }
 
 // What multiplies a value of a block with scale 2^(byte - 127) so that the value's E4M3 code comes to stand in bits 20..26 of
 // its binary32 pattern: 2^(127 - byte - 120), in one factor as long as that is a normal number.  Blocks above 2^6 * 448, whose
-// factor is not, first have their values multiplied by the rest (`excess`).
+// factor is not, first have their values multiplied by the rest (`excess`).  The largest patterns of values that are not finite
+// give bytes that have excess too.
 __device__ __forceinline__ float code_factor(int byte) { return __uint_as_float((uint32_t)(max(254 - 120 - byte, 1)) << 23); }
 __device__ __forceinline__ bool has_excess(int byte) { return byte > 133; }
-__device__ __forceinline__ float excess(int byte) { return __uint_as_float((uint32_t)(127 - (byte - 133)) << 23); }
+__device__ __forceinline__ float excess(int byte) { return has_excess(byte) ? __uint_as_float((uint32_t)(127 - (byte - 133)) << 23) : 1.f; }
 
-// One of the two codes around |x|, such that the expected value is |x|; `x` is already multiplied by its block's code factor.
-// 16 random bits, centred, are added below the last bit that is kept, and the carry decides.  An exact code stays.
-// The code comes back in the top byte, sign included.
+// Both roundings take x already multiplied by its block's code factor and give the code in bits 20..26 with the sign in bit 31
+// (what lies below does not count): see gather_codes.
+
+// One of the two codes around |x|, such that the expected value is |x|: 16 random bits, centred, are added below the last bit that
+// is kept, and the carry decides.  An exact code stays.
 __device__ __forceinline__ uint32_t round_first(float x, uint32_t rnd)
 {
-    const uint32_t b = __float_as_uint(fabsf(x)) + ((rnd >> 12 & 0xFFFF0u) | 8u);
-    return (b << 4 & 0x7F000000u) | (__float_as_uint(x) & 0x80000000u);
+    return __float_as_uint(x) + ((rnd >> 12 & 0xFFFF0u) | 8u);
 }
 
-// One of the two codes a <= x < b, such that the expected square is x^2: b with probability (x^2 - a^2) / (b^2 - a^2), so where
-// x^2 > a^2 + u (b^2 - a^2).  0 only for 0.  `t` is x multiplied by its block's code factor.  The code comes back in the top byte.
-__device__ __forceinline__ uint32_t round_second(float t, uint32_t rnd)
+// One of the two codes a <= x < b, such that the expected square is x^2: b with probability (x^2 - a^2) / (b^2 - a^2).  With the
+// codes' step as the unit, a = n and x = n + f, that is f (2n + f) / (2n + 1); n + f is 8 times the significand of x, or x itself
+// over the step where the code is subnormal (there alone 0 is near, and only 0 stays 0).  Two elements at a time.
+template <bool SUBNORMAL>
+__device__ __forceinline__ void round_second(float x0, float x1, uint32_t rnd0, uint32_t rnd1, uint32_t& c0, uint32_t& c1)
 {
-    const uint32_t ab = __float_as_uint(t) & 0xFFF00000u;
-    const float x = __fmul_rn(t, 0x1p120f);
-    const float a = __fmul_rn(__uint_as_float(ab), 0x1p120f), b = __fmul_rn(__uint_as_float(ab + 0x100000u), 0x1p120f);
-    const float u1 = __uint_as_float(0x3F800040u | (rnd << 7 & 0x7FFF80u));          // 1 + u, u = (16 bits + 0.5) / 2^16
-    const float d = __fmul_rn(__fsub_rn(b, a), __fadd_rn(b, a));
-    const bool up = __fmul_rn(__fsub_rn(x, a), __fadd_rn(x, a)) > __fmul_rn(__fsub_rn(u1, 1.f), d);
-    const uint32_t c = (up ? ab + 0x100000u : ab) << 4;
-    return max(c, t > 0.f ? 0x1000000u : 0u);
+    c0 = __float_as_uint(x0);
+    c1 = __float_as_uint(x1);
+    pair s = make_pair(__uint_as_float((c0 & 0x7FFFFFu) | 0x41000000u), __uint_as_float((c1 & 0x7FFFFFu) | 0x41000000u));
+    pair n = make_pair(__uint_as_float((c0 & 0x700000u) | 0x41000000u), __uint_as_float((c1 & 0x700000u) | 0x41000000u));
+    if (SUBNORMAL) {
+        const pair less = make_pair(c0 < 0x800000u ? -8.f : 0.f, c1 < 0x800000u ? -8.f : 0.f);
+        s = add2(s, less);
+        n = add2(n, less);
+    }
+    // u = (16 random bits + 0.5) / 2^16, first as 1 + u
+    const pair u = add2(make_pair(__uint_as_float(0x3F800040u | (rnd0 << 7 & 0x7FFF80u)), __uint_as_float(0x3F800040u | (rnd1 << 7 & 0x7FFF80u))), both(-1.f));
+    const pair lhs = mul2(u, fma2(both(2.f), n, both(1.f)));
+    const pair rhs = mul2(fma2(both(-1.f), n, s), add2(n, s));
+    float l0, l1, r0, r1;
+    split(lhs, l0, l1);
+    split(rhs, r0, r1);
+    if (l0 < r0) c0 += 0x100000u;
+    if (l1 < r1) c1 += 0x100000u;
+    if (SUBNORMAL && x0 > 0.f) c0 = max(c0, 0x100000u);
+    if (SUBNORMAL && x1 > 0.f) c1 = max(c1, 0x100000u);
 }
 
-// Four codes from their top bytes.
+// Four codes next to one another: the upper halves pairwise, shifted and cut two at a time.
 __device__ __forceinline__ uint32_t gather_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+    const uint32_t ab = __byte_perm(a, b, 0x7632), cd = __byte_perm(c, d, 0x7632);
+    const uint32_t x = (ab << 4 & 0x7F007F00u) | (ab & 0x80008000u), y = (cd << 4 & 0x7F007F00u) | (cd & 0x80008000u);
+    return __byte_perm(x, y, 0x7531);
 }
 
+__device__ __forceinline__ uint2 gather8(const uint32_t* c)
+{
+    return make_uint2(gather_codes(c[0], c[1], c[2], c[3]), gather_codes(c[4], c[5], c[6], c[7]));
+}
+
+// Eight patterns cut to bf16.
+__device__ __forceinline__ void store_upper(__nv_bfloat16* p, const f8& x, bool wide, int left)
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) u[q] = __byte_perm(__float_as_uint(x.v[2 * q]), __float_as_uint(x.v[2 * q + 1]), 0x7632);
+    if (wide) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        return;
+    }
+    unsigned short* const h = reinterpret_cast<unsigned short*>(p);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < left) h[q] = (unsigned short)(u[q >> 1] >> 16 * (q & 1));
+}
+
+// Square root and reciprocal by the hardware's approximations, 1 unit in the last place.  Subnormal operands count as zero: a second
+// moment below 2^-126 belongs to gradients below 10^-17.
 __device__ __forceinline__ float root_approx(float x)
 {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
-// ---------------------------------------------------------------------------- the step
-template <int CAP, typename P, typename G, bool B8>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper hy)
+// Largest of eight magnitudes; NaN if one of them is.
+__device__ __forceinline__ float top8(const f8& x)
 {
-    const Item& it = table.item[find_item(table, blockIdx.x)];
-    const int64_t at = (int64_t)(blockIdx.x - it.first) * kChunk + threadIdx.x * 8;
-    const int64_t rest = it.n - at;
-    const int left = rest < 0 ? 0 : rest > 8 ? 8 : (int)rest;
-    const bool wide = it.wide && left == 8;
-    float c = 1.f;
-    if (hy.scale) {
-        c = *hy.scale;
-        if (!finite(c)) return;                   // the whole grid: nothing of the step happens
-    }
-    if (!B8 && left == 0) return;
+    float a, b, c;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x.v[3]), "f"(x.v[4]), "f"(x.v[5]));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(c) : "f"(x.v[6]), "f"(x.v[7]), "f"(a));
+    asm("max.NaN.abs.f32 %0, %1, %2, %2;" : "=f"(a) : "f"(b), "f"(c));
+    return a;
+}
 
-    P* const pp = static_cast<P*>(it.p) + at;
-    f8 p = load_some(pp, wide, left);
-    f8 g = load_some(static_cast<const G*>(it.g) + at, wide, left);
-    f8 m, v;
-    if constexpr (B8) {
-        const uint2 mc = load_codes(static_cast<const uint8_t*>(it.m) + at, wide, left);
-        const uint2 vc = load_codes(static_cast<const uint8_t*>(it.v) + at, wide, left);
-        int mb = 0, vb = 0;
-        if (left > 0) {
-            mb = it.ms[at / kBlock];
-            vb = it.vs[at / kBlock];
-        }
-        const float sm = scale_value(mb), sv = scale_value(vb);
-        m = decode8(mc);
-        v = decode8(vc);
+// ---------------------------------------------------------------------------- the step
+// Where a block's share of a tensor starts in each of its arrays.
+struct Share {
+    void* p;
+    const void* g;
+    void* m;
+    void* v;
+    uint8_t* ms;
+    uint8_t* vs;
+    __nv_bfloat16* copy;
+    uint64_t rng;
+    float keep;
+    bool wide;
+};
+
+// The block's codes and scales from its new moments m and r = sqrt(v) (zeros behind the end of the tensor).
+__device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t* rnd, int& mb, int& vb, uint2& mc, uint2& vc)
+{
+    const uint32_t half = threadIdx.x & 16 ? 0xFFFF0000u : 0xFFFFu;       // the 16 lanes that hold the block
+    mb = scale_byte(__uint_as_float(__reduce_max_sync(half, __float_as_uint(top8(m)))));
+    vb = scale_byte(__uint_as_float(__reduce_max_sync(half, __float_as_uint(top8(r)))));
+    uint32_t cm[8], cr[8], low = 0xFFFFFFFFu;
+    f8 x;
+    {
+        const pair fm = both(code_factor(mb)), fr = both(code_factor(vb));
+        p4 y = to_pairs(m);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            m.v[q] = __fmul_rn(m.v[q], sm);
-            v.v[q] = __fmul_rn(v.v[q], sv);
-            v.v[q] = __fmul_rn(v.v[q], v.v[q]);
-        }
+        for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], fm);
+        x = to_values(y);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) cm[q] = round_first(x.v[q], rnd[q]);
+        y = to_pairs(r);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], fr);
+        x = to_values(y);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) low = min(low, __float_as_uint(x.v[q]));
+    }
+    if (max(mb, vb) <= 133 && low >= 0x800000u) {
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) round_second<false>(x.v[q], x.v[q + 1], rnd[q], rnd[q + 1], cr[q], cr[q + 1]);
     } else {
-        m = load_some(static_cast<const float*>(it.m) + at, wide, left);
-        v = load_some(static_cast<const float*>(it.v) + at, wide, left);
-    }
-
-    // With 32-bit moments HBM is what bounds the kernel, and root and quotient are correctly rounded; with 8-bit moments
-    // instructions are, and they are the hardware's approximations (2 units in the last place, of a step that is added to p).
-    f8 r;                                          // sqrt(v), which the step divides by and the 8-bit form keeps
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        const float gq = __fmul_rn(g.v[q], c);
-        m.v[q] = __fadd_rn(__fmul_rn(hy.beta1, m.v[q]), __fmul_rn(hy.rest1, gq));
-        v.v[q] = __fadd_rn(__fmul_rn(hy.beta2, v.v[q]), __fmul_rn(hy.rest2, __fmul_rn(gq, gq)));
-        r.v[q] = B8 ? root_approx(v.v[q]) : __fsqrt_rn(v.v[q]);
-        const float below = __fmaf_rn(r.v[q], hy.root, hy.eps);
-        const float step = B8 ? __fdividef(m.v[q], below) : __fdiv_rn(m.v[q], below);
-        p.v[q] = __fmaf_rn(-hy.rate, step, __fmul_rn(p.v[q], it.keep));
-    }
-
-    uint32_t rnd[8];
-    constexpr bool kPB = sizeof(P) == 2;
-    if constexpr (B8 || kPB) {
-        const uint64_t q0 = it.rng + (uint64_t)at;
-        const uint32_t low = (uint32_t)q0, key1 = hy.key1 + (uint32_t)(q0 >> 32) * kN3;
-        if (low <= 0xFFFFFFF8u) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, key1);
-        } else {                                   // the position's upper half changes within the eight
-#pragma unroll
-            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, low + q < low ? key1 + kN3 : key1);
-        }
-    }
-    if constexpr (kPB) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {              // exact in bf16 afterwards: the store's own rounding does nothing
-            const uint32_t b = __float_as_uint(p.v[q]);
-            if (finite(p.v[q])) p.v[q] = __uint_as_float(b + (rnd[q] * kN2 >> 16) & 0xFFFF0000u);
-        }
-    }
-    store_some(pp, p, wide, left);
-    if (it.copy) store_some(it.copy + at, p, wide, left);
-
-    if constexpr (B8) {
-        // Largest magnitudes of the block, as bit patterns: what is not finite comes out on top of every number.  Elements
-        // behind the end of the tensor are zeros here (all their inputs are).
-        uint32_t tm = 0, tr = 0;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            tm = max(tm, __float_as_uint(fabsf(m.v[q])));
-            tr = max(tr, __float_as_uint(fabsf(r.v[q])));
-        }
-        const uint32_t half = threadIdx.x & 16 ? 0xFFFF0000u : 0xFFFFu;       // the 16 lanes that hold the block
-        uint32_t bm = __reduce_max_sync(half, tm), br = __reduce_max_sync(half, tr);
-        const bool odd = max(bm, br) >= 0x7F800000u;
-        if (odd) {                                 // rare: the scale is that of the finite values
-            tm = tr = 0;
+        // some second moment far below its block's largest, a very large block, or values that are not finite: the scales are those of
+        // the finite values
+        if (has_excess(mb) || has_excess(vb)) {
+            uint32_t tm = 0, tr = 0;
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 tm = max(tm, __float_as_uint(finite_magnitude(m.v[q])));
                 tr = max(tr, __float_as_uint(finite_magnitude(r.v[q])));
             }
-            bm = __reduce_max_sync(half, tm);
-            br = __reduce_max_sync(half, tr);
+            __syncwarp(half);
+            mb = scale_byte(__uint_as_float(__reduce_max_sync(half, tm)));
+            vb = scale_byte(__uint_as_float(__reduce_max_sync(half, tr)));
         }
-        const int mb = scale_byte(__uint_as_float(bm)), vb = scale_byte(__uint_as_float(br));
-        f8 sm = m, sr = r;
-        if (has_excess(mb) || has_excess(vb)) {
-            const float em = has_excess(mb) ? excess(mb) : 1.f, er = has_excess(vb) ? excess(vb) : 1.f;
+        const float em = excess(mb), er = excess(vb), fm = code_factor(mb), fr = code_factor(vb);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                sm.v[q] = __fmul_rn(sm.v[q], em);
-                sr.v[q] = __fmul_rn(sr.v[q], er);
+        for (int q = 0; q < 8; q += 2) {
+            round_second<true>(__fmul_rn(__fmul_rn(r.v[q], er), fr), __fmul_rn(__fmul_rn(r.v[q + 1], er), fr), rnd[q], rnd[q + 1], cr[q], cr[q + 1]);
+#pragma unroll
+            for (int k = q; k < q + 2; ++k) {
+                cm[k] = finite(m.v[k]) ? round_first(__fmul_rn(__fmul_rn(m.v[k], em), fm), rnd[k]) : 0x7F00000u;
+                if (!finite(r.v[k])) cr[k] = 0x7F00000u;
             }
         }
-        const float fm = code_factor(mb), fr = code_factor(vb);
-        uint32_t cm[8], cr[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            cm[q] = round_first(__fmul_rn(sm.v[q], fm), rnd[q]);
-            cr[q] = round_second(__fmul_rn(sr.v[q], fr), rnd[q]);
-        }
-        if (odd) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                if (!finite(m.v[q])) cm[q] = 0x7F000000u;
-                if (!finite(r.v[q])) cr[q] = 0x7F000000u;
-            }
-        }
-        store_codes(static_cast<uint8_t*>(it.m) + at, make_uint2(gather_codes(cm[0], cm[1], cm[2], cm[3]), gather_codes(cm[4], cm[5], cm[6], cm[7])), wide, left);
-        store_codes(static_cast<uint8_t*>(it.v) + at, make_uint2(gather_codes(cr[0], cr[1], cr[2], cr[3]), gather_codes(cr[4], cr[5], cr[6], cr[7])), wide, left);
-        if (left > 0 && (threadIdx.x & 15) == 0) {
-            it.ms[at / kBlock] = (uint8_t)mb;
-            it.vs[at / kBlock] = (uint8_t)vb;
+    }
+    mc = gather8(cm);
+    vc = gather8(cr);
+}
+
+// One group of eight per thread, `left` of them inside the tensor, at elements o.. of the block's share.  All threads of a warp come
+// here.  FULL: the whole block has eight elements a thread and wide accesses, which leaves no branch in the way of the loads.
+template <typename P, typename G, bool B8, bool FULL>
+__device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, float c, int o, int left)
+{
+    const bool wide = FULL || (it.wide && left == 8);
+    P* const pp = static_cast<P*>(it.p) + o;
+    f8 p = load_some(pp, wide, left);
+    const f8 g = load_some(static_cast<const G*>(it.g) + o, wide, left);
+    f8 m, v, r;                                    // r = sqrt(v), which the step divides by and the 8-bit form keeps
+    uint2 mc, vc;
+    int mb = 0, vb = 0;
+    if constexpr (B8) {
+        mc = load_codes(static_cast<const uint8_t*>(it.m) + o, wide, left);
+        vc = load_codes(static_cast<const uint8_t*>(it.v) + o, wide, left);
+        if (FULL || left > 0) {
+            mb = it.ms[o / kBlock];
+            vb = it.vs[o / kBlock];
         }
     } else {
-        store_some(static_cast<float*>(it.m) + at, m, wide, left);
-        store_some(static_cast<float*>(it.v) + at, v, wide, left);
+        m = load_some(static_cast<const float*>(it.m) + o, wide, left);
+        v = load_some(static_cast<const float*>(it.v) + o, wide, left);
+    }
+    if (!finite(c)) return;                        // the whole grid: nothing of the step happens
+
+    // With 32-bit moments HBM is what bounds the kernel, and root and quotient are correctly rounded; with 8-bit moments
+    // instructions are, and they are the hardware's approximations, of a step that is added to p.
+    if constexpr (B8) {
+        const pair sm = both(scale_value(mb)), sv = both(scale_value(vb));
+        p4 pm = decode8(mc), pv = decode8(vc), pg = to_pairs(g), px = to_pairs(p);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            pm.v[q] = mul2(pm.v[q], sm);
+            pv.v[q] = mul2(pv.v[q], sv);
+            pv.v[q] = mul2(pv.v[q], pv.v[q]);
+            pg.v[q] = mul2(pg.v[q], both(c));
+            pm.v[q] = add2(mul2(pm.v[q], both(hy.beta1)), mul2(pg.v[q], both(hy.rest1)));
+            pv.v[q] = add2(mul2(pv.v[q], both(hy.beta2)), mul2(mul2(pg.v[q], pg.v[q]), both(hy.rest2)));
+        }
+        m = to_values(pm);
+        v = to_values(pv);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) r.v[q] = root_approx(v.v[q]);
+        const p4 pr = to_pairs(r);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float b0, b1;
+            split(fma2(pr.v[q], both(hy.root), both(hy.eps)), b0, b1);
+            const pair step = mul2(pm.v[q], make_pair(reciprocal_approx(b0), reciprocal_approx(b1)));
+            px.v[q] = fma2(both(-hy.rate), step, mul2(px.v[q], both(it.keep)));
+        }
+        p = to_values(px);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float gq = __fmul_rn(g.v[q], c);
+            m.v[q] = __fadd_rn(__fmul_rn(hy.beta1, m.v[q]), __fmul_rn(hy.rest1, gq));
+            v.v[q] = __fadd_rn(__fmul_rn(hy.beta2, v.v[q]), __fmul_rn(hy.rest2, __fmul_rn(gq, gq)));
+            r.v[q] = __fsqrt_rn(v.v[q]);
+            const float step = __fdiv_rn(m.v[q], __fmaf_rn(r.v[q], hy.root, hy.eps));
+            p.v[q] = __fmaf_rn(-hy.rate, step, __fmul_rn(p.v[q], it.keep));
+        }
+    }
+
+    uint32_t rnd[8];
+    constexpr bool kPB = sizeof(P) == 2;
+    if constexpr (B8 || kPB) {
+        const uint64_t q0 = it.rng + (uint64_t)o;
+        const uint32_t low = (uint32_t)q0, turn = (hy.key1 + (uint32_t)(q0 >> 32) * kN3) * kN2;
+        if (low <= 0xFFFFFFF8u) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, turn);
+        } else {                                   // the position's upper half changes within the eight
+#pragma unroll
+            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, low + q < low ? turn + kN3 * kN2 : turn);
+        }
+    }
+    if constexpr (kPB) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)                // the upper half of the pattern is what is kept
+            if (finite(p.v[q])) p.v[q] = __uint_as_float(__float_as_uint(p.v[q]) + (rnd[q] * kN2 >> 16));
+        store_upper(pp, p, wide, left);
+    } else {
+        store_some(pp, p, wide, left);
+        if (it.copy) store_some(it.copy + o, p, wide, left);
+    }
+
+    if constexpr (B8) {
+        encode8(m, r, rnd, mb, vb, mc, vc);
+        store_codes(static_cast<uint8_t*>(it.m) + o, mc, wide, left);
+        store_codes(static_cast<uint8_t*>(it.v) + o, vc, wide, left);
+        if ((FULL || left > 0) && (threadIdx.x & 15) == 0) {
+            it.ms[o / kBlock] = (uint8_t)mb;
+            it.vs[o / kBlock] = (uint8_t)vb;
+        }
+    } else {
+        store_some(static_cast<float*>(it.m) + o, m, wide, left);
+        store_some(static_cast<float*>(it.v) + o, v, wide, left);
+    }
+}
+
+// Block b handles `span` elements, a whole number of chunks, of one tensor.
+template <int CAP, typename P, typename G, bool B8>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper hy)
+{
+    const Item& it = table.item[find_item(table, blockIdx.x)];
+    const float c = hy.scale ? *hy.scale : 1.f;
+    const int64_t at = (int64_t)(blockIdx.x - it.first) * hy.span;
+    const int here = (int)min((int64_t)hy.span, it.n - at);
+    Share sh;
+    sh.p = static_cast<P*>(it.p) + at;
+    sh.g = static_cast<const G*>(it.g) + at;
+    sh.m = static_cast<char*>(it.m) + at * (B8 ? 1 : 4);
+    sh.v = static_cast<char*>(it.v) + at * (B8 ? 1 : 4);
+    sh.ms = it.ms + at / kBlock;
+    sh.vs = it.vs + at / kBlock;
+    sh.copy = it.copy ? it.copy + at : nullptr;
+    sh.rng = it.rng + (uint64_t)at;
+    sh.keep = it.keep;
+    sh.wide = it.wide;
+    for (int s = 0; s < here; s += kChunk) {
+        const int o = s + threadIdx.x * 8;
+        if (sh.wide && here - s >= kChunk) adamw_group<P, G, B8, true>(sh, hy, c, o, 8);
+        else adamw_group<P, G, B8, false>(sh, hy, c, o, max(0, min(8, here - o)));
     }
 }
 
@@ -421,13 +592,18 @@ uint32_t fill_table(const hpsgd_adamw_tensor* t, int n, int* at, int64_t chunk_e
 }
 
 template <int CAP, typename P, typename G, bool B8>
-int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, const Hyper& hy, cudaStream_t s)
+int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, Hyper hy, int sms, cudaStream_t s)
 {
+    // With 8-bit moments finding the tensor and its addresses is a tenth of a block's instructions if it handles one chunk; with
+    // enough chunks to fill the device all the same, a block takes kSpanChunks of them.
+    int64_t total = 0;
+    for (int k = 0; k < n; ++k) total += t[k].n;
+    hy.span = B8 && total >= (int64_t)kSpanChunks * kChunk * sms * 16 ? kSpanChunks * kChunk : kChunk;
     const size_t ap = sizeof(P) == 4 ? 32 : 16, ag = sizeof(G) == 4 ? 32 : 16, as = B8 ? 8 : 32;
     int at = 0;
     Table<CAP> table;
     while (at < n) {
-        const uint32_t chunks = fill_table(t, n, &at, kChunk, &table, [&](const hpsgd_adamw_tensor& x, Item* it) {
+        const uint32_t chunks = fill_table(t, n, &at, hy.span, &table, [&](const hpsgd_adamw_tensor& x, Item* it) {
             it->p = x.param; it->m = x.m; it->v = x.v; it->ms = x.m_scale; it->vs = x.v_scale;
             it->copy = static_cast<__nv_bfloat16*>(x.copy);
             it->rng = x.rng_offset;
@@ -442,13 +618,13 @@ int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, const Hyper& hy
 }
 
 template <int CAP>
-int step_types(const hpsgd_adamw_tensor* t, int n, int pd, int gd, int bits, double lr, const Hyper& hy, cudaStream_t s)
+int step_types(const hpsgd_adamw_tensor* t, int n, int pd, int gd, int bits, double lr, const Hyper& hy, int sms, cudaStream_t s)
 {
     using bf = __nv_bfloat16;
-    if (pd == HPSGD_F32 && gd == HPSGD_F32) return bits == 8 ? step_launches<CAP, float, float, true>(t, n, lr, hy, s) : step_launches<CAP, float, float, false>(t, n, lr, hy, s);
-    if (pd == HPSGD_F32) return bits == 8 ? step_launches<CAP, float, bf, true>(t, n, lr, hy, s) : step_launches<CAP, float, bf, false>(t, n, lr, hy, s);
-    if (gd == HPSGD_F32) return bits == 8 ? step_launches<CAP, bf, float, true>(t, n, lr, hy, s) : step_launches<CAP, bf, float, false>(t, n, lr, hy, s);
-    return bits == 8 ? step_launches<CAP, bf, bf, true>(t, n, lr, hy, s) : step_launches<CAP, bf, bf, false>(t, n, lr, hy, s);
+    if (pd == HPSGD_F32 && gd == HPSGD_F32) return bits == 8 ? step_launches<CAP, float, float, true>(t, n, lr, hy, sms, s) : step_launches<CAP, float, float, false>(t, n, lr, hy, sms, s);
+    if (pd == HPSGD_F32) return bits == 8 ? step_launches<CAP, float, bf, true>(t, n, lr, hy, sms, s) : step_launches<CAP, float, bf, false>(t, n, lr, hy, sms, s);
+    if (gd == HPSGD_F32) return bits == 8 ? step_launches<CAP, bf, float, true>(t, n, lr, hy, sms, s) : step_launches<CAP, bf, float, false>(t, n, lr, hy, sms, s);
+    return bits == 8 ? step_launches<CAP, bf, bf, true>(t, n, lr, hy, sms, s) : step_launches<CAP, bf, bf, false>(t, n, lr, hy, sms, s);
 }
 
 template <int CAP, typename G>
@@ -508,7 +684,7 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
     if (param_dtype != HPSGD_F32 && param_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown param_dtype %d", what, param_dtype);
     if (state_bits != 8 && state_bits != 32) return report(HPSGD_E_BADARG, "%s: state_bits must be 8 or 32", what);
     if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return report(HPSGD_E_BADARG, "%s: beta1 and beta2 must be in [0, 1)", what);
-    if (!(eps > 0.0) || !std::isfinite(eps) || (float)eps == 0.f) return report(HPSGD_E_BADARG, "%s: eps must be positive in binary32", what);
+    if (!(eps >= 0x1p-126) || !std::isfinite((float)eps)) return report(HPSGD_E_BADARG, "%s: eps must be a normal positive number in binary32", what);
     if (!(lr >= 0.0) || !std::isfinite(lr)) return report(HPSGD_E_BADARG, "%s: lr must be >= 0", what);
     if (step < 1) return report(HPSGD_E_BADARG, "%s: step counts from 1", what);
     if (!aligned(grad_scale, 4)) return report(HPSGD_E_BADARG, "%s: grad_scale is not 4-byte aligned", what);
@@ -535,8 +711,8 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
     hy.key0 = (uint32_t)key; hy.key1 = (uint32_t)(key >> 32);
     hy.scale = grad_scale;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (n_tensors <= 8) return step_types<8>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, s);
-    return step_types<kMaxItems>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, s);
+    if (n_tensors <= 8) return step_types<8>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
+    return step_types<kMaxItems>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
 }
 
 int hpsgd_grad_norm(const hpsgd_adamw_tensor* tensors, int n_tensors, int grad_dtype, double max_norm, void* workspace, float* out,
