@@ -1,6 +1,7 @@
 /*
  * libhpsgd, operators: what a program that trains or runs a language model needs beside the
- * replica update and the merge of hpsgd.h: the optimizer step over many tensors.
+ * replica update and the merge of hpsgd.h: the optimizer step over many tensors, and the layer in 8-bit
+ * floating point that its gradients come from (norm, quantisation, matrix product).
  * (The HPSGD paper has no counterpart for any of them.)
  *
  * Conventions (in addition to those of hpsgd.h)
@@ -22,6 +23,13 @@
  * against an arbitrary factor, multiplying by it is exact, and values can be moved to blocks along the
  * other axis without being rounded again (except where they fall below the smallest code).  Values
  * that are not finite become the NaN code 0x7F and do not count for the scale.
+ *
+ * A matrix [rows x cols] in this format (its blocks run along the columns):
+ *   codes    one byte each, row r at r * ld; ld >= cols, a multiple of 16, the address 16-byte aligned; the
+ *            codes behind the last column, up to a multiple of 16, are written as zeros
+ *   scales   the byte of block b of row r at ((b / 4) * lds + r) * 4 + b % 4, lds >= rows (four blocks make a
+ *            32-bit word, and the words of consecutive rows follow one another); 4-byte aligned,
+ *            ceil(ceil(cols / 128) / 4) * lds * 4 bytes; the bytes behind a row's last block are written as zeros
  */
 #ifndef HPSGD_OPS_H_
 #define HPSGD_OPS_H_
@@ -108,6 +116,92 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
 #define HPSGD_GRAD_NORM_WORKSPACE 65536
 int hpsgd_grad_norm(const hpsgd_adamw_tensor* tensors, int n_tensors, int grad_dtype, double max_norm,
                     void* workspace, float* out, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Root-mean-square norm with the residual's addition and an 8-bit output.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * Per row of x [rows x cols]:
+ *     h = x + residual            rounded to dtype, which is what is stored and what is normalised (the backward
+ *                                 pass then sees the same numbers); h = x without a residual
+ *     rstd = 1 / sqrt(mean(h^2) + eps)
+ *     y = h * rstd * weight       in binary32, rounded once to what is stored
+ *   dtype, weight_dtype   HPSGD_F32 or HPSGD_BF16
+ *   residual, h     both or neither; h may be x's or the residual's own memory
+ *   y8, y_scale     the 8-bit block format (both or neither);  y   values of dtype.  At least one of y8, y.
+ *   rstd            rows floats, for the backward pass, or NULL
+ *   ld*             elements (bytes for ldy8) from row to row; 0 = cols (for ldy8 cols up to a multiple of 16);
+ *                   ldys: the lds of the scales, 0 = rows
+ * Rows whose addresses and strides are multiples of 32 bytes (16 for bf16) take the wide accesses.  cols <= 16384
+ * (else HPSGD_E_UNSUPPORTED).
+ */
+typedef struct hpsgd_rmsnorm_forward_args {
+    int64_t rows, cols;
+    double eps;
+    int dtype, weight_dtype;
+    const void* x;
+    const void* residual;
+    const void* weight;
+    void* h;
+    void* y;
+    void* y8;
+    uint8_t* y_scale;
+    float* rstd;
+    int64_t ldx, ldres, ldh, ldy, ldy8, ldys;
+} hpsgd_rmsnorm_forward_args;
+int hpsgd_rmsnorm_forward(const hpsgd_rmsnorm_forward_args* args, void* stream);
+
+/*
+ * Gradients of the norm, through its quantisation as if that were the identity.  With xn = h * rstd, d = dy * weight:
+ *     dx = rstd * (d - xn * mean(d * xn)) + dres      the gradient of h, so of x and of the residual alike
+ *     dweight = sum over rows of dy * xn              cols floats
+ *   dy, dres, dx   values of dtype; dres (the gradient that reaches h by the residual stream) may be NULL; dx may be dy's
+ *                  or dres's own memory
+ *   workspace      hpsgd_rmsnorm_backward_bytes(rows, cols) bytes of device memory, 16-byte aligned; no contents needed
+ * With rows = 0 dweight is set to zero.
+ */
+typedef struct hpsgd_rmsnorm_backward_args {
+    int64_t rows, cols;
+    int dtype, weight_dtype;
+    const void* h;
+    const void* weight;
+    const float* rstd;
+    const void* dy;
+    const void* dres;
+    void* dx;
+    float* dweight;
+    void* workspace;
+    int64_t ldh, lddy, lddres, lddx;
+} hpsgd_rmsnorm_backward_args;
+size_t hpsgd_rmsnorm_backward_bytes(int64_t rows, int64_t cols);
+int hpsgd_rmsnorm_backward(const hpsgd_rmsnorm_backward_args* args, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * To the 8-bit block format, along rows and along columns in one pass.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * x [rows x cols] -> q, scale: the matrix in the block format, and / or qt, scale_t: its transpose [cols x rows] in the
+ * block format, whose blocks run along x's columns.  Rounding is to nearest even.
+ *   dtype    HPSGD_F32, HPSGD_BF16, or HPSGD_FP8: x is itself in the block format (x_scale given; ldx bytes), and only the
+ *            transpose can be asked for.  Moving to the other blocks is exact but for values below the new block's smallest code.
+ *   ld*      elements (bytes for codes) from row to row; 0 = the least: cols for x, multiples of 16 for codes
+ *   lds*     the lds of the scales, 0 = the rows of that matrix
+ */
+enum { HPSGD_FP8 = 2 };
+typedef struct hpsgd_quantize_fp8_args {
+    int64_t rows, cols;
+    int dtype;
+    const void* x;
+    const uint8_t* x_scale;
+    void* q;
+    uint8_t* scale;
+    void* qt;
+    uint8_t* scale_t;
+    int64_t ldx, ldxs, ldq, lds, ldqt, ldst;
+} hpsgd_quantize_fp8_args;
+int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* stream);
 
 #ifdef __cplusplus
 }

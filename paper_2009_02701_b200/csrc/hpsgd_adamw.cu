@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kAdamThreads = 128;
 constexpr int kChunk = kAdamThreads * 8;       // elements a block handles: eight 8-bit blocks
-constexpr int kSpanChunks = 4;
+constexpr int kSpanChunks = 2;
 constexpr int kMaxItems = 360;                 // what 32764 bytes of kernel parameters hold
 
 // Constants of the element's random bits: frac(sqrt 2, 3, 5) * 2^32 with the low bit set.
@@ -205,8 +205,9 @@ __device__ __forceinline__ void round_second(float x0, float x1, uint32_t rnd0, 
         s = add2(s, less);
         n = add2(n, less);
     }
-    // u = (16 random bits + 0.5) / 2^16, first as 1 + u
-    const pair u = add2(make_pair(__uint_as_float(0x3F800040u | (rnd0 << 7 & 0x7FFF80u)), __uint_as_float(0x3F800040u | (rnd1 << 7 & 0x7FFF80u))), both(-1.f));
+    // u = (16 random bits + 0.5) / 2^16: the bits below an exponent of 23 are 2^23 + bits, and the sum below is exact
+    const pair u = fma2(make_pair(__uint_as_float(__byte_perm(rnd0, 0x4B00u, 0x5410)), __uint_as_float(__byte_perm(rnd1, 0x4B00u, 0x5410))),
+                        both(0x1p-16f), both(0x1p-17f - 128.f));
     const pair lhs = mul2(u, fma2(both(2.f), n, both(1.f)));
     const pair rhs = mul2(fma2(both(-1.f), n, s), add2(n, s));
     float l0, l1, r0, r1;
@@ -262,15 +263,14 @@ __device__ __forceinline__ float reciprocal_approx(float x)
     return y;
 }
 
-// Largest of eight magnitudes; NaN if one of them is.
-__device__ __forceinline__ float top8(const f8& x)
+// Smallest of eight numbers >= 0.
+__device__ __forceinline__ float bottom8(const f8& x)
 {
     float a, b, c;
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]));
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x.v[3]), "f"(x.v[4]), "f"(x.v[5]));
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(c) : "f"(x.v[6]), "f"(x.v[7]), "f"(a));
-    asm("max.NaN.abs.f32 %0, %1, %2, %2;" : "=f"(a) : "f"(b), "f"(c));
-    return a;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x.v[3]), "f"(x.v[4]), "f"(x.v[5]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(c) : "f"(x.v[6]), "f"(x.v[7]), "f"(a));
+    return fminf(b, c);
 }
 
 // ---------------------------------------------------------------------------- the step
@@ -291,10 +291,10 @@ struct Share {
 // The block's codes and scales from its new moments m and r = sqrt(v) (zeros behind the end of the tensor).
 __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t* rnd, int& mb, int& vb, uint2& mc, uint2& vc)
 {
-    const uint32_t half = threadIdx.x & 16 ? 0xFFFF0000u : 0xFFFFu;       // the 16 lanes that hold the block
-    mb = scale_byte(__uint_as_float(__reduce_max_sync(half, __float_as_uint(top8(m)))));
-    vb = scale_byte(__uint_as_float(__reduce_max_sync(half, __float_as_uint(top8(r)))));
-    uint32_t cm[8], cr[8], low = 0xFFFFFFFFu;
+    mb = scale_byte(__uint_as_float(block_top(__float_as_uint(top8(m)), 0xFFFFFFFFu)));
+    vb = scale_byte(__uint_as_float(block_top(__float_as_uint(top8(r)), 0xFFFFFFFFu)));
+    uint32_t cm[8], cr[8];
+    float low;
     f8 x;
     {
         const pair fm = both(code_factor(mb)), fr = both(code_factor(vb));
@@ -308,10 +308,9 @@ __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t
 #pragma unroll
         for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], fr);
         x = to_values(y);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) low = min(low, __float_as_uint(x.v[q]));
+        low = bottom8(x);
     }
-    if (max(mb, vb) <= 133 && low >= 0x800000u) {
+    if (max(mb, vb) <= 133 && __float_as_uint(low) >= 0x800000u) {
 #pragma unroll
         for (int q = 0; q < 8; q += 2) round_second<false>(x.v[q], x.v[q + 1], rnd[q], rnd[q + 1], cr[q], cr[q + 1]);
     } else {
@@ -324,9 +323,9 @@ __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t
                 tm = max(tm, __float_as_uint(finite_magnitude(m.v[q])));
                 tr = max(tr, __float_as_uint(finite_magnitude(r.v[q])));
             }
-            __syncwarp(half);
-            mb = scale_byte(__uint_as_float(__reduce_max_sync(half, tm)));
-            vb = scale_byte(__uint_as_float(__reduce_max_sync(half, tr)));
+            const uint32_t half = threadIdx.x & 16 ? 0xFFFF0000u : 0xFFFFu;       // the whole block is here, the warp need not be
+            mb = scale_byte(__uint_as_float(block_top(tm, half)));
+            vb = scale_byte(__uint_as_float(block_top(tr, half)));
         }
         const float em = excess(mb), er = excess(vb), fm = code_factor(mb), fr = code_factor(vb);
 #pragma unroll
@@ -343,28 +342,84 @@ __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t
     vc = gather8(cr);
 }
 
+// Eight values as they are stored, so that a group can be requested while the one before it is worked on.
+template <typename T>
+struct Stored;
+template <>
+struct Stored<float> {
+    f8 x;
+    __device__ __forceinline__ void load(const float* p) { x = load8(p); }
+    __device__ __forceinline__ f8 values() const { return x; }
+};
+template <>
+struct Stored<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p)
+    {
+        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    }
+    __device__ __forceinline__ f8 values() const
+    {
+        f8 x;
+        widen_pair(u.x, x.v[0], x.v[1]);
+        widen_pair(u.y, x.v[2], x.v[3]);
+        widen_pair(u.z, x.v[4], x.v[5]);
+        widen_pair(u.w, x.v[6], x.v[7]);
+        return x;
+    }
+};
+
+// What a thread reads for one group with 8-bit moments.
+template <typename P, typename G>
+struct Group8 {
+    Stored<P> p;
+    Stored<G> g;
+    uint2 mc, vc;
+    uint32_t mb, vb;
+    __device__ __forceinline__ void load(const Share& it, int o)
+    {
+        p.load(static_cast<const P*>(it.p) + o);
+        g.load(static_cast<const G*>(it.g) + o);
+        const uint8_t *m = static_cast<const uint8_t*>(it.m) + o, *v = static_cast<const uint8_t*>(it.v) + o;
+        asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(mc.x), "=r"(mc.y) : "l"(m));
+        asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(vc.x), "=r"(vc.y) : "l"(v));
+        asm volatile("ld.global.u8 %0, [%1];" : "=r"(mb) : "l"(it.ms + o / kBlock));
+        asm volatile("ld.global.u8 %0, [%1];" : "=r"(vb) : "l"(it.vs + o / kBlock));
+    }
+};
+
 // One group of eight per thread, `left` of them inside the tensor, at elements o.. of the block's share.  All threads of a warp come
-// here.  FULL: the whole block has eight elements a thread and wide accesses, which leaves no branch in the way of the loads.
+// here.  FULL: the whole block has eight elements a thread and wide accesses, which leaves no branch in the way of the loads; with
+// 8-bit moments they have been made already (`ready`).
 template <typename P, typename G, bool B8, bool FULL>
-__device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, float c, int o, int left)
+__device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, float c, int o, int left, const Group8<P, G>* ready = nullptr)
 {
     const bool wide = FULL || (it.wide && left == 8);
     P* const pp = static_cast<P*>(it.p) + o;
-    f8 p = load_some(pp, wide, left);
-    const f8 g = load_some(static_cast<const G*>(it.g) + o, wide, left);
-    f8 m, v, r;                                    // r = sqrt(v), which the step divides by and the 8-bit form keeps
+    f8 p, g, m, v, r;                              // r = sqrt(v), which the step divides by and the 8-bit form keeps
     uint2 mc, vc;
     int mb = 0, vb = 0;
-    if constexpr (B8) {
-        mc = load_codes(static_cast<const uint8_t*>(it.m) + o, wide, left);
-        vc = load_codes(static_cast<const uint8_t*>(it.v) + o, wide, left);
-        if (FULL || left > 0) {
-            mb = it.ms[o / kBlock];
-            vb = it.vs[o / kBlock];
-        }
+    if constexpr (B8 && FULL) {
+        p = ready->p.values();
+        g = ready->g.values();
+        mc = ready->mc;
+        vc = ready->vc;
+        mb = (int)ready->mb;
+        vb = (int)ready->vb;
     } else {
-        m = load_some(static_cast<const float*>(it.m) + o, wide, left);
-        v = load_some(static_cast<const float*>(it.v) + o, wide, left);
+        p = load_some(pp, wide, left);
+        g = load_some(static_cast<const G*>(it.g) + o, wide, left);
+        if constexpr (B8) {
+            mc = load_codes(static_cast<const uint8_t*>(it.m) + o, wide, left);
+            vc = load_codes(static_cast<const uint8_t*>(it.v) + o, wide, left);
+            if (left > 0) {
+                mb = it.ms[o / kBlock];
+                vb = it.vs[o / kBlock];
+            }
+        } else {
+            m = load_some(static_cast<const float*>(it.m) + o, wide, left);
+            v = load_some(static_cast<const float*>(it.v) + o, wide, left);
+        }
     }
     if (!finite(c)) return;                        // the whole grid: nothing of the step happens
 
@@ -412,18 +467,19 @@ __device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, fl
     if constexpr (B8 || kPB) {
         const uint64_t q0 = it.rng + (uint64_t)o;
         const uint32_t low = (uint32_t)q0, turn = (hy.key1 + (uint32_t)(q0 >> 32) * kN3) * kN2;
-        if (low <= 0xFFFFFFF8u) {
+        if ((low & 7u) == 0) {                     // the position is one bit operation away from the first's
 #pragma unroll
-            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, turn);
-        } else {                                   // the position's upper half changes within the eight
+            for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low ^ hy.key0, q, turn);
+        } else {                                   // its upper half may change within the eight
 #pragma unroll
             for (int q = 0; q < 8; ++q) rnd[q] = random_bits(low + q, hy.key0, low + q < low ? turn + kN3 * kN2 : turn);
         }
     }
     if constexpr (kPB) {
+        const bool all = finite(top8(p));
 #pragma unroll
         for (int q = 0; q < 8; ++q)                // the upper half of the pattern is what is kept
-            if (finite(p.v[q])) p.v[q] = __uint_as_float(__float_as_uint(p.v[q]) + (rnd[q] * kN2 >> 16));
+            if (all || finite(p.v[q])) p.v[q] = __uint_as_float(__float_as_uint(p.v[q]) + (rnd[q] * kN2 >> 16));
         store_upper(pp, p, wide, left);
     } else {
         store_some(pp, p, wide, left);
@@ -446,7 +502,7 @@ __device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, fl
 
 // Block b handles `span` elements, a whole number of chunks, of one tensor.
 template <int CAP, typename P, typename G, bool B8>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper hy)
+__global__ void __launch_bounds__(kAdamThreads, B8 ? 6 : 7) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper hy)
 {
     const Item& it = table.item[find_item(table, blockIdx.x)];
     const float c = hy.scale ? *hy.scale : 1.f;
@@ -463,11 +519,24 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     sh.rng = it.rng + (uint64_t)at;
     sh.keep = it.keep;
     sh.wide = it.wide;
-    for (int s = 0; s < here; s += kChunk) {
-        const int o = s + threadIdx.x * 8;
-        if (sh.wide && here - s >= kChunk) adamw_group<P, G, B8, true>(sh, hy, c, o, 8);
-        else adamw_group<P, G, B8, false>(sh, hy, c, o, max(0, min(8, here - o)));
+    const int tid8 = threadIdx.x * 8;
+    if constexpr (B8) {
+        if (sh.wide && here == hy.span) {
+            Group8<P, G> now, next;
+            now.load(sh, tid8);
+#pragma unroll 1
+            for (int s = tid8; s < here; s += kChunk) {
+                if (s + kChunk < here) next.load(sh, s + kChunk);
+                adamw_group<P, G, true, true>(sh, hy, c, s, 8, &now);
+                now = next;
+            }
+            return;
+        }
+    } else if (sh.wide && here == hy.span) {
+        adamw_group<P, G, false, true>(sh, hy, c, tid8, 8);
+        return;
     }
+    for (int s = 0; s < here; s += kChunk) adamw_group<P, G, B8, false>(sh, hy, c, s + tid8, max(0, min(8, here - s - tid8)));
 }
 
 // ---------------------------------------------------------------------------- the norm
@@ -595,7 +664,9 @@ template <int CAP, typename P, typename G, bool B8>
 int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, Hyper hy, int sms, cudaStream_t s)
 {
     // With 8-bit moments finding the tensor and its addresses is a tenth of a block's instructions if it handles one chunk; with
-    // enough chunks to fill the device all the same, a block takes kSpanChunks of them.
+    // enough chunks to fill the device all the same, a block takes two and requests the second while it works on the first
+    // (138 M elements in bf16: two 364, four 399 us; 25.6 M in fp32 with its norm: 112, 121 us).
+    // With 32-bit moments the kernel waits for HBM whatever a block takes.
     int64_t total = 0;
     for (int k = 0; k < n; ++k) total += t[k].n;
     hy.span = B8 && total >= (int64_t)kSpanChunks * kChunk * sms * 16 ? kSpanChunks * kChunk : kChunk;

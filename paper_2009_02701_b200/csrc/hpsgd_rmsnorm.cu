@@ -1,0 +1,368 @@
+// Root-mean-square norm: residual addition, normalisation and 8-bit output in one pass; its gradients in one pass and a
+// short sum.
+//
+// Bound by HBM: 7 bytes an element forward (bf16 in, residual in, sum out, codes out), 8 backward.  A row is held in the
+// registers of 32 to 512 threads, eight consecutive columns a thread and group, so it is read once; 16 neighbouring threads hold a
+// 128-column block of the output, whose scale is then a matter of shuffles.
+#include "hpsgd_ops_common.cuh"
+
+namespace hpsgd {
+namespace ops {
+
+HPSGD_HIDDEN int check_fp8(const char* what, const char* name, const void* q, const void* s, int64_t* ld, int64_t* lds, int64_t rows, int64_t cols);
+
+namespace {
+
+constexpr int64_t kMaxCols = 16384;
+
+// Sum over the T threads of a row; T <= 32 within the warp, else through shared memory (one value per warp, two buffers in turn, so
+// that one barrier a row is enough).
+template <int T>
+__device__ __forceinline__ float row_sum(float x, float (*buf)[32], int turn)
+{
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    if constexpr (T > 32) {
+        constexpr int kWarps = T / 32;
+        const int warp = threadIdx.x >> 5, first = warp / kWarps * kWarps;
+        if ((threadIdx.x & 31) == 0) buf[turn][warp] = x;
+        __syncthreads();
+        x = buf[turn][first];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) x += buf[turn][first + w];
+    }
+    return x;
+}
+
+// ---------------------------------------------------------------------------- forward
+struct Forward {
+    int64_t rows, cols, ldx, ldres, ldh, ldy, ldy8, ldys;
+    const void* x;
+    const void* res;
+    const void* w;
+    void* h;
+    void* y;
+    uint8_t* y8;
+    uint8_t* ys;
+    float* rstd;
+    float eps, inv_cols;
+    bool wide, wide_w;
+};
+
+// T threads a row, V groups of eight a thread, R = threads of a block / T rows a block.
+template <typename X, typename W, int T, int V>
+__global__ void __launch_bounds__(T < 128 ? 128 : T) rmsnorm_forward_kernel(const Forward a)
+{
+    __shared__ float buf[1][32];
+    constexpr int kRows = T < 128 ? 128 / T : 1;
+    const int t = threadIdx.x % T;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / T;
+    const bool in = row < a.rows;
+    const X* const xp = static_cast<const X*>(a.x) + row * a.ldx;
+    f8 f[V], r[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
+        f[k] = load_some(xp + c, a.wide && left == 8, left);
+        if (a.res) r[k] = load_some(static_cast<const X*>(a.res) + row * a.ldres + c, a.wide && left == 8, left);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
+        if (a.res) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float s = __fadd_rn(f[k].v[q], r[k].v[q]);
+                f[k].v[q] = sizeof(X) == 2 ? __bfloat162float(__float2bfloat16_rn(s)) : s;
+            }
+            store_some(static_cast<X*>(a.h) + row * a.ldh + c, f[k], a.wide && left == 8, left);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) ss = __fmaf_rn(f[k].v[q], f[k].v[q], ss);
+    }
+    ss = row_sum<T>(ss, buf, 0);
+    const float rstd = __frcp_rn(__fsqrt_rn(__fmaf_rn(ss, a.inv_cols, a.eps)));
+    if (in && t == 0 && a.rstd) a.rstd[row] = rstd;
+    const int blocks = (int)((a.cols + kBlock - 1) / kBlock), words4 = (blocks + 3) / 4 * 4, pad = (int)((a.cols + 15) / 16 * 16);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
+        const f8 w = load_some(static_cast<const W*>(a.w) + c, a.wide_w && left == 8, left);
+        f8 y;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y.v[q] = __fmul_rn(__fmul_rn(f[k].v[q], rstd), w.v[q]);
+        if (left < 8) {                               // zeros behind the last column, even in a row whose rstd is NaN
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q >= left) y.v[q] = 0.f;
+        }
+        if (a.y) store_some(static_cast<X*>(a.y) + row * a.ldy + c, y, a.wide && left == 8, left);
+        if (a.y8) {
+            const int byte = block_scale(y);
+            if (in && c < pad) *reinterpret_cast<uint2*>(a.y8 + row * a.ldy8 + c) = encode_nearest(y, byte);
+            const int b = c / kBlock;                 // a row's threads cover whole words of four blocks, so the padding comes with them
+            const int upper = __shfl_down_sync(0xFFFFFFFFu, byte, 16);
+            if (in && (threadIdx.x & 31) == 0 && b < words4)
+                *reinterpret_cast<uint16_t*>(a.ys + scale_index(b, row, a.ldys)) = (uint16_t)(byte | upper << 8);
+        }
+    }
+}
+
+template <typename X, typename W, int T, int V>
+int forward_launch(const Forward& a, cudaStream_t s)
+{
+    constexpr int kRows = T < 128 ? 128 / T : 1;
+    const int64_t blocks = (a.rows + kRows - 1) / kRows;
+    if (blocks > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "hpsgd_rmsnorm_forward: too many rows");
+    rmsnorm_forward_kernel<X, W, T, V><<<(unsigned)blocks, T < 128 ? 128 : T, 0, s>>>(a);
+    return launched("hpsgd_rmsnorm_forward");
+}
+
+template <typename X, typename W>
+int forward_types(const Forward& a, cudaStream_t s)
+{
+    // a row's threads cover at least 512 columns (whole words of scales)
+    if (a.cols <= 512) return forward_launch<X, W, 64, 1>(a, s);
+    if (a.cols <= 1024) return forward_launch<X, W, 128, 1>(a, s);
+    if (a.cols <= 2048) return forward_launch<X, W, 256, 1>(a, s);
+    if (a.cols <= 4096) return forward_launch<X, W, 512, 1>(a, s);
+    if (a.cols <= 8192) return forward_launch<X, W, 512, 2>(a, s);
+    return forward_launch<X, W, 512, 4>(a, s);
+}
+
+// ---------------------------------------------------------------------------- backward
+struct Backward {
+    int64_t rows, cols, ldh, lddy, lddres, lddx;
+    const void* h;
+    const void* w;
+    const float* rstd;
+    const void* dy;
+    const void* dres;
+    void* dx;
+    float* part;           // [blocks][cols]
+    float inv_cols;
+    bool wide, wide_w;
+};
+
+constexpr int kBackBlocks = 592;      // partial sums of dweight: four blocks on each of 148 SMs
+
+// A block takes rows block, block + grid, ...; a thread's columns stay the same from row to row, so their dweight is added in registers.
+// With one group a thread the next row's values are requested before the present row's sum is waited for; with two, the registers
+// go to the row itself; with four, the row and the weights are read a second time behind the sum, from L1 and L2.
+template <typename X, typename W, int T, int V>
+__global__ void __launch_bounds__(T) rmsnorm_backward_kernel(const Backward a)
+{
+    __shared__ float buf[2][32];
+    constexpr bool kAhead = V == 1, kKeep = V <= 2;
+    const int t = threadIdx.x;
+    f8 w[V], dw[V], h[V], dy[V];
+    const auto left = [&](int k) { return max(0, min(8, (int)a.cols - (k * T + t) * 8)); };
+    const auto load_w = [&](int k) { return load_some(static_cast<const W*>(a.w) + (k * T + t) * 8, a.wide_w && left(k) == 8, left(k)); };
+    const auto fetch = [&](const void* p, int64_t ld, int64_t r, int k) {
+        return load_some(static_cast<const X*>(p) + r * ld + (k * T + t) * 8, a.wide && left(k) == 8, left(k));
+    };
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        if (kKeep) w[k] = load_w(k);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) dw[k].v[q] = 0.f;
+    }
+    int64_t row = blockIdx.x;                      // the grid has no more blocks than there are rows
+    f8 nh = {}, ndy = {};
+    float next_rstd = 0.f;
+    if (kAhead) {
+        nh = fetch(a.h, a.ldh, row, 0);
+        ndy = fetch(a.dy, a.lddy, row, 0);
+        next_rstd = a.rstd[row];
+    }
+    for (int turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float rs = kAhead ? next_rstd : a.rstd[row];
+        f8 dres[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            if (kKeep) h[k] = kAhead ? nh : fetch(a.h, a.ldh, row, k);
+            if (kKeep) dy[k] = kAhead ? ndy : fetch(a.dy, a.lddy, row, k);
+            if (kAhead && a.dres) dres[k] = fetch(a.dres, a.lddres, row, k);
+        }
+        if (kAhead && row + gridDim.x < a.rows) {
+            nh = fetch(a.h, a.ldh, row + gridDim.x, 0);
+            ndy = fetch(a.dy, a.lddy, row + gridDim.x, 0);
+            next_rstd = a.rstd[row + gridDim.x];
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const f8 wk = kKeep ? w[k] : load_w(k), hk = kKeep ? h[k] : fetch(a.h, a.ldh, row, k), dk = kKeep ? dy[k] : fetch(a.dy, a.lddy, row, k);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float xn = __fmul_rn(hk.v[q], rs);
+                dw[k].v[q] = __fmaf_rn(dk.v[q], xn, dw[k].v[q]);
+                dot = __fmaf_rn(__fmul_rn(dk.v[q], wk.v[q]), xn, dot);
+            }
+        }
+        const float mean = __fmul_rn(row_sum<T>(dot, buf, turn), a.inv_cols);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const f8 wk = kKeep ? w[k] : load_w(k), hk = kKeep ? h[k] : fetch(a.h, a.ldh, row, k), dk = kKeep ? dy[k] : fetch(a.dy, a.lddy, row, k);
+            if (!kAhead && a.dres) dres[k] = fetch(a.dres, a.lddres, row, k);
+            f8 x;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float xn = __fmul_rn(hk.v[q], rs);
+                x.v[q] = __fmul_rn(__fmaf_rn(-xn, mean, __fmul_rn(dk.v[q], wk.v[q])), rs);
+                if (a.dres) x.v[q] = __fadd_rn(x.v[q], dres[k].v[q]);
+            }
+            store_some(static_cast<X*>(a.dx) + row * a.lddx + (k * T + t) * 8, x, a.wide && left(k) == 8, left(k));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < left(k)) a.part[(int64_t)blockIdx.x * a.cols + (k * T + t) * 8 + q] = dw[k].v[q];
+}
+
+// dweight[c] = sum of the blocks' partial sums, in an order that depends on their number alone: 8 threads a column.
+__global__ void __launch_bounds__(256) dweight_kernel(const float* part, float* dweight, int64_t cols, int blocks)
+{
+    __shared__ float sum[8][32];
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (c < cols)
+#pragma unroll 4
+        for (int b = y; b < blocks; b += 8) s += part[(int64_t)b * cols + c];
+    sum[y][lane] = s;
+    __syncthreads();
+    if (y == 0 && c < cols) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) s += sum[k][lane];
+        dweight[c] = s;
+    }
+}
+
+template <typename X, typename W, int T, int V>
+int backward_launch(const Backward& a, float* dweight, cudaStream_t s)
+{
+    const int blocks = (int)(a.rows < kBackBlocks ? a.rows : kBackBlocks);
+    rmsnorm_backward_kernel<X, W, T, V><<<blocks, T, 0, s>>>(a);
+    OPS_TRY(launched("hpsgd_rmsnorm_backward"));
+    dweight_kernel<<<(unsigned)((a.cols + 31) / 32), 256, 0, s>>>(a.part, dweight, a.cols, blocks);
+    return launched("hpsgd_rmsnorm_backward");
+}
+
+template <typename X, typename W>
+int backward_types(const Backward& a, float* dweight, cudaStream_t s)
+{
+    if (a.cols <= 256) return backward_launch<X, W, 32, 1>(a, dweight, s);
+    if (a.cols <= 512) return backward_launch<X, W, 64, 1>(a, dweight, s);
+    if (a.cols <= 1024) return backward_launch<X, W, 128, 1>(a, dweight, s);
+    if (a.cols <= 2048) return backward_launch<X, W, 256, 1>(a, dweight, s);
+    if (a.cols <= 4096) return backward_launch<X, W, 512, 1>(a, dweight, s);
+    if (a.cols <= 8192) return backward_launch<X, W, 512, 2>(a, dweight, s);
+    return backward_launch<X, W, 512, 4>(a, dweight, s);
+}
+
+int check_sizes(const char* what, int64_t rows, int64_t cols, int dtype, int weight_dtype)
+{
+    if (rows < 0 || cols < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
+    if ((dtype != HPSGD_F32 && dtype != HPSGD_BF16) || (weight_dtype != HPSGD_F32 && weight_dtype != HPSGD_BF16))
+        return report(HPSGD_E_BADARG, "%s: unknown dtype", what);
+    if (cols > kMaxCols) return report(HPSGD_E_UNSUPPORTED, "%s: at most %lld columns", what, (long long)kMaxCols);
+    if (rows > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "%s: too many rows", what);
+    return HPSGD_OK;
+}
+
+int check_rows(const char* what, const char* name, const void* p, int64_t* ld, int64_t cols, int dtype, bool* wide)
+{
+    const int64_t esz = dtype == HPSGD_F32 ? 4 : 2, unit = esz * 8;
+    if (!p) return HPSGD_OK;
+    if (*ld == 0) *ld = cols;
+    if (*ld < cols) return report(HPSGD_E_BADARG, "%s: the stride of %s is below cols", what, name);
+    if (!aligned(p, esz)) return report(HPSGD_E_BADARG, "%s: %s is not aligned to its elements", what, name);
+    *wide = *wide && aligned(p, unit) && *ld * esz % unit == 0;
+    return HPSGD_OK;
+}
+
+}  // namespace
+}  // namespace ops
+}  // namespace hpsgd
+
+using namespace hpsgd;
+using namespace hpsgd::ops;
+
+extern "C" {
+
+int hpsgd_rmsnorm_forward(const hpsgd_rmsnorm_forward_args* args, void* stream)
+{
+    const char* what = "hpsgd_rmsnorm_forward";
+    if (!args) return report(HPSGD_E_BADARG, "%s: args is NULL", what);
+    hpsgd_rmsnorm_forward_args p = *args;
+    OPS_TRY(check_sizes(what, p.rows, p.cols, p.dtype, p.weight_dtype));
+    if (!(p.eps >= 0.0) || !std::isfinite((float)p.eps)) return report(HPSGD_E_BADARG, "%s: eps must be >= 0", what);
+    if (p.rows == 0 || p.cols == 0) return HPSGD_OK;
+    if (!p.x || !p.weight) return report(HPSGD_E_BADARG, "%s: x or weight is NULL", what);
+    if (!p.residual != !p.h) return report(HPSGD_E_BADARG, "%s: residual and h go together", what);
+    if (!p.y && !p.y8) return report(HPSGD_E_BADARG, "%s: no output is asked for", what);
+    if (!aligned(p.weight, p.weight_dtype == HPSGD_F32 ? 4 : 2) || !aligned(p.rstd, 4)) return report(HPSGD_E_BADARG, "%s: weight or rstd is not aligned to its elements", what);
+    Forward a{};
+    a.wide = true;
+    OPS_TRY(check_rows(what, "x", p.x, &p.ldx, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "residual", p.residual, &p.ldres, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "h", p.h, &p.ldh, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "y", p.y, &p.ldy, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_fp8(what, "y8", p.y8, p.y_scale, &p.ldy8, &p.ldys, p.rows, p.cols));
+    int sms = 0;
+    OPS_TRY(device_sms(&sms));
+    a.rows = p.rows; a.cols = p.cols; a.ldx = p.ldx; a.ldres = p.ldres; a.ldh = p.ldh; a.ldy = p.ldy; a.ldy8 = p.ldy8; a.ldys = p.ldys;
+    a.x = p.x; a.res = p.residual; a.w = p.weight; a.h = p.h; a.y = p.y; a.y8 = static_cast<uint8_t*>(p.y8); a.ys = p.y_scale; a.rstd = p.rstd;
+    a.eps = (float)p.eps;
+    a.inv_cols = (float)(1.0 / (double)p.cols);
+    a.wide_w = aligned(p.weight, p.weight_dtype == HPSGD_F32 ? 32 : 16);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p.dtype == HPSGD_F32) return p.weight_dtype == HPSGD_F32 ? forward_types<float, float>(a, s) : forward_types<float, __nv_bfloat16>(a, s);
+    return p.weight_dtype == HPSGD_F32 ? forward_types<__nv_bfloat16, float>(a, s) : forward_types<__nv_bfloat16, __nv_bfloat16>(a, s);
+}
+
+size_t hpsgd_rmsnorm_backward_bytes(int64_t rows, int64_t cols)
+{
+    if (rows <= 0 || cols <= 0 || cols > kMaxCols) return 0;
+    return (size_t)(rows < kBackBlocks ? rows : kBackBlocks) * (size_t)cols * sizeof(float);
+}
+
+int hpsgd_rmsnorm_backward(const hpsgd_rmsnorm_backward_args* args, void* stream)
+{
+    const char* what = "hpsgd_rmsnorm_backward";
+    if (!args) return report(HPSGD_E_BADARG, "%s: args is NULL", what);
+    hpsgd_rmsnorm_backward_args p = *args;
+    OPS_TRY(check_sizes(what, p.rows, p.cols, p.dtype, p.weight_dtype));
+    if (p.cols == 0) return HPSGD_OK;
+    if (!p.dweight || !aligned(p.dweight, 4)) return report(HPSGD_E_BADARG, "%s: dweight is NULL or not 4-byte aligned", what);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int sms = 0;
+    if (p.rows == 0) {
+        OPS_TRY(device_sms(&sms));
+        OPS_CUDA(cudaMemsetAsync(p.dweight, 0, (size_t)p.cols * 4, s));
+        return HPSGD_OK;
+    }
+    if (!p.h || !p.weight || !p.rstd || !p.dy || !p.dx) return report(HPSGD_E_BADARG, "%s: h, weight, rstd, dy or dx is NULL", what);
+    if (!p.workspace || !aligned(p.workspace, 16)) return report(HPSGD_E_BADARG, "%s: workspace is NULL or not 16-byte aligned", what);
+    if (!aligned(p.weight, p.weight_dtype == HPSGD_F32 ? 4 : 2) || !aligned(p.rstd, 4)) return report(HPSGD_E_BADARG, "%s: weight or rstd is not aligned to its elements", what);
+    Backward a{};
+    a.wide = true;
+    OPS_TRY(check_rows(what, "h", p.h, &p.ldh, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "dy", p.dy, &p.lddy, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "dres", p.dres, &p.lddres, p.cols, p.dtype, &a.wide));
+    OPS_TRY(check_rows(what, "dx", p.dx, &p.lddx, p.cols, p.dtype, &a.wide));
+    OPS_TRY(device_sms(&sms));
+    a.rows = p.rows; a.cols = p.cols; a.ldh = p.ldh; a.lddy = p.lddy; a.lddres = p.lddres; a.lddx = p.lddx;
+    a.h = p.h; a.w = p.weight; a.rstd = p.rstd; a.dy = p.dy; a.dres = p.dres; a.dx = p.dx; a.part = static_cast<float*>(p.workspace);
+    a.inv_cols = (float)(1.0 / (double)p.cols);
+    a.wide_w = aligned(p.weight, p.weight_dtype == HPSGD_F32 ? 32 : 16);
+    if (p.dtype == HPSGD_F32)
+        return p.weight_dtype == HPSGD_F32 ? backward_types<float, float>(a, p.dweight, s) : backward_types<float, __nv_bfloat16>(a, p.dweight, s);
+    return p.weight_dtype == HPSGD_F32 ? backward_types<__nv_bfloat16, float>(a, p.dweight, s) : backward_types<__nv_bfloat16, __nv_bfloat16>(a, p.dweight, s);
+}
+
+}  // extern "C"

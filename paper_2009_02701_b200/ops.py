@@ -9,9 +9,12 @@ import ctypes
 from . import binding as _b
 from .binding import _ci, _f64, _i64, _ptr, _stream, _u64, _vp
 
-__all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm"]
+__all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm",
+           "make_rmsnorm_forward", "hpsgd_rmsnorm_forward", "make_rmsnorm_backward", "hpsgd_rmsnorm_backward", "hpsgd_rmsnorm_backward_bytes",
+           "make_quantize_fp8", "hpsgd_quantize_fp8"]
 
 HPSGD_GRAD_NORM_WORKSPACE = 65536
+HPSGD_FP8 = 2
 
 
 class hpsgd_adamw_tensor(ctypes.Structure):
@@ -19,7 +22,29 @@ class hpsgd_adamw_tensor(ctypes.Structure):
                 ("n", _i64), ("rng_offset", _u64), ("weight_decay", _f64)]
 
 
+class hpsgd_rmsnorm_forward_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("eps", _f64), ("dtype", _ci), ("weight_dtype", _ci)] + \
+        [(n, _vp) for n in ("x", "residual", "weight", "h", "y", "y8", "y_scale", "rstd")] + \
+        [(n, _i64) for n in ("ldx", "ldres", "ldh", "ldy", "ldy8", "ldys")]
+
+
+class hpsgd_rmsnorm_backward_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("dtype", _ci), ("weight_dtype", _ci)] + \
+        [(n, _vp) for n in ("h", "weight", "rstd", "dy", "dres", "dx", "dweight", "workspace")] + \
+        [(n, _i64) for n in ("ldh", "lddy", "lddres", "lddx")]
+
+
+class hpsgd_quantize_fp8_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("dtype", _ci)] + \
+        [(n, _vp) for n in ("x", "x_scale", "q", "scale", "qt", "scale_t")] + \
+        [(n, _i64) for n in ("ldx", "ldxs", "ldq", "lds", "ldqt", "ldst")]
+
+
 SIGNATURES = {
+    "hpsgd_rmsnorm_forward": (_ci, [_vp, _vp]),
+    "hpsgd_rmsnorm_backward_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "hpsgd_rmsnorm_backward": (_ci, [_vp, _vp]),
+    "hpsgd_quantize_fp8": (_ci, [_vp, _vp]),
     "hpsgd_adamw_step": (_ci, [_vp, _ci, _ci, _ci, _ci, _f64, _f64, _f64, _f64, _i64, _u64, _vp, _vp]),
     "hpsgd_grad_norm": (_ci, [_vp, _ci, _ci, _f64, _vp, _vp, _vp]),
 }
@@ -63,3 +88,51 @@ def hpsgd_adamw_step(table, lr, beta1, beta2, eps, step, seed=0, grad_scale=None
 def hpsgd_grad_norm(table, max_norm, workspace, out, stream=None):
     return _b._check(_b.load().hpsgd_grad_norm(table.address, table.count, table.grad_dtype, max_norm, _ptr(workspace), _ptr(out),
                                                _stream(stream)))
+
+
+# ---- argument blocks -------------------------------------------------------------------
+class Args:
+    """A filled argument struct with its address, and what it points to."""
+
+    def __init__(self, struct, pointers, strides, **plain):
+        self.struct, self.keep = struct(), pointers
+        kinds = dict(struct._fields_)
+        for name, value in pointers.items():
+            setattr(self.struct, name, _ptr(value))
+        for name, value in {**strides, **plain}.items():
+            if name not in kinds or kinds[name] is _vp:
+                raise TypeError("not a field of %s: %s" % (struct.__name__, name))
+            setattr(self.struct, name, value)
+        self.address = ctypes.addressof(self.struct)
+
+
+def make_rmsnorm_forward(rows, cols, eps, dtype, x, weight, residual=None, h=None, y=None, y8=None, y_scale=None, rstd=None,
+                         weight_dtype=None, **strides):
+    return Args(hpsgd_rmsnorm_forward_args, dict(x=x, residual=residual, weight=weight, h=h, y=y, y8=y8, y_scale=y_scale, rstd=rstd), strides,
+                rows=rows, cols=cols, eps=eps, dtype=dtype, weight_dtype=dtype if weight_dtype is None else weight_dtype)
+
+
+def hpsgd_rmsnorm_forward(args, stream=None):
+    return _b._check(_b.load().hpsgd_rmsnorm_forward(args.address, _stream(stream)))
+
+
+def hpsgd_rmsnorm_backward_bytes(rows, cols):
+    return int(_b.load().hpsgd_rmsnorm_backward_bytes(rows, cols))
+
+
+def make_rmsnorm_backward(rows, cols, dtype, h, weight, rstd, dy, dx, dweight, workspace, dres=None, weight_dtype=None, **strides):
+    return Args(hpsgd_rmsnorm_backward_args, dict(h=h, weight=weight, rstd=rstd, dy=dy, dres=dres, dx=dx, dweight=dweight, workspace=workspace),
+                strides, rows=rows, cols=cols, dtype=dtype, weight_dtype=dtype if weight_dtype is None else weight_dtype)
+
+
+def hpsgd_rmsnorm_backward(args, stream=None):
+    return _b._check(_b.load().hpsgd_rmsnorm_backward(args.address, _stream(stream)))
+
+
+def make_quantize_fp8(rows, cols, dtype, x, q=None, scale=None, qt=None, scale_t=None, x_scale=None, **strides):
+    return Args(hpsgd_quantize_fp8_args, dict(x=x, x_scale=x_scale, q=q, scale=scale, qt=qt, scale_t=scale_t), strides,
+                rows=rows, cols=cols, dtype=dtype)
+
+
+def hpsgd_quantize_fp8(args, stream=None):
+    return _b._check(_b.load().hpsgd_quantize_fp8(args.address, _stream(stream)))

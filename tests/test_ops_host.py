@@ -106,3 +106,68 @@ def test_no_fallback_without_a_device():
 def test_tables_number_their_random_bits():
     t = hp.make_adamw_table([dict(ROW, n=5), dict(ROW, n=7), dict(ROW, n=1, rng_offset=1 << 40), dict(ROW, n=2)], 0, 0, 32)
     assert [x.rng_offset for x in t.array] == [0, 5, 1 << 40, (1 << 40) + 1]
+
+
+# ---------------------------------------------------------------------------------------------- norm and quantisation
+def norm_args(**change):
+    kw = dict(rows=4, cols=256, eps=1e-5, dtype=hp.HPSGD_BF16, x=A, weight=A, residual=A, h=A, y=A, y8=A, y_scale=A, rstd=A)
+    return hp.make_rmsnorm_forward(**{**kw, **change})
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(cols=-1), dict(dtype=9), dict(weight_dtype=9), dict(eps=-1.0), dict(eps=math.nan), dict(eps=1e60),
+                                    dict(x=None), dict(weight=None), dict(h=None), dict(residual=None), dict(y=None, y8=None, y_scale=None),
+                                    dict(y8=None), dict(y_scale=None), dict(x=A + 1), dict(weight=A + 1), dict(rstd=A + 2), dict(h=A + 1), dict(y=A + 1),
+                                    dict(y8=A + 8), dict(y_scale=A + 1), dict(ldx=255), dict(ldres=1), dict(ldh=255), dict(ldy=200), dict(ldy8=255),
+                                    dict(ldy8=264), dict(ldys=3)], ids=str)
+def test_norm_forward_refuses(change):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_rmsnorm_forward, norm_args(**change))
+
+
+def back_args(**change):
+    kw = dict(rows=4, cols=256, dtype=hp.HPSGD_F32, h=A, weight=A, rstd=A, dy=A, dx=A, dweight=A, workspace=A, dres=A)
+    return hp.make_rmsnorm_backward(**{**kw, **change})
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(cols=-1), dict(dtype=2), dict(weight_dtype=-1), dict(h=None), dict(weight=None), dict(rstd=None),
+                                    dict(dy=None), dict(dx=None), dict(dweight=None), dict(workspace=None), dict(workspace=A + 8), dict(dweight=A + 2),
+                                    dict(h=A + 2), dict(dy=A + 1), dict(dres=A + 2), dict(dx=A + 2), dict(ldh=255), dict(lddy=1), dict(lddres=255),
+                                    dict(lddx=255)], ids=str)
+def test_norm_backward_refuses(change):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_rmsnorm_backward, back_args(**change))
+
+
+def test_norm_limits():
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_rmsnorm_forward, norm_args(cols=16385))
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_rmsnorm_backward, back_args(cols=16385))
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_rmsnorm_forward, norm_args(rows=1 << 31))
+    assert hp.hpsgd_rmsnorm_backward_bytes(10, 100) == 4000 and hp.hpsgd_rmsnorm_backward_bytes(10 ** 6, 100) == 592 * 400
+    assert hp.hpsgd_rmsnorm_backward_bytes(0, 100) == 0 and hp.hpsgd_rmsnorm_backward_bytes(5, 20000) == 0
+    hp.hpsgd_rmsnorm_forward(norm_args(rows=0))          # nothing to do: no device is asked for
+    hp.hpsgd_rmsnorm_backward(back_args(cols=0))
+    lib = hp.load()
+    for call in (lib.hpsgd_rmsnorm_forward, lib.hpsgd_rmsnorm_backward, lib.hpsgd_quantize_fp8):
+        assert call(None, None) == hp.HPSGD_E_BADARG
+    with pytest.raises(TypeError):
+        norm_args(ldz=5)
+
+
+def quant_args(**change):
+    kw = dict(rows=200, cols=256, dtype=hp.HPSGD_F32, x=A, q=A, scale=A, qt=A, scale_t=A)
+    return hp.make_quantize_fp8(**{**kw, **change})
+
+
+@pytest.mark.parametrize("change", [dict(rows=-1), dict(cols=-1), dict(dtype=3), dict(x=None), dict(q=None, scale=None, qt=None, scale_t=None), dict(q=None),
+                                    dict(scale=None), dict(qt=None), dict(scale_t=None), dict(x=A + 2), dict(q=A + 8), dict(qt=A + 4), dict(scale=A + 1),
+                                    dict(scale_t=A + 2), dict(ldx=255), dict(ldq=255), dict(ldq=264), dict(ldqt=200), dict(lds=199), dict(ldst=255),
+                                    dict(dtype=hp.HPSGD_FP8, x_scale=A), dict(dtype=hp.HPSGD_FP8, q=None, scale=None),
+                                    dict(dtype=hp.HPSGD_FP8, q=None, scale=None, x_scale=A, x=A + 8),
+                                    dict(dtype=hp.HPSGD_FP8, q=None, scale=None, x_scale=A, ldx=255),
+                                    dict(dtype=hp.HPSGD_FP8, q=None, scale=None, x_scale=A, ldxs=100)], ids=str)
+def test_quantize_refuses(change):
+    refused(hp.HPSGD_E_BADARG, hp.hpsgd_quantize_fp8, quant_args(**change))
+
+
+def test_quantize_limits():
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_quantize_fp8, quant_args(rows=1 << 31))
+    hp.hpsgd_quantize_fp8(quant_args(rows=0))
+    hp.hpsgd_quantize_fp8(quant_args(cols=0))
