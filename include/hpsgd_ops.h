@@ -203,6 +203,49 @@ typedef struct hpsgd_quantize_fp8_args {
 } hpsgd_quantize_fp8_args;
 int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Matrix product of two matrices in the 8-bit block format.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * D[m, n] = sum over k of A[m, k] B[n, k]      A [M x K] and B [N x K] in the block format, D of d_dtype, row-major
+ * With x the input, w the weights [N x K] and dy the gradient of a layer's output, all three products of its training have this form:
+ * y = (x, w); dx = (dy, w transposed); dw = (dy transposed, x transposed), the transposes from hpsgd_quantize_fp8.  With M = 1 (one
+ * token) it streams the weights.
+ *   Every product is exact, and they are added in binary32 (on the tensor cores, in an order that depends on the sizes alone).
+ *   Values held as the NaN code make the results they enter NaN.
+ *   d_dtype       HPSGD_F32 or HPSGD_BF16 (rounded once)
+ *   accumulate    1: D += the product (HPSGD_F32 only), for gradients over several batches
+ *   ldd           elements from row to row of D, 0 = N; any alignment
+ *   lda, ldb, ldsa, ldsb   as in hpsgd_quantize_fp8
+ *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 for many sizes), 16-byte aligned, filled with zeros before
+ *                 its first use; every call leaves it ready for the next call of the same sizes.  Calls that share a workspace have
+ *                 to be ordered on one stream.  workspace_bytes: its size.
+ * K = 0 gives zeros.
+ * The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).
+ */
+typedef struct hpsgd_gemm_fp8_args {
+    int64_t M, N, K;
+    const void* a;
+    const uint8_t* a_scale;
+    const void* b;
+    const uint8_t* b_scale;
+    void* d;
+    void* workspace;
+    size_t workspace_bytes;
+    int64_t lda, ldsa, ldb, ldsb, ldd;
+    int d_dtype, accumulate;
+} hpsgd_gemm_fp8_args;
+size_t hpsgd_gemm_fp8_bytes(int64_t M, int64_t N, int64_t K);
+int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
+
+/*
+ * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
+ * since the last call (the results written since are incomplete; their workspaces have to be zeroed again), HPSGD_E_CUDA if the work
+ * failed.
+ */
+int hpsgd_ops_check(void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,7 @@ _UNITS = {
     "hpsgd_adamw.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_rmsnorm.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_quantize.cu": ["hpsgd_ops_common.cuh"],
+    "hpsgd_gemm.cu": ["hpsgd_ops_common.cuh"],
 }
 SOURCES = [os.path.join(CSRC, u) for u in _UNITS]
 # --fmad=false: the compiler never contracts a*b+c on its own; fused multiply-adds are

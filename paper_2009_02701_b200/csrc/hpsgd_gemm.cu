@@ -1,0 +1,533 @@
+// Matrix product of two matrices in the 8-bit block format on the fifth-generation tensor cores.
+//
+// D[m, n] = sum over blocks b of 2^(ea[m, b] + eb[n, b]) * sum over the block's 128 k of A[m, k] B[n, k].  The scales are powers
+// of two, so they are exactly the scale operands of the block-scaled tcgen05.mma (E8M0, one for each row and 32 k; the four
+// instructions of a 128-block name the same one), and the sums stay in tensor memory in binary32 from the first k to the last.
+//
+// B's rows (a layer's outputs) lie on the accumulator's 128 lanes and A's rows (tokens) on its columns: with one token a tile is
+// 128 x 16 and the kernel streams the weights, with many it is 128 x 256, and in either case 32 lanes hold 32 neighbouring outputs of
+// a token, so results leave in coalesced rows whatever N, the stride and the alignment are.
+//
+// One block per SM works through its tiles: a thread that keeps a ring of stages full by TMA (128 k of both operands a stage,
+// 128-byte swizzle), a warp that puts the scales beside them, a thread that issues the products, and four warps that empty
+// one accumulator while the next is filled.  Few tiles are split along k over the SMs; the last of a tile's blocks to finish adds the
+// parts in their order.
+#include "hpsgd_ops_common.cuh"
+
+#include <algorithm>
+#include <cuda.h>
+#include <mutex>
+
+namespace hpsgd {
+namespace ops {
+
+HPSGD_HIDDEN int check_fp8(const char* what, const char* name, const void* q, const void* s, int64_t* ld, int64_t* lds, int64_t rows, int64_t cols);
+
+namespace {
+
+constexpr int kSms = 148;                  // what work is divided by
+constexpr int kLanes = 128;                // rows of B in a tile
+constexpr int kStageK = 128;               // k of a stage: one scale block, one row of the 128-byte swizzle
+constexpr int kGemmThreads = 256;
+constexpr int kTicketBytes = 4096;         // four counters per tile that is split (fewer than kSms tiles)
+
+__device__ unsigned int g_gemm_timeouts;   // blocks whose wait ran out
+
+template <int BN>
+struct Shape {
+    static constexpr int kStages = BN <= 64 ? 8 : BN <= 128 ? 6 : 4;
+    static constexpr int kAtoms = BN <= 128 ? 1 : 2;                     // groups of 128 columns' scales
+    static constexpr int kBytesB = kLanes * kStageK, kBytesA = BN * kStageK, kBytesS = 512 * (1 + kAtoms);
+    static constexpr int kStageBytes = kBytesB + kBytesA;
+    static constexpr int kAccs = BN <= 128 ? 2 : 1;
+    static constexpr int kScaleCols = 4 * (1 + kAtoms);                  // tensor-memory columns of one group of scales
+    static constexpr int kCols = kAccs * BN + kStages * kScaleCols;
+    static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static constexpr int kSmem = 1024 + kStages * (kStageBytes + kBytesS) + 256;
+};
+
+struct GemmArgs {
+    int M, N, K;
+    int tiles_n, tiles, splits, per_split;     // k blocks of a split
+    const uint32_t* sa;
+    const uint32_t* sb;
+    int64_t ldsa, ldsb, ldd;
+    void* d;
+    int accumulate;
+    unsigned int* ticket;
+    float* part;
+};
+
+// ---------------------------------------------------------------------------- instructions
+__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+
+__device__ __forceinline__ uint64_t nanoseconds()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Wait for a phase, for two seconds at most.  Then, or as soon as another wait of the block has given up, false: the roles leave their
+// loops, the block frees its tensor memory and ends, and hpsgd_ops_check reports it.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* given_up)
+{
+    if (barrier_try(bar, parity)) return true;
+    const uint64_t start = nanoseconds();
+    for (uint32_t i = 0;; ++i) {
+        if (barrier_try(bar, parity)) return true;
+        if ((i & 255u) == 255u) {
+            if (*given_up) return false;
+            if (nanoseconds() - start > 2000000000ull) {
+                *given_up = 1;
+                return false;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+
+// Shared-memory descriptor of an operand whose rows are 128 bytes, swizzled: eight rows make a group of 1024 bytes.
+__device__ __forceinline__ uint64_t operand_descriptor(uint32_t address)
+{
+    return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// And of 32 rows of 16 bytes, one after the other, without swizzle: 128 rows' scales.
+__device__ __forceinline__ uint64_t scale_descriptor(uint32_t address)
+{
+    return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+// Instruction descriptor: E4M3 operands, both along k, N = BN, M = 128, E8M0 scales; `id` names the byte of the scale words.
+template <int BN>
+__device__ __forceinline__ uint32_t instruction(uint32_t id)
+{
+    return id << 4 | (uint32_t)(BN >> 3) << 17 | 1u << 23 | (uint32_t)(kLanes >> 4) << 24 | id << 29;
+}
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Sixteen accumulator columns of this thread's lane.
+__device__ __forceinline__ void load_columns(uint32_t tmem, float* x)
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(tmem));
+}
+
+// ---------------------------------------------------------------------------- the kernel
+// Unit u of a block's work: tile u / splits, part u % splits of its k blocks.
+struct Unit {
+    int n0, m0, k0, k1, tile, split;
+};
+template <int BN>
+__device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u)
+{
+    Unit x;
+    x.tile = u / a.splits;
+    x.split = u % a.splits;
+    x.n0 = x.tile % a.tiles_n * kLanes;
+    x.m0 = x.tile / a.tiles_n * BN;
+    const int blocks = (a.K + kStageK - 1) / kStageK;
+    x.k0 = x.split * a.per_split;
+    x.k1 = min(blocks, x.k0 + a.per_split);
+    return x;
+}
+
+template <typename D>
+__device__ __forceinline__ void store_result(const GemmArgs& a, int m, int n, float x)
+{
+    D* const p = static_cast<D*>(a.d) + (int64_t)m * a.ldd + n;
+    if (sizeof(D) == 4 && a.accumulate) x = __fadd_rn(load1(p), x);
+    store1(p, x);
+}
+
+template <int BN, typename D>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ GemmArgs a)
+{
+    using S = Shape<BN>;
+    extern __shared__ uint8_t raw[];
+    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* const scales = smem + S::kStages * S::kStageBytes;
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(scales + S::kStages * S::kBytesS);
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int given_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t full = smem_address(bars), empty = full + S::kStages * 8, acc_full = empty + S::kStages * 8, acc_empty = acc_full + S::kAccs * 8,
+                   drained = acc_empty + S::kAccs * 8;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            barrier_init(full + s * 8, 2);          // the loads' expectation and the scales
+            barrier_init(empty + s * 8, 1);
+        }
+        for (int s = 0; s < S::kAccs; ++s) {
+            barrier_init(acc_full + s * 8, 1);
+            barrier_init(acc_empty + s * 8, 4);
+        }
+        barrier_init(drained, 1);
+        given_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
+    const int units = a.tiles * a.splits;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+                const Unit x = unit_of<BN>(a, u);
+                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
+                    const int s = it % S::kStages;
+                    if (!(ok = barrier_wait(empty + s * 8, (it / S::kStages & 1) ^ 1, &given_up))) break;
+                    const uint32_t dst = smem_address(smem + s * S::kStageBytes), bar = full + s * 8;
+                    barrier_expect(bar, S::kStageBytes);
+                    tma_load(dst, &map_b, kb * kStageK, x.n0, bar);
+                    tma_load(dst + S::kBytesB, &map_a, kb * kStageK, x.m0, bar);
+                }
+            }
+            // giving up: the copies in flight still land (a stage whose scales never came completes no phase, so the wait is for time)
+            if (!ok) {
+                const uint64_t t = nanoseconds();
+                while (nanoseconds() - t < 10000000ull) {}
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int it = 0, fills = 0, done = 0;
+            bool ok = true;
+            for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++done) {
+                const Unit x = unit_of<BN>(a, u);
+                const int acc = done % S::kAccs;
+                if (!(ok = barrier_wait(acc_empty + acc * 8, (done / S::kAccs & 1) ^ 1, &given_up))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t sb = 0, sa = 0;
+                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
+                    const int s = it % S::kStages;
+                    if (!(ok = barrier_wait(full + s * 8, it / S::kStages & 1, &given_up))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (kb == x.k0 || (kb & 3) == 0) {
+                        // A group of four blocks' scales to a place of its own among kStages.  The place was last used kStages fills ago, so at
+                        // least kStages stages ago, and those products are done: this stage could not be full otherwise.
+                        sb = tmem_scales + fills++ % S::kStages * S::kScaleCols;
+                        sa = sb + 4;
+                        const uint32_t src = smem_address(scales + s * S::kBytesS);
+                        copy_scales(sb, scale_descriptor(src));
+#pragma unroll
+                        for (int t = 0; t < S::kAtoms; ++t) copy_scales(sa + 4 * t, scale_descriptor(src + 512 * (1 + t)));
+                    }
+                    const uint64_t db = operand_descriptor(smem_address(smem + s * S::kStageBytes)),
+                                   da = operand_descriptor(smem_address(smem + s * S::kStageBytes + S::kBytesB));
+                    const uint32_t id = instruction<BN>(kb & 3);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma(tmem + acc * BN, db + 2 * k, da + 2 * k, id, sb, sa, kb > x.k0 || k > 0);
+                    commit(empty + s * 8);
+                }
+                if (ok) commit(acc_full + acc * 8);
+            }
+            if (!ok) {                              // products in flight read shared memory: let them end
+                commit(drained);
+                const uint64_t t = nanoseconds();
+                while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
+            }
+        }
+    } else if (warp == 2) {
+        // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.  The next
+        // group's words are requested before this one's stage is waited for.
+        int it = 0;
+        bool ok = true;
+        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+            const Unit x = unit_of<BN>(a, u);
+            uint32_t w[1 + S::kAtoms][4];
+            const auto fetch = [&](int kb) {
+                const int64_t g = kb >> 2;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = lane + 32 * j;
+                    w[0][j] = x.n0 + r < a.N ? __ldg(a.sb + g * a.ldsb + x.n0 + r) : 0u;
+#pragma unroll
+                    for (int t = 0; t < S::kAtoms; ++t) w[1 + t][j] = x.m0 + 128 * t + r < a.M ? __ldg(a.sa + g * a.ldsa + x.m0 + 128 * t + r) : 0u;
+                }
+            };
+            fetch(x.k0);
+            for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
+                const int s = it % S::kStages;
+                ok = __all_sync(0xFFFFFFFFu, barrier_wait(empty + s * 8, (it / S::kStages & 1) ^ 1, &given_up));
+                if (!ok) break;
+                if (kb == x.k0 || (kb & 3) == 0) {
+                    uint4* const dst = reinterpret_cast<uint4*>(scales + s * S::kBytesS);
+#pragma unroll
+                    for (int t = 0; t < 1 + S::kAtoms; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    const int next = (kb | 3) + 1;
+                    if (next < x.k1) fetch(next);
+                }
+                __syncwarp();
+                if (lane == 0) barrier_arrive(full + s * 8);
+            }
+        }
+    } else if (warp >= 4) {
+        const int part = warp & 3;                  // the quarter of the lanes that this warp can read
+        int done = 0;
+        for (int u = blockIdx.x; u < units; u += gridDim.x, ++done) {
+            const Unit x = unit_of<BN>(a, u);
+            const int acc = done % S::kAccs;
+            const bool ok = barrier_wait(acc_full + acc * 8, done / S::kAccs & 1, &given_up);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t src = tmem + acc * BN + ((uint32_t)part << 21);
+            const int n = x.n0 + part * 32 + lane, cols = min(BN, a.M - x.m0);
+            float* const mine = a.part + ((int64_t)x.tile * a.splits + x.split) * (kLanes * BN) + part * 32 + lane;
+#pragma unroll 1
+            for (int c = 0; c < BN; c += 16) {
+                float v[16];
+                __syncwarp();
+                load_columns(src + c, v);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                if (a.splits > 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < cols) mine[(int64_t)(c + j) * kLanes] = v[j];
+                } else if (n < a.N) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < cols) store_result<D>(a, x.m0 + c + j, n, v[j]);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) barrier_arrive(acc_empty + acc * 8);
+            if (a.splits > 1) {
+                // The last of the tile's parts to finish adds them; each warp counts and adds for its own 32 lanes.
+                __threadfence();
+                __syncwarp();
+                unsigned int before = 0;
+                if (lane == 0) before = atomicAdd(a.ticket + x.tile * 4 + part, 1u);
+                before = __shfl_sync(0xFFFFFFFFu, before, 0);
+                if (before == (unsigned)(a.splits - 1)) {
+                    __threadfence();
+                    if (lane == 0) a.ticket[x.tile * 4 + part] = 0u;          // ready for the next call
+                    const float* const all = a.part + (int64_t)x.tile * a.splits * (kLanes * BN) + part * 32 + lane;
+                    if (n < a.N) {
+                        for (int c = 0; c < cols; ++c) {
+                            float sum = __ldcg(all + (int64_t)c * kLanes);
+                            for (int k = 1; k < a.splits; ++k) sum = __fadd_rn(sum, __ldcg(all + (int64_t)k * (kLanes * BN) + (int64_t)c * kLanes));
+                            store_result<D>(a, x.m0 + c, n, sum);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0 && given_up) atomicAdd(&g_gemm_timeouts, 1u);
+    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+}
+
+// ---------------------------------------------------------------------------- host side
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encoder(EncodeTiled* out)
+{
+    static std::mutex lock;
+    static EncodeTiled found = nullptr;
+    std::lock_guard<std::mutex> hold(lock);
+    if (!found) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult state;
+        OPS_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &state));
+        if (state != cudaDriverEntryPointSuccess || !fn) return report(HPSGD_E_CUDA, "cuTensorMapEncodeTiled is not available");
+        found = reinterpret_cast<EncodeTiled>(fn);
+    }
+    *out = found;
+    return HPSGD_OK;
+}
+
+// Boxes of `rows` rows of 128 bytes; what lies outside the matrix reads as zeros.
+int make_map(const char* what, CUtensorMap* map, const void* q, int64_t ld, int64_t rows, int64_t cols, int box)
+{
+    EncodeTiled encode;
+    OPS_TRY(encoder(&encode));
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t boxes[2] = {(cuuint32_t)kStageK, (cuuint32_t)box}, steps[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(q), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return report(HPSGD_E_CUDA, "%s: cuTensorMapEncodeTiled failed with %d", what, (int)r);
+    return HPSGD_OK;
+}
+
+struct Plan {
+    int bn, tiles_n, tiles, splits, per_split;
+};
+
+// Tokens' side of a tile: the least power of two that holds them all, 256 at most.  Splitting along k: as many parts as leave no SM
+// with nothing to do, of at least two k blocks each.
+Plan plan_of(int64_t M, int64_t N, int64_t K)
+{
+    Plan p{};
+    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+    p.tiles_n = (int)((N + kLanes - 1) / kLanes);
+    const int64_t tiles = p.tiles_n * ((M + p.bn - 1) / p.bn);
+    p.tiles = (int)tiles;
+    const int blocks = (int)((K + kStageK - 1) / kStageK);
+    p.splits = tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / tiles, blocks / 2)) : 1;
+    p.per_split = (blocks + p.splits - 1) / p.splits;
+    p.splits = (blocks + p.per_split - 1) / p.per_split;
+    return p;
+}
+
+size_t workspace_of(const Plan& p)
+{
+    return p.splits > 1 ? kTicketBytes + (size_t)p.tiles * p.splits * kLanes * p.bn * sizeof(float) : 0;
+}
+
+template <int BN, typename D>
+int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
+{
+    using S = Shape<BN>;
+    static bool set[64] = {};                       // per device: the shared-memory size has been opted into
+    int dev = 0;
+    OPS_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !set[dev]) {
+        OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        if (dev < 64) set[dev] = true;
+    }
+    const int64_t units = (int64_t)a.tiles * a.splits;
+    gemm_fp8_kernel<BN, D><<<(unsigned)std::min<int64_t>(units, sms), kGemmThreads, S::kSmem, s>>>(ma, mb, a);
+    return launched("hpsgd_gemm_fp8");
+}
+
+template <typename D>
+int launch_shape(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
+{
+    switch (bn) {
+    case 16: return launch<16, D>(ma, mb, a, sms, s);
+    case 32: return launch<32, D>(ma, mb, a, sms, s);
+    case 64: return launch<64, D>(ma, mb, a, sms, s);
+    case 128: return launch<128, D>(ma, mb, a, sms, s);
+    default: return launch<256, D>(ma, mb, a, sms, s);
+    }
+}
+
+}  // namespace
+}  // namespace ops
+}  // namespace hpsgd
+
+using namespace hpsgd;
+using namespace hpsgd::ops;
+
+extern "C" {
+
+size_t hpsgd_gemm_fp8_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (M <= 0 || N <= 0 || K <= 0 || M > 0x7FFFFFFF || N > 0x7FFFFFFF || K > 0x7FFFFFFF) return 0;
+    return workspace_of(plan_of(M, N, K));
+}
+
+int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
+{
+    const char* what = "hpsgd_gemm_fp8";
+    if (!args) return report(HPSGD_E_BADARG, "%s: args is NULL", what);
+    hpsgd_gemm_fp8_args p = *args;
+    if (p.M < 0 || p.N < 0 || p.K < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
+    // coordinates of boxes that reach past the end stay below 2^31, tiles below 2^31
+    const int64_t most = 0x7FFFFFFF - 4096;
+    if (p.M > most || p.N > most || p.K > most || ((p.N + 127) / 128) * ((p.M + 255) / 256) > most)
+        return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    if (p.d_dtype != HPSGD_F32 && p.d_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown d_dtype %d", what, p.d_dtype);
+    if (p.accumulate != 0 && (p.accumulate != 1 || p.d_dtype != HPSGD_F32)) return report(HPSGD_E_BADARG, "%s: accumulate must be 0, or 1 with an fp32 result", what);
+    if (p.M == 0 || p.N == 0) return HPSGD_OK;
+    const size_t esz = p.d_dtype == HPSGD_F32 ? 4 : 2;
+    if (p.ldd == 0) p.ldd = p.N;
+    if (!p.d || !aligned(p.d, esz) || p.ldd < p.N) return report(HPSGD_E_BADARG, "%s: d is NULL, not aligned to its elements, or its stride is below N", what);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int sms = 0;
+    if (p.K == 0) {
+        OPS_TRY(device_sms(&sms));
+        if (!p.accumulate) OPS_CUDA(cudaMemset2DAsync(p.d, (size_t)p.ldd * esz, 0, (size_t)p.N * esz, (size_t)p.M, s));
+        return HPSGD_OK;
+    }
+    if (!p.a || !p.b) return report(HPSGD_E_BADARG, "%s: a or b is NULL", what);
+    OPS_TRY(check_fp8(what, "a", p.a, p.a_scale, &p.lda, &p.ldsa, p.M, p.K));
+    OPS_TRY(check_fp8(what, "b", p.b, p.b_scale, &p.ldb, &p.ldsb, p.N, p.K));
+    const Plan plan = plan_of(p.M, p.N, p.K);
+    const size_t need = workspace_of(plan);
+    if (need && (!p.workspace || !aligned(p.workspace, 16))) return report(HPSGD_E_BADARG, "%s: workspace is NULL or not 16-byte aligned", what);
+    if (need > p.workspace_bytes) return report(HPSGD_E_NOMEM, "%s: workspace of %zu bytes is smaller than the %zu needed", what, p.workspace_bytes, need);
+    OPS_TRY(device_sms(&sms));
+    CUtensorMap ma, mb;
+    OPS_TRY(make_map(what, &ma, p.a, p.lda, p.M, p.K, plan.bn));
+    OPS_TRY(make_map(what, &mb, p.b, p.ldb, p.N, p.K, kLanes));
+    GemmArgs a{};
+    a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
+    a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split;
+    a.sa = reinterpret_cast<const uint32_t*>(p.a_scale); a.sb = reinterpret_cast<const uint32_t*>(p.b_scale);
+    a.ldsa = p.ldsa; a.ldsb = p.ldsb; a.ldd = p.ldd; a.d = p.d; a.accumulate = p.accumulate;
+    a.ticket = static_cast<unsigned int*>(p.workspace);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(p.workspace) + kTicketBytes);
+    return p.d_dtype == HPSGD_F32 ? launch_shape<float>(plan.bn, ma, mb, a, sms, s) : launch_shape<__nv_bfloat16>(plan.bn, ma, mb, a, sms, s);
+}
+
+int hpsgd_ops_check(void* stream)
+{
+    int sms = 0;
+    OPS_TRY(device_sms(&sms));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    OPS_CUDA(cudaStreamSynchronize(s));
+    unsigned int n = 0;
+    OPS_CUDA(cudaMemcpyFromSymbol(&n, g_gemm_timeouts, sizeof n));
+    if (n != 0) {
+        const unsigned int zero = 0;
+        OPS_CUDA(cudaMemcpyToSymbol(g_gemm_timeouts, &zero, sizeof zero));
+        return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks gave up waiting for their own loads or products after two seconds; results are incomplete", n);
+    }
+    return HPSGD_OK;
+}
+
+}  // extern "C"

@@ -11,7 +11,7 @@ from .binding import _ci, _f64, _i64, _ptr, _stream, _u64, _vp
 
 __all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm",
            "make_rmsnorm_forward", "hpsgd_rmsnorm_forward", "make_rmsnorm_backward", "hpsgd_rmsnorm_backward", "hpsgd_rmsnorm_backward_bytes",
-           "make_quantize_fp8", "hpsgd_quantize_fp8"]
+           "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes", "hpsgd_ops_check"]
 
 HPSGD_GRAD_NORM_WORKSPACE = 65536
 HPSGD_FP8 = 2
@@ -40,7 +40,15 @@ class hpsgd_quantize_fp8_args(ctypes.Structure):
         [(n, _i64) for n in ("ldx", "ldxs", "ldq", "lds", "ldqt", "ldst")]
 
 
+class hpsgd_gemm_fp8_args(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("M", "N", "K")] + [(n, _vp) for n in ("a", "a_scale", "b", "b_scale", "d", "workspace")] + \
+        [("workspace_bytes", ctypes.c_size_t)] + [(n, _i64) for n in ("lda", "ldsa", "ldb", "ldsb", "ldd")] + [("d_dtype", _ci), ("accumulate", _ci)]
+
+
 SIGNATURES = {
+    "hpsgd_gemm_fp8_bytes": (ctypes.c_size_t, [_i64, _i64, _i64]),
+    "hpsgd_gemm_fp8": (_ci, [_vp, _vp]),
+    "hpsgd_ops_check": (_ci, [_vp]),
     "hpsgd_rmsnorm_forward": (_ci, [_vp, _vp]),
     "hpsgd_rmsnorm_backward_bytes": (ctypes.c_size_t, [_i64, _i64]),
     "hpsgd_rmsnorm_backward": (_ci, [_vp, _vp]),
@@ -136,3 +144,23 @@ def make_quantize_fp8(rows, cols, dtype, x, q=None, scale=None, qt=None, scale_t
 
 def hpsgd_quantize_fp8(args, stream=None):
     return _b._check(_b.load().hpsgd_quantize_fp8(args.address, _stream(stream)))
+
+
+def hpsgd_gemm_fp8_bytes(M, N, K):
+    return int(_b.load().hpsgd_gemm_fp8_bytes(M, N, K))
+
+
+def make_gemm_fp8(M, N, K, a, a_scale, b, b_scale, d, d_dtype, accumulate=False, workspace=None, workspace_bytes=None, **strides):
+    """``workspace_bytes`` left out: the size of the tensor given as workspace."""
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return Args(hpsgd_gemm_fp8_args, dict(a=a, a_scale=a_scale, b=b, b_scale=b_scale, d=d, workspace=workspace), strides,
+                M=M, N=N, K=K, d_dtype=d_dtype, accumulate=int(accumulate), workspace_bytes=workspace_bytes)
+
+
+def hpsgd_gemm_fp8(args, stream=None):
+    return _b._check(_b.load().hpsgd_gemm_fp8(args.address, _stream(stream)))
+
+
+def hpsgd_ops_check(stream=None):
+    return _b._check(_b.load().hpsgd_ops_check(_stream(stream)))
