@@ -107,8 +107,8 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
 /*
  * Global norm of the gradients of a table (only grad and n are read) and what clips it:
  *     out[0] = sqrt(sum over all tensors of grad^2)
- *     out[1] = max_norm / out[0] if out[0] > max_norm, else 1; NaN if the norm is not finite
- * Squares are added in binary32 eight at a time, those sums in binary64.  max_norm > 0; infinity is legal
+ *     out[1] = max_norm / out[0] if out[0] > max_norm, else 1; NaN if the sum is not finite in binary32
+ * Squares are added in binary32 eight at a time, those sums in binary64; the sum, its root and the quotient are rounded to binary32.  max_norm > 0; infinity is legal
  * (the norm alone).  `workspace`: HPSGD_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned, filled with
  * zeros before its first use; every call leaves it ready for the next.  Calls that share a workspace have to
  * be ordered on one stream.  Without tensors out is {0, 1}.

@@ -113,12 +113,6 @@ __device__ __forceinline__ pair make_pair(float lo, float hi)
     return x;
 }
 __device__ __forceinline__ void split(pair x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
-__device__ __forceinline__ pair mul2(pair a, pair b)
-{
-    pair x;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
 __device__ __forceinline__ pair add2(pair a, pair b)
 {
     pair x;
@@ -132,6 +126,21 @@ __device__ __forceinline__ pair fma2(pair a, pair b, pair c)
     return x;
 }
 __device__ __forceinline__ pair both(float x) { return make_pair(x, x); }
+__device__ __forceinline__ pair mul2(pair a, pair b)
+{
+    pair x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+// A sum of products that are each rounded: a packed addition behind packed multiplications was seen to come out with one rounding fewer,
+// so this one is scalar.
+__device__ __forceinline__ pair sum_of_rounded(pair a, pair b)
+{
+    float a0, a1, b0, b1;
+    split(a, a0, a1);
+    split(b, b0, b1);
+    return make_pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
+}
 
 struct p4 {
     pair v[4];
@@ -248,14 +257,7 @@ __device__ __forceinline__ void store_upper(__nv_bfloat16* p, const f8& x, bool 
         if (q < left) h[q] = (unsigned short)(u[q >> 1] >> 16 * (q & 1));
 }
 
-// Square root and reciprocal by the hardware's approximations, 1 unit in the last place.  Subnormal operands count as zero: a second
-// moment below 2^-126 belongs to gradients below 10^-17.
-__device__ __forceinline__ float root_approx(float x)
-{
-    float y;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
+// Reciprocal by the hardware's approximation, 1 unit in the last place.
 __device__ __forceinline__ float reciprocal_approx(float x)
 {
     float y;
@@ -423,8 +425,9 @@ __device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, fl
     }
     if (!finite(c)) return;                        // the whole grid: nothing of the step happens
 
-    // With 32-bit moments HBM is what bounds the kernel, and root and quotient are correctly rounded; with 8-bit moments
-    // instructions are, and they are the hardware's approximations, of a step that is added to p.
+    // With 32-bit moments HBM is what bounds the kernel, and the quotient is correctly rounded; with 8-bit moments instructions are, and
+    // it is a product with the hardware's reciprocal (of a step that is added to p, where two units in its last place do not count).  The
+    // root decides which code is kept and is correctly rounded in both.
     if constexpr (B8) {
         const pair sm = both(scale_value(mb)), sv = both(scale_value(vb));
         p4 pm = decode8(mc), pv = decode8(vc), pg = to_pairs(g), px = to_pairs(p);
@@ -434,13 +437,13 @@ __device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, fl
             pv.v[q] = mul2(pv.v[q], sv);
             pv.v[q] = mul2(pv.v[q], pv.v[q]);
             pg.v[q] = mul2(pg.v[q], both(c));
-            pm.v[q] = add2(mul2(pm.v[q], both(hy.beta1)), mul2(pg.v[q], both(hy.rest1)));
-            pv.v[q] = add2(mul2(pv.v[q], both(hy.beta2)), mul2(mul2(pg.v[q], pg.v[q]), both(hy.rest2)));
+            pm.v[q] = sum_of_rounded(mul2(pm.v[q], both(hy.beta1)), mul2(pg.v[q], both(hy.rest1)));
+            pv.v[q] = sum_of_rounded(mul2(pv.v[q], both(hy.beta2)), mul2(mul2(pg.v[q], pg.v[q]), both(hy.rest2)));
         }
         m = to_values(pm);
         v = to_values(pv);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) r.v[q] = root_approx(v.v[q]);
+        for (int q = 0; q < 8; ++q) r.v[q] = __fsqrt_rn(v.v[q]);
         const p4 pr = to_pairs(r);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -545,7 +548,7 @@ constexpr int kNormChunk = kNormThreads * 8 * 4;       // four groups of eight i
 constexpr int kNormPartials = (HPSGD_GRAD_NORM_WORKSPACE - 64) / 8;
 
 struct NormOut {
-    double max_norm;
+    float max_norm;
     unsigned int* ticket;      // blocks that have finished; put back to 0 by the last
     double* partial;           // one per block of all launches of the call
     int before, total;         // blocks of earlier launches, blocks of all
@@ -608,9 +611,9 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     if (threadIdx.x == 0) {
         double s = 0.0;
         for (int k = 0; k < kNormThreads / 32; ++k) s += part[k];
-        const double norm = sqrt(s);
-        no.out[0] = (float)norm;
-        no.out[1] = !finite((float)norm) ? __uint_as_float(0x7FC00000u) : norm > no.max_norm ? (float)(no.max_norm / norm) : 1.f;
+        const float norm = __fsqrt_rn((float)s);
+        no.out[0] = norm;
+        no.out[1] = !finite(norm) ? __uint_as_float(0x7FC00000u) : norm > no.max_norm ? __fdiv_rn(no.max_norm, norm) : 1.f;
         *no.ticket = 0u;
     }
 }
@@ -714,7 +717,7 @@ int norm_launches(const hpsgd_adamw_tensor* t, int n, int sms, double max_norm, 
     at = 0;
     while (at < n) total += grid_of(fill_table(t, n, &at, kNormChunk, &table, fill));
     if (total == 0) total = 1;                     // no tensors: one block writes the norm of nothing
-    NormOut no{max_norm, static_cast<unsigned int*>(ws), reinterpret_cast<double*>(static_cast<char*>(ws) + 64), 0, total, 0, out};
+    NormOut no{(float)max_norm, static_cast<unsigned int*>(ws), reinterpret_cast<double*>(static_cast<char*>(ws) + 64), 0, total, 0, out};
     at = 0;
     do {
         no.chunks = fill_table(t, n, &at, kNormChunk, &table, fill);
