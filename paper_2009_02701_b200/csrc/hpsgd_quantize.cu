@@ -2,16 +2,17 @@
 //
 // A 128 x 128 tile is a whole block of each of its rows and of each of its columns, so one read of the tile gives both
 // matrices and all 256 scales.  Bound by HBM: 6 bytes an element from fp32 with both outputs, 4 from bf16, 2 when a matrix
-// in the format is transposed.  A thread holds an 8 x 8 patch: the 16 threads of a half warp cover a row, so the row maxima
-// are shuffles and a row's codes leave as 128 contiguous bytes; a column's eight codes of a patch are eight consecutive bytes of the
-// transpose, which is put together in 16 KB of shared memory and leaves in rows of 128 bytes as well.
+// in the format is transposed.  A thread holds a patch of 4 rows x 8 columns: the 16 threads of a half warp cover a row, so the row
+// maxima are shuffles and a row's codes leave as 128 contiguous bytes; a column's four codes of a patch are one word of the
+// transpose, which is put together in 16 KB of shared memory and leaves in rows of 128 bytes as well.  (Patches of 8 x 8 with half the
+// threads left too few warps to wait with: 49 us where this takes 39 us for 30000 x 1024 in fp32.)
 #include "hpsgd_ops_common.cuh"
 
 namespace hpsgd {
 namespace ops {
 namespace {
 
-constexpr int kQThreads = 256;
+constexpr int kQThreads = 512;
 constexpr int kTile = 128;
 
 struct QuantArgs {
@@ -44,26 +45,29 @@ __device__ __forceinline__ void store_scale(uint8_t* s, int64_t b, int64_t block
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kQThreads) quantize_kernel(const QuantArgs a)
+__global__ void __launch_bounds__(kQThreads, 2) quantize_kernel(const QuantArgs a)
 {
-    __shared__ uint32_t col_top[16][kTile];          // largest magnitudes (patterns) of each patch's columns
-    __shared__ uint2 tile[kTile][16];                // the transpose: [column][eight rows], chunks permuted by the column's patch
+    constexpr int kRows = 4, kWarps = kQThreads / 32;
+    __shared__ uint32_t col_top[kWarps][kTile];      // largest magnitudes (patterns) of each warp's eight rows
+    __shared__ alignas(16) uint32_t tile[kTile][kTile / 4];      // the transpose: [column][four rows], words permuted by the column's patch
+    __shared__ alignas(16) uint8_t col_byte[kTile];
+    __shared__ int odd;                              // some column of the tile has values that are not finite
     constexpr bool kCodes = sizeof(T) == 1;
-    const int lane = threadIdx.x & 15, patch = threadIdx.x >> 4;
+    const int lane = threadIdx.x & 15, patch = threadIdx.x >> 4, warp = threadIdx.x >> 5;
     const int64_t tiles_c = (a.cols + kTile - 1) / kTile;
     const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * kTile, c0 = (int64_t)(blockIdx.x % tiles_c) * kTile;
-    const int64_t row0 = r0 + patch * 8, col0 = c0 + lane * 8;
+    const int64_t row0 = r0 + patch * kRows, col0 = c0 + lane * 8;
     const int left = (int)max((int64_t)0, min((int64_t)8, a.cols - col0));
+    if (threadIdx.x == 0) odd = 0;
 
-    f8 x[8];
+    f8 x[kRows];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const bool in = row0 + k < a.rows;
-        const int here = in ? left : 0;
+    for (int k = 0; k < kRows; ++k) {
+        const int here = row0 + k < a.rows ? left : 0;
         if constexpr (kCodes) {
             uint2 u = make_uint2(0u, 0u);
             int byte = 0;
-            if (here) {                               // codes behind the last column are zeros and can be read
+            if (here) {                               // the codes behind the last column, up to 16, can be read: they are masked below
                 u = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.x) + (row0 + k) * a.ldx + col0);
                 byte = a.xs[scale_index(c0 / kTile, row0 + k, a.ldxs)];
             }
@@ -78,76 +82,71 @@ __global__ void __launch_bounds__(kQThreads) quantize_kernel(const QuantArgs a)
 
     if constexpr (!kCodes) {
         if (a.q) {
-            const int64_t blocks = tiles_c, b = c0 / kTile, pad = (a.cols + 15) / 16 * 16;
+            const int64_t b = c0 / kTile, pad = (a.cols + 15) / 16 * 16;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kRows; ++k) {
                 f8 y = x[k];
                 const int byte = block_scale(y);
                 if (row0 + k < a.rows) {
                     if (col0 < pad) *reinterpret_cast<uint2*>(a.q + (row0 + k) * a.ldq + col0) = encode_nearest(y, byte);
-                    if (lane == 0) store_scale(a.s, b, blocks, row0 + k, a.lds, byte);
+                    if (lane == 0) store_scale(a.s, b, tiles_c, row0 + k, a.lds, byte);
                 }
             }
         }
     }
     if (!a.qt) return;
 
-    // column maxima: over the patch's rows here, over the 16 patches through shared memory
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        f8 y;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y.v[k] = x[k].v[j];
-        col_top[patch][lane * 8 + j] = __float_as_uint(top8(y));
-    }
-    __syncthreads();
-    if (threadIdx.x < kTile) {
-        uint32_t t = 0;
-#pragma unroll
-        for (int p = 0; p < 16; ++p) t = max(t, col_top[p][threadIdx.x]);
-        col_top[0][threadIdx.x] = t;
-    }
-    __syncthreads();
-    bool odd = false;                                 // some column of the tile has values that are not finite
-#pragma unroll
-    for (int j = 0; j < 8; ++j) odd |= col_top[0][lane * 8 + j] >= 0x7F800000u;
-    if (__syncthreads_or(odd)) {
+    // column maxima: over the rows of a warp here, over the warps through shared memory
+    const auto maxima = [&](bool only_finite) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint32_t t = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (finite(x[k].v[j])) t = max(t, __float_as_uint(fabsf(x[k].v[j])));
-                else x[k].v[j] = __uint_as_float(0x7FC00000u);
+            for (int k = 0; k < kRows; ++k) {
+                const uint32_t u = __float_as_uint(fabsf(x[k].v[j]));
+                if (!only_finite || u < 0x7F800000u) t = max(t, u);
             }
-            col_top[patch][lane * 8 + j] = t;
+            t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
+            if (threadIdx.x & 16 ? j >= 4 : j < 4) col_top[warp][lane * 8 + j] = t;
         }
         __syncthreads();
         if (threadIdx.x < kTile) {
             uint32_t t = 0;
 #pragma unroll
-            for (int p = 0; p < 16; ++p) t = max(t, col_top[p][threadIdx.x]);
-            col_top[0][threadIdx.x] = t;
+            for (int p = 0; p < kWarps; ++p) t = max(t, col_top[p][threadIdx.x]);
+            if (t >= 0x7F800000u) odd = 1;
+            const int byte = scale_byte(__uint_as_float(t));
+            col_byte[threadIdx.x] = (uint8_t)byte;
+            if (t < 0x7F800000u && c0 + threadIdx.x < a.cols)
+                store_scale(a.st, r0 / kTile, (a.rows + kTile - 1) / kTile, c0 + threadIdx.x, a.ldst, byte);
         }
         __syncthreads();
+    };
+    maxima(false);
+    if (odd) {                                        // rare: the scales are those of the finite values, and the others become NaN
+        maxima(true);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (!finite(x[k].v[j])) x[k].v[j] = __uint_as_float(0x7FC00000u);
     }
-    const int64_t blocks_t = (a.rows + kTile - 1) / kTile, bt = r0 / kTile;
+    const uint2 bytes = *reinterpret_cast<const uint2*>(col_byte + lane * 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        f8 y;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y.v[k] = x[k].v[j];
-        const int byte = scale_byte(__uint_as_float(col_top[0][lane * 8 + j]));
-        tile[lane * 8 + j][patch ^ lane] = encode_nearest(y, byte);
-        if (patch == 0 && col0 + j < a.cols) store_scale(a.st, bt, blocks_t, col0 + j, a.ldst, byte);
+        const float inv = scale_inverse((j < 4 ? bytes.x : bytes.y) >> 8 * (j & 3) & 0xFFu);
+        unsigned short lo, hi;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fmul_rn(x[1].v[j], inv)), "f"(__fmul_rn(x[0].v[j], inv)));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fmul_rn(x[3].v[j], inv)), "f"(__fmul_rn(x[2].v[j], inv)));
+        tile[lane * 8 + j][patch ^ 2 * lane] = lo | (uint32_t)hi << 16;
     }
     __syncthreads();
     const int64_t pad_t = (a.rows + 15) / 16 * 16;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int c = k * 16 + patch;                 // a half warp takes one row of the transpose
+    for (int k = 0; k < 4; ++k) {
+        const int c = k * 32 + patch;                 // a half warp takes one row of the transpose
         if (c0 + c < a.cols && r0 + lane * 8 < pad_t)
-            *reinterpret_cast<uint2*>(a.qt + (c0 + c) * a.ldqt + r0 + lane * 8) = tile[c][lane ^ (c >> 3)];
+            *reinterpret_cast<uint2*>(a.qt + (c0 + c) * a.ldqt + r0 + lane * 8) = *reinterpret_cast<const uint2*>(&tile[c][2 * lane ^ 2 * (c >> 3)]);
     }
 }
 
