@@ -5,8 +5,9 @@
 // instructions of a 128-block name the same one), and the sums stay in tensor memory in binary32 from the first k to the last.
 //
 // B's rows (a layer's outputs) lie on the accumulator's 128 lanes and A's rows (tokens) on its columns: with one token a tile is
-// 128 x 16 and the kernel streams the weights, with many it is 128 x 256, and in either case 32 lanes hold 32 neighbouring outputs of
-// a token, so results leave in coalesced rows whatever N, the stride and the alignment are.
+// 128 x 16 and the kernel streams the weights, and in any case 32 lanes hold 32 neighbouring outputs of a token, so results leave in
+// coalesced rows whatever N, the stride and the alignment are.  With many tokens two SMs work on one tile of 256 x 256 (cta_group::2):
+// each holds its 128 rows of B and half of A's, so a product of 128 x 256 x 128 on an SM takes 32 KB out of L2 in place of 48.
 //
 // One block per SM works through its tiles: a thread that keeps a ring of stages full by TMA (128 k of both operands a stage,
 // 128-byte swizzle), a warp that puts the scales beside them, a thread that issues the products, and four warps that empty
@@ -28,22 +29,25 @@ namespace {
 constexpr int kSms = 148;                  // what work is divided by
 constexpr int kLanes = 128;                // rows of B in a tile
 constexpr int kStageK = 128;               // k of a stage: one scale block, one row of the 128-byte swizzle
-constexpr int kGemmThreads = 256;
-constexpr int kTicketBytes = 4096;         // four counters per tile that is split (fewer than kSms tiles)
+constexpr int kGemmThreads = 384;          // copies, products, scales, one idle warp; eight warps for results
+constexpr int kTicketBytes = 8192;         // eight counters per block of a tile that is split (fewer than kSms)
 
 __device__ unsigned int g_gemm_timeouts;   // blocks whose wait ran out
 
-template <int BN>
+// BN: A's rows in a tile.  PAIR: two blocks (a cluster) share a tile of 256 rows of B, each with 128 of them and half of A's rows.
+template <int BN, bool PAIR>
 struct Shape {
-    static constexpr int kStages = BN <= 64 ? 8 : BN <= 128 ? 6 : 4;
+    static constexpr int kStages = BN <= 64 ? 8 : 6;
     static constexpr int kAtoms = BN <= 128 ? 1 : 2;                     // groups of 128 columns' scales
-    static constexpr int kBytesB = kLanes * kStageK, kBytesA = BN * kStageK, kBytesS = 512 * (1 + kAtoms);
+    static constexpr int kRowsA = PAIR ? BN / 2 : BN;                    // of A, in this block's shared memory
+    static constexpr int kBytesB = kLanes * kStageK, kBytesA = kRowsA * kStageK, kBytesS = 512 * (1 + kAtoms);
     static constexpr int kStageBytes = kBytesB + kBytesA;
     static constexpr int kAccs = BN <= 128 ? 2 : 1;
-    static constexpr int kScaleCols = 4 * (1 + kAtoms);                  // tensor-memory columns of one group of scales
-    static constexpr int kCols = kAccs * BN + kStages * kScaleCols;
+    static constexpr int kPlaces = 4;                                    // groups of scales (four k blocks) in shared memory
+    static constexpr int kScaleCols = 4 * (1 + kAtoms);                  // tensor-memory columns of one group, of which one more is kept there
+    static constexpr int kCols = kAccs * BN + (kPlaces + 1) * kScaleCols;
     static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static constexpr int kSmem = 1024 + kStages * (kStageBytes + kBytesS) + 256;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kPlaces * kBytesS + 256;
 };
 
 struct GemmArgs {
@@ -66,6 +70,17 @@ __device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mba
 __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// On a barrier of the cluster's first block, from either.
+__device__ __forceinline__ uint32_t first_block_address(uint32_t address)
+{
+    uint32_t x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(x) : "r"(address));
+    return x;
+}
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
@@ -99,11 +114,18 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
     }
 }
 
+// A box to this block's shared memory; `bar` may be a barrier of the cluster's first block when two blocks work together.
+template <bool PAIR>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
 }
 
 // Shared-memory descriptor of an operand whose rows are 128 bytes, swizzled: eight rows make a group of 1024 bytes.
@@ -117,51 +139,91 @@ __device__ __forceinline__ uint64_t scale_descriptor(uint32_t address)
     return (uint64_t)(address >> 4 & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-// Instruction descriptor: E4M3 operands, both along k, N = BN, M = 128, E8M0 scales; `id` names the byte of the scale words.
-template <int BN>
+// Instruction descriptor: E4M3 operands, both along k, N = BN, M = 128 or 256, E8M0 scales; `id` names the byte of the scale words.
+template <int BN, bool PAIR>
 __device__ __forceinline__ uint32_t instruction(uint32_t id)
 {
-    return id << 4 | (uint32_t)(BN >> 3) << 17 | 1u << 23 | (uint32_t)(kLanes >> 4) << 24 | id << 29;
+    return id << 4 | (uint32_t)(BN >> 3) << 17 | 1u << 23 | (uint32_t)((PAIR ? 2 * kLanes : kLanes) >> 4) << 24 | id << 29;
 }
 
+template <bool PAIR>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
+                     : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+// When the products issued so far are done: an arrival at the barrier, in both blocks of a pair.
+template <bool PAIR>
 __device__ __forceinline__ void commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// One lane of a whole warp.  The copies' and products' operands live in uniform registers: behind this, rather than behind a comparison of
+// the lane's number, the compiler knows that there is one value of each.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Sixteen accumulator columns of this thread's lane.
+// C accumulator columns of this thread's lane; complete behind loads_done.
+template <int C>
 __device__ __forceinline__ void load_columns(uint32_t tmem, float* x)
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(tmem));
+    if constexpr (C == 8)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(tmem));
+    else
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                       "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                     : "r"(tmem));
+}
+// (the registers are named so that nothing that reads them moves in front of the wait)
+template <int C>
+__device__ __forceinline__ void loads_done(float* x)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < C; ++j) asm volatile("" : "+f"(x[j]));
 }
 
 // ---------------------------------------------------------------------------- the kernel
-// Unit u of a block's work: tile u / splits, part u % splits of its k blocks.
+// Unit u of a block's (or pair's) work: tile u / splits, part u % splits of its k blocks.  n0: this block's first row of B.
 struct Unit {
     int n0, m0, k0, k1, tile, split;
 };
-template <int BN>
-__device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u)
+template <int BN, bool PAIR>
+__device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u, int rank)
 {
     Unit x;
     x.tile = u / a.splits;
     x.split = u % a.splits;
-    x.n0 = x.tile % a.tiles_n * kLanes;
+    x.n0 = x.tile % a.tiles_n * (PAIR ? 2 * kLanes : kLanes) + rank * kLanes;
     x.m0 = x.tile / a.tiles_n * BN;
     const int blocks = (a.K + kStageK - 1) / kStageK;
     x.k0 = x.split * a.per_split;
@@ -169,200 +231,247 @@ __device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u)
     return x;
 }
 
-template <typename D>
-__device__ __forceinline__ void store_result(const GemmArgs& a, int m, int n, float x)
+// One result.  Adding to what is there is left to the memory side: it returns nothing that the warp would have to wait for (a load, an
+// addition and a store for each of 256 columns took 132 us where the product takes 27), and each element receives exactly one.
+template <typename D, bool ADD>
+__device__ __forceinline__ void store_result(D* p, float x)
 {
-    D* const p = static_cast<D*>(a.d) + (int64_t)m * a.ldd + n;
-    if constexpr (sizeof(D) == 4) {
-        // The addition is left to the memory side: it returns nothing that the warp would have to wait for (a load, an addition and a
-        // store for each of 256 columns took 132 us where the product takes 27), and each element receives exactly one.
-        if (a.accumulate) {
-            asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory");
-            return;
-        }
-    }
-    store1(p, x);
+    if constexpr (ADD) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory");
+    else store1(p, x);
 }
 
-template <int BN, typename D>
+// C columns of one lane to rows of D that are ldd apart, `left` of them there.
+template <int C, typename D, bool ADD>
+__device__ __forceinline__ void store_columns(D* p, int64_t ldd, const float* x, int left)
+{
+    if (left >= C) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) store_result<D, ADD>(p + j * ldd, x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (j < left) store_result<D, ADD>(p + j * ldd, x[j]);
+    }
+}
+
+template <int BN, bool PAIR, typename D>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ GemmArgs a)
 {
-    using S = Shape<BN>;
+    using S = Shape<BN, PAIR>;
     extern __shared__ uint8_t raw[];
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const scales = smem + S::kStages * S::kStageBytes;
-    uint64_t* const bars = reinterpret_cast<uint64_t*>(scales + S::kStages * S::kBytesS);
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(scales + S::kPlaces * S::kBytesS);
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int given_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x,
+              stride = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;      // the first block of a pair issues the products of both
     const uint32_t full = smem_address(bars), empty = full + S::kStages * 8, acc_full = empty + S::kStages * 8, acc_empty = acc_full + S::kAccs * 8,
-                   drained = acc_empty + S::kAccs * 8;
+                   scale_full = acc_empty + S::kAccs * 8, scale_empty = scale_full + S::kPlaces * 8, drained = scale_empty + S::kPlaces * 8;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
-            barrier_init(full + s * 8, 2);          // the loads' expectation and the scales
+            barrier_init(full + s * 8, 1);
             barrier_init(empty + s * 8, 1);
+        }
+        for (int s = 0; s < S::kPlaces; ++s) {
+            barrier_init(scale_full + s * 8, PAIR ? 2 : 1);          // the scales of each block
+            barrier_init(scale_empty + s * 8, 1);
         }
         for (int s = 0; s < S::kAccs; ++s) {
             barrier_init(acc_full + s * 8, 1);
-            barrier_init(acc_empty + s * 8, 4);
+            barrier_init(acc_empty + s * 8, PAIR ? 16 : 8);          // the warps that read it
         }
         barrier_init(drained, 1);
         given_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 3) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
     const int units = a.tiles * a.splits;
 
+    // The roles' waits are the whole warp's, so that what they decide is the same for all of its lanes.
+    const auto wait = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, &given_up)); };
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0;
-            bool ok = true;
-            for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-                const Unit x = unit_of<BN>(a, u);
-                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
-                    const int s = it % S::kStages;
-                    if (!(ok = barrier_wait(empty + s * 8, (it / S::kStages & 1) ^ 1, &given_up))) break;
-                    const uint32_t dst = smem_address(smem + s * S::kStageBytes), bar = full + s * 8;
-                    barrier_expect(bar, S::kStageBytes);
-                    tma_load(dst, &map_b, kb * kStageK, x.n0, bar);
-                    tma_load(dst + S::kBytesB, &map_a, kb * kStageK, x.m0, bar);
+        int s = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit x = unit_of<BN, PAIR>(a, u, rank);
+            for (int kb = x.k0; kb < x.k1; ++kb) {
+                if (!(ok = wait(empty + s * 8, phase))) break;
+                if (elected()) {
+                    // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
+                    const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
+                    if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes);
+                    tma_load<PAIR>(dst, &map_b, kb * kStageK, x.n0, bar);
+                    tma_load<PAIR>(dst + S::kBytesB, &map_a, kb * kStageK, x.m0 + rank * S::kRowsA, bar);
                 }
-            }
-            // giving up: the copies in flight still land (a stage whose scales never came completes no phase, so the wait is for time)
-            if (!ok) {
-                const uint64_t t = nanoseconds();
-                while (nanoseconds() - t < 10000000ull) {}
+                __syncwarp();
+                if (++s == S::kStages) s = 0, phase ^= 1;
             }
         }
+        // giving up: the copies in flight still land (a stage whose scales never came completes no phase, so the wait is for time)
+        if (!ok) {
+            const uint64_t t = nanoseconds();
+            while (nanoseconds() - t < 10000000ull) {}
+        }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int it = 0, fills = 0, done = 0;
+        if (rank == 0) {
+            const uint64_t desc_b = operand_descriptor(smem_address(smem)), desc_a = operand_descriptor(smem_address(smem) + S::kBytesB),
+                           desc_s = scale_descriptor(smem_address(scales));
+            int s = 0, place = 0, column = 0, acc = 0;
+            uint32_t phase = 0, place_phase = 0, acc_phase = 1;
             bool ok = true;
-            for (int u = blockIdx.x; u < units && ok; u += gridDim.x, ++done) {
-                const Unit x = unit_of<BN>(a, u);
-                const int acc = done % S::kAccs;
-                if (!(ok = barrier_wait(acc_empty + acc * 8, (done / S::kAccs & 1) ^ 1, &given_up))) break;
+            for (int u = first; u < units && ok; u += stride) {
+                const Unit x = unit_of<BN, PAIR>(a, u, rank);
+                if (!(ok = wait(acc_empty + acc * 8, acc_phase))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t sb = 0, sa = 0;
-                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
-                    const int s = it % S::kStages;
-                    if (!(ok = barrier_wait(full + s * 8, it / S::kStages & 1, &given_up))) break;
+                uint32_t sb = 0;
+                for (int kb = x.k0; kb < x.k1; ++kb) {
+                    if (!(ok = wait(full + s * 8, phase))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (kb == x.k0 || (kb & 3) == 0) {
-                        // A group of four blocks' scales to a place of its own among kStages.  The place was last used kStages fills ago, so at
-                        // least kStages stages ago, and those products are done: this stage could not be full otherwise.
-                        sb = tmem_scales + fills++ % S::kStages * S::kScaleCols;
-                        sa = sb + 4;
-                        const uint32_t src = smem_address(scales + s * S::kBytesS);
-                        copy_scales(sb, scale_descriptor(src));
-#pragma unroll
-                        for (int t = 0; t < S::kAtoms; ++t) copy_scales(sa + 4 * t, scale_descriptor(src + 512 * (1 + t)));
+                    const bool scale_group = kb == x.k0 || (kb & 3) == 0;
+                    int from = 0;
+                    if (scale_group) {
+                        // The next group's scales, to the column group after the last one's.  Those columns were used kPlaces + 1 groups ago.  This
+                        // place was refilled behind the commit of kPlaces groups ago, which waited for all products before its own: they are done.
+                        if (!(ok = wait(scale_full + place * 8, place_phase))) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        sb = tmem_scales + column * S::kScaleCols;
+                        from = place;
+                        if (++column == S::kPlaces + 1) column = 0;
+                        if (++place == S::kPlaces) place = 0, place_phase ^= 1;
                     }
-                    const uint64_t db = operand_descriptor(smem_address(smem + s * S::kStageBytes)),
-                                   da = operand_descriptor(smem_address(smem + s * S::kStageBytes + S::kBytesB));
-                    const uint32_t id = instruction<BN>(kb & 3);
+                    if (elected()) {
+                        if (scale_group) {
+                            const uint64_t src = desc_s + (uint32_t)(from * (S::kBytesS >> 4));
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma(tmem + acc * BN, db + 2 * k, da + 2 * k, id, sb, sa, kb > x.k0 || k > 0);
-                    commit(empty + s * 8);
+                            for (int t = 0; t < 1 + S::kAtoms; ++t) copy_scales<PAIR>(sb + 4 * t, src + 32 * t);
+                            commit<PAIR>(scale_empty + from * 8);
+                        }
+                        const uint64_t db = desc_b + (uint32_t)(s * (S::kStageBytes >> 4)), da = desc_a + (uint32_t)(s * (S::kStageBytes >> 4));
+                        const uint32_t id = instruction<BN, PAIR>(kb & 3);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma<PAIR>(tmem + acc * BN, db + 2 * k, da + 2 * k, id, sb, sb + 4, kb > x.k0 || k > 0);
+                        commit<PAIR>(empty + s * 8);
+                        if (kb + 1 == x.k1) commit<PAIR>(acc_full + acc * 8);
+                    }
+                    __syncwarp();
+                    if (++s == S::kStages) s = 0, phase ^= 1;
                 }
-                if (ok) commit(acc_full + acc * 8);
+                if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
             }
             if (!ok) {                              // products in flight read shared memory: let them end
-                commit(drained);
+                if (elected()) commit<PAIR>(drained);
                 const uint64_t t = nanoseconds();
                 while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
             }
         }
     } else if (warp == 2) {
-        // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.  The next
-        // group's words are requested before this one's stage is waited for.
-        int it = 0;
+        // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.  A group's words are
+        // requested before the place of the group before it is waited for.
+        uint32_t w[1 + S::kAtoms][4];
+        const auto fetch = [&](const Unit& x, int kb) {
+            const int64_t g = kb >> 2;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = lane + 32 * j;
+                w[0][j] = x.n0 + r < a.N ? __ldg(a.sb + g * a.ldsb + x.n0 + r) : 0u;
+#pragma unroll
+                for (int t = 0; t < S::kAtoms; ++t) w[1 + t][j] = x.m0 + 128 * t + r < a.M ? __ldg(a.sa + g * a.ldsa + x.m0 + 128 * t + r) : 0u;
+            }
+        };
+        int place = 0;
+        uint32_t phase = 1;
         bool ok = true;
-        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-            const Unit x = unit_of<BN>(a, u);
-            uint32_t w[1 + S::kAtoms][4];
-            const auto fetch = [&](int kb) {
-                const int64_t g = kb >> 2;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit x = unit_of<BN, PAIR>(a, u, rank);
+            for (int kb = x.k0; kb < x.k1; kb = (kb | 3) + 1) {
+                fetch(x, kb);
+                if (!(ok = wait(scale_empty + place * 8, phase))) break;
+                uint4* const dst = reinterpret_cast<uint4*>(scales + place * S::kBytesS);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = lane + 32 * j;
-                    w[0][j] = x.n0 + r < a.N ? __ldg(a.sb + g * a.ldsb + x.n0 + r) : 0u;
-#pragma unroll
-                    for (int t = 0; t < S::kAtoms; ++t) w[1 + t][j] = x.m0 + 128 * t + r < a.M ? __ldg(a.sa + g * a.ldsa + x.m0 + 128 * t + r) : 0u;
-                }
-            };
-            fetch(x.k0);
-            for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
-                const int s = it % S::kStages;
-                ok = __all_sync(0xFFFFFFFFu, barrier_wait(empty + s * 8, (it / S::kStages & 1) ^ 1, &given_up));
-                if (!ok) break;
-                if (kb == x.k0 || (kb & 3) == 0) {
-                    uint4* const dst = reinterpret_cast<uint4*>(scales + s * S::kBytesS);
-#pragma unroll
-                    for (int t = 0; t < 1 + S::kAtoms; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    const int next = (kb | 3) + 1;
-                    if (next < x.k1) fetch(next);
-                }
+                for (int t = 0; t < 1 + S::kAtoms; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) barrier_arrive(full + s * 8);
+                if (lane == 0) {
+                    // (across the cluster this release takes about a microsecond: once for four k blocks it stays out of the way, once for
+                    // each it was what the kernel waited for)
+                    if constexpr (PAIR) barrier_arrive_cluster(first_block_address(scale_full + place * 8));
+                    else barrier_arrive(scale_full + place * 8);
+                }
+                if (++place == S::kPlaces) place = 0, phase ^= 1;
             }
         }
     } else if (warp >= 4) {
-        const int part = warp & 3;                  // the quarter of the lanes that this warp can read
+        // Two warps for each quarter of the lanes, half of the columns each.  A warp has its scheduler nearly to itself, so what counts is
+        // that nothing waits: the next columns are requested before these are stored, and addresses do not depend on one another.
+        constexpr int kHalf = BN / 2, kC = kHalf < 16 ? kHalf : 16;
+        const int part = warp & 3, c0 = (warp >> 2) - 1 ? kHalf : 0;
         int done = 0;
-        for (int u = blockIdx.x; u < units; u += gridDim.x, ++done) {
-            const Unit x = unit_of<BN>(a, u);
+        for (int u = first; u < units; u += stride, ++done) {
+            const Unit x = unit_of<BN, PAIR>(a, u, rank);
             const int acc = done % S::kAccs;
-            const bool ok = barrier_wait(acc_full + acc * 8, done / S::kAccs & 1, &given_up);
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (!wait(acc_full + acc * 8, done / S::kAccs & 1)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t src = tmem + acc * BN + ((uint32_t)part << 21);
-            const int n = x.n0 + part * 32 + lane, cols = min(BN, a.M - x.m0);
-            float* const mine = a.part + ((int64_t)x.tile * a.splits + x.split) * (kLanes * BN) + part * 32 + lane;
-#pragma unroll 1
-            for (int c = 0; c < BN; c += 16) {
-                float v[16];
-                __syncwarp();
-                load_columns(src + c, v);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if (a.splits > 1) {
+            const uint32_t src = tmem + acc * BN + c0 + ((uint32_t)part << 21);
+            const int n = x.n0 + part * 32 + lane, cols = a.M - x.m0 - c0, piece = PAIR ? x.tile * 2 + rank : x.tile;
+            float* const parts = a.part + (int64_t)piece * a.splits * (kLanes * BN) + (int64_t)c0 * kLanes + part * 32 + lane;
+            D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
+            float v[2][kC];
+            load_columns<kC>(src, v[0]);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c + j < cols) mine[(int64_t)(c + j) * kLanes] = v[j];
-                } else if (n < a.N) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c + j < cols) store_result<D>(a, x.m0 + c + j, n, v[j]);
+            for (int c = 0; c < kHalf; c += kC) {
+                float* const now = v[c / kC & 1];
+                loads_done<kC>(now);
+                if (c + kC < kHalf) load_columns<kC>(src + c + kC, v[(c / kC & 1) ^ 1]);
+                if (c >= cols) continue;
+                if (a.splits > 1) store_columns<kC, float, false>(parts + (int64_t)x.split * (kLanes * BN) + c * kLanes, kLanes, now, cols - c);
+                else if (n < a.N) {
+                    if (sizeof(D) == 4 && a.accumulate) store_columns<kC, D, sizeof(D) == 4>(d + c * a.ldd, a.ldd, now, cols - c);
+                    else store_columns<kC, D, false>(d + c * a.ldd, a.ldd, now, cols - c);
                 }
+                __syncwarp();
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) barrier_arrive(acc_empty + acc * 8);
+            if (lane == 0) {
+                if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
+                else barrier_arrive(acc_empty + acc * 8);
+            }
             if (a.splits > 1) {
-                // The last of the tile's parts to finish adds them; each warp counts and adds for its own 32 lanes.
+                // The last of the tile's parts to finish adds them; each warp counts and adds for its own lanes and columns.
+                unsigned int* const ticket = a.ticket + (piece * 8 + warp - 4);
                 __threadfence();
                 __syncwarp();
                 unsigned int before = 0;
-                if (lane == 0) before = atomicAdd(a.ticket + x.tile * 4 + part, 1u);
+                if (lane == 0) before = atomicAdd(ticket, 1u);
                 before = __shfl_sync(0xFFFFFFFFu, before, 0);
                 if (before == (unsigned)(a.splits - 1)) {
                     __threadfence();
-                    if (lane == 0) a.ticket[x.tile * 4 + part] = 0u;          // ready for the next call
-                    const float* const all = a.part + (int64_t)x.tile * a.splits * (kLanes * BN) + part * 32 + lane;
+                    if (lane == 0) *ticket = 0u;              // ready for the next call
                     if (n < a.N) {
-                        for (int c = 0; c < cols; ++c) {
-                            float sum = __ldcg(all + (int64_t)c * kLanes);
-                            for (int k = 1; k < a.splits; ++k) sum = __fadd_rn(sum, __ldcg(all + (int64_t)k * (kLanes * BN) + (int64_t)c * kLanes));
-                            store_result<D>(a, x.m0 + c, n, sum);
+                        const int most = min(cols, kHalf);
+#pragma unroll 4
+                        for (int c = 0; c < most; ++c) {
+                            float sum = __ldcg(parts + (int64_t)c * kLanes);
+                            for (int k = 1; k < a.splits; ++k) sum = __fadd_rn(sum, __ldcg(parts + (int64_t)k * (kLanes * BN) + (int64_t)c * kLanes));
+                            if (sizeof(D) == 4 && a.accumulate) store_result<D, sizeof(D) == 4>(d + (int64_t)c * a.ldd, sum);
+                            else store_result<D, false>(d + (int64_t)c * a.ldd, sum);
                         }
                     }
                 }
@@ -373,7 +482,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0 && given_up) atomicAdd(&g_gemm_timeouts, 1u);
-    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+    if constexpr (PAIR) cluster_sync();              // the other block's arrivals and products reach into this one
+    if (warp == 3) {
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+    }
 }
 
 // ---------------------------------------------------------------------------- host side
@@ -410,20 +523,22 @@ int make_map(const char* what, CUtensorMap* map, const void* q, int64_t ld, int6
 }
 
 struct Plan {
-    int bn, tiles_n, tiles, splits, per_split;
+    int bn, pair, tiles_n, tiles, splits, per_split;
 };
 
-// Tokens' side of a tile: the least power of two that holds them all, 256 at most.  Splitting along k: as many parts as leave no SM
-// with nothing to do, of at least two k blocks each.
+// A's side of a tile: the least power of two that holds all its rows, 256 at most, and then on pairs of SMs unless B has no more rows
+// than one of them takes.  Splitting along k: as many parts as leave no SM with nothing to do, of at least two k blocks each.
 Plan plan_of(int64_t M, int64_t N, int64_t K)
 {
     Plan p{};
-    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-    p.tiles_n = (int)((N + kLanes - 1) / kLanes);
+    p.pair = M > 128 && N > kLanes;
+    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : p.pair ? 256 : 128;
+    const int lanes = p.pair ? 2 * kLanes : kLanes, workers = p.pair ? kSms / 2 : kSms;
+    p.tiles_n = (int)((N + lanes - 1) / lanes);
     const int64_t tiles = p.tiles_n * ((M + p.bn - 1) / p.bn);
     p.tiles = (int)tiles;
     const int blocks = (int)((K + kStageK - 1) / kStageK);
-    p.splits = tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / tiles, blocks / 2)) : 1;
+    p.splits = tiles < workers ? (int)std::max<int64_t>(1, std::min<int64_t>(workers / tiles, blocks / 2)) : 1;
     p.per_split = (blocks + p.splits - 1) / p.splits;
     p.splits = (blocks + p.per_split - 1) / p.per_split;
     return p;
@@ -431,22 +546,40 @@ Plan plan_of(int64_t M, int64_t N, int64_t K)
 
 size_t workspace_of(const Plan& p)
 {
-    return p.splits > 1 ? kTicketBytes + (size_t)p.tiles * p.splits * kLanes * p.bn * sizeof(float) : 0;
+    return p.splits > 1 ? kTicketBytes + (size_t)p.tiles * (p.pair ? 2 : 1) * p.splits * kLanes * p.bn * sizeof(float) : 0;
 }
 
-template <int BN, typename D>
+template <int BN, bool PAIR, typename D>
 int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
 {
-    using S = Shape<BN>;
-    static bool set[64] = {};                       // per device: the shared-memory size has been opted into
+    using S = Shape<BN, PAIR>;
+    // Per device: the blocks (or pairs) that it holds at a time.  Pairs need both their SMs in one GPU cluster, so there may be fewer than
+    // half the SMs' number, and work given to more would wait for a second round.
+    static int workers[64] = {};
     int dev = 0;
     OPS_CUDA(cudaGetDevice(&dev));
-    if (dev >= 64 || !set[dev]) {
-        OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
-        if (dev < 64) set[dev] = true;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr{};
+    cfg.gridDim = dim3(PAIR ? 2 : 1);
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = s;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = PAIR ? 2 : 1;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = PAIR ? 1 : 0;
+    int at_once = dev < 64 ? workers[dev] : 0;
+    if (at_once == 0) {
+        OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, PAIR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        at_once = sms;
+        if (PAIR) OPS_CUDA(cudaOccupancyMaxActiveClusters(&at_once, gemm_fp8_kernel<BN, PAIR, D>, &cfg));
+        at_once = std::max(1, at_once);
+        if (dev < 64) workers[dev] = at_once;
     }
     const int64_t units = (int64_t)a.tiles * a.splits;
-    gemm_fp8_kernel<BN, D><<<(unsigned)std::min<int64_t>(units, sms), kGemmThreads, S::kSmem, s>>>(ma, mb, a);
+    cfg.gridDim = dim3((PAIR ? 2u : 1u) * (unsigned)std::min<int64_t>(units, at_once));
+    OPS_CUDA(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<BN, PAIR, D>, ma, mb, a));
     return launched("hpsgd_gemm_fp8");
 }
 
@@ -454,11 +587,11 @@ template <typename D>
 int launch_shape(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
 {
     switch (bn) {
-    case 16: return launch<16, D>(ma, mb, a, sms, s);
-    case 32: return launch<32, D>(ma, mb, a, sms, s);
-    case 64: return launch<64, D>(ma, mb, a, sms, s);
-    case 128: return launch<128, D>(ma, mb, a, sms, s);
-    default: return launch<256, D>(ma, mb, a, sms, s);
+    case 16: return launch<16, false, D>(ma, mb, a, sms, s);
+    case 32: return launch<32, false, D>(ma, mb, a, sms, s);
+    case 64: return launch<64, false, D>(ma, mb, a, sms, s);
+    case 128: return launch<128, false, D>(ma, mb, a, sms, s);
+    default: return launch<256, true, D>(ma, mb, a, sms, s);
     }
 }
 
@@ -509,7 +642,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     if (need > p.workspace_bytes) return report(HPSGD_E_NOMEM, "%s: workspace of %zu bytes is smaller than the %zu needed", what, p.workspace_bytes, need);
     OPS_TRY(device_sms(&sms));
     CUtensorMap ma, mb;
-    OPS_TRY(make_map(what, &ma, p.a, p.lda, p.M, p.K, plan.bn));
+    OPS_TRY(make_map(what, &ma, p.a, p.lda, p.M, p.K, plan.pair ? plan.bn / 2 : plan.bn));
     OPS_TRY(make_map(what, &mb, p.b, p.ldb, p.N, p.K, kLanes));
     GemmArgs a{};
     a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
