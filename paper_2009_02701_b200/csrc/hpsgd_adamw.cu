@@ -344,44 +344,17 @@ __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t
     vc = gather8(cr);
 }
 
-// Eight values as they are stored, so that a group can be requested while the one before it is worked on.
-template <typename T>
-struct Stored;
-template <>
-struct Stored<float> {
-    f8 x;
-    __device__ __forceinline__ void load(const float* p) { x = load8(p); }
-    __device__ __forceinline__ f8 values() const { return x; }
-};
-template <>
-struct Stored<__nv_bfloat16> {
-    uint4 u;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p)
-    {
-        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
-    }
-    __device__ __forceinline__ f8 values() const
-    {
-        f8 x;
-        widen_pair(u.x, x.v[0], x.v[1]);
-        widen_pair(u.y, x.v[2], x.v[3]);
-        widen_pair(u.z, x.v[4], x.v[5]);
-        widen_pair(u.w, x.v[6], x.v[7]);
-        return x;
-    }
-};
-
 // What a thread reads for one group with 8-bit moments.
 template <typename P, typename G>
 struct Group8 {
-    Stored<P> p;
-    Stored<G> g;
+    Raw8<P> p;
+    Raw8<G> g;
     uint2 mc, vc;
     uint32_t mb, vb;
     __device__ __forceinline__ void load(const Share& it, int o)
     {
-        p.load(static_cast<const P*>(it.p) + o);
-        g.load(static_cast<const G*>(it.g) + o);
+        p.load(static_cast<const P*>(it.p) + o, true, 8);
+        g.load(static_cast<const G*>(it.g) + o, true, 8);
         const uint8_t *m = static_cast<const uint8_t*>(it.m) + o, *v = static_cast<const uint8_t*>(it.v) + o;
         asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(mc.x), "=r"(mc.y) : "l"(m));
         asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(vc.x), "=r"(vc.y) : "l"(v));

@@ -152,6 +152,42 @@ __device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int lef
         if (q < left) store1(p + q, x.v[q]);
 }
 
+// Eight values as they are stored (half the registers of their binary32 values where they are bf16): requested early, widened when used.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    f8 x;
+    __device__ __forceinline__ void load(const float* p, bool wide, int left) { x = load_some(p, wide, left); }
+    __device__ __forceinline__ f8 values() const { return x; }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool wide, int left)
+    {
+        if (wide) {
+            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+            return;
+        }
+        const unsigned short* const h = reinterpret_cast<const unsigned short*>(p);
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < left) w[q >> 1] |= (uint32_t)h[q] << 16 * (q & 1);
+        u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ f8 values() const
+    {
+        f8 x;
+        widen_pair(u.x, x.v[0], x.v[1]);
+        widen_pair(u.y, x.v[2], x.v[3]);
+        widen_pair(u.z, x.v[4], x.v[5]);
+        widen_pair(u.w, x.v[6], x.v[7]);
+        return x;
+    }
+};
+
 // ---------------------------------------------------------------------------- blocks of 16 lanes times eight values
 // Largest of eight magnitudes; NaN if one of them is.
 __device__ __forceinline__ float top8(const f8& x)

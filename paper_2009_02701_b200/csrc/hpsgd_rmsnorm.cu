@@ -59,21 +59,30 @@ __global__ void __launch_bounds__(T < 128 ? 128 : T) rmsnorm_forward_kernel(cons
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / T;
     const bool in = row < a.rows;
     const X* const xp = static_cast<const X*>(a.x) + row * a.ldx;
-    f8 f[V], r[V];
+    f8 f[V];
+    Raw8<X> x[V], r[V];
+    Raw8<W> w[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
-        f[k] = load_some(xp + c, a.wide && left == 8, left);
-        if (a.res) r[k] = load_some(static_cast<const X*>(a.res) + row * a.ldres + c, a.wide && left == 8, left);
+        x[k].load(xp + c, a.wide && left == 8, left);
+        if (a.res) r[k].load(static_cast<const X*>(a.res) + row * a.ldres + c, a.wide && left == 8, left);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
+        w[k].load(static_cast<const W*>(a.w) + c, a.wide_w && left == 8, left);
     }
     float ss = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
+        f[k] = x[k].values();
         if (a.res) {
+            const f8 rk = r[k].values();
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                const float s = __fadd_rn(f[k].v[q], r[k].v[q]);
+                const float s = __fadd_rn(f[k].v[q], rk.v[q]);
                 f[k].v[q] = sizeof(X) == 2 ? __bfloat162float(__float2bfloat16_rn(s)) : s;
             }
             store_some(static_cast<X*>(a.h) + row * a.ldh + c, f[k], a.wide && left == 8, left);
@@ -88,10 +97,10 @@ __global__ void __launch_bounds__(T < 128 ? 128 : T) rmsnorm_forward_kernel(cons
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
-        const f8 w = load_some(static_cast<const W*>(a.w) + c, a.wide_w && left == 8, left);
+        const f8 wk = w[k].values();
         f8 y;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) y.v[q] = __fmul_rn(__fmul_rn(f[k].v[q], rstd), w.v[q]);
+        for (int q = 0; q < 8; ++q) y.v[q] = __fmul_rn(__fmul_rn(f[k].v[q], rstd), wk.v[q]);
         if (left < 8) {                               // zeros behind the last column, even in a row whose rstd is NaN
 #pragma unroll
             for (int q = 0; q < 8; ++q)
@@ -122,11 +131,14 @@ int forward_launch(const Forward& a, cudaStream_t s)
 template <typename X, typename W>
 int forward_types(const Forward& a, cudaStream_t s)
 {
-    // a row's threads cover at least 512 columns (whole words of scales)
+    // A row's threads cover at least 512 columns (whole words of scales).  With rows enough to fill the device a thread takes two groups of
+    // a row, and has twice the bytes under way while it waits for the row's sum (16384 x 4096 bf16 with a residual: 83 us, 103 with one);
+    // with fewer, a row is finished sooner by more threads.
+    const bool many = a.rows >= 8 * 148;
     if (a.cols <= 512) return forward_launch<X, W, 64, 1>(a, s);
-    if (a.cols <= 1024) return forward_launch<X, W, 128, 1>(a, s);
-    if (a.cols <= 2048) return forward_launch<X, W, 256, 1>(a, s);
-    if (a.cols <= 4096) return forward_launch<X, W, 512, 1>(a, s);
+    if (a.cols <= 1024) return many ? forward_launch<X, W, 64, 2>(a, s) : forward_launch<X, W, 128, 1>(a, s);
+    if (a.cols <= 2048) return many ? forward_launch<X, W, 128, 2>(a, s) : forward_launch<X, W, 256, 1>(a, s);
+    if (a.cols <= 4096) return many ? forward_launch<X, W, 256, 2>(a, s) : forward_launch<X, W, 512, 1>(a, s);
     if (a.cols <= 8192) return forward_launch<X, W, 512, 2>(a, s);
     return forward_launch<X, W, 512, 4>(a, s);
 }
@@ -145,55 +157,76 @@ struct Backward {
     bool wide, wide_w;
 };
 
-constexpr int kBackBlocks = 592;      // partial sums of dweight: four blocks on each of 148 SMs
+constexpr int kBackBlocks = 592;      // most partial sums of dweight: four blocks on each of 148 SMs
 
-// A block takes rows block, block + grid, ...; a thread's columns stay the same from row to row, so their dweight is added in registers.
+// T threads a row; a block of 256 takes 256 / T rows at a time (512 threads take one), and goes through the rows in steps of the grid.  A
+// thread's columns stay the same from row to row, so their dweight is added in registers.
 // With one group a thread the next row's values are requested before the present row's sum is waited for; with two, the registers
 // go to the row itself; with four, the row and the weights are read a second time behind the sum, from L1 and L2.
+template <int T>
+struct Back {
+    static constexpr int kThreads = T < 256 ? 256 : T;
+};
+
 template <typename X, typename W, int T, int V>
-__global__ void __launch_bounds__(T) rmsnorm_backward_kernel(const Backward a)
+__global__ void __launch_bounds__(Back<T>::kThreads, V == 1 ? (sizeof(X) == 2 ? 1024 : 768) / Back<T>::kThreads : 1) rmsnorm_backward_kernel(const Backward a)
 {
     __shared__ float buf[2][32];
     constexpr bool kAhead = V == 1, kKeep = V <= 2;
-    const int t = threadIdx.x;
-    f8 w[V], dw[V], h[V], dy[V];
+    constexpr int kRows = Back<T>::kThreads / T;
+    const int t = threadIdx.x % T, group = threadIdx.x / T;
+    f8 dw[V];
+    Raw8<W> w[V];
+    Raw8<X> h[V], dy[V], dres[V];
     const auto left = [&](int k) { return max(0, min(8, (int)a.cols - (k * T + t) * 8)); };
-    const auto load_w = [&](int k) { return load_some(static_cast<const W*>(a.w) + (k * T + t) * 8, a.wide_w && left(k) == 8, left(k)); };
-    const auto fetch = [&](const void* p, int64_t ld, int64_t r, int k) {
-        return load_some(static_cast<const X*>(p) + r * ld + (k * T + t) * 8, a.wide && left(k) == 8, left(k));
+    const auto load_w = [&](int k) { w[k].load(static_cast<const W*>(a.w) + (k * T + t) * 8, a.wide_w && left(k) == 8, left(k)); };
+    const auto fetch = [&](Raw8<X>& x, const void* p, int64_t ld, int64_t r, int k) {
+        const int here = r < a.rows ? left(k) : 0;
+        x.load(static_cast<const X*>(p) + r * ld + (k * T + t) * 8, a.wide && here == 8, here);
     };
+    const auto rstd_of = [&](int64_t r) { return r < a.rows ? a.rstd[r] : 0.f; };
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        if (kKeep) w[k] = load_w(k);
+        if (kKeep) load_w(k);
 #pragma unroll
         for (int q = 0; q < 8; ++q) dw[k].v[q] = 0.f;
     }
-    int64_t row = blockIdx.x;                      // the grid has no more blocks than there are rows
-    f8 nh = {}, ndy = {};
+    int64_t first = (int64_t)blockIdx.x * kRows;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    Raw8<X> nh = {}, ndy = {}, ndres = {};
     float next_rstd = 0.f;
-    if (kAhead) {
-        nh = fetch(a.h, a.ldh, row, 0);
-        ndy = fetch(a.dy, a.lddy, row, 0);
-        next_rstd = a.rstd[row];
-    }
-    for (int turn = 0; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const float rs = kAhead ? next_rstd : a.rstd[row];
-        f8 dres[V];
+    const auto ahead = [&](int64_t r) {
+        fetch(nh, a.h, a.ldh, r, 0);
+        fetch(ndy, a.dy, a.lddy, r, 0);
+        if (a.dres) fetch(ndres, a.dres, a.lddres, r, 0);
+        next_rstd = rstd_of(r);
+    };
+    if (kAhead) ahead(first + group);
+    for (int turn = 0; first < a.rows; first += step, turn ^= 1) {
+        const int64_t row = first + group;
+        const float rs = kAhead ? next_rstd : rstd_of(row);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            if (kKeep) h[k] = kAhead ? nh : fetch(a.h, a.ldh, row, k);
-            if (kKeep) dy[k] = kAhead ? ndy : fetch(a.dy, a.lddy, row, k);
-            if (kAhead && a.dres) dres[k] = fetch(a.dres, a.lddres, row, k);
+            if (kAhead) {
+                h[k] = nh;
+                dy[k] = ndy;
+                dres[k] = ndres;
+            } else if (kKeep) {
+                fetch(h[k], a.h, a.ldh, row, k);
+                fetch(dy[k], a.dy, a.lddy, row, k);
+                if (a.dres) fetch(dres[k], a.dres, a.lddres, row, k);
+            }
         }
-        if (kAhead && row + gridDim.x < a.rows) {
-            nh = fetch(a.h, a.ldh, row + gridDim.x, 0);
-            ndy = fetch(a.dy, a.lddy, row + gridDim.x, 0);
-            next_rstd = a.rstd[row + gridDim.x];
-        }
+        if (kAhead && first + step < a.rows) ahead(row + step);
         float dot = 0.f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const f8 wk = kKeep ? w[k] : load_w(k), hk = kKeep ? h[k] : fetch(a.h, a.ldh, row, k), dk = kKeep ? dy[k] : fetch(a.dy, a.lddy, row, k);
+            if (!kKeep) {
+                load_w(k);
+                fetch(h[k], a.h, a.ldh, row, k);
+                fetch(dy[k], a.dy, a.lddy, row, k);
+            }
+            const f8 wk = w[k].values(), hk = h[k].values(), dk = dy[k].values();
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const float xn = __fmul_rn(hk.v[q], rs);
@@ -204,51 +237,77 @@ __global__ void __launch_bounds__(T) rmsnorm_backward_kernel(const Backward a)
         const float mean = __fmul_rn(row_sum<T>(dot, buf, turn), a.inv_cols);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const f8 wk = kKeep ? w[k] : load_w(k), hk = kKeep ? h[k] : fetch(a.h, a.ldh, row, k), dk = kKeep ? dy[k] : fetch(a.dy, a.lddy, row, k);
-            if (!kAhead && a.dres) dres[k] = fetch(a.dres, a.lddres, row, k);
+            if (!kKeep) {
+                load_w(k);
+                fetch(h[k], a.h, a.ldh, row, k);
+                fetch(dy[k], a.dy, a.lddy, row, k);
+                if (a.dres) fetch(dres[k], a.dres, a.lddres, row, k);
+            }
+            const f8 wk = w[k].values(), hk = h[k].values(), dk = dy[k].values(), rk = dres[k].values();
             f8 x;
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const float xn = __fmul_rn(hk.v[q], rs);
                 x.v[q] = __fmul_rn(__fmaf_rn(-xn, mean, __fmul_rn(dk.v[q], wk.v[q])), rs);
-                if (a.dres) x.v[q] = __fadd_rn(x.v[q], dres[k].v[q]);
+                if (a.dres) x.v[q] = __fadd_rn(x.v[q], rk.v[q]);
             }
-            store_some(static_cast<X*>(a.dx) + row * a.lddx + (k * T + t) * 8, x, a.wide && left(k) == 8, left(k));
+            const int here = row < a.rows ? left(k) : 0;
+            store_some(static_cast<X*>(a.dx) + row * a.lddx + (k * T + t) * 8, x, a.wide && here == 8, here);
         }
     }
+    // the block's sums: its groups' in their order
+    if constexpr (kRows > 1) {
+        __shared__ float all[kRows][T * 8];
 #pragma unroll
-    for (int k = 0; k < V; ++k)
+        for (int q = 0; q < 8; ++q) all[group][t * 8 + q] = dw[0].v[q];
+        __syncthreads();
+        for (int c = threadIdx.x; c < (int)a.cols; c += Back<T>::kThreads) {
+            float s = all[0][c];
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < left(k)) a.part[(int64_t)blockIdx.x * a.cols + (k * T + t) * 8 + q] = dw[k].v[q];
+            for (int g = 1; g < kRows; ++g) s += all[g][c];
+            a.part[(int64_t)blockIdx.x * a.cols + c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < left(k)) a.part[(int64_t)blockIdx.x * a.cols + (k * T + t) * 8 + q] = dw[k].v[q];
+    }
 }
 
-// dweight[c] = sum of the blocks' partial sums, in an order that depends on their number alone: 8 threads a column.
-__global__ void __launch_bounds__(256) dweight_kernel(const float* part, float* dweight, int64_t cols, int blocks)
+// dweight[c] = sum of the blocks' partial sums, in an order that depends on their number alone: 32 threads a column, each adding every
+// 32nd block's, then a tree.
+__global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float* dweight, int64_t cols, int blocks)
 {
-    __shared__ float sum[8][32];
+    __shared__ float sum[32][33];
     const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (c < cols)
-#pragma unroll 4
-        for (int b = y; b < blocks; b += 8) s += part[(int64_t)b * cols + c];
+    if (c < cols) {
+#pragma unroll 10
+        for (int b = y; b < blocks; b += 32) s += part[(int64_t)b * cols + c];
+    }
     sum[y][lane] = s;
     __syncthreads();
-    if (y == 0 && c < cols) {
+    s = sum[lane][y];                              // now the column is block * 32 + y, and its 32 sums lie along the warp
 #pragma unroll
-        for (int k = 1; k < 8; ++k) s += sum[k][lane];
-        dweight[c] = s;
-    }
+    for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    const int64_t cy = (int64_t)blockIdx.x * 32 + y;
+    if (lane == 0 && cy < cols) dweight[cy] = s;
 }
 
 template <typename X, typename W, int T, int V>
 int backward_launch(const Backward& a, float* dweight, cudaStream_t s)
 {
-    const int blocks = (int)(a.rows < kBackBlocks ? a.rows : kBackBlocks);
-    rmsnorm_backward_kernel<X, W, T, V><<<blocks, T, 0, s>>>(a);
+    // as many blocks as are resident at once, of which each has a row to begin with
+    constexpr int kRows = Back<T>::kThreads / T, kResident = V == 1 ? 148 * (sizeof(X) == 2 ? 1024 : 768) / Back<T>::kThreads : 148;
+    static_assert(kResident <= kBackBlocks, "the workspace holds kBackBlocks partial sums");
+    const int64_t need = (a.rows + kRows - 1) / kRows;
+    const int blocks = (int)(need < kResident ? need : kResident);
+    rmsnorm_backward_kernel<X, W, T, V><<<blocks, Back<T>::kThreads, 0, s>>>(a);
     OPS_TRY(launched("hpsgd_rmsnorm_backward"));
-    dweight_kernel<<<(unsigned)((a.cols + 31) / 32), 256, 0, s>>>(a.part, dweight, a.cols, blocks);
+    dweight_kernel<<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a.part, dweight, a.cols, blocks);
     return launched("hpsgd_rmsnorm_backward");
 }
 
