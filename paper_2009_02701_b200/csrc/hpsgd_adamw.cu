@@ -8,7 +8,6 @@
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
-#include <cuda_fp16.h>
 
 namespace hpsgd {
 namespace ops {
@@ -102,36 +101,6 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 u, bool wide, int 
         if (q < left) p[q] = (uint8_t)((q < 4 ? u.x : u.y) >> 8 * (q & 3));
 }
 
-// ---------------------------------------------------------------------------- two values at a time
-// The packed binary32 instructions round each half as the scalar ones do and take one issue slot for two results.
-typedef unsigned long long pair;
-
-__device__ __forceinline__ pair make_pair(float lo, float hi)
-{
-    pair x;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
-    return x;
-}
-__device__ __forceinline__ void split(pair x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
-__device__ __forceinline__ pair add2(pair a, pair b)
-{
-    pair x;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
-__device__ __forceinline__ pair fma2(pair a, pair b, pair c)
-{
-    pair x;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
-    return x;
-}
-__device__ __forceinline__ pair both(float x) { return make_pair(x, x); }
-__device__ __forceinline__ pair mul2(pair a, pair b)
-{
-    pair x;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
 // A sum of products that are each rounded: a packed addition behind packed multiplications was seen to come out with one rounding fewer,
 // so this one is scalar.
 __device__ __forceinline__ pair sum_of_rounded(pair a, pair b)
@@ -142,45 +111,7 @@ __device__ __forceinline__ pair sum_of_rounded(pair a, pair b)
     return make_pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
 }
 
-struct p4 {
-    pair v[4];
-};
-
-__device__ __forceinline__ p4 to_pairs(const f8& x)
-{
-    p4 y;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) y.v[q] = make_pair(x.v[2 * q], x.v[2 * q + 1]);
-    return y;
-}
-__device__ __forceinline__ f8 to_values(const p4& x)
-{
-    f8 y;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) split(x.v[q], y.v[2 * q], y.v[2 * q + 1]);
-    return y;
-}
-
 // ---------------------------------------------------------------------------- codes
-// Two codes (the low 16 bits) to two values: the conversion goes through f16, which holds every E4M3 value and its NaN.
-__device__ __forceinline__ pair decode_pair(uint32_t two)
-{
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    return make_pair(f.x, f.y);
-}
-
-__device__ __forceinline__ p4 decode8(uint2 u)
-{
-    p4 x;
-    x.v[0] = decode_pair(u.x);
-    x.v[1] = decode_pair(u.x >> 16);
-    x.v[2] = decode_pair(u.y);
-    x.v[3] = decode_pair(u.y >> 16);
-    return x;
-}
-
 // What multiplies a value of a block with scale 2^(byte - 127) so that the value's E4M3 code comes to stand in bits 20..26 of
 // its binary32 pattern: 2^(127 - byte - 120), in one factor as long as that is a normal number.  Blocks above 2^6 * 448, whose
 // factor is not, first have their values multiplied by the rest (`excess`).  The largest patterns of values that are not finite

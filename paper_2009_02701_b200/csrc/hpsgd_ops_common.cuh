@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "hpsgd_internal.h"
 
@@ -152,6 +153,74 @@ __device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int lef
         if (q < left) store1(p + q, x.v[q]);
 }
 
+// ---------------------------------------------------------------------------- two values at a time
+// The packed binary32 instructions round each half as the scalar ones do and take one issue slot for two results.
+typedef unsigned long long pair;
+
+__device__ __forceinline__ pair make_pair(float lo, float hi)
+{
+    pair x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
+    return x;
+}
+__device__ __forceinline__ void split(pair x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ pair add2(pair a, pair b)
+{
+    pair x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ pair fma2(pair a, pair b, pair c)
+{
+    pair x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ pair both(float x) { return make_pair(x, x); }
+__device__ __forceinline__ pair mul2(pair a, pair b)
+{
+    pair x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+struct p4 {
+    pair v[4];
+};
+
+__device__ __forceinline__ p4 to_pairs(const f8& x)
+{
+    p4 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y.v[q] = make_pair(x.v[2 * q], x.v[2 * q + 1]);
+    return y;
+}
+__device__ __forceinline__ f8 to_values(const p4& x)
+{
+    f8 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) split(x.v[q], y.v[2 * q], y.v[2 * q + 1]);
+    return y;
+}
+
+// Two codes (the low 16 bits) to two values: the conversion goes through f16, which holds every E4M3 value and its NaN.
+__device__ __forceinline__ pair decode_pair(uint32_t two)
+{
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    return make_pair(f.x, f.y);
+}
+
+__device__ __forceinline__ p4 decode8(uint2 u)
+{
+    p4 x;
+    x.v[0] = decode_pair(u.x);
+    x.v[1] = decode_pair(u.x >> 16);
+    x.v[2] = decode_pair(u.y);
+    x.v[3] = decode_pair(u.y >> 16);
+    return x;
+}
+
 // Eight values as they are stored (half the registers of their binary32 values where they are bf16): requested early, widened when used.
 template <typename T>
 struct Raw8;
@@ -225,15 +294,24 @@ __device__ __forceinline__ int block_scale(f8& x)
     return scale_byte(__uint_as_float(block_top(t, half)));
 }
 
-// Codes to nearest even of eight values of a block with that scale (magnitudes up to 448 times it, or NaN).
+// Four codes to nearest even (of magnitudes up to 448, or NaN).
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
+{
+    unsigned short lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return lo | (uint32_t)hi << 16;
+}
+
+// Codes of eight values of a block with that scale.
 __device__ __forceinline__ uint2 encode_nearest(const f8& x, int byte)
 {
-    const float inv = scale_inverse(byte);
-    unsigned short h[4];
+    const pair inv = both(scale_inverse(byte));
+    p4 y = to_pairs(x);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[q]) : "f"(__fmul_rn(x.v[2 * q + 1], inv)), "f"(__fmul_rn(x.v[2 * q], inv)));
-    return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+    for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], inv);
+    const f8 z = to_values(y);
+    return make_uint2(codes4(z.v[0], z.v[1], z.v[2], z.v[3]), codes4(z.v[4], z.v[5], z.v[6], z.v[7]));
 }
 
 // Where the scale of block b of row r stands: words of four blocks, the rows' words of one group of four next to one another.

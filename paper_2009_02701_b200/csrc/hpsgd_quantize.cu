@@ -28,125 +28,147 @@ struct QuantArgs {
 
 struct Fp8 {};
 
-__device__ __forceinline__ f8 decode_nearest(uint2 u, float scale)
-{
-    f8 x;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) x.v[q] = __fmul_rn(e4m3_value((q < 4 ? u.x : u.y) >> 8 * (q & 3) & 0xFFu), scale);
-    return x;
-}
-
-// The padding behind a row's last block in its last word of scales.
-__device__ __forceinline__ void store_scale(uint8_t* s, int64_t b, int64_t blocks, int64_t r, int64_t ld, int byte)
-{
-    s[scale_index(b, r, ld)] = (uint8_t)byte;
-    if (b == blocks - 1)
-        for (int64_t k = b + 1; k & 3; ++k) s[scale_index(k, r, ld)] = 0;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kQThreads, 2) quantize_kernel(const QuantArgs a)
 {
     constexpr int kRows = 4, kWarps = kQThreads / 32;
-    __shared__ uint32_t col_top[kWarps][kTile];      // largest magnitudes (patterns) of each warp's eight rows
+    __shared__ float col_top[kWarps][kTile];         // largest magnitudes of each warp's eight rows
     __shared__ alignas(16) uint32_t tile[kTile][kTile / 4];      // the transpose: [column][four rows], words permuted by the column's patch
-    __shared__ alignas(16) uint8_t col_byte[kTile];
+    __shared__ alignas(16) float col_inverse[kTile];
     __shared__ int odd;                              // some column of the tile has values that are not finite
     constexpr bool kCodes = sizeof(T) == 1;
     const int lane = threadIdx.x & 15, patch = threadIdx.x >> 4, warp = threadIdx.x >> 5;
-    const int64_t tiles_c = (a.cols + kTile - 1) / kTile;
-    const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * kTile, c0 = (int64_t)(blockIdx.x % tiles_c) * kTile;
-    const int64_t row0 = r0 + patch * kRows, col0 = c0 + lane * 8;
-    const int left = (int)max((int64_t)0, min((int64_t)8, a.cols - col0));
+    const int tiles_c = (int)((a.cols + kTile - 1) / kTile), tiles_r = (int)((a.rows + kTile - 1) / kTile);
+    const int br = (int)(blockIdx.x / (unsigned)tiles_c), bc = (int)(blockIdx.x % (unsigned)tiles_c);      // the tile, and the blocks' numbers
+    const int row0 = br * kTile + patch * kRows, col0 = bc * kTile + lane * 8;
+    const int left = max(0, min(8, (int)a.cols - col0)), rows = (int)a.rows - row0;      // of this patch
     if (threadIdx.x == 0) odd = 0;
 
     f8 x[kRows];
+    if constexpr (kCodes) {
+        const uint8_t* p = static_cast<const uint8_t*>(a.x) + row0 * a.ldx + col0;
+        const uint8_t* s = a.xs + scale_index(bc, row0, a.ldxs);
+        uint2 u[kRows];
+        int byte[kRows];
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        const int here = row0 + k < a.rows ? left : 0;
-        if constexpr (kCodes) {
-            uint2 u = make_uint2(0u, 0u);
-            int byte = 0;
-            if (here) {                               // the codes behind the last column, up to 16, can be read: they are masked below
-                u = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.x) + (row0 + k) * a.ldx + col0);
-                byte = a.xs[scale_index(c0 / kTile, row0 + k, a.ldxs)];
-            }
-            x[k] = decode_nearest(u, scale_value(byte));
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j >= here) x[k].v[j] = 0.f;
-        } else {
-            x[k] = load_some(static_cast<const T*>(a.x) + (row0 + k) * a.ldx + col0, a.wide && here == 8, here);
+        for (int k = 0; k < kRows; ++k) {            // the codes behind the last column, up to 16, can be read: they are masked below
+            const bool in = k < rows && left > 0;
+            u[k] = in ? *reinterpret_cast<const uint2*>(p + k * a.ldx) : make_uint2(0u, 0u);
+            byte[k] = in ? s[4 * k] : 0;
         }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            p4 y = decode8(u[k]);
+            const pair f = both(scale_value(byte[k]));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], f);
+            x[k] = to_values(y);
+            if (left < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j >= left) x[k].v[j] = 0.f;
+            }
+        }
+    } else {
+        const T* p = static_cast<const T*>(a.x) + row0 * a.ldx + col0;
+        Raw8<T> raw[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int here = k < rows ? left : 0;
+            raw[k].load(p + k * a.ldx, a.wide && here == 8, here);
+        }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) x[k] = raw[k].values();
     }
 
     if constexpr (!kCodes) {
         if (a.q) {
-            const int64_t b = c0 / kTile, pad = (a.cols + 15) / 16 * 16;
+            int byte[kRows];
+            uint8_t* const q = a.q + row0 * a.ldq + col0;
+            const bool inside = col0 < (a.cols + 15) / 16 * 16;
 #pragma unroll
             for (int k = 0; k < kRows; ++k) {
                 f8 y = x[k];
-                const int byte = block_scale(y);
-                if (row0 + k < a.rows) {
-                    if (col0 < pad) *reinterpret_cast<uint2*>(a.q + (row0 + k) * a.ldq + col0) = encode_nearest(y, byte);
-                    if (lane == 0) store_scale(a.s, b, tiles_c, row0 + k, a.lds, byte);
-                }
+                byte[k] = block_scale(y);
+                const uint2 codes = encode_nearest(y, byte[k]);
+                if (inside && k < rows) *reinterpret_cast<uint2*>(q + k * a.ldq) = codes;
+            }
+            if (lane < min(kRows, rows)) {            // one lane a row
+                uint8_t* const s = a.s + scale_index(bc, row0 + lane, a.lds);
+                *s = (uint8_t)(lane & 2 ? lane & 1 ? byte[3] : byte[2] : lane & 1 ? byte[1] : byte[0]);
+                if (bc == tiles_c - 1)                // zeros behind the row's last block
+                    for (int k = 1; (bc + k) & 3; ++k) s[k] = 0;
             }
         }
     }
     if (!a.qt) return;
 
     // column maxima: over the rows of a warp here, over the warps through shared memory
-    const auto maxima = [&](bool only_finite) {
+    const auto maxima = [&]() {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            uint32_t t = 0;
-#pragma unroll
-            for (int k = 0; k < kRows; ++k) {
-                const uint32_t u = __float_as_uint(fabsf(x[k].v[j]));
-                if (!only_finite || u < 0x7F800000u) t = max(t, u);
-            }
-            t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
+            float t;
+            asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(t) : "f"(x[0].v[j]), "f"(x[1].v[j]), "f"(x[2].v[j]));
+            asm("max.NaN.abs.f32 %0, %1, %2, %2;" : "=f"(t) : "f"(t), "f"(x[3].v[j]));
+            const float other = __shfl_xor_sync(0xFFFFFFFFu, t, 16);
+            asm("max.NaN.f32 %0, %0, %1;" : "+f"(t) : "f"(other));
             if (threadIdx.x & 16 ? j >= 4 : j < 4) col_top[warp][lane * 8 + j] = t;
         }
         __syncthreads();
         if (threadIdx.x < kTile) {
-            uint32_t t = 0;
+            float t = 0.f;
 #pragma unroll
-            for (int p = 0; p < kWarps; ++p) t = max(t, col_top[p][threadIdx.x]);
-            if (t >= 0x7F800000u) odd = 1;
-            const int byte = scale_byte(__uint_as_float(t));
-            col_byte[threadIdx.x] = (uint8_t)byte;
-            if (t < 0x7F800000u && c0 + threadIdx.x < a.cols)
-                store_scale(a.st, r0 / kTile, (a.rows + kTile - 1) / kTile, c0 + threadIdx.x, a.ldst, byte);
+            for (int p = 0; p < kWarps; ++p) asm("max.NaN.f32 %0, %0, %1;" : "+f"(t) : "f"(col_top[p][threadIdx.x]));
+            if (!finite(t)) odd = 1;
+            const int byte = scale_byte(t), c = bc * kTile + threadIdx.x;
+            col_inverse[threadIdx.x] = scale_inverse(byte);
+            if (finite(t) && c < a.cols) {
+                uint8_t* const s = a.st + scale_index(br, c, a.ldst);
+                *s = (uint8_t)byte;
+                if (br == tiles_r - 1)
+                    for (int k = 1; (br + k) & 3; ++k) s[k] = 0;
+            }
         }
         __syncthreads();
     };
-    maxima(false);
-    if (odd) {                                        // rare: the scales are those of the finite values, and the others become NaN
-        maxima(true);
+    maxima();
+    uint32_t bad = 0;                                 // which of the patch's values become NaN
+    if (odd) {                                        // rare: the scales are those of the finite values
 #pragma unroll
         for (int k = 0; k < kRows; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (!finite(x[k].v[j])) x[k].v[j] = __uint_as_float(0x7FC00000u);
-    }
-    const uint2 bytes = *reinterpret_cast<const uint2*>(col_byte + lane * 8);
+                if (!finite(x[k].v[j])) {
+                    bad |= 1u << (k * 8 + j);
+                    x[k].v[j] = 0.f;
+                }
+        maxima();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float inv = scale_inverse((j < 4 ? bytes.x : bytes.y) >> 8 * (j & 3) & 0xFFu);
-        unsigned short lo, hi;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fmul_rn(x[1].v[j], inv)), "f"(__fmul_rn(x[0].v[j], inv)));
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fmul_rn(x[3].v[j], inv)), "f"(__fmul_rn(x[2].v[j], inv)));
-        tile[lane * 8 + j][patch ^ 2 * lane] = lo | (uint32_t)hi << 16;
+        for (int k = 0; k < kRows; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (bad >> (k * 8 + j) & 1u) x[k].v[j] = __uint_as_float(0x7FC00000u);
     }
+    const float4 i0 = *reinterpret_cast<const float4*>(col_inverse + lane * 8), i1 = *reinterpret_cast<const float4*>(col_inverse + lane * 8 + 4);
+    const pair inverse[4] = {make_pair(i0.x, i0.y), make_pair(i0.z, i0.w), make_pair(i1.x, i1.y), make_pair(i1.z, i1.w)};
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        p4 y = to_pairs(x[k]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y.v[q] = mul2(y.v[q], inverse[q]);
+        x[k] = to_values(y);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[lane * 8 + j][patch ^ 2 * lane] = codes4(x[0].v[j], x[1].v[j], x[2].v[j], x[3].v[j]);
     __syncthreads();
-    const int64_t pad_t = (a.rows + 15) / 16 * 16;
+    // a half warp takes one row of the transpose
+    if (br * kTile + lane * 8 < (a.rows + 15) / 16 * 16) {
+        uint8_t* const qt = a.qt + (int64_t)(bc * kTile + patch) * a.ldqt + br * kTile + lane * 8;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int c = k * 32 + patch;                 // a half warp takes one row of the transpose
-        if (c0 + c < a.cols && r0 + lane * 8 < pad_t)
-            *reinterpret_cast<uint2*>(a.qt + (c0 + c) * a.ldqt + r0 + lane * 8) = *reinterpret_cast<const uint2*>(&tile[c][2 * lane ^ 2 * (c >> 3)]);
+        for (int k = 0; k < 4; ++k) {
+            const int c = k * 32 + patch;
+            if (bc * kTile + c < a.cols) *reinterpret_cast<uint2*>(qt + k * 32 * a.ldqt) = *reinterpret_cast<const uint2*>(&tile[c][2 * lane ^ 2 * (c >> 3)]);
+        }
     }
 }
 
