@@ -32,15 +32,14 @@ struct Item {
     int64_t n;
     uint64_t rng;
     float keep;            // 1 - lr * weight_decay
-    uint32_t first;        // first chunk of this tensor
     uint32_t wide;         // all addresses allow the wide accesses
-    uint32_t pad;
 };
 
 template <int CAP>
 struct Table {
-    Item item[CAP];
     int count;
+    uint32_t first[CAP];   // first chunk of each tensor (by themselves: a block's search touches few lines of the parameters)
+    Item item[CAP];
 };
 
 struct Hyper {
@@ -60,7 +59,7 @@ __device__ __forceinline__ int find_item(const Table<CAP>& t, uint32_t chunk)
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (t.item[mid].first <= chunk) lo = mid;
+        if (t.first[mid] <= chunk) lo = mid;
         else hi = mid - 1;
     }
     return lo;
@@ -411,9 +410,9 @@ __device__ __forceinline__ void adamw_group(const Share& it, const Hyper& hy, fl
 template <int CAP, typename P, typename G, bool B8>
 __global__ void __launch_bounds__(kAdamThreads, B8 ? 6 : 7) adamw_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ Hyper hy)
 {
-    const Item& it = table.item[find_item(table, blockIdx.x)];
-    const float c = hy.scale ? *hy.scale : 1.f;
-    const int64_t at = (int64_t)(blockIdx.x - it.first) * hy.span;
+    const int which = find_item(table, blockIdx.x);
+    const Item& it = table.item[which];
+    const int64_t at = (int64_t)(blockIdx.x - table.first[which]) * hy.span;
     const int here = (int)min((int64_t)hy.span, it.n - at);
     Share sh;
     sh.p = static_cast<P*>(it.p) + at;
@@ -426,6 +425,8 @@ __global__ void __launch_bounds__(kAdamThreads, B8 ? 6 : 7) adamw_kernel(const _
     sh.rng = it.rng + (uint64_t)at;
     sh.keep = it.keep;
     sh.wide = it.wide;
+    after_previous();
+    const float c = hy.scale ? *hy.scale : 1.f;
     const int tid8 = threadIdx.x * 8;
     if constexpr (B8) {
         if (sh.wide && here == hy.span) {
@@ -475,10 +476,12 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     __shared__ double part[kNormThreads / 32];
     __shared__ bool last;
     double sum = 0.0;
+    after_previous();
     for (uint32_t chunk = blockIdx.x; chunk < no.chunks; chunk += gridDim.x) {
-        const Item& it = table.item[find_item(table, chunk)];
+        const int which = find_item(table, chunk);
+        const Item& it = table.item[which];
         const G* const gp = static_cast<const G*>(it.g);
-        const int64_t base = (int64_t)(chunk - it.first) * kNormChunk + threadIdx.x * 8;
+        const int64_t base = (int64_t)(chunk - table.first[which]) * kNormChunk + threadIdx.x * 8;
         f8 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -560,7 +563,7 @@ uint32_t fill_table(const hpsgd_adamw_tensor* t, int n, int* at, int64_t chunk_e
         it = Item{};
         it.n = t[*at].n;
         it.g = t[*at].grad;
-        it.first = (uint32_t)chunks;
+        out->first[out->count - 1] = (uint32_t)chunks;
         fill(t[*at], &it);
         chunks += here;
     }
@@ -589,8 +592,7 @@ int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, Hyper hy, int s
             it->wide = aligned(x.param, ap) && aligned(x.grad, ag) && aligned(x.m, as) && aligned(x.v, as) && aligned(x.copy, 16);
         });
         if (!chunks) continue;
-        adamw_kernel<CAP, P, G, B8><<<chunks, kAdamThreads, 0, s>>>(table, hy);
-        OPS_TRY(launched("hpsgd_adamw_step"));
+        OPS_TRY(launch_early("hpsgd_adamw_step", adamw_kernel<CAP, P, G, B8>, dim3(chunks), kAdamThreads, 0, s, table, hy));
     }
     return HPSGD_OK;
 }
@@ -626,8 +628,7 @@ int norm_launches(const hpsgd_adamw_tensor* t, int n, int sms, double max_norm, 
     do {
         no.chunks = fill_table(t, n, &at, kNormChunk, &table, fill);
         const int grid = grid_of(no.chunks);
-        grad_norm_kernel<CAP, G><<<grid, kNormThreads, 0, s>>>(table, no);
-        OPS_TRY(launched("hpsgd_grad_norm"));
+        OPS_TRY(launch_early("hpsgd_grad_norm", grad_norm_kernel<CAP, G>, dim3(grid), kNormThreads, 0, s, table, no));
         no.before += grid;
     } while (at < n);
     return HPSGD_OK;
@@ -689,7 +690,9 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
     hy.key0 = (uint32_t)key; hy.key1 = (uint32_t)(key >> 32);
     hy.scale = grad_scale;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // The host copies a kernel's parameters at every launch: 62 tensors' step with its norm takes 72 us by the largest table, 66 by the middle one (and launched early).
     if (n_tensors <= 8) return step_types<8>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
+    if (n_tensors <= 64) return step_types<64>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
     return step_types<kMaxItems>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
 }
 
@@ -708,6 +711,9 @@ int hpsgd_grad_norm(const hpsgd_adamw_tensor* tensors, int n_tensors, int grad_d
     if (n_tensors <= 8)
         return f ? norm_launches<8, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
                  : norm_launches<8, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
+    if (n_tensors <= 64)
+        return f ? norm_launches<64, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
+                 : norm_launches<64, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
     return f ? norm_launches<kMaxItems, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
              : norm_launches<kMaxItems, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
 }

@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     __syncthreads();
     if constexpr (PAIR) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    after_previous();
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
     const int units = a.tiles * a.splits;
 
@@ -559,16 +560,18 @@ int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int 
     int dev = 0;
     OPS_CUDA(cudaGetDevice(&dev));
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr{};
+    cudaLaunchAttribute attr[2] = {};
     cfg.gridDim = dim3(PAIR ? 2 : 1);
     cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = s;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = PAIR ? 2 : 1;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = PAIR ? 1 : 0;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;          // see launch_early
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2 : 1;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
     int at_once = dev < 64 ? workers[dev] : 0;
     if (at_once == 0) {
         OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, PAIR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));

@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(kQThreads, 2) quantize_kernel(const QuantArgs 
     const int row0 = br * kTile + patch * kRows, col0 = bc * kTile + lane * 8;
     const int left = max(0, min(8, (int)a.cols - col0)), rows = (int)a.rows - row0;      // of this patch
     if (threadIdx.x == 0) odd = 0;
+    after_previous();
 
     f8 x[kRows];
     if constexpr (kCodes) {
@@ -227,8 +228,7 @@ extern "C" int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* str
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int64_t unit = p.dtype == HPSGD_F32 ? 32 : 16, esz = p.dtype == HPSGD_F32 ? 4 : 2;
     a.wide = aligned(p.x, unit) && p.ldx * esz % unit == 0;
-    if (p.dtype == HPSGD_F32) quantize_kernel<float><<<(unsigned)tiles, kQThreads, 0, s>>>(a);
-    else if (p.dtype == HPSGD_BF16) quantize_kernel<__nv_bfloat16><<<(unsigned)tiles, kQThreads, 0, s>>>(a);
-    else quantize_kernel<Fp8><<<(unsigned)tiles, kQThreads, 0, s>>>(a);
-    return launched(what);
+    if (p.dtype == HPSGD_F32) return launch_early(what, quantize_kernel<float>, dim3((unsigned)tiles), kQThreads, 0, s, a);
+    if (p.dtype == HPSGD_BF16) return launch_early(what, quantize_kernel<__nv_bfloat16>, dim3((unsigned)tiles), kQThreads, 0, s, a);
+    return launch_early(what, quantize_kernel<Fp8>, dim3((unsigned)tiles), kQThreads, 0, s, a);
 }

@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(T < 128 ? 128 : T) rmsnorm_forward_kernel(cons
     f8 f[V];
     Raw8<X> x[V], r[V];
     Raw8<W> w[V];
+    after_previous();
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = (k * T + t) * 8, left = in ? max(0, min(8, (int)a.cols - c)) : 0;
@@ -124,8 +125,7 @@ int forward_launch(const Forward& a, cudaStream_t s)
     constexpr int kRows = T < 128 ? 128 / T : 1;
     const int64_t blocks = (a.rows + kRows - 1) / kRows;
     if (blocks > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "hpsgd_rmsnorm_forward: too many rows");
-    rmsnorm_forward_kernel<X, W, T, V><<<(unsigned)blocks, T < 128 ? 128 : T, 0, s>>>(a);
-    return launched("hpsgd_rmsnorm_forward");
+    return launch_early("hpsgd_rmsnorm_forward", rmsnorm_forward_kernel<X, W, T, V>, dim3((unsigned)blocks), T < 128 ? 128 : T, 0, s, a);
 }
 
 template <typename X, typename W>
@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(Back<T>::kThreads, V == 1 ? (sizeof(X) == 2 ? 
         const int here = r < a.rows ? left(k) : 0;
         x.load(static_cast<const X*>(p) + r * ld + (k * T + t) * 8, a.wide && here == 8, here);
     };
+    after_previous();
     const auto rstd_of = [&](int64_t r) { return r < a.rows ? a.rstd[r] : 0.f; };
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -284,6 +285,7 @@ __global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float*
     const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.f;
+    after_previous();
     if (c < cols) {
 #pragma unroll 10
         for (int b = y; b < blocks; b += 32) s += part[(int64_t)b * cols + c];
@@ -305,10 +307,8 @@ int backward_launch(const Backward& a, float* dweight, cudaStream_t s)
     static_assert(kResident <= kBackBlocks, "the workspace holds kBackBlocks partial sums");
     const int64_t need = (a.rows + kRows - 1) / kRows;
     const int blocks = (int)(need < kResident ? need : kResident);
-    rmsnorm_backward_kernel<X, W, T, V><<<blocks, Back<T>::kThreads, 0, s>>>(a);
-    OPS_TRY(launched("hpsgd_rmsnorm_backward"));
-    dweight_kernel<<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a.part, dweight, a.cols, blocks);
-    return launched("hpsgd_rmsnorm_backward");
+    OPS_TRY(launch_early("hpsgd_rmsnorm_backward", rmsnorm_backward_kernel<X, W, T, V>, dim3(blocks), Back<T>::kThreads, 0, s, a));
+    return launch_early("hpsgd_rmsnorm_backward", dweight_kernel, dim3((unsigned)((a.cols + 31) / 32)), 1024, 0, s, (const float*)a.part, dweight, a.cols, blocks);
 }
 
 template <typename X, typename W>
