@@ -295,6 +295,30 @@ int hpsgd_local_step_all(const void* grads, int64_t worker_stride_bytes);
 int hpsgd_local_step_all_ex(const hpsgd_grad_desc* descs);
 
 /*
+ * (The paper trains with SGD only; this is the local step that language models are trained with.)
+ *
+ * One local step of worker `worker` with AdamW in place of SGD, over the whole flat buffer: replica r_i is stepped as the one
+ * tensor of hpsgd_adamw_step (hpsgd_ops.h has the formula, the 8-bit format of the moments and their stochastic rounding; the
+ * seed is hpsgd_init's seed + worker * M1, see hpsgd_gen_grads).  The learning rate, momentum and weight decay of hpsgd_init and
+ * hpsgd_set_option are not used.  `grads` is as in hpsgd_local_step.  The moments are the caller's, one set for each worker, in
+ * the flat layout (P_pad elements; with state_bits 8 ceil(P_pad / 128) scale bytes each) and zero before the first step; they are
+ * neither merged nor part of hpsgd_export_state.  Everything else is as for hpsgd_local_step: the merge averages the replica
+ * changes, whatever made them.  Enqueued on the main stream; never held back by HPSGD_OPT_FUSE.  Replica-change form only (else
+ * HPSGD_E_STATE).
+ */
+typedef struct hpsgd_adamw_args {
+    void* m;
+    void* v;
+    uint8_t* m_scale;         /* state_bits 8 only */
+    uint8_t* v_scale;
+    int state_bits;           /* 32 or 8 */
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;             /* this worker's step, from 1 */
+    const float* grad_scale;  /* device; what multiplies the gradient (hpsgd_grad_norm), or NULL */
+} hpsgd_adamw_args;
+int hpsgd_local_step_adamw(int worker, const void* grads, const hpsgd_adamw_args* args);
+
+/*
  * (The paper has no counterpart for this call; it exists for deployment reasons only.)
  *
  * A sparse-row local step that allocates nothing.  Some programs that would like to call

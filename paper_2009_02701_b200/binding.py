@@ -34,6 +34,12 @@ class hpsgd_grad_desc(ctypes.Structure):
                 ("n_rows", ctypes.c_int32), ("row_vals", ctypes.c_void_p)]
 
 
+class hpsgd_adamw_args(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("state_bits", ctypes.c_int), ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("grad_scale", ctypes.c_void_p)]
+
+
 class HpsgdError(RuntimeError):
     def __init__(self, code, text):
         super().__init__("hpsgd status %d: %s" % (code, text))
@@ -59,6 +65,7 @@ SIGNATURES = {
     "hpsgd_set_option": (_ci, [_ci, _f64]),
     "hpsgd_set_sparse_segment": (_ci, [_ci, _i64, _i64]),
     "hpsgd_local_step_ex": (_ci, [_ci, _P(hpsgd_grad_desc)]),
+    "hpsgd_local_step_adamw": (_ci, [_ci, _vp, _P(hpsgd_adamw_args)]),
     "hpsgd_local_step_all": (_ci, [_vp, _i64]),
     "hpsgd_local_step_all_ex": (_ci, [_P(hpsgd_grad_desc)]),
     "hpsgd_local_step_sparse_noalloc": (_ci, [_vp, _vp, _i64, _P(hpsgd_grad_desc), _ci, _i64, _i64, _i64,
@@ -210,6 +217,13 @@ def make_desc(dense, row_idx=None, n_rows=0, row_vals=None):
 
 def hpsgd_local_step_ex(worker, desc):
     return _check(load().hpsgd_local_step_ex(int(worker), ctypes.byref(desc)))
+
+
+def hpsgd_local_step_adamw(worker, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, state_bits=32,
+                           m_scale=None, v_scale=None, grad_scale=None):
+    a = hpsgd_adamw_args(_ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), int(state_bits), float(lr), float(beta1), float(beta2),
+                         float(eps), float(weight_decay), int(step), _ptr(grad_scale))
+    return _check(load().hpsgd_local_step_adamw(int(worker), _ptr(grads), ctypes.byref(a)))
 
 
 def hpsgd_local_step_all(grads, worker_stride_bytes):

@@ -3,6 +3,8 @@
 // kernel launches in hpsgd_schedule.cuh, the device code in hpsgd_kernels.cuh.
 #include "hpsgd_schedule.cuh"
 
+#include "../../include/hpsgd_ops.h"
+
 namespace hpsgd {
 
 int report(int code, const char* fmt, ...)
@@ -404,6 +406,60 @@ int hpsgd_local_step(int worker, const void* grads)
     if (lazy_clones()) return hold_step(worker, gp, 0, false);     // fuse 2: held back for the merge it will run with
     TRY(flush_deferred());
     return enqueue_local(worker, 1, gp, false);
+}
+
+int hpsgd_local_step_adamw(int worker, const void* grads, const hpsgd_adamw_args* args)
+{
+    TRY(need_init());
+    TRY(check_worker(worker));
+    TRY(check_grad_ptr(grads, "grads"));
+    if (!args) return fail(HPSGD_E_BADARG, "args is NULL");
+    if (g.form != HPSGD_FORM_REPLICA_CHANGE) return fail(HPSGD_E_STATE, "hpsgd_local_step_adamw needs the replica-change form");
+    const size_t gsz = g.grad_dtype == HPSGD_BF16 ? 2 : 4, ssz = args->state_bits == 8 ? 1 : 4;
+    hpsgd_adamw_tensor t{};
+    t.weight_decay = args->weight_decay;
+    const auto step = [&](int64_t n, int64_t at) {
+        float* const row = g.r + (int64_t)worker * g.stride + at;
+        t.n = n;
+        t.param = row;
+        t.grad = static_cast<const char*>(grads) + at * gsz;
+        t.m = args->m ? static_cast<char*>(args->m) + at * ssz : nullptr;
+        t.v = args->v ? static_cast<char*>(args->v) + at * ssz : nullptr;
+        t.m_scale = args->m_scale ? args->m_scale + at / 128 : nullptr;
+        t.v_scale = args->v_scale ? args->v_scale + at / 128 : nullptr;
+        t.rng_offset = (uint64_t)at;
+        return hpsgd_adamw_step(&t, 1, HPSGD_F32, g.grad_dtype, args->state_bits, args->lr, args->beta1, args->beta2, args->eps, args->step,
+                                g.seed + (uint64_t)worker * kM1, args->grad_scale, g.main);
+    };
+    if (!args->m || !args->v || (args->state_bits == 8 && (!args->m_scale || !args->v_scale))) return fail(HPSGD_E_BADARG, "a moment or its scale is NULL");
+    TRY(step(0, 0));                       // an empty step: every other argument is checked, nothing is enqueued
+    TRY(flush_deferred());
+    // a replica that is still a clone of w, read from there (lazy clone, pipelined schedule), gets its row first
+    const bool clone = g.pipeline ? !g.touched[worker] : !g.row_valid[worker];
+    for (int c = 0; c < g.chunks; ++c) {
+        int64_t lo, hi;                    // chunks begin at multiples of 8192 elements, so no 8-bit block is cut
+        chunk_range(c, &lo, &hi);
+        if (hi <= lo) continue;
+        if (g.merge_unwaited[c]) {
+            CUDA_TRY(cudaStreamWaitEvent(g.main, g.ev_merge[c], 0));
+            g.merge_unwaited[c] = 0;
+        }
+        const int64_t at = lo * 8, n = (hi - lo) * 8;
+        if (clone)
+            CUDA_TRY(cudaMemcpyAsync(g.r + (int64_t)worker * g.stride + at, g.w + at, (size_t)n * 4, cudaMemcpyDeviceToDevice, g.main));
+        TRY(step(n, at));
+        if (g.overlap) {
+            CUDA_TRY(cudaEventRecord(g.ev_local[c], g.main));
+            g.local_recorded[c] = 1;
+        }
+    }
+    if (g.pipeline) {
+        g.touched[worker] = 1;
+    } else {
+        g.row_valid[worker] = 1;
+        g.at_w[worker] = 0;
+    }
+    return check_async();
 }
 
 int hpsgd_local_step_ex(int worker, const hpsgd_grad_desc* desc)
