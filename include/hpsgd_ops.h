@@ -218,9 +218,8 @@ int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* stream);
  *   accumulate    1: D += the product (HPSGD_F32 only), for gradients over several batches
  *   ldd           elements from row to row of D, 0 = N; any alignment
  *   lda, ldb, ldsa, ldsb   as in hpsgd_quantize_fp8
- *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 for many sizes), 16-byte aligned, filled with zeros before
- *                 its first use; every call leaves it ready for the next call of the same sizes.  Calls that share a workspace have
- *                 to be ordered on one stream.  workspace_bytes: its size.
+ *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 for many sizes), 16-byte aligned; no contents needed.  Calls
+ *                 that share a workspace have to be ordered on one stream.  workspace_bytes: its size.
  * K = 0 gives zeros.
  * The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).
  */
@@ -241,8 +240,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
 
 /*
  * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
- * since the last call (the results written since are incomplete; their workspaces have to be zeroed again), HPSGD_E_CUDA if the work
- * failed.
+ * since the last call (the results written since are incomplete), HPSGD_E_CUDA if the work failed.
  */
 int hpsgd_ops_check(void* stream);
 

@@ -10,9 +10,8 @@
 // each holds its 128 rows of B and half of A's, so a product of 128 x 256 x 128 on an SM takes 32 KB out of L2 in place of 48.
 //
 // One block per SM works through its tiles: a thread that keeps a ring of stages full by TMA (128 k of both operands a stage,
-// 128-byte swizzle), a warp that puts the scales beside them, a thread that issues the products, and four warps that empty
-// one accumulator while the next is filled.  Few tiles are split along k over the SMs; the last of a tile's blocks to finish adds the
-// parts in their order.
+// 128-byte swizzle), a warp that puts the scales beside them, a thread that issues the products, and eight warps that empty
+// one accumulator while the next is filled.  Few tiles are split along k over the SMs, and a second kernel adds the parts in their order.
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
@@ -30,7 +29,6 @@ constexpr int kSms = 148;                  // what work is divided by
 constexpr int kLanes = 128;                // rows of B in a tile
 constexpr int kStageK = 128;               // k of a stage: one scale block, one row of the 128-byte swizzle
 constexpr int kGemmThreads = 384;          // copies, products, scales, one idle warp; eight warps for results
-constexpr int kTicketBytes = 8192;         // eight counters per block of a tile that is split (fewer than kSms)
 
 __device__ unsigned int g_gemm_timeouts;   // blocks whose wait ran out
 
@@ -58,8 +56,7 @@ struct GemmArgs {
     int64_t ldsa, ldsb, ldd;
     void* d;
     int accumulate;
-    unsigned int* ticket;
-    float* part;
+    float* part;                               // with splits > 1: [tile (and block of a pair)][split][column][lane]
 };
 
 // ---------------------------------------------------------------------------- instructions
@@ -454,29 +451,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
                 else barrier_arrive(acc_empty + acc * 8);
             }
-            if (a.splits > 1) {
-                // The last of the tile's parts to finish adds them; each warp counts and adds for its own lanes and columns.
-                unsigned int* const ticket = a.ticket + (piece * 8 + warp - 4);
-                __threadfence();
-                __syncwarp();
-                unsigned int before = 0;
-                if (lane == 0) before = atomicAdd(ticket, 1u);
-                before = __shfl_sync(0xFFFFFFFFu, before, 0);
-                if (before == (unsigned)(a.splits - 1)) {
-                    __threadfence();
-                    if (lane == 0) *ticket = 0u;              // ready for the next call
-                    if (n < a.N) {
-                        const int most = min(cols, kHalf);
-#pragma unroll 4
-                        for (int c = 0; c < most; ++c) {
-                            float sum = __ldcg(parts + (int64_t)c * kLanes);
-                            for (int k = 1; k < a.splits; ++k) sum = __fadd_rn(sum, __ldcg(parts + (int64_t)k * (kLanes * BN) + (int64_t)c * kLanes));
-                            if (sizeof(D) == 4 && a.accumulate) store_result<D, sizeof(D) == 4>(d + (int64_t)c * a.ldd, sum);
-                            else store_result<D, false>(d + (int64_t)c * a.ldd, sum);
-                        }
-                    }
-                }
-            }
         }
     }
     __syncwarp();
@@ -488,6 +462,34 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
         else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
     }
+}
+
+// The sum of a tile's parts, in their order: a warp takes one column (128 lanes, four a thread).  In the product's own last block this was
+// a chain of loads (256 x 4096 x 4096: 96 us; with every SM at it 14).
+constexpr int kSumThreads = 256;
+template <int BN, bool PAIR, typename D>
+__global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_constant__ GemmArgs a)
+{
+    after_previous();
+    const int64_t i = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
+    const int piece = (int)(i / BN), col = (int)(i % BN), tile = PAIR ? piece >> 1 : piece, lane4 = (threadIdx.x & 31) * 4;
+    const int m = tile / a.tiles_n * BN + col, n = tile % a.tiles_n * (PAIR ? 2 * kLanes : kLanes) + (PAIR ? (piece & 1) * kLanes : 0) + lane4;
+    if (tile >= a.tiles || m >= a.M || n >= a.N) return;
+    const float4* const p = reinterpret_cast<const float4*>(a.part + ((int64_t)piece * a.splits * BN + col) * kLanes + lane4);
+    float4 x = __ldcg(p);
+#pragma unroll 4
+    for (int k = 1; k < a.splits; ++k) {
+        const float4 y = __ldcg(p + (int64_t)k * (BN * kLanes / 4));
+        x = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
+    }
+    D* const d = static_cast<D*>(a.d) + (int64_t)m * a.ldd + n;
+    const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (n + j < a.N) {
+            if (sizeof(D) == 4 && a.accumulate) store_result<D, sizeof(D) == 4>(d + j, v[j]);
+            else store_result<D, false>(d + j, v[j]);
+        }
 }
 
 // ---------------------------------------------------------------------------- host side
@@ -528,7 +530,9 @@ struct Plan {
 };
 
 // A's side of a tile: the least power of two that holds all its rows, 256 at most, and then on pairs of SMs unless B has no more rows
-// than one of them takes.  Splitting along k: as many parts as leave no SM with nothing to do, of at least two k blocks each.
+// than one of them takes.  Splitting along k: as many parts as leave no SM with nothing to do, of at least eight k blocks each (one token,
+// 4096 outputs: with K = 1024 one part takes 5.0 us, four parts of two blocks 8.5; with K = 4096 four parts 8.9, two 9.2 us).
+constexpr int kLeastBlocks = 8;
 Plan plan_of(int64_t M, int64_t N, int64_t K)
 {
     Plan p{};
@@ -539,7 +543,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K)
     const int64_t tiles = p.tiles_n * ((M + p.bn - 1) / p.bn);
     p.tiles = (int)tiles;
     const int blocks = (int)((K + kStageK - 1) / kStageK);
-    p.splits = tiles < workers ? (int)std::max<int64_t>(1, std::min<int64_t>(workers / tiles, blocks / 2)) : 1;
+    p.splits = tiles < workers ? (int)std::max<int64_t>(1, std::min<int64_t>(workers / tiles, blocks / kLeastBlocks)) : 1;
     p.per_split = (blocks + p.splits - 1) / p.splits;
     p.splits = (blocks + p.per_split - 1) / p.per_split;
     return p;
@@ -547,7 +551,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K)
 
 size_t workspace_of(const Plan& p)
 {
-    return p.splits > 1 ? kTicketBytes + (size_t)p.tiles * (p.pair ? 2 : 1) * p.splits * kLanes * p.bn * sizeof(float) : 0;
+    return p.splits > 1 ? (size_t)p.tiles * (p.pair ? 2 : 1) * p.splits * kLanes * p.bn * sizeof(float) : 0;
 }
 
 template <int BN, bool PAIR, typename D>
@@ -583,7 +587,10 @@ int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int 
     const int64_t units = (int64_t)a.tiles * a.splits;
     cfg.gridDim = dim3((PAIR ? 2u : 1u) * (unsigned)std::min<int64_t>(units, at_once));
     OPS_CUDA(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<BN, PAIR, D>, ma, mb, a));
-    return launched("hpsgd_gemm_fp8");
+    OPS_TRY(launched("hpsgd_gemm_fp8"));
+    if (a.splits == 1) return HPSGD_OK;
+    const int64_t columns = (int64_t)a.tiles * (PAIR ? 2 : 1) * BN;
+    return launch_early("hpsgd_gemm_fp8", sum_parts_kernel<BN, PAIR, D>, dim3((unsigned)((columns + kSumThreads / 32 - 1) / (kSumThreads / 32))), kSumThreads, 0, s, a);
 }
 
 template <typename D>
@@ -652,8 +659,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split;
     a.sa = reinterpret_cast<const uint32_t*>(p.a_scale); a.sb = reinterpret_cast<const uint32_t*>(p.b_scale);
     a.ldsa = p.ldsa; a.ldsb = p.ldsb; a.ldd = p.ldd; a.d = p.d; a.accumulate = p.accumulate;
-    a.ticket = static_cast<unsigned int*>(p.workspace);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(p.workspace) + kTicketBytes);
+    a.part = static_cast<float*>(p.workspace);
     return p.d_dtype == HPSGD_F32 ? launch_shape<float>(plan.bn, ma, mb, a, sms, s) : launch_shape<__nv_bfloat16>(plan.bn, ma, mb, a, sms, s);
 }
 

@@ -41,7 +41,7 @@ class Operand:
 
 
 def product(M, N, K, a, b, d, **kw):
-    ws = torch.zeros(hp.hpsgd_gemm_fp8_bytes(M, N, K), dtype=U8, device="cuda")
+    ws = torch.full((hp.hpsgd_gemm_fp8_bytes(M, N, K),), 0xFF, dtype=U8, device="cuda")      # NaN, if it were read before it is written
     args = hp.make_gemm_fp8(M, N, K, a.q, a.s, b.q, b.s, d, KIND[d.dtype], workspace=ws, lda=a.ld, ldsa=a.lds, ldb=b.ld, ldsb=b.lds, **kw)
     hp.hpsgd_gemm_fp8(args)
     hp.hpsgd_ops_check()
