@@ -244,6 +244,13 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
  */
 int hpsgd_ops_check(void* stream);
 
+/*
+ * Checked build only; HPSGD_E_UNSUPPORTED otherwise.  1: the barriers of hpsgd_gemm_fp8 are told to expect 16 bytes more than its copies
+ * bring, so that its waits run out after two seconds: the way to see the time-out path (no results, HPSGD_E_TIMEOUT from
+ * hpsgd_ops_check, the device usable as before) without a fault.
+ */
+int hpsgd_ops_debug_stall(int enable);
+
 #ifdef __cplusplus
 }
 #endif

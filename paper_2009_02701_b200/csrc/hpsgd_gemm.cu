@@ -56,6 +56,7 @@ struct GemmArgs {
     int64_t ldsa, ldsb, ldd;
     void* d;
     int accumulate;
+    uint32_t stall;                            // checked build: bytes that a stage's barrier expects and never gets
     float* part;                               // with splits > 1: [tile (and block of a pair)][split][column][lane]
 };
 
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if (elected()) {
                     // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
                     const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
-                    if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes);
+                    if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + a.stall);
                     tma_load<PAIR>(dst, &map_b, kb * kStageK, x.n0, bar);
                     tma_load<PAIR>(dst + S::kBytesB, &map_a, kb * kStageK, x.m0 + rank * S::kRowsA, bar);
                 }
@@ -525,6 +526,8 @@ int make_map(const char* what, CUtensorMap* map, const void* q, int64_t ld, int6
     return HPSGD_OK;
 }
 
+bool g_stall = false;                           // hpsgd_ops_debug_stall
+
 struct Plan {
     int bn, pair, tiles_n, tiles, splits, per_split;
 };
@@ -658,9 +661,22 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
     a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split;
     a.sa = reinterpret_cast<const uint32_t*>(p.a_scale); a.sb = reinterpret_cast<const uint32_t*>(p.b_scale);
+    a.stall = g_stall ? 16 : 0;
     a.ldsa = p.ldsa; a.ldsb = p.ldsb; a.ldd = p.ldd; a.d = p.d; a.accumulate = p.accumulate;
     a.part = static_cast<float*>(p.workspace);
     return p.d_dtype == HPSGD_F32 ? launch_shape<float>(plan.bn, ma, mb, a, sms, s) : launch_shape<__nv_bfloat16>(plan.bn, ma, mb, a, sms, s);
+}
+
+int hpsgd_ops_debug_stall(int enable)
+{
+#ifdef HPSGD_DEBUG
+    if (enable != 0 && enable != 1) return report(HPSGD_E_BADARG, "hpsgd_ops_debug_stall: enable must be 0 or 1");
+    g_stall = enable != 0;
+    return HPSGD_OK;
+#else
+    (void)enable;
+    return report(HPSGD_E_UNSUPPORTED, "hpsgd_ops_debug_stall: only in the checked build");
+#endif
 }
 
 int hpsgd_ops_check(void* stream)

@@ -11,7 +11,8 @@ from .binding import _ci, _f64, _i64, _ptr, _stream, _u64, _vp
 
 __all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm",
            "make_rmsnorm_forward", "hpsgd_rmsnorm_forward", "make_rmsnorm_backward", "hpsgd_rmsnorm_backward", "hpsgd_rmsnorm_backward_bytes",
-           "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes", "hpsgd_ops_check"]
+           "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes", "hpsgd_ops_check",
+           "hpsgd_ops_debug_stall"]
 
 HPSGD_GRAD_NORM_WORKSPACE = 65536
 HPSGD_FP8 = 2
@@ -49,6 +50,7 @@ SIGNATURES = {
     "hpsgd_gemm_fp8_bytes": (ctypes.c_size_t, [_i64, _i64, _i64]),
     "hpsgd_gemm_fp8": (_ci, [_vp, _vp]),
     "hpsgd_ops_check": (_ci, [_vp]),
+    "hpsgd_ops_debug_stall": (_ci, [_ci]),
     "hpsgd_rmsnorm_forward": (_ci, [_vp, _vp]),
     "hpsgd_rmsnorm_backward_bytes": (ctypes.c_size_t, [_i64, _i64]),
     "hpsgd_rmsnorm_backward": (_ci, [_vp, _vp]),
@@ -164,3 +166,7 @@ def hpsgd_gemm_fp8(args, stream=None):
 
 def hpsgd_ops_check(stream=None):
     return _b._check(_b.load().hpsgd_ops_check(_stream(stream)))
+
+
+def hpsgd_ops_debug_stall(enable):
+    return _b._check(_b.load().hpsgd_ops_debug_stall(int(enable)))

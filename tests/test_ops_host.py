@@ -197,3 +197,7 @@ def test_product_limits():
     assert hp.hpsgd_gemm_fp8_bytes(0, 5, 5) == 0 and hp.hpsgd_gemm_fp8_bytes(1 << 40, 5, 5) == 0
     # enough tiles for every SM: no workspace.  One tile and a long sum: parts
     assert hp.hpsgd_gemm_fp8_bytes(4096, 4096, 4096) == 0 and hp.hpsgd_gemm_fp8_bytes(1, 128, 8192) > 0
+
+
+def test_the_stall_is_for_the_checked_build():
+    refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_ops_debug_stall, 1)
