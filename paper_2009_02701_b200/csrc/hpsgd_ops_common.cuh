@@ -92,15 +92,6 @@ __device__ __forceinline__ float scale_value(int byte)
 }
 __device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 
-// The bits of an E4M3 code without its sign are the top of a binary32 that is 2^120 times smaller (exponent
-// biases 7 and 127), subnormal codes included: a shift and one exact multiplication convert either way.
-__device__ __forceinline__ float e4m3_magnitude(uint32_t code) { return __fmul_rn(__uint_as_float(code << 20), 0x1p120f); }
-__device__ __forceinline__ float e4m3_value(uint32_t code)
-{
-    const float x = __uint_as_float(__float_as_uint(e4m3_magnitude(code & 0x7Fu)) | (code & 0x80u) << 24);
-    return (code & 0x7Fu) == 0x7Fu ? __uint_as_float(0x7FC00000u) : x;
-}
-
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 __device__ __forceinline__ float finite_magnitude(float x) { return finite(x) ? fabsf(x) : 0.f; }
 
