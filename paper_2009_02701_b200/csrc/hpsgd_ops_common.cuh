@@ -163,6 +163,7 @@ __device__ __forceinline__ f8 load_some(const T* p, bool wide, int left)
     return x;
 }
 
+// The same for a store.
 template <typename T>
 __device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int left)
 {
@@ -173,6 +174,44 @@ __device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int lef
 #pragma unroll
     for (int q = 0; q < 8; ++q)
         if (q < left) store1(p + q, x.v[q]);
+}
+
+// And for rows that do not allow the wide access: in the widest units that the address does.
+__device__ __forceinline__ void store_unaligned(float* p, const f8& x, int left)
+{
+    const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(p);
+    if (left == 8 && (at & 15) == 0) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x.v[4], x.v[5], x.v[6], x.v[7]);
+    } else if (left == 8 && (at & 7) == 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) reinterpret_cast<float2*>(p)[q] = make_float2(x.v[2 * q], x.v[2 * q + 1]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < left) store1(p + q, x.v[q]);
+    }
+}
+
+__device__ __forceinline__ void store_unaligned(__nv_bfloat16* p, const f8& x, int left)
+{
+    const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(p);
+    if (left == 8 && (at & 3) == 0) {
+        uint32_t u[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) u[q] = pack_bf16(x.v[2 * q], x.v[2 * q + 1]);
+        if ((at & 7) == 0) {
+            reinterpret_cast<uint2*>(p)[0] = make_uint2(u[0], u[1]);
+            reinterpret_cast<uint2*>(p)[1] = make_uint2(u[2], u[3]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) reinterpret_cast<uint32_t*>(p)[q] = u[q];
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < left) store1(p + q, x.v[q]);
+    }
 }
 
 // ---------------------------------------------------------------------------- two values at a time
@@ -243,13 +282,48 @@ __device__ __forceinline__ p4 decode8(uint2 u)
     return x;
 }
 
+// WORDS consecutive 32-bit words from an address of any alignment: the 16-byte pieces that hold them, moved down by words and, with 16-bit
+// elements, by half a word.  False, and nothing read, where a piece would reach outside [lo, hi), the memory of the tensor.  (What
+// the pieces hold beside the words is never used, so it does not matter if another thread is writing it.)
+template <int WORDS>
+__device__ __forceinline__ bool load_unaligned(const void* p, const void* lo, const void* hi, uint32_t* out)
+{
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u;
+    const char* const first = static_cast<const char*>(p) - off;
+    if (first < static_cast<const char*>(lo) || first + WORDS * 4 + 16 > static_cast<const char*>(hi)) return false;
+    uint32_t w[WORDS + 4];
+#pragma unroll
+    for (int k = 0; k < WORDS / 4 + 1; ++k)
+        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * k]), "=r"(w[4 * k + 1]), "=r"(w[4 * k + 2]), "=r"(w[4 * k + 3]) : "l"(first + 16 * k));
+    const bool two = off & 8u, one = off & 4u;
+#pragma unroll
+    for (int i = 0; i < WORDS + 2; ++i) w[i] = two ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < WORDS + 1; ++i) w[i] = one ? w[i + 1] : w[i];
+    const uint32_t bits = (off & 2u) * 8u;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) out[i] = __funnelshift_r(w[i], w[i + 1], bits);
+    return true;
+}
+
 // Eight values as they are stored (half the registers of their binary32 values where they are bf16): requested early, widened when used.
+// The second form is for rows that do not allow the wide access (an odd width, a view); [lo, hi) is the tensor's memory.
 template <typename T>
 struct Raw8;
 template <>
 struct Raw8<float> {
     f8 x;
     __device__ __forceinline__ void load(const float* p, bool wide, int left) { x = load_some(p, wide, left); }
+    __device__ __forceinline__ void load(const float* p, int left, const void* lo, const void* hi)
+    {
+        uint32_t w[8];
+        if (left > 0 && load_unaligned<8>(p, lo, hi, w)) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x.v[q] = q < left ? __uint_as_float(w[q]) : 0.f;
+        } else {
+            x = load_some(p, false, left);
+        }
+    }
     __device__ __forceinline__ f8 values() const { return x; }
 };
 template <>
@@ -267,6 +341,19 @@ struct Raw8<__nv_bfloat16> {
         for (int q = 0; q < 8; ++q)
             if (q < left) w[q >> 1] |= (uint32_t)h[q] << 16 * (q & 1);
         u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, const void* lo, const void* hi)
+    {
+        uint32_t w[4];
+        if (left > 0 && load_unaligned<4>(p, lo, hi, w)) {
+            if (left < 8) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] &= left >= 2 * q + 2 ? 0xFFFFFFFFu : left == 2 * q + 1 ? 0xFFFFu : 0u;
+            }
+            u = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            load(p, false, left);
+        }
     }
     __device__ __forceinline__ f8 values() const
     {
