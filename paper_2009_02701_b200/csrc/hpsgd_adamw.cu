@@ -52,9 +52,19 @@ struct Hyper {
     int span;                                  // elements per block
 };
 
-// The tensor that a chunk belongs to: the last whose first chunk is not behind it.
+// What the norm needs of a tensor is a fifth of that, and the table holds five times as many.
+constexpr int kMaxNormItems = 1600;
 template <int CAP>
-__device__ __forceinline__ int find_item(const Table<CAP>& t, uint32_t chunk)
+struct NormTable {
+    int count;
+    uint32_t first[CAP];
+    const void* g[CAP];
+    int64_t n2[CAP];       // twice the number of elements, and 1 if the address allows the wide accesses
+};
+
+// The tensor that a chunk belongs to: the last whose first chunk is not behind it.
+template <typename Tab>
+__device__ __forceinline__ int find_item(const Tab& t, uint32_t chunk)
 {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
@@ -471,7 +481,7 @@ __device__ __forceinline__ double warp_sum(double x)
 // Each block adds the chunks block, block + grid, ... of its launch; the last block of the call to finish adds the blocks' sums in
 // their order, so the result does not depend on which one that is.
 template <int CAP, typename G>
-__global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ NormOut no)
+__global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormTable<CAP> table, const __grid_constant__ NormOut no)
 {
     __shared__ double part[kNormThreads / 32];
     __shared__ bool last;
@@ -479,15 +489,16 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     after_previous();
     for (uint32_t chunk = blockIdx.x; chunk < no.chunks; chunk += gridDim.x) {
         const int which = find_item(table, chunk);
-        const Item& it = table.item[which];
-        const G* const gp = static_cast<const G*>(it.g);
+        const G* const gp = static_cast<const G*>(table.g[which]);
+        const int64_t n = table.n2[which] >> 1;
+        const bool wide = table.n2[which] & 1;
         const int64_t base = (int64_t)(chunk - table.first[which]) * kNormChunk + threadIdx.x * 8;
         f8 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int64_t at = base + k * (kNormThreads * 8), rest = it.n - at;
+            const int64_t at = base + k * (kNormThreads * 8), rest = n - at;
             const int left = rest < 0 ? 0 : rest > 8 ? 8 : (int)rest;
-            x[k] = load_some(gp + at, it.wide && left == 8, left);
+            x[k] = load_some(gp + at, wide && left == 8, left);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -537,6 +548,7 @@ int check_table(const hpsgd_adamw_tensor* t, int n, int grad_dtype, const char* 
 {
     if (n < 0) return report(HPSGD_E_BADARG, "%s: n_tensors is negative", what);
     if (n > 0 && !t) return report(HPSGD_E_BADARG, "%s: tensors is NULL", what);
+    if (n > 1 << 20) return report(HPSGD_E_UNSUPPORTED, "%s: more than 2^20 tensors", what);
     if (grad_dtype != HPSGD_F32 && grad_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown grad_dtype %d", what, grad_dtype);
     const size_t gs = grad_dtype == HPSGD_F32 ? 4 : 2;
     for (int k = 0; k < n; ++k) {
@@ -549,22 +561,18 @@ int check_table(const hpsgd_adamw_tensor* t, int n, int grad_dtype, const char* 
     return HPSGD_OK;
 }
 
-// The next launch's worth of tensors starting at *at: fills `out` and returns its number of chunks.  Empty tensors are left out.
-template <int CAP, typename Fill>
-uint32_t fill_table(const hpsgd_adamw_tensor* t, int n, int* at, int64_t chunk_elems, Table<CAP>* out, Fill fill)
+// The next launch's worth of tensors starting at *at, at most `cap`: calls add(tensor, its place, its first chunk) for each and returns their
+// number of chunks.  Empty tensors are left out.
+template <typename Add>
+uint32_t next_launch(const hpsgd_adamw_tensor* t, int n, int* at, int cap, int64_t chunk_elems, Add add)
 {
     uint64_t chunks = 0;
-    out->count = 0;
-    for (; *at < n && out->count < CAP; ++*at) {
+    int place = 0;
+    for (; *at < n && place < cap; ++*at) {
         if (t[*at].n == 0) continue;
         const uint64_t here = (uint64_t)(t[*at].n + chunk_elems - 1) / chunk_elems;
         if (chunks + here > 0x7FFFFFFFull) break;      // a launch has at most that many blocks; 2^40 elements fit one alone
-        Item& it = out->item[out->count++];
-        it = Item{};
-        it.n = t[*at].n;
-        it.g = t[*at].grad;
-        out->first[out->count - 1] = (uint32_t)chunks;
-        fill(t[*at], &it);
+        add(t[*at], place++, (uint32_t)chunks);
         chunks += here;
     }
     return (uint32_t)chunks;
@@ -584,12 +592,17 @@ int step_launches(const hpsgd_adamw_tensor* t, int n, double lr, Hyper hy, int s
     int at = 0;
     Table<CAP> table;
     while (at < n) {
-        const uint32_t chunks = fill_table(t, n, &at, hy.span, &table, [&](const hpsgd_adamw_tensor& x, Item* it) {
-            it->p = x.param; it->m = x.m; it->v = x.v; it->ms = x.m_scale; it->vs = x.v_scale;
-            it->copy = static_cast<__nv_bfloat16*>(x.copy);
-            it->rng = x.rng_offset;
-            it->keep = (float)(1.0 - lr * x.weight_decay);
-            it->wide = aligned(x.param, ap) && aligned(x.grad, ag) && aligned(x.m, as) && aligned(x.v, as) && aligned(x.copy, 16);
+        table.count = 0;
+        const uint32_t chunks = next_launch(t, n, &at, CAP, hy.span, [&](const hpsgd_adamw_tensor& x, int place, uint32_t first) {
+            table.count = place + 1;
+            table.first[place] = first;
+            Item& it = table.item[place];
+            it.p = x.param; it.g = x.grad; it.m = x.m; it.v = x.v; it.ms = x.m_scale; it.vs = x.v_scale;
+            it.copy = static_cast<__nv_bfloat16*>(x.copy);
+            it.n = x.n;
+            it.rng = x.rng_offset;
+            it.keep = (float)(1.0 - lr * x.weight_decay);
+            it.wide = aligned(x.param, ap) && aligned(x.grad, ag) && aligned(x.m, as) && aligned(x.v, as) && aligned(x.copy, 16);
         });
         if (!chunks) continue;
         OPS_TRY(launch_early("hpsgd_adamw_step", adamw_kernel<CAP, P, G, B8>, dim3(chunks), kAdamThreads, 0, s, table, hy));
@@ -611,22 +624,28 @@ template <int CAP, typename G>
 int norm_launches(const hpsgd_adamw_tensor* t, int n, int sms, double max_norm, void* ws, float* out, cudaStream_t s)
 {
     // blocks of every launch, so that the last block of the last launch knows what it has to wait for
-    Table<CAP> table;
-    const auto fill = [](const hpsgd_adamw_tensor& x, Item* it) { it->wide = aligned(x.grad, sizeof(G) == 4 ? 32 : 16); };
+    const auto pass = [](const hpsgd_adamw_tensor&, int, uint32_t) {};
     int at = 0, total = 0, launches = 0;
     while (at < n) {
-        fill_table(t, n, &at, kNormChunk, &table, fill);
+        next_launch(t, n, &at, CAP, kNormChunk, pass);
         ++launches;
     }
     const int most = std::max(1, std::min(sms * 8, kNormPartials / std::max(1, launches)));
     const auto grid_of = [&](uint32_t chunks) { return (int)std::min<uint32_t>(std::max<uint32_t>(chunks, 1), most); };
     at = 0;
-    while (at < n) total += grid_of(fill_table(t, n, &at, kNormChunk, &table, fill));
+    while (at < n) total += grid_of(next_launch(t, n, &at, CAP, kNormChunk, pass));
     if (total == 0) total = 1;                     // no tensors: one block writes the norm of nothing
     NormOut no{(float)max_norm, static_cast<unsigned int*>(ws), reinterpret_cast<double*>(static_cast<char*>(ws) + 64), 0, total, 0, out};
     at = 0;
+    NormTable<CAP> table;
     do {
-        no.chunks = fill_table(t, n, &at, kNormChunk, &table, fill);
+        table.count = 0;
+        no.chunks = next_launch(t, n, &at, CAP, kNormChunk, [&](const hpsgd_adamw_tensor& x, int place, uint32_t first) {
+            table.count = place + 1;
+            table.first[place] = first;
+            table.g[place] = x.grad;
+            table.n2[place] = x.n * 2 + aligned(x.grad, sizeof(G) == 4 ? 32 : 16);
+        });
         const int grid = grid_of(no.chunks);
         OPS_TRY(launch_early("hpsgd_grad_norm", grad_norm_kernel<CAP, G>, dim3(grid), kNormThreads, 0, s, table, no));
         no.before += grid;
@@ -690,9 +709,10 @@ int hpsgd_adamw_step(const hpsgd_adamw_tensor* tensors, int n_tensors, int param
     hy.key0 = (uint32_t)key; hy.key1 = (uint32_t)(key >> 32);
     hy.scale = grad_scale;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // The host copies a kernel's parameters at every launch: 62 tensors' step with its norm takes 72 us by the largest table, 66 by the middle one (and launched early).
+    // The host copies a kernel's parameters at every launch: 65 small tensors' step takes 8.1 us by the largest table, 5.9 by the third.
     if (n_tensors <= 8) return step_types<8>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
     if (n_tensors <= 64) return step_types<64>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
+    if (n_tensors <= 192) return step_types<192>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
     return step_types<kMaxItems>(tensors, n_tensors, param_dtype, grad_dtype, state_bits, lr, hy, sms, s);
 }
 
@@ -711,11 +731,11 @@ int hpsgd_grad_norm(const hpsgd_adamw_tensor* tensors, int n_tensors, int grad_d
     if (n_tensors <= 8)
         return f ? norm_launches<8, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
                  : norm_launches<8, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
-    if (n_tensors <= 64)
-        return f ? norm_launches<64, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
-                 : norm_launches<64, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
-    return f ? norm_launches<kMaxItems, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
-             : norm_launches<kMaxItems, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
+    if (n_tensors <= 192)
+        return f ? norm_launches<192, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
+                 : norm_launches<192, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
+    return f ? norm_launches<kMaxNormItems, float>(tensors, n_tensors, sms, max_norm, workspace, out, s)
+             : norm_launches<kMaxNormItems, __nv_bfloat16>(tensors, n_tensors, sms, max_norm, workspace, out, s);
 }
 
 }  // extern "C"
