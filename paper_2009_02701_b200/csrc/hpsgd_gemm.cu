@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
     } else if (warp >= 4) {
         // Two warps for each quarter of the lanes, half of the columns each.  A warp has its scheduler nearly to itself, so what counts is
-        // that nothing waits: the next columns are requested before these are stored, and addresses do not depend on one another.
+        // that nothing waits: the columns are requested together, and addresses do not depend on one another.
         constexpr int kHalf = BN / 2, kC = kHalf < 16 ? kHalf : 16;
         const int part = warp & 3, c0 = (warp >> 2) - 1 ? kHalf : 0;
         int done = 0;
@@ -431,27 +431,27 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             const int n = x.n0 + part * 32 + lane, cols = a.M - x.m0 - c0, piece = PAIR ? x.tile * 2 + rank : x.tile;
             float* const parts = a.part + (int64_t)piece * a.splits * (kLanes * BN) + (int64_t)c0 * kLanes + part * 32 + lane;
             D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
-            float v[2][kC];
-            load_columns<kC>(src, v[0]);
+            // all of them to registers first, so that the accumulator is free while they are stored
+            float v[kHalf];
 #pragma unroll
-            for (int c = 0; c < kHalf; c += kC) {
-                float* const now = v[c / kC & 1];
-                loads_done<kC>(now);
-                if (c + kC < kHalf) load_columns<kC>(src + c + kC, v[(c / kC & 1) ^ 1]);
-                if (c >= cols) continue;
-                if (a.splits > 1) store_columns<kC, float, false>(parts + (int64_t)x.split * (kLanes * BN) + c * kLanes, kLanes, now, cols - c);
-                else if (n < a.N) {
-                    if (sizeof(D) == 4 && a.accumulate) store_columns<kC, D, sizeof(D) == 4>(d + c * a.ldd, a.ldd, now, cols - c);
-                    else store_columns<kC, D, false>(d + c * a.ldd, a.ldd, now, cols - c);
-                }
-                __syncwarp();
-            }
+            for (int c = 0; c < kHalf; c += kC) load_columns<kC>(src + c, v + c);
+            loads_done<kHalf>(v);
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
                 else barrier_arrive(acc_empty + acc * 8);
             }
+#pragma unroll
+            for (int c = 0; c < kHalf; c += kC) {
+                if (c >= cols) continue;
+                if (a.splits > 1) store_columns<kC, float, false>(parts + (int64_t)x.split * (kLanes * BN) + c * kLanes, kLanes, v + c, cols - c);
+                else if (n < a.N) {
+                    if (sizeof(D) == 4 && a.accumulate) store_columns<kC, D, sizeof(D) == 4>(d + c * a.ldd, a.ldd, v + c, cols - c);
+                    else store_columns<kC, D, false>(d + c * a.ldd, a.ldd, v + c, cols - c);
+                }
+            }
+            __syncwarp();
         }
     }
     __syncwarp();
