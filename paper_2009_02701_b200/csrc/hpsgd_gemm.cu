@@ -302,24 +302,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
     const int units = a.tiles * a.splits;
 
-    // The roles' waits are the whole warp's, so that what they decide is the same for all of its lanes.
+    // Copies and products are requested by one thread for the whole of the loop: with the warp in step, a vote after each wait and an election for
+    // each stage, 1 x 30000 x 1024 took 8.0 us in place of 6.7 and 1 x 18944 x 8192 29.9 in place of 27.8 (256 tokens and more: the same).
+    // The other roles' waits are the whole warp's, so that what they decide is the same for all of its lanes.
+    const auto wait_one = [&](uint32_t bar, uint32_t parity) { return barrier_wait(bar, parity, &given_up); };
     const auto wait = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, &given_up)); };
-    if (warp == 0) {
+    if (warp == 0 && elected()) {
         int s = 0;
         uint32_t phase = 1;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
             const Unit x = unit_of<BN, PAIR>(a, u, rank);
             for (int kb = x.k0; kb < x.k1; ++kb) {
-                if (!(ok = wait(empty + s * 8, phase))) break;
-                if (elected()) {
-                    // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
-                    const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
-                    if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + a.stall);
-                    tma_load<PAIR>(dst, &map_b, kb * kStageK, x.n0, bar);
-                    tma_load<PAIR>(dst + S::kBytesB, &map_a, kb * kStageK, x.m0 + rank * S::kRowsA, bar);
-                }
-                __syncwarp();
+                if (!(ok = wait_one(empty + s * 8, phase))) break;
+                // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
+                const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
+                if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + a.stall);
+                tma_load<PAIR>(dst, &map_b, kb * kStageK, x.n0, bar);
+                tma_load<PAIR>(dst + S::kBytesB, &map_a, kb * kStageK, x.m0 + rank * S::kRowsA, bar);
                 if (++s == S::kStages) s = 0, phase ^= 1;
             }
         }
@@ -328,57 +328,47 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             const uint64_t t = nanoseconds();
             while (nanoseconds() - t < 10000000ull) {}
         }
-    } else if (warp == 1) {
-        if (rank == 0) {
-            const uint64_t desc_b = operand_descriptor(smem_address(smem)), desc_a = operand_descriptor(smem_address(smem) + S::kBytesB),
-                           desc_s = scale_descriptor(smem_address(scales));
-            int s = 0, place = 0, column = 0, acc = 0;
-            uint32_t phase = 0, place_phase = 0, acc_phase = 1;
-            bool ok = true;
-            for (int u = first; u < units && ok; u += stride) {
-                const Unit x = unit_of<BN, PAIR>(a, u, rank);
-                if (!(ok = wait(acc_empty + acc * 8, acc_phase))) break;
+    } else if (warp == 1 && rank == 0 && elected()) {
+        const uint64_t desc_b = operand_descriptor(smem_address(smem)), desc_a = operand_descriptor(smem_address(smem) + S::kBytesB),
+                       desc_s = scale_descriptor(smem_address(scales));
+        int s = 0, place = 0, column = 0, acc = 0;
+        uint32_t phase = 0, place_phase = 0, acc_phase = 1;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const Unit x = unit_of<BN, PAIR>(a, u, rank);
+            if (!(ok = wait_one(acc_empty + acc * 8, acc_phase))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t sb = 0;
+            for (int kb = x.k0; kb < x.k1; ++kb) {
+                if (!(ok = wait_one(full + s * 8, phase))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t sb = 0;
-                for (int kb = x.k0; kb < x.k1; ++kb) {
-                    if (!(ok = wait(full + s * 8, phase))) break;
+                if (kb == x.k0 || (kb & 3) == 0) {
+                    // The next group's scales, to the column group after the last one's.  Those columns were used kPlaces + 1 groups ago.  This
+                    // place was refilled behind the commit of kPlaces groups ago, which waited for all products before its own: they are done.
+                    if (!(ok = wait_one(scale_full + place * 8, place_phase))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const bool scale_group = kb == x.k0 || (kb & 3) == 0;
-                    int from = 0;
-                    if (scale_group) {
-                        // The next group's scales, to the column group after the last one's.  Those columns were used kPlaces + 1 groups ago.  This
-                        // place was refilled behind the commit of kPlaces groups ago, which waited for all products before its own: they are done.
-                        if (!(ok = wait(scale_full + place * 8, place_phase))) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        sb = tmem_scales + column * S::kScaleCols;
-                        from = place;
-                        if (++column == S::kPlaces + 1) column = 0;
-                        if (++place == S::kPlaces) place = 0, place_phase ^= 1;
-                    }
-                    if (elected()) {
-                        if (scale_group) {
-                            const uint64_t src = desc_s + (uint32_t)(from * (S::kBytesS >> 4));
+                    sb = tmem_scales + column * S::kScaleCols;
+                    const uint64_t src = desc_s + (uint32_t)(place * (S::kBytesS >> 4));
 #pragma unroll
-                            for (int t = 0; t < 1 + S::kAtoms; ++t) copy_scales<PAIR>(sb + 4 * t, src + 32 * t);
-                            commit<PAIR>(scale_empty + from * 8);
-                        }
-                        const uint64_t db = desc_b + (uint32_t)(s * (S::kStageBytes >> 4)), da = desc_a + (uint32_t)(s * (S::kStageBytes >> 4));
-                        const uint32_t id = instruction<BN, PAIR>(kb & 3);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) mma<PAIR>(tmem + acc * BN, db + 2 * k, da + 2 * k, id, sb, sb + 4, kb > x.k0 || k > 0);
-                        commit<PAIR>(empty + s * 8);
-                        if (kb + 1 == x.k1) commit<PAIR>(acc_full + acc * 8);
-                    }
-                    __syncwarp();
-                    if (++s == S::kStages) s = 0, phase ^= 1;
+                    for (int t = 0; t < 1 + S::kAtoms; ++t) copy_scales<PAIR>(sb + 4 * t, src + 32 * t);
+                    commit<PAIR>(scale_empty + place * 8);
+                    if (++column == S::kPlaces + 1) column = 0;
+                    if (++place == S::kPlaces) place = 0, place_phase ^= 1;
                 }
-                if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
+                const uint64_t db = desc_b + (uint32_t)(s * (S::kStageBytes >> 4)), da = desc_a + (uint32_t)(s * (S::kStageBytes >> 4));
+                const uint32_t id = instruction<BN, PAIR>(kb & 3);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma<PAIR>(tmem + acc * BN, db + 2 * k, da + 2 * k, id, sb, sb + 4, kb > x.k0 || k > 0);
+                commit<PAIR>(empty + s * 8);
+                if (kb + 1 == x.k1) commit<PAIR>(acc_full + acc * 8);
+                if (++s == S::kStages) s = 0, phase ^= 1;
             }
-            if (!ok) {                              // products in flight read shared memory: let them end
-                if (elected()) commit<PAIR>(drained);
-                const uint64_t t = nanoseconds();
-                while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
-            }
+            if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
+        }
+        if (!ok) {                                  // products in flight read shared memory: let them end
+            commit<PAIR>(drained);
+            const uint64_t t = nanoseconds();
+            while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
         }
     } else if (warp == 2) {
         // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.  A group's words are
