@@ -218,7 +218,7 @@ int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* stream);
  *   accumulate    1: D += the product (HPSGD_F32 only), for gradients over several batches
  *   ldd           elements from row to row of D, 0 = N; any alignment
  *   lda, ldb, ldsa, ldsb   as in hpsgd_quantize_fp8
- *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 for many sizes), 16-byte aligned; no contents needed.  Calls
+ *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 but for few rows and very long sums), 16-byte aligned; no contents needed.  Calls
  *                 that share a workspace have to be ordered on one stream.  workspace_bytes: its size.
  * K = 0 gives zeros.
  * The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).

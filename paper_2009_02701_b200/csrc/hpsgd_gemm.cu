@@ -11,7 +11,8 @@
 //
 // One block per SM works through its tiles: a thread that keeps a ring of stages full by TMA (128 k of both operands a stage,
 // 128-byte swizzle), a warp that puts the scales beside them, a thread that issues the products, and eight warps that empty
-// one accumulator while the next is filled.  Few tiles are split along k over the SMs, and a second kernel adds the parts in their order.
+// one accumulator while the next is filled.  Few tiles are split along k over the SMs: the blocks of a cluster, which add their parts out of
+// each other's shared memory, or for very long sums as many as there are SMs, whose parts a second kernel adds, in their order in any case.
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
@@ -50,14 +51,16 @@ struct Shape {
 
 struct GemmArgs {
     int M, N, K;
-    int tiles_n, tiles, splits, per_split;     // k blocks of a split
+    int tiles_n, tiles;
+    int splits, per_split, longer;             // parts along k, a part's k blocks, and how many of the first parts have one more
+    int wide;                                  // four neighbouring results may be stored at once
     const uint32_t* sa;
     const uint32_t* sb;
     int64_t ldsa, ldsb, ldd;
     void* d;
     int accumulate;
     uint32_t stall;                            // checked build: bytes that a stage's barrier expects and never gets
-    float* part;                               // with splits > 1: [tile (and block of a pair)][split][column][lane]
+    float* part;                               // parts that go through memory: [tile][split][column][lane]
 };
 
 // ---------------------------------------------------------------------------- instructions
@@ -186,6 +189,16 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Four values at this block's address `at`, out of the memory of block `rank` of its cluster.
+__device__ __forceinline__ float4 load_from_block(uint32_t at, int rank)
+{
+    float4 x;
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(there) : "memory");
+    return x;
+}
+
 // C accumulator columns of this thread's lane; complete behind loads_done.
 template <int C>
 __device__ __forceinline__ void load_columns(uint32_t tmem, float* x)
@@ -211,7 +224,8 @@ __device__ __forceinline__ void loads_done(float* x)
 }
 
 // ---------------------------------------------------------------------------- the kernel
-// Unit u of a block's (or pair's) work: tile u / splits, part u % splits of its k blocks.  n0: this block's first row of B.
+// Unit u of a block's (or pair's) work: tile u / splits, part u % splits of its k blocks (with joined parts, the block's number in its
+// cluster).  n0: this block's first row of B.  Pairs' sums are not split.
 struct Unit {
     int n0, m0, k0, k1, tile, split;
 };
@@ -219,13 +233,12 @@ template <int BN, bool PAIR>
 __device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u, int rank)
 {
     Unit x;
-    x.tile = u / a.splits;
-    x.split = u % a.splits;
+    x.tile = PAIR ? u : u / a.splits;
+    x.split = PAIR ? 0 : u % a.splits;
     x.n0 = x.tile % a.tiles_n * (PAIR ? 2 * kLanes : kLanes) + rank * kLanes;
     x.m0 = x.tile / a.tiles_n * BN;
-    const int blocks = (a.K + kStageK - 1) / kStageK;
-    x.k0 = x.split * a.per_split;
-    x.k1 = min(blocks, x.k0 + a.per_split);
+    x.k0 = PAIR ? 0 : x.split * a.per_split + min(x.split, a.longer);
+    x.k1 = PAIR ? a.per_split : x.k0 + a.per_split + (x.split < a.longer);
     return x;
 }
 
@@ -236,6 +249,26 @@ __device__ __forceinline__ void store_result(D* p, float x)
 {
     if constexpr (ADD) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory");
     else store1(p, x);
+}
+
+// Four neighbours in a row of D, `left` of them there; `wide`: aligned to all four.
+template <typename D>
+__device__ __forceinline__ void store_four(D* p, const float* v, int left, int wide, int accumulate)
+{
+    if (wide && left >= 4 && !accumulate) {
+        if constexpr (sizeof(D) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else {
+            __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+            *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(h);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < left) {
+            if (sizeof(D) == 4 && accumulate) store_result<D, sizeof(D) == 4>(p + j, v[j]);
+            else store_result<D, false>(p + j, v[j]);
+        }
 }
 
 // C columns of one lane to rows of D that are ldd apart, `left` of them there.
@@ -252,7 +285,37 @@ __device__ __forceinline__ void store_columns(D* p, int64_t ldd, const float* x,
     }
 }
 
-template <int BN, bool PAIR, typename D>
+// The sum of a tile's P parts, in their order, out of the shared memory of the P blocks that have them ([column][lane] in each): a warp takes
+// 16 / P columns of a part's share at a time, a thread four lanes of each.
+template <int P, typename D>
+__device__ __forceinline__ void join_parts(const GemmArgs& a, uint32_t parts, const Unit& x, int cols)
+{
+    constexpr int kWarps = kGemmThreads / 32, kAtOnce = 16 / P;
+    const int lane4 = (threadIdx.x & 31) * 4, n = x.n0 + lane4, step = kWarps * P;
+    if (n >= a.N) return;
+    for (int c0 = (threadIdx.x >> 5) * P + x.split; c0 < cols; c0 += step * kAtOnce) {
+        float4 t[kAtOnce][P];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+            for (int k = 0; k < P; ++k)
+                if (c0 + i * step < cols) t[i][k] = load_from_block(parts + ((c0 + i * step) * kLanes + lane4) * 4, k);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (c0 + i * step >= cols) continue;
+            float v[4] = {t[i][0].x, t[i][0].y, t[i][0].z, t[i][0].w};
+#pragma unroll
+            for (int k = 1; k < P; ++k) {
+                v[0] = __fadd_rn(v[0], t[i][k].x), v[1] = __fadd_rn(v[1], t[i][k].y);
+                v[2] = __fadd_rn(v[2], t[i][k].z), v[3] = __fadd_rn(v[3], t[i][k].w);
+            }
+            store_four<D>(static_cast<D*>(a.d) + (int64_t)(x.m0 + c0 + i * step) * a.ldd + n, v, a.N - n, a.wide, a.accumulate);
+        }
+    }
+}
+
+// JOIN: the blocks of a cluster have a tile's parts, one each.
+template <int BN, bool PAIR, bool JOIN, typename D>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     gemm_fp8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ GemmArgs a)
 {
@@ -300,7 +363,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     after_previous();
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
-    const int units = a.tiles * a.splits;
+    const int units = PAIR ? a.tiles : a.tiles * a.splits;
 
     // Copies and products are requested by one thread for the whole of the loop: with the warp in step, a vote after each wait and an election for
     // each stage, 1 x 30000 x 1024 took 8.0 us in place of 6.7 and 1 x 18944 x 8192 29.9 in place of 27.8 (256 tokens and more: the same).
@@ -418,9 +481,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             if (!wait(acc_full + acc * 8, done / S::kAccs & 1)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t src = tmem + acc * BN + c0 + ((uint32_t)part << 21);
-            const int n = x.n0 + part * 32 + lane, cols = a.M - x.m0 - c0, piece = PAIR ? x.tile * 2 + rank : x.tile;
-            float* const parts = a.part + (int64_t)piece * a.splits * (kLanes * BN) + (int64_t)c0 * kLanes + part * 32 + lane;
-            D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
+            const int n = x.n0 + part * 32 + lane, cols = a.M - x.m0 - c0;
+            // [column][lane]: a part's own place in device memory, or where this block's stages were (its only unit's products have read them)
+            float* const sums = (JOIN ? reinterpret_cast<float*>(smem) : a.part + ((int64_t)x.tile * a.splits + x.split) * (kLanes * BN)) + c0 * kLanes +
+                                part * 32 + lane;
             // all of them to registers first, so that the accumulator is free while they are stored
             float v[kHalf];
 #pragma unroll
@@ -432,10 +496,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
                 else barrier_arrive(acc_empty + acc * 8);
             }
+            D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
 #pragma unroll
             for (int c = 0; c < kHalf; c += kC) {
                 if (c >= cols) continue;
-                if (a.splits > 1) store_columns<kC, float, false>(parts + (int64_t)x.split * (kLanes * BN) + c * kLanes, kLanes, v + c, cols - c);
+                if (JOIN || (!PAIR && a.splits > 1)) store_columns<kC, float, false>(sums + c * kLanes, kLanes, v + c, cols - c);
                 else if (n < a.N) {
                     if (sizeof(D) == 4 && a.accumulate) store_columns<kC, D, sizeof(D) == 4>(d + c * a.ldd, a.ldd, v + c, cols - c);
                     else store_columns<kC, D, false>(d + c * a.ldd, a.ldd, v + c, cols - c);
@@ -448,6 +513,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0 && given_up) atomicAdd(&g_gemm_timeouts, 1u);
+    if constexpr (JOIN) {
+        cluster_sync();
+        const Unit x = unit_of<BN, PAIR>(a, first, 0);
+        const int cols = min(BN, a.M - x.m0);
+        if (a.splits == 2) join_parts<2, D>(a, smem_address(smem), x, cols);
+        else if (a.splits == 4) join_parts<4, D>(a, smem_address(smem), x, cols);
+        else join_parts<8, D>(a, smem_address(smem), x, cols);
+        __syncwarp();
+        cluster_sync();                              // this block's memory stays until the others have read it
+    }
     if constexpr (PAIR) cluster_sync();              // the other block's arrivals and products reach into this one
     if (warp == 3) {
         if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
@@ -455,32 +530,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
 }
 
-// The sum of a tile's parts, in their order: a warp takes one column (128 lanes, four a thread).  In the product's own last block this was
-// a chain of loads (256 x 4096 x 4096: 96 us; with every SM at it 14).
+// The sum of a tile's parts, in their order, out of device memory: a warp takes one column (128 lanes, four a thread).
 constexpr int kSumThreads = 256;
-template <int BN, bool PAIR, typename D>
+template <int BN, typename D>
 __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_constant__ GemmArgs a)
 {
     after_previous();
     const int64_t i = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
-    const int piece = (int)(i / BN), col = (int)(i % BN), tile = PAIR ? piece >> 1 : piece, lane4 = (threadIdx.x & 31) * 4;
-    const int m = tile / a.tiles_n * BN + col, n = tile % a.tiles_n * (PAIR ? 2 * kLanes : kLanes) + (PAIR ? (piece & 1) * kLanes : 0) + lane4;
+    const int tile = (int)(i / BN), col = (int)(i % BN), lane4 = (threadIdx.x & 31) * 4;
+    const int m = tile / a.tiles_n * BN + col, n = tile % a.tiles_n * kLanes + lane4;
     if (tile >= a.tiles || m >= a.M || n >= a.N) return;
-    const float4* const p = reinterpret_cast<const float4*>(a.part + ((int64_t)piece * a.splits * BN + col) * kLanes + lane4);
+    const float4* const p = reinterpret_cast<const float4*>(a.part + ((int64_t)tile * a.splits * BN + col) * kLanes + lane4);
     float4 x = __ldcg(p);
 #pragma unroll 4
     for (int k = 1; k < a.splits; ++k) {
         const float4 y = __ldcg(p + (int64_t)k * (BN * kLanes / 4));
         x = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
     }
-    D* const d = static_cast<D*>(a.d) + (int64_t)m * a.ldd + n;
     const float v[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (n + j < a.N) {
-            if (sizeof(D) == 4 && a.accumulate) store_result<D, sizeof(D) == 4>(d + j, v[j]);
-            else store_result<D, false>(d + j, v[j]);
-        }
+    store_four<D>(static_cast<D*>(a.d) + (int64_t)m * a.ldd + n, v, a.N - n, a.wide, a.accumulate);
 }
 
 // ---------------------------------------------------------------------------- host side
@@ -519,35 +587,58 @@ int make_map(const char* what, CUtensorMap* map, const void* q, int64_t ld, int6
 bool g_stall = false;                           // hpsgd_ops_debug_stall
 
 struct Plan {
-    int bn, pair, tiles_n, tiles, splits, per_split;
+    int bn, pair, tiles_n, tiles, splits, joined, per_split, longer;
 };
 
-// A's side of a tile: the least power of two that holds all its rows, 256 at most, and then on pairs of SMs unless B has no more rows
-// than one of them takes.  Splitting along k: as many parts as leave no SM with nothing to do, of at least eight k blocks each (one token,
-// 4096 outputs: with K = 1024 one part takes 5.0 us, four parts of two blocks 8.5; with K = 4096 four parts 8.9, two 9.2 us).
-constexpr int kLeastBlocks = 8;
+// A's side of a tile: the least power of two that holds all its rows, 128 at most; or 256 x 256 on pairs of SMs, which takes half as much
+// out of L2 but has one accumulator, so that a tile's results are not stored behind the next one's products.  In a round of tiles an SM spent
+// 0.25 us for each k block and 0.2 us more on 128 x 128, 0.37 and 1.8 us on its half of 256 x 256 (4096 x 4096 x 1024: 19.3 against 22.3 us;
+// 4096 x 4096 x 4096: 54.8 against 52.2; 8192 x 4096 x 4096: 112 against 95): the fewer of these, rounds counted whole.
+//
+// Splitting along k, where tiles are fewer than half the SMs and there are 16 k blocks (100 x 1000 x 1000 with its 8: 6.7 us whole, 7.5 to
+// 7.8 in parts; 32 x 2048 x 2048 with 16: 6.1 in four parts, 6.7 in two): two, four or eight parts of four blocks or more, a cluster's, as
+// many as leave every cluster its SMs at once (the device held 33 clusters of four, 15 of eight; 16 of eight take a second round, 17.9 us
+// in place of 10.2).  Beyond 128 k blocks, where there is room for 16 parts, these go through memory: with 1 x 128, K = 16384 takes 7.3 us
+// in a cluster and 8.2 through memory, K = 32768 10.2 and 8.5.
+constexpr int kSplitBlocks = 16, kLeastBlocks = 4, kJoinBlocks = 128, kMemoryParts = 16, kMemoryBlocks = 8;
 Plan plan_of(int64_t M, int64_t N, int64_t K)
 {
+    const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     Plan p{};
-    p.pair = M > 128 && N > kLanes;
-    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : p.pair ? 256 : 128;
-    const int lanes = p.pair ? 2 * kLanes : kLanes, workers = p.pair ? kSms / 2 : kSms;
-    p.tiles_n = (int)((N + lanes - 1) / lanes);
-    const int64_t tiles = p.tiles_n * ((M + p.bn - 1) / p.bn);
+    const int blocks = (int)up(K, kStageK);
+    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    int64_t tiles_n = up(N, kLanes), tiles = tiles_n * up(M, p.bn);
+    if (M > 128) {
+        const int64_t pairs_n = up(N, 2 * kLanes), pairs = pairs_n * up(M, 256);
+        if ((double)up(pairs, kSms / 2) * (9.0 * blocks + 44.0) < (double)up(tiles, kSms) * (6.0 * blocks + 4.0)) {
+            p.pair = 1;
+            p.bn = 256;
+            tiles_n = pairs_n;
+            tiles = pairs;
+        }
+    }
+    p.tiles_n = (int)tiles_n;
     p.tiles = (int)tiles;
-    const int blocks = (int)((K + kStageK - 1) / kStageK);
-    p.splits = tiles < workers ? (int)std::max<int64_t>(1, std::min<int64_t>(workers / tiles, blocks / kLeastBlocks)) : 1;
-    p.per_split = (blocks + p.splits - 1) / p.splits;
-    p.splits = (blocks + p.per_split - 1) / p.per_split;
+    p.splits = 1;
+    if (!p.pair && tiles <= kSms / 2 && blocks >= kSplitBlocks) {
+        const int most = (int)std::min<int64_t>(kSms / tiles, blocks / kMemoryBlocks);
+        if (blocks > kJoinBlocks && most >= kMemoryParts) p.splits = most;
+        else {
+            p.joined = 1;
+            p.splits = tiles > 32 ? 2 : tiles > 14 || blocks < 8 * kLeastBlocks ? 4 : 8;
+        }
+    }
+    p.per_split = blocks / p.splits;
+    p.longer = blocks % p.splits;
     return p;
 }
 
 size_t workspace_of(const Plan& p)
 {
-    return p.splits > 1 ? (size_t)p.tiles * (p.pair ? 2 : 1) * p.splits * kLanes * p.bn * sizeof(float) : 0;
+    return p.splits > 1 && !p.joined ? (size_t)p.tiles * p.splits * kLanes * p.bn * sizeof(float) : 0;
 }
 
-template <int BN, bool PAIR, typename D>
+template <int BN, bool PAIR, bool JOIN, typename D>
 int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
 {
     using S = Shape<BN, PAIR>;
@@ -565,36 +656,39 @@ int launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int 
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;          // see launch_early
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = PAIR ? 2 : 1;
+    attr[1].val.clusterDim.x = PAIR ? 2 : JOIN ? (unsigned)a.splits : 1;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = PAIR ? 2 : 1;
+    cfg.numAttrs = PAIR || JOIN ? 2 : 1;
     int at_once = dev < 64 ? workers[dev] : 0;
     if (at_once == 0) {
-        OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, PAIR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        OPS_CUDA(cudaFuncSetAttribute(gemm_fp8_kernel<BN, PAIR, JOIN, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
         at_once = sms;
-        if (PAIR) OPS_CUDA(cudaOccupancyMaxActiveClusters(&at_once, gemm_fp8_kernel<BN, PAIR, D>, &cfg));
+        if (PAIR) OPS_CUDA(cudaOccupancyMaxActiveClusters(&at_once, gemm_fp8_kernel<BN, PAIR, JOIN, D>, &cfg));
         at_once = std::max(1, at_once);
         if (dev < 64) workers[dev] = at_once;
     }
     const int64_t units = (int64_t)a.tiles * a.splits;
-    cfg.gridDim = dim3((PAIR ? 2u : 1u) * (unsigned)std::min<int64_t>(units, at_once));
-    OPS_CUDA(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<BN, PAIR, D>, ma, mb, a));
+    cfg.gridDim = dim3((PAIR ? 2u : 1u) * (unsigned)(JOIN ? units : std::min<int64_t>(units, at_once)));
+    OPS_CUDA(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<BN, PAIR, JOIN, D>, ma, mb, a));
     OPS_TRY(launched("hpsgd_gemm_fp8"));
-    if (a.splits == 1) return HPSGD_OK;
-    const int64_t columns = (int64_t)a.tiles * (PAIR ? 2 : 1) * BN;
-    return launch_early("hpsgd_gemm_fp8", sum_parts_kernel<BN, PAIR, D>, dim3((unsigned)((columns + kSumThreads / 32 - 1) / (kSumThreads / 32))), kSumThreads, 0, s, a);
+    if (PAIR || JOIN || a.splits == 1) return HPSGD_OK;
+    if constexpr (!PAIR && !JOIN) {
+        const int64_t columns = (int64_t)a.tiles * BN;
+        return launch_early("hpsgd_gemm_fp8", sum_parts_kernel<BN, D>, dim3((unsigned)((columns + kSumThreads / 32 - 1) / (kSumThreads / 32))), kSumThreads, 0, s, a);
+    }
+    return HPSGD_OK;
 }
 
-template <typename D>
-int launch_shape(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
+template <bool JOIN, typename D>
+int launch_shape(const Plan& p, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& a, int sms, cudaStream_t s)
 {
-    switch (bn) {
-    case 16: return launch<16, false, D>(ma, mb, a, sms, s);
-    case 32: return launch<32, false, D>(ma, mb, a, sms, s);
-    case 64: return launch<64, false, D>(ma, mb, a, sms, s);
-    case 128: return launch<128, false, D>(ma, mb, a, sms, s);
-    default: return launch<256, true, D>(ma, mb, a, sms, s);
+    switch (p.bn) {
+    case 16: return launch<16, false, JOIN, D>(ma, mb, a, sms, s);
+    case 32: return launch<32, false, JOIN, D>(ma, mb, a, sms, s);
+    case 64: return launch<64, false, JOIN, D>(ma, mb, a, sms, s);
+    case 128: return launch<128, false, JOIN, D>(ma, mb, a, sms, s);
+    default: return launch<256, true, false, D>(ma, mb, a, sms, s);
     }
 }
 
@@ -621,7 +715,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     if (p.M < 0 || p.N < 0 || p.K < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
     // coordinates of boxes that reach past the end stay below 2^31, tiles below 2^31
     const int64_t most = 0x7FFFFFFF - 4096;
-    if (p.M > most || p.N > most || p.K > most || ((p.N + 127) / 128) * ((p.M + 255) / 256) > most)
+    if (p.M > most || p.N > most || p.K > most || ((p.N + 127) / 128) * ((p.M + 127) / 128) > most)
         return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
     if (p.d_dtype != HPSGD_F32 && p.d_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown d_dtype %d", what, p.d_dtype);
     if (p.accumulate != 0 && (p.accumulate != 1 || p.d_dtype != HPSGD_F32)) return report(HPSGD_E_BADARG, "%s: accumulate must be 0, or 1 with an fp32 result", what);
@@ -649,12 +743,15 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     OPS_TRY(make_map(what, &mb, p.b, p.ldb, p.N, p.K, kLanes));
     GemmArgs a{};
     a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
-    a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split;
+    a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; 
+    a.per_split = plan.per_split; a.longer = plan.longer;
+    a.wide = p.ldd % 4 == 0 && aligned(p.d, 4 * esz);
     a.sa = reinterpret_cast<const uint32_t*>(p.a_scale); a.sb = reinterpret_cast<const uint32_t*>(p.b_scale);
     a.stall = g_stall ? 16 : 0;
     a.ldsa = p.ldsa; a.ldsb = p.ldsb; a.ldd = p.ldd; a.d = p.d; a.accumulate = p.accumulate;
     a.part = static_cast<float*>(p.workspace);
-    return p.d_dtype == HPSGD_F32 ? launch_shape<float>(plan.bn, ma, mb, a, sms, s) : launch_shape<__nv_bfloat16>(plan.bn, ma, mb, a, sms, s);
+    if (p.d_dtype == HPSGD_F32) return plan.joined ? launch_shape<true, float>(plan, ma, mb, a, sms, s) : launch_shape<false, float>(plan, ma, mb, a, sms, s);
+    return plan.joined ? launch_shape<true, __nv_bfloat16>(plan, ma, mb, a, sms, s) : launch_shape<false, __nv_bfloat16>(plan, ma, mb, a, sms, s);
 }
 
 int hpsgd_ops_debug_stall(int enable)

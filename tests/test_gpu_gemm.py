@@ -76,6 +76,47 @@ def test_product(M, N, K, out):
     check(d, a, b, K)
 
 
+# Two, four and eight joined parts of even and uneven lengths on every width of tile; pairs of SMs, with a second tile for some of them and with
+# fewer rows of B than one of them takes; sums in so many parts that they go through memory.
+@pytest.mark.parametrize("M,N,K", [(1, 130, 2100), (2, 9000, 2048), (20, 4000, 2200), (40, 2000, 4100), (100, 1100, 5000), (300, 700, 3333), (1000, 1000, 2049),
+                                   (1300, 2100, 1700), (2300, 4000, 1700), (18900, 130, 1700), (1, 100, 40000), (33, 200, 33000), (128, 128, 65536)])
+@pytest.mark.parametrize("out", [F32, BF])
+def test_product_in_parts_and_on_pairs(M, N, K, out):
+    a, b = Operand(M, K, 21), Operand(N, K, 22)
+    d = torch.full((M, N), math.nan, dtype=out, device="cuda")
+    product(M, N, K, a, b, d)
+    check(d, a, b, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 130, 2100), (100, 1100, 5000), (1300, 2100, 1700), (3, 100, 40000)])
+@pytest.mark.parametrize("skew", [0, 1, 4])
+def test_parts_and_pairs_add_to_strided_results(M, N, K, skew):
+    a, b = Operand(M, K, 23), Operand(N, K, 24)
+    ldd = N + 2 + skew
+    buf = torch.full((M * ldd + 16,), 7.0, device="cuda")
+    d = buf[skew: skew + M * ldd].view(M, ldd)
+    d[:, :N] = torch.randn(M, N, device="cuda") * 1e4
+    before = d[:, :N].clone()
+    product(M, N, K, a, b, d, ldd=ldd, accumulate=True)
+    check(d[:, :N].contiguous(), a, b, K, before)
+    product(M, N, K, a, b, d, ldd=ldd)
+    check(d[:, :N].contiguous(), a, b, K)
+    assert bool((d[:, N:] == 7).all()) and bool((buf[:skew] == 7).all()) and bool((buf[skew + M * ldd:] == 7).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 130, 2100), (1000, 1000, 2049), (1300, 2100, 1700), (3, 100, 40000)])
+def test_parts_and_pairs_repeat(M, N, K):
+    a, b = Operand(M, K, 25), Operand(N, K, 26)
+    d = torch.empty(M, N, device="cuda")
+    args, ws = product(M, N, K, a, b, d)
+    first = d.clone()
+    for _ in range(20):
+        d.fill_(math.nan)
+        ws.fill_(0xFF)
+        hp.hpsgd_gemm_fp8(args)
+        assert torch.equal(d, first)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 200, 2048), (100, 300, 4096), (300, 200, 260)])
 def test_accumulate(M, N, K):
     a, b = Operand(M, K, 3), Operand(N, K, 4)

@@ -22,7 +22,7 @@ def checked_library():
         hp.use_library(None)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 256, 512), (300, 600, 512)], ids=["one block", "a pair"])
+@pytest.mark.parametrize("M,N,K", [(1, 256, 512), (300, 600, 512), (1, 256, 4096), (1300, 2100, 1700)], ids=["two blocks", "blocks", "joined blocks", "pairs"])
 def test_waits_that_run_out(checked_library, M, N, K):
     a, b = Operand(M, K, 1), Operand(N, K, 2)
     d = torch.zeros(M, N, device="cuda")

@@ -182,21 +182,22 @@ def gemm_args(**change):
 @pytest.mark.parametrize("change", [dict(M=-1), dict(N=-1), dict(K=-1), dict(d_dtype=2), dict(accumulate=2), dict(accumulate=1, d_dtype=hp.HPSGD_BF16),
                                     dict(a=None), dict(b=None), dict(a_scale=None), dict(b_scale=None), dict(d=None), dict(d=A + 2), dict(a=A + 8),
                                     dict(b=A + 8), dict(a_scale=A + 2), dict(b_scale=A + 1), dict(lda=255), dict(lda=264), dict(ldb=240), dict(ldsa=299),
-                                    dict(ldsb=199), dict(ldd=199), dict(M=1, K=4096, workspace=None), dict(M=1, K=4096, workspace=A + 8)], ids=str)
+                                    dict(ldsb=199), dict(ldd=199), dict(M=1, K=1 << 17, workspace=None), dict(M=1, K=1 << 17, workspace=A + 8)], ids=str)
 def test_product_refuses(change):
     refused(hp.HPSGD_E_BADARG, hp.hpsgd_gemm_fp8, gemm_args(**change))
 
 
 def test_product_limits():
-    refused(hp.HPSGD_E_NOMEM, hp.hpsgd_gemm_fp8, gemm_args(M=1, K=4096, workspace_bytes=100))
+    refused(hp.HPSGD_E_NOMEM, hp.hpsgd_gemm_fp8, gemm_args(M=1, K=1 << 17, workspace_bytes=100))
     refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_gemm_fp8, gemm_args(M=1 << 31))
     refused(hp.HPSGD_E_UNSUPPORTED, hp.hpsgd_gemm_fp8, gemm_args(K=(1 << 31) - 1))
     hp.hpsgd_gemm_fp8(gemm_args(M=0))
     hp.hpsgd_gemm_fp8(gemm_args(N=0))
     assert hp.load().hpsgd_gemm_fp8(None, None) == hp.HPSGD_E_BADARG
     assert hp.hpsgd_gemm_fp8_bytes(0, 5, 5) == 0 and hp.hpsgd_gemm_fp8_bytes(1 << 40, 5, 5) == 0
-    # enough tiles for every SM: no workspace.  One tile and a long sum: parts
-    assert hp.hpsgd_gemm_fp8_bytes(4096, 4096, 4096) == 0 and hp.hpsgd_gemm_fp8_bytes(1, 128, 8192) > 0
+    # a cluster joins its parts without a workspace; one tile and a very long sum: parts in memory
+    assert hp.hpsgd_gemm_fp8_bytes(4096, 4096, 4096) == 0 and hp.hpsgd_gemm_fp8_bytes(1, 128, 1 << 17) > 0
+    assert hp.hpsgd_gemm_fp8_bytes(1, 128, 8192) == 0
 
 
 def test_the_stall_is_for_the_checked_build():
