@@ -141,7 +141,7 @@ __device__ __forceinline__ uint32_t round_first(float x, uint32_t rnd)
 
 // One of the two codes a <= x < b, such that the expected square is x^2: b with probability (x^2 - a^2) / (b^2 - a^2).  With the
 // codes' step as the unit, a = n and x = n + f, that is f (2n + f) / (2n + 1); n + f is 8 times the significand of x, or x itself
-// over the step where the code is subnormal (there alone 0 is near, and only 0 stays 0).  Two elements at a time.
+// over the step where the code is subnormal (there alone 0 is near: the caller lifts what is not 0 to the first code).  Two elements at a time.
 template <bool SUBNORMAL>
 __device__ __forceinline__ void round_second(float x0, float x1, uint32_t rnd0, uint32_t rnd1, uint32_t& c0, uint32_t& c1)
 {
@@ -164,8 +164,6 @@ __device__ __forceinline__ void round_second(float x0, float x1, uint32_t rnd0, 
     split(rhs, r0, r1);
     if (l0 < r0) c0 += 0x100000u;
     if (l1 < r1) c1 += 0x100000u;
-    if (SUBNORMAL && x0 > 0.f) c0 = max(c0, 0x100000u);
-    if (SUBNORMAL && x1 > 0.f) c1 = max(c1, 0x100000u);
 }
 
 // Four codes next to one another: the upper halves pairwise, shifted and cut two at a time.
@@ -276,6 +274,8 @@ __device__ __forceinline__ void encode8(const f8& m, const f8& r, const uint32_t
 #pragma unroll
             for (int k = q; k < q + 2; ++k) {
                 cm[k] = finite(m.v[k]) ? round_first(__fmul_rn(__fmul_rn(m.v[k], em), fm), rnd[k]) : 0x7F00000u;
+                // r itself decides what is 0: scaled by its block's factor, one 2^39 below the block's largest has vanished
+                if (r.v[k] > 0.f) cr[k] = max(cr[k], 0x100000u);
                 if (!finite(r.v[k])) cr[k] = 0x7F00000u;
             }
         }
