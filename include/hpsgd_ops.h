@@ -240,14 +240,16 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
 
 /*
  * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
- * since the last call (the results written since are incomplete), HPSGD_E_CUDA if the work failed.
+ * since the last call, HPSGD_E_CUDA if the work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts
+ * along k, is left as it was, and nothing is added to it; other tiles may have been written.  Products whose parts go through the workspace
+ * write nothing from such a time-out on until it has been reported here (the whole device is waited for then).
  */
 int hpsgd_ops_check(void* stream);
 
 /*
  * Checked build only; HPSGD_E_UNSUPPORTED otherwise.  1: the barriers of hpsgd_gemm_fp8 are told to expect 16 bytes more than its copies
  * bring, so that its waits run out after two seconds: the way to see the time-out path (no results, HPSGD_E_TIMEOUT from
- * hpsgd_ops_check, the device usable as before) without a fault.
+ * hpsgd_ops_check, the device usable as before) without a fault.  2: those of thread blocks with odd numbers only.
  */
 int hpsgd_ops_debug_stall(int enable);
 

@@ -31,7 +31,7 @@ constexpr int kLanes = 128;                // rows of B in a tile
 constexpr int kStageK = 128;               // k of a stage: one scale block, one row of the 128-byte swizzle
 constexpr int kGemmThreads = 384;          // copies, products, scales, one idle warp; eight warps for results
 
-__device__ unsigned int g_gemm_timeouts;   // blocks whose wait ran out
+__device__ unsigned int g_gemm_timeouts;   // blocks whose wait ran out since the last report
 
 // BN: A's rows in a tile.  PAIR: two blocks (a cluster) share a tile of 256 rows of B, each with 128 of them and half of A's rows.
 template <int BN, bool PAIR>
@@ -59,7 +59,7 @@ struct GemmArgs {
     int64_t ldsa, ldsb, ldd;
     void* d;
     int accumulate;
-    uint32_t stall;                            // checked build: bytes that a stage's barrier expects and never gets
+    uint32_t stall, stall_odd;                 // checked build: bytes that a stage's barrier expects and never gets; in blocks of odd numbers only
     float* part;                               // parts that go through memory: [tile][split][column][lane]
 };
 
@@ -184,9 +184,12 @@ __device__ __forceinline__ bool elected()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
     return yes != 0;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 
 // Four values at this block's address `at`, out of the memory of block `rank` of its cluster.
@@ -197,6 +200,13 @@ __device__ __forceinline__ float4 load_from_block(uint32_t at, int rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(there) : "memory");
     return x;
+}
+
+__device__ __forceinline__ void word_to_block(uint32_t at, int rank, uint32_t x)
+{
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(x) : "memory");
 }
 
 // C accumulator columns of this thread's lane; complete behind loads_done.
@@ -360,6 +370,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if constexpr (PAIR) cluster_sync();
+    if constexpr (JOIN) cluster_arrive();            // given_up is there to be written by the others; waited for at the end
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     after_previous();
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * BN;
@@ -380,7 +391,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 if (!(ok = wait_one(empty + s * 8, phase))) break;
                 // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
                 const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
-                if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + a.stall);
+#ifdef HPSGD_DEBUG
+                const uint32_t stall = a.stall_odd && !(blockIdx.x & 1) ? 0u : a.stall;
+#else
+                constexpr uint32_t stall = 0;
+#endif
+                if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + stall);
                 tma_load<PAIR>(dst, &map_b, kb * kStageK, x.n0, bar);
                 tma_load<PAIR>(dst + S::kBytesB, &map_a, kb * kStageK, x.m0 + rank * S::kRowsA, bar);
                 if (++s == S::kStages) s = 0, phase ^= 1;
@@ -514,9 +530,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     __syncthreads();
     if (threadIdx.x == 0 && given_up) atomicAdd(&g_gemm_timeouts, 1u);
     if constexpr (JOIN) {
+        // A block that gave up has no part, and then none of the cluster's blocks writes anything of the tile.  (Told by the one that gave up: asked
+        // for by all behind the barrier it cost 0.05 to 0.1 us a product.)
+        cluster_wait();
+        if (given_up && threadIdx.x < a.splits) word_to_block(smem_address(const_cast<const int*>(&given_up)), threadIdx.x, 1u);
+        __syncwarp();
         cluster_sync();
         const Unit x = unit_of<BN, PAIR>(a, first, 0);
-        const int cols = min(BN, a.M - x.m0);
+        const int cols = given_up ? 0 : min(BN, a.M - x.m0);
         if (a.splits == 2) join_parts<2, D>(a, smem_address(smem), x, cols);
         else if (a.splits == 4) join_parts<4, D>(a, smem_address(smem), x, cols);
         else join_parts<8, D>(a, smem_address(smem), x, cols);
@@ -530,7 +551,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
 }
 
-// The sum of a tile's parts, in their order, out of device memory: a warp takes one column (128 lanes, four a thread).
+// The sum of a tile's parts, in their order, out of device memory: a warp takes one column (128 lanes, four a thread).  Once a block
+// has given up, nothing is written until hpsgd_ops_check has reported it.
 constexpr int kSumThreads = 256;
 template <int BN, typename D>
 __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_constant__ GemmArgs a)
@@ -540,6 +562,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_con
     const int tile = (int)(i / BN), col = (int)(i % BN), lane4 = (threadIdx.x & 31) * 4;
     const int m = tile / a.tiles_n * BN + col, n = tile % a.tiles_n * kLanes + lane4;
     if (tile >= a.tiles || m >= a.M || n >= a.N) return;
+    const unsigned int gave_up = __ldcg(&g_gemm_timeouts);      // requested in front of the parts, looked at behind their sum
     const float4* const p = reinterpret_cast<const float4*>(a.part + ((int64_t)tile * a.splits * BN + col) * kLanes + lane4);
     float4 x = __ldcg(p);
 #pragma unroll 4
@@ -547,6 +570,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_con
         const float4 y = __ldcg(p + (int64_t)k * (BN * kLanes / 4));
         x = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
     }
+    if (gave_up != 0u) return;
     const float v[4] = {x.x, x.y, x.z, x.w};
     store_four<D>(static_cast<D*>(a.d) + (int64_t)m * a.ldd + n, v, a.N - n, a.wide, a.accumulate);
 }
@@ -584,7 +608,7 @@ int make_map(const char* what, CUtensorMap* map, const void* q, int64_t ld, int6
     return HPSGD_OK;
 }
 
-bool g_stall = false;                           // hpsgd_ops_debug_stall
+int g_stall = 0;                                // hpsgd_ops_debug_stall
 
 struct Plan {
     int bn, pair, tiles_n, tiles, splits, joined, per_split, longer;
@@ -748,6 +772,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
     a.wide = p.ldd % 4 == 0 && aligned(p.d, 4 * esz);
     a.sa = reinterpret_cast<const uint32_t*>(p.a_scale); a.sb = reinterpret_cast<const uint32_t*>(p.b_scale);
     a.stall = g_stall ? 16 : 0;
+    a.stall_odd = g_stall == 2;
     a.ldsa = p.ldsa; a.ldsb = p.ldsb; a.ldd = p.ldd; a.d = p.d; a.accumulate = p.accumulate;
     a.part = static_cast<float*>(p.workspace);
     if (p.d_dtype == HPSGD_F32) return plan.joined ? launch_shape<true, float>(plan, ma, mb, a, sms, s) : launch_shape<false, float>(plan, ma, mb, a, sms, s);
@@ -757,8 +782,8 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream)
 int hpsgd_ops_debug_stall(int enable)
 {
 #ifdef HPSGD_DEBUG
-    if (enable != 0 && enable != 1) return report(HPSGD_E_BADARG, "hpsgd_ops_debug_stall: enable must be 0 or 1");
-    g_stall = enable != 0;
+    if (enable < 0 || enable > 2) return report(HPSGD_E_BADARG, "hpsgd_ops_debug_stall: enable must be 0, 1 or 2");
+    g_stall = enable;
     return HPSGD_OK;
 #else
     (void)enable;
@@ -776,8 +801,10 @@ int hpsgd_ops_check(void* stream)
     OPS_CUDA(cudaMemcpyFromSymbol(&n, g_gemm_timeouts, sizeof n));
     if (n != 0) {
         const unsigned int zero = 0;
+        OPS_CUDA(cudaDeviceSynchronize());             // a sum of parts on another stream may still have to see the count
+        OPS_CUDA(cudaMemcpyFromSymbol(&n, g_gemm_timeouts, sizeof n));
         OPS_CUDA(cudaMemcpyToSymbol(g_gemm_timeouts, &zero, sizeof zero));
-        return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks gave up waiting for their own loads or products after two seconds; results are incomplete", n);
+        return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks gave up waiting for their own loads or products after two seconds; their tiles were not written", n);
     }
     return HPSGD_OK;
 }
