@@ -215,7 +215,8 @@ int hpsgd_quantize_fp8(const hpsgd_quantize_fp8_args* args, void* stream);
  *   Every product is exact, and they are added in binary32 (on the tensor cores, in an order that depends on the sizes alone).
  *   Values held as the NaN code make the results they enter NaN.
  *   d_dtype       HPSGD_F32 or HPSGD_BF16 (rounded once)
- *   accumulate    1: D += the product (HPSGD_F32 only), for gradients over several batches
+ *   accumulate    1: D += the product (HPSGD_F32 only), for gradients over several batches; one binary32 addition an element, subnormal numbers
+ *                 included.  D is read and written like any other operand: calls that add to the same D have to be ordered
  *   ldd           elements from row to row of D, 0 = N; any alignment
  *   lda, ldb, ldsa, ldsb   as in hpsgd_quantize_fp8
  *   workspace     hpsgd_gemm_fp8_bytes(M, N, K) bytes of device memory (0 but for few rows and very long sums), 16-byte aligned; no contents needed.  Calls

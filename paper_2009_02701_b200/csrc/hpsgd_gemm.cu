@@ -252,20 +252,48 @@ __device__ __forceinline__ Unit unit_of(const GemmArgs& a, int u, int rank)
     return x;
 }
 
-// One result.  Adding to what is there is left to the memory side: it returns nothing that the warp would have to wait for (a load, an
-// addition and a store for each of 256 columns took 132 us where the product takes 27), and each element receives exactly one.
-template <typename D, bool ADD>
-__device__ __forceinline__ void store_result(D* p, float x)
+// What a result is added to is read, added in registers and written: an addition on the memory side returns nothing to wait for, but PTX has it flush
+// subnormal operands and results to 0, so that D += 0 would change D.  The loads go out before the sums are there.  Against that addition, D out of
+// HBM: 4096 x 4096 x 512 26.3 us (30.9), 1024 x 1025 x 2000 11.4 (12.4), 4096 x 1024 x 4095 22.8 (22.9), 4096 x 4096 x 8192 135 (126); with 16 MB of D
+// in L2, 4096 x 1024 x 512 takes 9.0 (6.9).
+__device__ __forceinline__ float load_old(const float* p)
 {
-    if constexpr (ADD) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x) : "memory");
-    else store1(p, x);
+    float x;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
+    return x;
+}
+
+// C columns of one lane out of rows that are ldd apart, `left` of them there.
+template <int C>
+__device__ __forceinline__ void load_old_columns(const float* p, int64_t ldd, float* x, int left)
+{
+    if (left >= C) {
+#pragma unroll
+        for (int j = 0; j < C; ++j, p += ldd) x[j] = load_old(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j, p += ldd) x[j] = j < left ? load_old(p) : 0.f;
+    }
 }
 
 // Four neighbours in a row of D, `left` of them there; `wide`: aligned to all four.
-template <typename D>
-__device__ __forceinline__ void store_four(D* p, const float* v, int left, int wide, int accumulate)
+__device__ __forceinline__ float4 load_old_four(const float* p, int left, int wide)
 {
-    if (wide && left >= 4 && !accumulate) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (wide && left >= 4) asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
+    else {
+        if (left > 0) x.x = load_old(p);
+        if (left > 1) x.y = load_old(p + 1);
+        if (left > 2) x.z = load_old(p + 2);
+        if (left > 3) x.w = load_old(p + 3);
+    }
+    return x;
+}
+
+template <typename D>
+__device__ __forceinline__ void store_four(D* p, const float* v, int left, int wide)
+{
+    if (wide && left >= 4) {
         if constexpr (sizeof(D) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
         else {
             __nv_bfloat162 h[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
@@ -275,36 +303,39 @@ __device__ __forceinline__ void store_four(D* p, const float* v, int left, int w
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (j < left) {
-            if (sizeof(D) == 4 && accumulate) store_result<D, sizeof(D) == 4>(p + j, v[j]);
-            else store_result<D, false>(p + j, v[j]);
-        }
+        if (j < left) store1(p + j, v[j]);
 }
 
 // C columns of one lane to rows of D that are ldd apart, `left` of them there.
-template <int C, typename D, bool ADD>
+template <int C, typename D>
 __device__ __forceinline__ void store_columns(D* p, int64_t ldd, const float* x, int left)
 {
     if (left >= C) {
 #pragma unroll
-        for (int j = 0; j < C; ++j) store_result<D, ADD>(p + j * ldd, x[j]);
+        for (int j = 0; j < C; ++j, p += ldd) store1(p, x[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < C; ++j)
-            if (j < left) store_result<D, ADD>(p + j * ldd, x[j]);
+        for (int j = 0; j < C; ++j, p += ldd)
+            if (j < left) store1(p, x[j]);
     }
 }
 
 // The sum of a tile's P parts, in their order, out of the shared memory of the P blocks that have them ([column][lane] in each): a warp takes
-// 16 / P columns of a part's share at a time, a thread four lanes of each.
-template <int P, typename D>
+// 16 / P columns of a part's share at a time (half as many with what they are added to), a thread four lanes of each.
+template <int P, typename D, bool ADD>
 __device__ __forceinline__ void join_parts(const GemmArgs& a, uint32_t parts, const Unit& x, int cols)
 {
-    constexpr int kWarps = kGemmThreads / 32, kAtOnce = 16 / P;
+    constexpr int kWarps = kGemmThreads / 32, kAtOnce = ADD ? 8 / P : 16 / P;
     const int lane4 = (threadIdx.x & 31) * 4, n = x.n0 + lane4, step = kWarps * P;
     if (n >= a.N) return;
     for (int c0 = (threadIdx.x >> 5) * P + x.split; c0 < cols; c0 += step * kAtOnce) {
-        float4 t[kAtOnce][P];
+        float4 t[kAtOnce][P], old[kAtOnce];
+        const auto place = [&](int i) { return static_cast<D*>(a.d) + (int64_t)(x.m0 + c0 + i * step) * a.ldd + n; };
+        if constexpr (ADD) {
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                if (c0 + i * step < cols) old[i] = load_old_four(place(i), a.N - n, a.wide);
+        }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
@@ -319,9 +350,18 @@ __device__ __forceinline__ void join_parts(const GemmArgs& a, uint32_t parts, co
                 v[0] = __fadd_rn(v[0], t[i][k].x), v[1] = __fadd_rn(v[1], t[i][k].y);
                 v[2] = __fadd_rn(v[2], t[i][k].z), v[3] = __fadd_rn(v[3], t[i][k].w);
             }
-            store_four<D>(static_cast<D*>(a.d) + (int64_t)(x.m0 + c0 + i * step) * a.ldd + n, v, a.N - n, a.wide, a.accumulate);
+            if (ADD) v[0] = __fadd_rn(old[i].x, v[0]), v[1] = __fadd_rn(old[i].y, v[1]), v[2] = __fadd_rn(old[i].z, v[2]), v[3] = __fadd_rn(old[i].w, v[3]);
+            store_four<D>(place(i), v, a.N - n, a.wide);
         }
     }
+}
+
+template <typename D, bool ADD>
+__device__ __forceinline__ void join_any(const GemmArgs& a, uint32_t parts, const Unit& x, int cols)
+{
+    if (a.splits == 2) join_parts<2, D, ADD>(a, parts, x, cols);
+    else if (a.splits == 4) join_parts<4, D, ADD>(a, parts, x, cols);
+    else join_parts<8, D, ADD>(a, parts, x, cols);
 }
 
 // JOIN: the blocks of a cluster have a tile's parts, one each.
@@ -490,14 +530,79 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         // that nothing waits: the columns are requested together, and addresses do not depend on one another.
         constexpr int kHalf = BN / 2, kC = kHalf < 16 ? kHalf : 16;
         const int part = warp & 3, c0 = (warp >> 2) - 1 ? kHalf : 0;
+        const uint32_t mine = tmem + c0 + ((uint32_t)part << 21);
+        const auto accumulator_read = [&](int acc) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
+                else barrier_arrive(acc_empty + acc * 8);
+            }
+        };
         int done = 0;
-        for (int u = first; u < units; u += stride, ++done) {
+        const bool adds = sizeof(D) == 4 && !JOIN && a.accumulate && (PAIR || a.splits == 1);
+        if constexpr (sizeof(D) == 4 && !JOIN) {
+            // What a unit is added to is requested before its products are waited for, as many columns as registers allow (112 of a pair's 128).  Where
+            // a second accumulator lets the next unit's products run ahead, its part of D comes to L2 meanwhile (4096 x 4096 x 512: 33.7 us without,
+            // 26.3 with; on pairs that gets in the copies' way: 4096 x 4096 x 8192 132 without, 142 with).
+            constexpr int kPieces = kHalf / kC, kSlots = kPieces < 7 ? kPieces : 7;
+            float old[kSlots][kC];
+            struct Place {
+                D* d;
+                int left;
+            };
+            const auto place_of = [&](int u) {
+                const Unit x = unit_of<BN, PAIR>(a, u, rank);
+                const int n = x.n0 + part * 32 + lane;
+                return Place{static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n, n < a.N ? a.M - x.m0 - c0 : 0};
+            };
+            for (int u = first; u < units && adds; u += stride, ++done) {
+                const int acc = done % S::kAccs;
+                const Place x = place_of(u);
+#pragma unroll
+                for (int k = 0; k < kSlots; ++k) load_old_columns<kC>(x.d + k * kC * a.ldd, a.ldd, old[k], x.left - k * kC);
+                if constexpr (!PAIR) {                // a lane a column: the lines that its 32 neighbouring results begin and end in
+                    const int next = u + stride;
+                    const Unit y = unit_of<BN, PAIR>(a, next, rank);
+                    const int n = y.n0 + part * 32;
+#pragma unroll
+                    for (int j = lane; j < kHalf; j += 32)
+                        if (next < units && n < a.N && y.m0 + c0 + j < a.M) {
+                            const D* const row = static_cast<D*>(a.d) + (int64_t)(y.m0 + c0 + j) * a.ldd;
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(row + n));
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(row + min(n + 31, a.N - 1)));
+                        }
+                }
+                if (!wait(acc_full + acc * 8, done / S::kAccs & 1)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    float v[kC], *const o = old[k % kSlots];
+                    load_columns<kC>(mine + acc * BN + k * kC, v);
+                    loads_done<kC>(v);
+                    if (k + 1 == kPieces) accumulator_read(acc);
+#pragma unroll
+                    for (int q = 0; q < kC; ++q) o[q] = __fadd_rn(o[q], v[q]);
+                    if (kPieces > kSlots) {
+                        store_columns<kC, D>(x.d + k * kC * a.ldd, a.ldd, o, x.left - k * kC);
+                        if (k + kSlots < kPieces) load_old_columns<kC>(x.d + (k + kSlots) * kC * a.ldd, a.ldd, o, x.left - (k + kSlots) * kC);
+                    }
+                }
+                if (kPieces == kSlots) {
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) store_columns<kC, D>(x.d + k * kC * a.ldd, a.ldd, old[k], x.left - k * kC);
+                }
+                __syncwarp();
+            }
+        }
+        for (int u = first; u < units && !adds; u += stride, ++done) {
             const Unit x = unit_of<BN, PAIR>(a, u, rank);
             const int acc = done % S::kAccs;
             if (!wait(acc_full + acc * 8, done / S::kAccs & 1)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t src = tmem + acc * BN + c0 + ((uint32_t)part << 21);
+            const uint32_t src = mine + acc * BN;
             const int n = x.n0 + part * 32 + lane, cols = a.M - x.m0 - c0;
+            D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
             // [column][lane]: a part's own place in device memory, or where this block's stages were (its only unit's products have read them)
             float* const sums = (JOIN ? reinterpret_cast<float*>(smem) : a.part + ((int64_t)x.tile * a.splits + x.split) * (kLanes * BN)) + c0 * kLanes +
                                 part * 32 + lane;
@@ -506,21 +611,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
             for (int c = 0; c < kHalf; c += kC) load_columns<kC>(src + c, v + c);
             loads_done<kHalf>(v);
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
-                else barrier_arrive(acc_empty + acc * 8);
-            }
-            D* const d = static_cast<D*>(a.d) + (int64_t)(x.m0 + c0) * a.ldd + n;
+            accumulator_read(acc);
 #pragma unroll
             for (int c = 0; c < kHalf; c += kC) {
                 if (c >= cols) continue;
-                if (JOIN || (!PAIR && a.splits > 1)) store_columns<kC, float, false>(sums + c * kLanes, kLanes, v + c, cols - c);
-                else if (n < a.N) {
-                    if (sizeof(D) == 4 && a.accumulate) store_columns<kC, D, sizeof(D) == 4>(d + c * a.ldd, a.ldd, v + c, cols - c);
-                    else store_columns<kC, D, false>(d + c * a.ldd, a.ldd, v + c, cols - c);
-                }
+                if (JOIN || (!PAIR && a.splits > 1)) store_columns<kC, float>(sums + c * kLanes, kLanes, v + c, cols - c);
+                else if (n < a.N) store_columns<kC, D>(d + c * a.ldd, a.ldd, v + c, cols - c);
             }
             __syncwarp();
         }
@@ -538,9 +634,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         cluster_sync();
         const Unit x = unit_of<BN, PAIR>(a, first, 0);
         const int cols = given_up ? 0 : min(BN, a.M - x.m0);
-        if (a.splits == 2) join_parts<2, D>(a, smem_address(smem), x, cols);
-        else if (a.splits == 4) join_parts<4, D>(a, smem_address(smem), x, cols);
-        else join_parts<8, D>(a, smem_address(smem), x, cols);
+        if (sizeof(D) == 4 && a.accumulate) join_any<D, sizeof(D) == 4>(a, smem_address(smem), x, cols);
+        else join_any<D, false>(a, smem_address(smem), x, cols);
         __syncwarp();
         cluster_sync();                              // this block's memory stays until the others have read it
     }
@@ -562,6 +657,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_con
     const int tile = (int)(i / BN), col = (int)(i % BN), lane4 = (threadIdx.x & 31) * 4;
     const int m = tile / a.tiles_n * BN + col, n = tile % a.tiles_n * kLanes + lane4;
     if (tile >= a.tiles || m >= a.M || n >= a.N) return;
+    D* const d = static_cast<D*>(a.d) + (int64_t)m * a.ldd + n;
+    float4 old;
+    if constexpr (sizeof(D) == 4)
+        if (a.accumulate) old = load_old_four(d, a.N - n, a.wide);
     const unsigned int gave_up = __ldcg(&g_gemm_timeouts);      // requested in front of the parts, looked at behind their sum
     const float4* const p = reinterpret_cast<const float4*>(a.part + ((int64_t)tile * a.splits * BN + col) * kLanes + lane4);
     float4 x = __ldcg(p);
@@ -571,8 +670,9 @@ __global__ void __launch_bounds__(kSumThreads) sum_parts_kernel(const __grid_con
         x = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
     }
     if (gave_up != 0u) return;
+    if (sizeof(D) == 4 && a.accumulate) x = make_float4(__fadd_rn(old.x, x.x), __fadd_rn(old.y, x.y), __fadd_rn(old.z, x.z), __fadd_rn(old.w, x.w));
     const float v[4] = {x.x, x.y, x.z, x.w};
-    store_four<D>(static_cast<D*>(a.d) + (int64_t)m * a.ldd + n, v, a.N - n, a.wide, a.accumulate);
+    store_four<D>(d, v, a.N - n, a.wide);
 }
 
 // ---------------------------------------------------------------------------- host side
