@@ -303,8 +303,8 @@ int hpsgd_local_step_all_ex(const hpsgd_grad_desc* descs);
  * hpsgd_set_option are not used.  `grads` is as in hpsgd_local_step.  The moments are the caller's, one set for each worker, in
  * the flat layout (P_pad elements; with state_bits 8 ceil(P_pad / 128) scale bytes each) and zero before the first step; they are
  * neither merged nor part of hpsgd_export_state.  Everything else is as for hpsgd_local_step: the merge averages the replica
- * changes, whatever made them.  Enqueued on the main stream; never held back by HPSGD_OPT_FUSE.  Replica-change form only (else
- * HPSGD_E_STATE).
+ * changes, whatever made them.  Enqueued on the main stream; never held back by HPSGD_OPT_FUSE; its kernels count as
+ * HPSGD_KERNEL_LOCAL_STEP under HPSGD_OPT_PROFILE.  Replica-change form only (else HPSGD_E_STATE).
  */
 typedef struct hpsgd_adamw_args {
     void* m;

@@ -447,7 +447,10 @@ int hpsgd_local_step_adamw(int worker, const void* grads, const hpsgd_adamw_args
         const int64_t at = lo * 8, n = (hi - lo) * 8;
         if (clone)
             CUDA_TRY(cudaMemcpyAsync(g.r + (int64_t)worker * g.stride + at, g.w + at, (size_t)n * 4, cudaMemcpyDeviceToDevice, g.main));
+        EventPair ep{};
+        TRY(prof_begin(g.main, HPSGD_KERNEL_LOCAL_STEP, &ep));
         TRY(step(n, at));
+        TRY(prof_end(g.main, &ep));
         if (g.overlap) {
             CUDA_TRY(cudaEventRecord(g.ev_local[c], g.main));
             g.local_recorded[c] = 1;
