@@ -432,6 +432,9 @@ int hpsgd_local_step_adamw(int worker, const void* grads, const hpsgd_adamw_args
                                 g.seed + (uint64_t)worker * kM1, args->grad_scale, g.main);
     };
     if (!args->m || !args->v || (args->state_bits == 8 && (!args->m_scale || !args->v_scale))) return fail(HPSGD_E_BADARG, "a moment or its scale is NULL");
+    // (the empty step below looks at no element pointer; an offset in a chunk or the row keeps what alignment they have)
+    if (args->state_bits == 32 && (reinterpret_cast<uintptr_t>(args->m) % 4 || reinterpret_cast<uintptr_t>(args->v) % 4))
+        return fail(HPSGD_E_BADARG, "a moment is not aligned to its elements");
     TRY(step(0, 0));                       // an empty step: every other argument is checked, nothing is enqueued
     TRY(flush_deferred());
     // a replica that is still a clone of w, read from there (lazy clone, pipelined schedule), gets its row first

@@ -1,8 +1,9 @@
-"""hpsgd_local_step_adamw as a call of the library: its launches are profiled like every other step's."""
+"""hpsgd_local_step_adamw as a call of the library: its launches are profiled like every other step's, and a refusal enqueues nothing."""
 import pytest
 import torch
 
 import paper_2009_02701_b200 as hp
+from tests.gpu_util import dev_tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,20 @@ def test_profile_counts_its_launches(bits, chunks, fuse):
         hp.hpsgd_set_option(hp.HPSGD_OPT_PROFILE, 0)
         run.step(1, 2)
         assert hp.hpsgd_profile_read(hp.HPSGD_KERNEL_LOCAL_STEP)[1] == 0
+
+
+@pytest.mark.parametrize("name", ["m", "v", "grad_scale"])
+def test_an_unaligned_address_is_refused_before_anything_is_enqueued(name):
+    """A held-back local step stays held back: the merge that comes next still runs with it as one kernel."""
+    with Run(32, FUSE=2) as run:
+        for worker in range(2):
+            hp.hpsgd_local_step(worker, run.g)
+        before = hp.hpsgd_launch_count()
+        with pytest.raises(hp.HpsgdError) as err:
+            run.step(0, **{name: run.m.data_ptr() + 2})
+        assert err.value.code == hp.HPSGD_E_BADARG
+        assert hp.hpsgd_launch_count() == before
+        hp.hpsgd_sync_merge()
+        assert hp.hpsgd_launch_count() == before + 1
+        hp.hpsgd_synchronize()
+        assert float(dev_tensor(hp.hpsgd_get_global(), run.P_pad).abs().max()) < 1.0
