@@ -173,17 +173,18 @@ constexpr int kBackBlocks = 592;      // most partial sums of dweight: four bloc
 // thread's columns stay the same from row to row, so their dweight is added in registers.
 // With one group a thread the next row's values are requested before the present row's sum is waited for; with two, the registers
 // go to the row itself; with four, the row and the weights are read a second time behind the sum, from L1 and L2.
-template <int T>
+template <typename X, int T, int V>
 struct Back {
     static constexpr int kThreads = T < 256 ? 256 : T;
+    static constexpr int kPerSm = V == 1 ? (sizeof(X) == 2 ? 1024 : 768) / kThreads : 1;      // blocks that an SM holds
 };
 
 template <typename X, typename W, int T, int V>
-__global__ void __launch_bounds__(Back<T>::kThreads, V == 1 ? (sizeof(X) == 2 ? 1024 : 768) / Back<T>::kThreads : 1) rmsnorm_backward_kernel(const Backward a)
+__global__ void __launch_bounds__(Back<X, T, V>::kThreads, Back<X, T, V>::kPerSm) rmsnorm_backward_kernel(const Backward a)
 {
     __shared__ float buf[2][32];
     constexpr bool kAhead = V == 1, kKeep = V <= 2;
-    constexpr int kRows = Back<T>::kThreads / T;
+    constexpr int kThreads = Back<X, T, V>::kThreads, kRows = kThreads / T;
     const int t = threadIdx.x % T, group = threadIdx.x / T;
     f8 dw[V];
     Raw8<W> w[V];
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(Back<T>::kThreads, V == 1 ? (sizeof(X) == 2 ? 
 #pragma unroll
         for (int q = 0; q < 8; ++q) all[group][t * 8 + q] = dw[0].v[q];
         __syncthreads();
-        for (int c = threadIdx.x; c < (int)a.cols; c += Back<T>::kThreads) {
+        for (int c = threadIdx.x; c < (int)a.cols; c += kThreads) {
             float s = all[0][c];
 #pragma unroll
             for (int g = 1; g < kRows; ++g) s += all[g][c];
@@ -312,12 +313,14 @@ __global__ void __launch_bounds__(1024) dweight_kernel(const float* part, float*
 template <typename X, typename W, int T, int V>
 int backward_launch(const Backward& a, float* dweight, cudaStream_t s)
 {
-    // as many blocks as are resident at once, of which each has a row to begin with
-    constexpr int kRows = Back<T>::kThreads / T, kResident = V == 1 ? 148 * (sizeof(X) == 2 ? 1024 : 768) / Back<T>::kThreads : 148;
+    // as many blocks as are resident at once, of which each has a row to begin with (half a block an SM more, with fp32 on 512 threads, went through
+    // the rows behind the others: 8192 x 4096: 101 us, 86 with whole blocks)
+    using B = Back<X, T, V>;
+    constexpr int kRows = B::kThreads / T, kResident = 148 * B::kPerSm;
     static_assert(kResident <= kBackBlocks, "the workspace holds kBackBlocks partial sums");
     const int64_t need = (a.rows + kRows - 1) / kRows;
     const int blocks = (int)(need < kResident ? need : kResident);
-    OPS_TRY(launch_early("hpsgd_rmsnorm_backward", rmsnorm_backward_kernel<X, W, T, V>, dim3(blocks), Back<T>::kThreads, 0, s, a));
+    OPS_TRY(launch_early("hpsgd_rmsnorm_backward", rmsnorm_backward_kernel<X, W, T, V>, dim3(blocks), B::kThreads, 0, s, a));
     return launch_early("hpsgd_rmsnorm_backward", dweight_kernel, dim3((unsigned)((a.cols + 31) / 32)), 1024, 0, s, (const float*)a.part, dweight, a.cols, blocks);
 }
 
