@@ -28,7 +28,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 def depends(unit: str) -> list:
     heads = [os.path.join(CSRC, h) for h in _COMMON + _UNITS[unit]]
-    return [os.path.join(CSRC, unit), *heads, os.path.join(INCLUDE, "hpsgd.h"), os.path.join(INCLUDE, "hpsgd_ops.h")]
+    # this file too: it has the flags
+    return [os.path.join(CSRC, unit), *heads, os.path.join(INCLUDE, "hpsgd.h"), os.path.join(INCLUDE, "hpsgd_ops.h"), os.path.abspath(__file__)]
 
 
 DEPENDS = sorted({p for u in _UNITS for p in depends(u)})
@@ -42,7 +43,7 @@ def nvcc() -> str:
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False, out: str | None = None) -> str:
-    """Compile the library if it is missing or older than its sources; returns its path.
+    """Compile the library if it is missing or older than its sources or than this file; returns its path.
 
     ``debug`` builds the checked variant (-DHPSGD_DEBUG: kernel guards that record and skip an
     out-of-range access, host-side validation of sparse row lists) into ``out`` (default
