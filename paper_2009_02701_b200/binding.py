@@ -221,9 +221,12 @@ def hpsgd_local_step_ex(worker, desc):
 
 def hpsgd_local_step_adamw(worker, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, state_bits=32,
                            m_scale=None, v_scale=None, grad_scale=None):
-    a = hpsgd_adamw_args(_ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale), int(state_bits), float(lr), float(beta1), float(beta2),
-                         float(eps), float(weight_decay), int(step), _ptr(grad_scale))
-    return _check(load().hpsgd_local_step_adamw(int(worker), _ptr(grads), ctypes.byref(a)))
+    from .ops import _BYTE, _on_device, _vector       # tensors are checked as those of the operators are
+    n, moment = hpsgd_get_sizes()[1], _BYTE if state_bits == 8 else HPSGD_F32
+    a = hpsgd_adamw_args(_vector("m", m, moment, n), _vector("v", v, moment, n), _vector("m_scale", m_scale, _BYTE, -(-n // 128)),
+                         _vector("v_scale", v_scale, _BYTE, -(-n // 128)), int(state_bits), float(lr), float(beta1), float(beta2),
+                         float(eps), float(weight_decay), int(step), _on_device("grad_scale", grad_scale))
+    return _check(load().hpsgd_local_step_adamw(int(worker), _on_device("grads", grads), ctypes.byref(a)))
 
 
 def hpsgd_local_step_all(grads, worker_stride_bytes):

@@ -68,3 +68,15 @@ def test_an_unaligned_address_is_refused_before_anything_is_enqueued(name):
         assert hp.hpsgd_launch_count() == before + 1
         hp.hpsgd_synchronize()
         assert float(dev_tensor(hp.hpsgd_get_global(), run.P_pad).abs().max()) < 1.0
+
+
+def test_tensors_that_cannot_be_moments_are_refused():
+    with Run(8) as run:
+        before = hp.hpsgd_launch_count()
+        for change in (dict(m=run.m.cpu()), dict(grads=run.g.cpu()), dict(grad_scale=torch.ones(1)), dict(v=run.v[9:]), dict(m=run.m.float()),
+                       dict(m_scale=run.s[0][1:]), dict(v_scale=run.s[1].float()), dict(state_bits=32)):
+            with pytest.raises(hp.HpsgdError) as err:
+                run.step(0, **change)
+            assert err.value.code == hp.HPSGD_E_BADARG
+        assert hp.hpsgd_launch_count() == before
+        run.step(0)
