@@ -41,7 +41,7 @@ typedef enum hpsgd_status {
     HPSGD_E_STATE = -2,       /* call not legal in the current state (e.g. before hpsgd_init) */
     HPSGD_E_NOMEM = -3,       /* arena too small or device allocation failed */
     HPSGD_E_CUDA = -4,        /* a CUDA call failed; see hpsgd_last_error() */
-    HPSGD_E_TIMEOUT = -5,     /* a bounded device-side wait ran out (only the staged merge of HPSGD_OPT_STAGING has one) */
+    HPSGD_E_TIMEOUT = -5,     /* a bounded device-side wait ran out (the staged merge of HPSGD_OPT_STAGING and hpsgd_gemm_fp8 have some) */
     HPSGD_E_UNSUPPORTED = -6  /* size beyond a documented limit */
 } hpsgd_status;
 
@@ -93,10 +93,10 @@ enum {
                                    the same order: bit-identical.  It exists so that the two ways of issuing the
                                    memory traffic can be timed against each other on the same state; the merge has
                                    no data reuse for shared memory to exploit, and the plain form is as fast or
-                                   faster.  The staged kernel is the only device code of this library that waits
-                                   (on its own loads, for one second at most): if a wait ever runs out, the
-                                   block writes nothing and the next call that waits for the device returns
-                                   HPSGD_E_TIMEOUT. */
+                                   faster.  The staged kernel is the only one of the path that waits on the device
+                                   (for its own loads, for one second at most; of the operators hpsgd_gemm_fp8
+                                   does): if a wait ever runs out, the block writes nothing and the next call that
+                                   waits for the device returns HPSGD_E_TIMEOUT. */
     HPSGD_OPT_DEBUG_STAGE_STALL = 10, /* Checked build only; HPSGD_E_UNSUPPORTED otherwise.  1: the barrier of the staged
                                    merge (HPSGD_OPT_STAGING) is told to expect 16 bytes more than its copies bring,
                                    so that its wait runs out after one second: the way to see the time-out path

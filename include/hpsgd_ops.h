@@ -5,9 +5,11 @@
  * (The HPSGD paper has no counterpart for any of them.)
  *
  * Conventions (in addition to those of hpsgd.h)
- *   - The operators need no hpsgd_init and keep no state: every buffer is the caller's, and work
+ *   - The operators need no hpsgd_init and keep nothing of a call: every buffer is the caller's, and work
  *     is enqueued on the stream that is given (a cudaStream_t; NULL = the default stream) and on
- *     no other.  They allocate nothing and wait for nothing, so they can be captured in a graph.
+ *     no other.  They allocate nothing and wait for nothing, so they can be captured in a graph.  Like the
+ *     rest of the library they are called from one host thread (the text of the last error, the launch count
+ *     and what a device holds at a time are the process's).
  *   - Structs and arrays of structs are HOST memory, read during the call; the pointers in them
  *     are DEVICE pointers.
  *   - Arguments are checked before anything is enqueued.  A size of zero is legal and does nothing
