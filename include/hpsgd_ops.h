@@ -241,6 +241,71 @@ typedef struct hpsgd_gemm_fp8_args {
 size_t hpsgd_gemm_fp8_bytes(int64_t M, int64_t N, int64_t K);
 int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * A gated linear recurrence over sequences.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * Rows are tokens, columns channels; per channel, with h in front of a sequence's first row its h0 (0 without):
+ *     a = sigmoid(f)
+ *     h = a h' + (1 - a) v        h' the row before
+ *     y = h * sigmoid(o)          y = h without o
+ * in binary32, y rounded once.  With rows == sequences it is a step of one token for each.
+ *   dtype      of f, v, o, y: HPSGD_F32 or HPSGD_BF16
+ *   offsets    DEVICE memory, sequences + 1 numbers: sequence s has the rows [offsets[s], offsets[s + 1]).  They have to ascend (equal ones: a
+ *              sequence without rows, whose state goes through) and lie in [0, rows]; others give undefined results, but no access outside the
+ *              call's memory.  Rows in front of the first sequence and behind the last are neither read nor written; a padded batch is one in which the padding
+ *              of each sequence is a sequence too.  NULL: sequences of rows / sequences rows each (rows a multiple of sequences)
+ *   h0         [sequences x cols], or NULL
+ *   h_last     [sequences x cols], receives the state behind each sequence, or NULL; may be h0's own memory
+ *   saved      hpsgd_gated_scan_saved_bytes(rows, cols) bytes for the backward pass, or NULL
+ *   ld*        elements from row to row; 0 = cols.  f, v and o may lie side by side in one matrix.
+ * Where cols and strides are even and addresses multiples of two elements, two channels are taken at once.
+ */
+typedef struct hpsgd_gated_scan_forward_args {
+    int64_t rows, cols, sequences;
+    int dtype;
+    const void* f;
+    const void* v;
+    const void* o;
+    const int64_t* offsets;
+    const float* h0;
+    float* h_last;
+    void* y;
+    float* saved;
+    int64_t ldf, ldv, ldo, ldy, ldh0, ldlast;
+} hpsgd_gated_scan_forward_args;
+size_t hpsgd_gated_scan_saved_bytes(int64_t rows, int64_t cols);
+int hpsgd_gated_scan_forward(const hpsgd_gated_scan_forward_args* args, void* stream);
+
+/*
+ * Its gradients.  With g = dy sigmoid(o), to which dh_last is added in a sequence's last row, and G = g + a'' G'' ('' the row behind; nothing
+ * comes into a sequence's last row):
+ *     dv = G (1 - a)      df = G (h' - v) a (1 - a)      do = dy h sigmoid(o) (1 - sigmoid(o))      dh0 = a G of the first row
+ *   f, v, o, offsets, h0   as in the forward call; saved: what it left
+ *   dy, df, dv, d_o        values of dtype.  df, dv and d_o may each be, element for element, the memory of f, v, o or dy.
+ *   dh_last                gradient of h_last, or NULL (0);  dh0: [sequences x cols], or NULL
+ *   o and d_o              both or neither
+ */
+typedef struct hpsgd_gated_scan_backward_args {
+    int64_t rows, cols, sequences;
+    int dtype;
+    const void* f;
+    const void* v;
+    const void* o;
+    const int64_t* offsets;
+    const float* h0;
+    const float* saved;
+    const void* dy;
+    const float* dh_last;
+    void* df;
+    void* dv;
+    void* d_o;
+    float* dh0;
+    int64_t ldf, ldv, ldo, ldh0, lddy, lddlast, lddf, lddv, lddo, lddh0;
+} hpsgd_gated_scan_backward_args;
+int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* stream);
+
 /*
  * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
  * since the last call, HPSGD_E_CUDA if the work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts

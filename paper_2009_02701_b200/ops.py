@@ -20,7 +20,9 @@ from .binding import _ci, _f64, _i64, _stream, _u64, _vp
 
 __all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make_adamw_table", "hpsgd_adamw_step", "hpsgd_grad_norm",
            "make_rmsnorm_forward", "hpsgd_rmsnorm_forward", "make_rmsnorm_backward", "hpsgd_rmsnorm_backward", "hpsgd_rmsnorm_backward_bytes",
-           "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes", "hpsgd_ops_check",
+           "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes",
+           "make_gated_scan_forward", "hpsgd_gated_scan_forward", "make_gated_scan_backward", "hpsgd_gated_scan_backward", "hpsgd_gated_scan_saved_bytes",
+           "hpsgd_ops_check",
            "hpsgd_ops_debug_stall"]
 
 HPSGD_GRAD_NORM_WORKSPACE = 65536
@@ -55,7 +57,22 @@ class hpsgd_gemm_fp8_args(ctypes.Structure):
         [("workspace_bytes", ctypes.c_size_t)] + [(n, _i64) for n in ("lda", "ldsa", "ldb", "ldsb", "ldd")] + [("d_dtype", _ci), ("accumulate", _ci)]
 
 
+class hpsgd_gated_scan_forward_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("sequences", _i64), ("dtype", _ci)] + \
+        [(n, _vp) for n in ("f", "v", "o", "offsets", "h0", "h_last", "y", "saved")] + \
+        [(n, _i64) for n in ("ldf", "ldv", "ldo", "ldy", "ldh0", "ldlast")]
+
+
+class hpsgd_gated_scan_backward_args(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("sequences", _i64), ("dtype", _ci)] + \
+        [(n, _vp) for n in ("f", "v", "o", "offsets", "h0", "saved", "dy", "dh_last", "df", "dv", "d_o", "dh0")] + \
+        [(n, _i64) for n in ("ldf", "ldv", "ldo", "ldh0", "lddy", "lddlast", "lddf", "lddv", "lddo", "lddh0")]
+
+
 SIGNATURES = {
+    "hpsgd_gated_scan_saved_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "hpsgd_gated_scan_forward": (_ci, [_vp, _vp]),
+    "hpsgd_gated_scan_backward": (_ci, [_vp, _vp]),
     "hpsgd_gemm_fp8_bytes": (ctypes.c_size_t, [_i64, _i64, _i64]),
     "hpsgd_gemm_fp8": (_ci, [_vp, _vp]),
     "hpsgd_ops_check": (_ci, [_vp]),
@@ -82,9 +99,11 @@ def _on(stream):
 
 # ---- what a tensor has to be -----------------------------------------------------------
 _BYTE = 8                       # beside HPSGD_F32 and HPSGD_BF16: codes and scales
+_INT32, _INT64 = 32, 64         # positions
 _TYPES = {_b.HPSGD_F32: ("torch.float32", "torch.int32", "torch.uint32"), _b.HPSGD_BF16: ("torch.bfloat16", "torch.int16", "torch.uint16"),
-          _BYTE: ("torch.uint8", "torch.int8", "torch.float8_e4m3fn", "torch.float8_e8m0fnu")}
-_SIZE = {_b.HPSGD_F32: 4, _b.HPSGD_BF16: 2, _BYTE: 1}
+          _BYTE: ("torch.uint8", "torch.int8", "torch.float8_e4m3fn", "torch.float8_e8m0fnu"),
+          _INT32: ("torch.int32",), _INT64: ("torch.int64",)}
+_SIZE = {_b.HPSGD_F32: 4, _b.HPSGD_BF16: 2, _BYTE: 1, _INT32: 4, _INT64: 8}
 _known = defaultdict(set)       # kind -> torch's types that may stand there, of those seen so far
 
 
@@ -318,6 +337,38 @@ def make_gemm_fp8(M, N, K, a, a_scale, b, b_scale, d, d_dtype, accumulate=False,
 
 def hpsgd_gemm_fp8(args, stream=None):
     return _b._check(_b.load().hpsgd_gemm_fp8(args.address, _on(stream)))
+
+
+# ---- a gated linear recurrence ---------------------------------------------------------
+def hpsgd_gated_scan_saved_bytes(rows, cols):
+    return int(_b.load().hpsgd_gated_scan_saved_bytes(rows, cols))
+
+
+def make_gated_scan_forward(rows, cols, sequences, dtype, f, v, y, o=None, offsets=None, h0=None, h_last=None, saved=None, **strides):
+    pointers = dict(f=f, v=v, o=o, offsets=offsets, h0=h0, h_last=h_last, y=y, saved=saved)
+    ld = _strides(hpsgd_gated_scan_forward_args, strides)
+    at = {name: _matrix(name, pointers[name], dtype, rows, cols, ld["ld" + name] or cols) for name in ("f", "v", "o", "y")}
+    at.update({name: _matrix(name, pointers[name], _b.HPSGD_F32, sequences, cols, ld[s] or cols) for name, s in (("h0", "ldh0"), ("h_last", "ldlast"))})
+    at.update(offsets=_vector("offsets", offsets, _INT64, sequences + 1), saved=_bytes("saved", saved, hpsgd_gated_scan_saved_bytes(rows, cols)))
+    return Args(hpsgd_gated_scan_forward_args, pointers, at, ld, rows=rows, cols=cols, sequences=sequences, dtype=dtype)
+
+
+def hpsgd_gated_scan_forward(args, stream=None):
+    return _b._check(_b.load().hpsgd_gated_scan_forward(args.address, _on(stream)))
+
+
+def make_gated_scan_backward(rows, cols, sequences, dtype, f, v, saved, dy, df, dv, o=None, do=None, offsets=None, h0=None, dh_last=None, dh0=None, **strides):
+    pointers = dict(f=f, v=v, o=o, offsets=offsets, h0=h0, saved=saved, dy=dy, dh_last=dh_last, df=df, dv=dv, do=do, dh0=dh0)
+    ld = _strides(hpsgd_gated_scan_backward_args, strides)
+    at = {name: _matrix(name, pointers[name], dtype, rows, cols, ld["ld" + name] or cols) for name in ("f", "v", "o", "dy", "df", "dv")}
+    at["d_o"] = _matrix("do", do, dtype, rows, cols, ld["lddo"] or cols)
+    at.update({name: _matrix(name, pointers[name], _b.HPSGD_F32, sequences, cols, ld[s] or cols) for name, s in (("h0", "ldh0"), ("dh_last", "lddlast"), ("dh0", "lddh0"))})
+    at.update(offsets=_vector("offsets", offsets, _INT64, sequences + 1), saved=_bytes("saved", saved, hpsgd_gated_scan_saved_bytes(rows, cols)))
+    return Args(hpsgd_gated_scan_backward_args, pointers, at, ld, rows=rows, cols=cols, sequences=sequences, dtype=dtype)
+
+
+def hpsgd_gated_scan_backward(args, stream=None):
+    return _b._check(_b.load().hpsgd_gated_scan_backward(args.address, _on(stream)))
 
 
 def hpsgd_ops_check(stream=None):
