@@ -306,6 +306,49 @@ typedef struct hpsgd_gated_scan_backward_args {
 } hpsgd_gated_scan_backward_args;
 int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * The loss over a label and a teacher's top logits.
+ * ---------------------------------------------------------------------------------- */
+
+/*
+ * Per row z of logits [rows x vocab], with T the temperature:
+ *     CE = lse(z) - z[label]                                                     lse(x) = log(sum exp(x))
+ *     KL = sum over the teacher's entries j of p_j (log p_j - z[i_j] / T + lse(z / T))     p the softmax of the row's k teacher logits / T
+ *     loss = label_weight CE + teacher_weight T^2 KL
+ *     dlogits = c ( label_weight (softmax(z) - 1 at the label) + teacher_weight T (softmax(z / T) - p_j at i_j) )      c = grad_scale dloss[row]
+ * in binary32; dlogits is rounded once.  Without a teacher it is cross-entropy.
+ *   dtype, teacher_dtype   HPSGD_F32 or HPSGD_BF16, of logits and dlogits and of teacher_logits
+ *   labels          rows numbers, or NULL; a negative one: the row has no label and no CE
+ *   teacher_index, teacher_logits   [rows x k], k <= 1024 (else HPSGD_E_UNSUPPORTED); an entry whose index is negative or whose logit is
+ *                   -infinity is not there, and a row without any has no KL.  Indices may repeat.
+ *   loss            rows floats, or NULL;   lse: rows x 2 floats, lse(z) and lse(z / T), for the second call, or NULL
+ *   dlogits         the gradient in the same pass, or NULL; may be the logits' own memory
+ *   dloss           rows floats, the gradients of the rows' losses, or NULL (1).  Where c is 0, dlogits is 0 whatever the logits are.
+ *   ld*             elements from row to row; 0 = vocab, for the teacher's two matrices k
+ * Rows with neither label nor teacher have loss and gradient 0, whatever their logits are.  Logits of -infinity have probability 0 (a label or
+ * a teacher's entry there makes the loss infinite); NaN and +infinity make their row NaN, and so does a label or an index that is not below vocab.
+ * A term with weight 0 is left out: its arguments are not read.  Rows whose addresses and strides are multiples of 32 bytes (16 for bf16) take the wide
+ * accesses.
+ */
+typedef struct hpsgd_distill_loss_args {
+    int64_t rows, vocab, k;
+    double temperature, label_weight, teacher_weight, grad_scale;
+    int dtype, teacher_dtype;
+    const void* logits;
+    const int64_t* labels;
+    const int32_t* teacher_index;
+    const void* teacher_logits;
+    float* loss;
+    float* lse;
+    void* dlogits;
+    const float* dloss;
+    int64_t ldlogits, ldteacher, lddlogits;
+} hpsgd_distill_loss_args;
+int hpsgd_distill_loss(const hpsgd_distill_loss_args* args, void* stream);
+
+/* dlogits alone, where dloss comes later: lse is what the first call wrote; loss is not touched. */
+int hpsgd_distill_loss_backward(const hpsgd_distill_loss_args* args, void* stream);
+
 /*
  * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
  * since the last call, HPSGD_E_CUDA if the work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts

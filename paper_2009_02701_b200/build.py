@@ -19,6 +19,7 @@ _UNITS = {
     "hpsgd_quantize.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_gemm.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_scan.cu": ["hpsgd_ops_common.cuh"],
+    "hpsgd_loss.cu": ["hpsgd_ops_common.cuh"],
 }
 SOURCES = [os.path.join(CSRC, u) for u in _UNITS]
 # --fmad=false: the compiler never contracts a*b+c on its own; fused multiply-adds are

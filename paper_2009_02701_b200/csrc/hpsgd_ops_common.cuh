@@ -42,26 +42,34 @@ inline int launched(const char* what)
 // Launch a kernel whose blocks may be set up while the one before it on the stream still runs (programmatic dependent launch): its
 // parameters are fetched and its barriers made by the time its input is there.  Such a kernel calls after_previous() before it touches
 // global memory, in every thread that does, and that waits for the whole of the kernel before it; so nothing changes for the caller.  Between
-// two small kernels it takes 1 to 2 us off.
+// two small kernels it takes 1 to 2 us off.  The second form has blocks in clusters of `cluster` (1: no clusters).
 template <typename Kernel, typename... Args>
-inline int launch_early(const char* what, Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t s, const Args&... args)
+inline int launch_clusters(const char* what, Kernel kernel, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, const Args&... args)
 {
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr{};
+    cudaLaunchAttribute attr[2] = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return report(HPSGD_E_CUDA, "%s: launch failed: %s", what, cudaGetErrorString(e));
     }
     return launched(what);
+}
+template <typename Kernel, typename... Args>
+inline int launch_early(const char* what, Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t s, const Args&... args)
+{
+    return launch_clusters(what, kernel, grid, threads, smem, 1, s, args...);
 }
 
 __device__ __forceinline__ void after_previous()
@@ -71,6 +79,27 @@ __device__ __forceinline__ void after_previous()
 }
 
 inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// ---------------------------------------------------------------------------- powers of two and quotients
+// One instruction each: 2^x to 2^-22 of itself, 1 / x to 2^-23; subnormal results are 0.
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---------------------------------------------------------------------------- blocks of a cluster
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------- the 8-bit block format
 constexpr int kBlock = 128;

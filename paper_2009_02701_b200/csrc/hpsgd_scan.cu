@@ -145,21 +145,6 @@ __device__ __forceinline__ void store_two(__nv_bfloat16* p, pair v, int left)
     }
 }
 
-__device__ __forceinline__ float exp2_of(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float reciprocal(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-constexpr float kLog2e = 1.44269504f;
-
 // s = sigmoid(x) and 1 - s, each to a few units of its own last place: e = 2^(-x log2 e), s = 1 / (1 + e), 1 - s = e s.  e is held to 2^126, so that s
 // is not 0 where e s has to be 1; a NaN stays one.
 __device__ __forceinline__ void sigmoid(pair x, pair& s, pair& rest)
@@ -209,9 +194,6 @@ struct Map {
 };
 __device__ __forceinline__ Map identity() { return Map{both(1.f), both(0.f)}; }
 
-__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void map_to_block(const ulonglong2* at, int rank, const Map& m)
 {
     uint32_t there;
@@ -512,20 +494,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t sequences, int R)
 template <typename Kernel, typename Args>
 int launch_scan(const char* what, Kernel kernel, const Args& a, const Plan& p, cudaStream_t s)
 {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[2] = {};
-    cfg.gridDim = dim3((unsigned)(p.slabs * p.walkers * p.blocks));
-    cfg.blockDim = dim3(kScanThreads);
-    cfg.stream = s;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;          // see launch_early
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)p.blocks;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.blocks > 1 ? 2 : 1;
-    OPS_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
-    return launched(what);
+    return launch_clusters(what, kernel, dim3((unsigned)(p.slabs * p.walkers * p.blocks)), kScanThreads, 0, p.blocks, s, a);
 }
 
 template <typename T, bool GATE, bool WIDE>

@@ -22,6 +22,7 @@ __all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make
            "make_rmsnorm_forward", "hpsgd_rmsnorm_forward", "make_rmsnorm_backward", "hpsgd_rmsnorm_backward", "hpsgd_rmsnorm_backward_bytes",
            "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes",
            "make_gated_scan_forward", "hpsgd_gated_scan_forward", "make_gated_scan_backward", "hpsgd_gated_scan_backward", "hpsgd_gated_scan_saved_bytes",
+           "make_distill_loss", "hpsgd_distill_loss", "hpsgd_distill_loss_backward",
            "hpsgd_ops_check",
            "hpsgd_ops_debug_stall"]
 
@@ -69,7 +70,16 @@ class hpsgd_gated_scan_backward_args(ctypes.Structure):
         [(n, _i64) for n in ("ldf", "ldv", "ldo", "ldh0", "lddy", "lddlast", "lddf", "lddv", "lddo", "lddh0")]
 
 
+class hpsgd_distill_loss_args(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("rows", "vocab", "k")] + [(n, _f64) for n in ("temperature", "label_weight", "teacher_weight", "grad_scale")] + \
+        [("dtype", _ci), ("teacher_dtype", _ci)] + \
+        [(n, _vp) for n in ("logits", "labels", "teacher_index", "teacher_logits", "loss", "lse", "dlogits", "dloss")] + \
+        [(n, _i64) for n in ("ldlogits", "ldteacher", "lddlogits")]
+
+
 SIGNATURES = {
+    "hpsgd_distill_loss": (_ci, [_vp, _vp]),
+    "hpsgd_distill_loss_backward": (_ci, [_vp, _vp]),
     "hpsgd_gated_scan_saved_bytes": (ctypes.c_size_t, [_i64, _i64]),
     "hpsgd_gated_scan_forward": (_ci, [_vp, _vp]),
     "hpsgd_gated_scan_backward": (_ci, [_vp, _vp]),
@@ -369,6 +379,30 @@ def make_gated_scan_backward(rows, cols, sequences, dtype, f, v, saved, dy, df, 
 
 def hpsgd_gated_scan_backward(args, stream=None):
     return _b._check(_b.load().hpsgd_gated_scan_backward(args.address, _on(stream)))
+
+
+# ---- the loss --------------------------------------------------------------------------
+def make_distill_loss(rows, vocab, k, dtype, logits, labels=None, teacher_index=None, teacher_logits=None, temperature=1.0, label_weight=1.0,
+                      teacher_weight=0.0, loss=None, lse=None, dlogits=None, dloss=None, grad_scale=1.0, teacher_dtype=None, **strides):
+    """``teacher_dtype`` left out: that of the tensor given as teacher_logits (fp32 for an address)."""
+    if teacher_dtype is None:
+        teacher_dtype = _b.HPSGD_BF16 if str(getattr(teacher_logits, "dtype", "")) == "torch.bfloat16" else _b.HPSGD_F32
+    pointers = dict(logits=logits, labels=labels, teacher_index=teacher_index, teacher_logits=teacher_logits, loss=loss, lse=lse, dlogits=dlogits, dloss=dloss)
+    ld = _strides(hpsgd_distill_loss_args, strides)
+    at = {name: _matrix(name, pointers[name], dtype, rows, vocab, ld["ld" + name] or vocab) for name in ("logits", "dlogits")}
+    at.update(labels=_vector("labels", labels, _INT64, rows), loss=_vector("loss", loss, _b.HPSGD_F32, rows), dloss=_vector("dloss", dloss, _b.HPSGD_F32, rows),
+              lse=_vector("lse", lse, _b.HPSGD_F32, 2 * rows), teacher_index=_matrix("teacher_index", teacher_index, _INT32, rows, k, ld["ldteacher"] or k),
+              teacher_logits=_matrix("teacher_logits", teacher_logits, teacher_dtype, rows, k, ld["ldteacher"] or k))
+    return Args(hpsgd_distill_loss_args, pointers, at, ld, rows=rows, vocab=vocab, k=k, dtype=dtype, teacher_dtype=teacher_dtype, temperature=temperature,
+                label_weight=label_weight, teacher_weight=teacher_weight, grad_scale=grad_scale)
+
+
+def hpsgd_distill_loss(args, stream=None):
+    return _b._check(_b.load().hpsgd_distill_loss(args.address, _on(stream)))
+
+
+def hpsgd_distill_loss_backward(args, stream=None):
+    return _b._check(_b.load().hpsgd_distill_loss_backward(args.address, _on(stream)))
 
 
 def hpsgd_ops_check(stream=None):
