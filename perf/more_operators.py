@@ -229,9 +229,8 @@ def _calls(hp, case, s):
         return [(hp.hpsgd_distill_loss_backward if case["grad"] == "later" else hp.hpsgd_distill_loss, a)]
     M, N, K = case["M"], case["N"], case["K"]
     act = {"silu": hp.HPSGD_SILU, "gelu": hp.HPSGD_GELU}[case["act"]]
-    s["workspace"] = torch.zeros(hp.hpsgd_gated_ffn_forward_bytes(M, N, K), dtype=torch.uint8, device="cuda")
     calls = [(hp.hpsgd_gated_ffn_forward, hp.make_gated_ffn_forward(M, N, K, act, s["x"], s["x_scale"], s["w"], s["w_scale"], z8=s["z"], z_scale=s["z_scale"],
-                                                                    gu=s.get("gu"), workspace=s["workspace"]))]
+                                                                    gu=s.get("gu")))]
     if case["train"]:
         calls.append((hp.hpsgd_gated_ffn_backward, hp.make_gated_ffn_backward(M, N, act, s["gu"], s["dz"], hp.HPSGD_BF16, dq=s["dq"], dq_scale=s["dq_scale"],
                                                                               dqt=s["dqt"], dqt_scale=s["dqt_scale"])))
