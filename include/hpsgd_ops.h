@@ -349,8 +349,61 @@ int hpsgd_distill_loss(const hpsgd_distill_loss_args* args, void* stream);
 /* dlogits alone, where dloss comes later: lse is what the first call wrote; loss is not touched. */
 int hpsgd_distill_loss_backward(const hpsgd_distill_loss_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * The gated feed-forward layer in the 8-bit block format.
+ * ---------------------------------------------------------------------------------- */
+
 /*
- * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 ran out on this device
+ * With x [M x K] and w [2 N x K] in the block format, w's first N rows the gate's weights and the others those of what it gates:
+ *     g = x w[0..N)^T      u = x w[N..2N)^T      z = act(g) u        in binary32, z rounded once to what is stored
+ *   act        HPSGD_SILU: g sigmoid(g).   HPSGD_GELU: g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
+ *   z8, z_scale    z [M x N] in the block format (both or neither): what the projection back takes;  z: values of z_dtype (HPSGD_F32 or HPSGD_BF16).
+ *              At least one of z8, z.
+ *   gu         [M x 2 N] bf16, receives g | u rounded, for the backward pass, or NULL
+ *   ld*        as in hpsgd_quantize_fp8; ldz, ldgu: elements from row to row, 0 = N and 2 N
+ * K >= 1.  With M = 1 (one token) it streams the weights.  Products are exact and added in binary32 in an order that depends on the sizes alone; values held as the NaN
+ * code make the results they enter NaN.  The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).
+ */
+enum { HPSGD_SILU = 0, HPSGD_GELU = 1 };
+typedef struct hpsgd_gated_ffn_forward_args {
+    int64_t M, N, K;
+    int act, z_dtype;
+    const void* x;
+    const uint8_t* x_scale;
+    const void* w;
+    const uint8_t* w_scale;
+    void* z8;
+    uint8_t* z_scale;
+    void* z;
+    void* gu;
+    int64_t ldx, ldsx, ldw, ldsw, ldz8, ldsz, ldz, ldgu;
+} hpsgd_gated_ffn_forward_args;
+int hpsgd_gated_ffn_forward(const hpsgd_gated_ffn_forward_args* args, void* stream);
+
+/*
+ * What the layer's gradients are products of: with g, u as they are kept in gu,
+ *     dg = dz u act'(g)      du = dz act(g)      d = dg | du  [M x 2 N]
+ * in the block format along rows (dq) and along columns (dqt: the transpose [2 N x M]), and / or in bf16 (dgu); dx is then the product of dq and w's transpose,
+ * the gradient of w that of dqt and x's transpose.
+ *   dz         [M x N] of dz_dtype, the gradient of z (through its quantisation as if that were the identity)
+ *   dgu        not gu's memory
+ */
+typedef struct hpsgd_gated_ffn_backward_args {
+    int64_t M, N;
+    int act, dz_dtype;
+    const void* gu;
+    const void* dz;
+    void* dq;
+    uint8_t* dq_scale;
+    void* dqt;
+    uint8_t* dqt_scale;
+    void* dgu;
+    int64_t ldgu, lddz, lddq, ldsdq, lddqt, ldsdqt, lddgu;
+} hpsgd_gated_ffn_backward_args;
+int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* stream);
+
+/*
+ * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 or hpsgd_gated_ffn_forward ran out on this device
  * since the last call, HPSGD_E_CUDA if the work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts
  * along k, is left as it was, and nothing is added to it; other tiles may have been written.  Products whose parts go through the workspace
  * write nothing from such a time-out on until it has been reported here (the whole device is waited for then).

@@ -16,10 +16,11 @@ _UNITS = {
     "hpsgd_api.cu": ["hpsgd_kernels.cuh", "hpsgd_state.cuh", "hpsgd_schedule.cuh", "hpsgd_staged.cuh"],
     "hpsgd_adamw.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_rmsnorm.cu": ["hpsgd_ops_common.cuh"],
-    "hpsgd_quantize.cu": ["hpsgd_ops_common.cuh"],
-    "hpsgd_gemm.cu": ["hpsgd_ops_common.cuh"],
+    "hpsgd_quantize.cu": ["hpsgd_ops_common.cuh", "hpsgd_quantize.cuh"],
+    "hpsgd_gemm.cu": ["hpsgd_ops_common.cuh", "hpsgd_tensor_core.cuh"],
     "hpsgd_scan.cu": ["hpsgd_ops_common.cuh"],
     "hpsgd_loss.cu": ["hpsgd_ops_common.cuh"],
+    "hpsgd_ffn.cu": ["hpsgd_ops_common.cuh", "hpsgd_tensor_core.cuh", "hpsgd_quantize.cuh"],
 }
 SOURCES = [os.path.join(CSRC, u) for u in _UNITS]
 # --fmad=false: the compiler never contracts a*b+c on its own; fused multiply-adds are

@@ -1,0 +1,630 @@
+// The gated feed-forward layer on matrices in the 8-bit block format: both projections, the activation and the product in one kernel, and
+// the gradients of what they are multiplied to.
+//
+// Forward, z = act(x Wg^T) * (x Wu^T): the product of hpsgd_gemm.cu with two accumulators, whose lanes are the same 128 features: the gate's rows
+// of the weights on one, those of what it gates on the other, tokens on the columns of both.  A stage of shared memory has 128 k of both weights and of
+// the tokens, so the tokens are read once for the two.  What leaves: eight columns of both accumulators go through shared memory, so that a warp has
+// the 128 features of one token, which are a block of the result: their activation, the block's largest magnitude and its codes stay in the warp, and
+// 128 bytes of codes are written at once; the sums themselves, which the backward pass needs, in bf16.
+#include "hpsgd_quantize.cuh"
+#include "hpsgd_tensor_core.cuh"
+
+#include <algorithm>
+
+namespace hpsgd {
+namespace ops {
+
+HPSGD_HIDDEN int check_fp8(const char* what, const char* name, const void* q, const void* s, int64_t* ld, int64_t* lds, int64_t rows, int64_t cols);
+HPSGD_HIDDEN int stall_mode();
+
+namespace {
+
+constexpr int kSms = 148;
+constexpr int kFfnThreads = 384;           // copies, products, scales, one idle warp; eight warps for results
+constexpr int kChunk = 8;                  // columns that go through shared memory at a time, for each half of the eight warps
+
+__device__ unsigned int g_ffn_timeouts;    // blocks whose wait ran out since the last report
+
+// BN: tokens of a tile.
+template <int BN>
+struct FfnShape {
+    static constexpr int kStages = BN <= 64 ? 5 : 4;
+    static constexpr int kBytesW = kLanes * kStageK, kBytesX = BN * kStageK;      // of one of the weights, and of the tokens
+    static constexpr int kStageBytes = 2 * kBytesW + kBytesX;
+    static constexpr int kAccs = BN <= 64 ? 2 : 1;
+    static constexpr int kPlaces = 4;                                    // groups of scales (four k blocks) in shared memory
+    static constexpr int kBytesS = 512 * 3;                              // of one group: gate, gated, tokens
+    static constexpr int kScaleCols = 4 * 3;
+    static constexpr int kCols = kAccs * 2 * BN + (kPlaces + 1) * kScaleCols;
+    static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static constexpr int kBytesOut = 2 * 2 * kChunk * kLanes * 4;        // two halves, two sums
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kPlaces * kBytesS + kBytesOut + 256;
+};
+
+// Where a token's results go.
+struct FfnOut {
+    int N;
+    int act;
+    uint8_t* z8;
+    uint8_t* zs;
+    void* z;
+    __nv_bfloat16* gu;
+    int64_t ldz8, ldzs, ldz, ldgu;
+    int z_bf16, wide_z, wide_gu;               // wide: four neighbours may be stored at once
+};
+
+struct FfnArgs {
+    FfnOut out;
+    int M, K;
+    int tiles_n, tiles;
+    int splits, per_split, longer;             // parts along k, a part's k blocks, and how many of the first parts have one more
+    const uint32_t* sx;
+    const uint32_t* sw;
+    int64_t ldsx, ldsw;
+    uint32_t stall, stall_odd;                 // checked build, as in hpsgd_gemm.cu
+};
+
+// ---------------------------------------------------------------------------- the activation
+constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.044715f;      // 2 sqrt(2 / pi): (1 + tanh(w / 2)) / 2 = sigmoid(w)
+
+__device__ __forceinline__ float sigmoid(float x) { return reciprocal(__fadd_rn(1.f, exp2_of(__fmul_rn(x, -kLog2e)))); }
+
+__device__ __forceinline__ float activation(float g, int act)
+{
+    const float w = act == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, __fmul_rn(g, g)), g, g));
+    return __fmul_rn(g, sigmoid(w));
+}
+
+// act(g) and its derivative: with s = sigmoid(w), s + g s (1 - s) w'.
+__device__ __forceinline__ void activation(float g, int act, float& value, float& slope)
+{
+    const float g2 = __fmul_rn(g, g);
+    const float w = act == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, g2), g, g));
+    const float dw = act == HPSGD_SILU ? 1.f : __fmul_rn(kGelu1, __fmaf_rn(3.f * kGelu3, g2, 1.f));
+    const float e = exp2_of(fminf(__fmul_rn(w, -kLog2e), 126.f)), s = reciprocal(__fadd_rn(1.f, e));
+    value = __fmul_rn(g, s);
+    slope = __fmaf_rn(__fmul_rn(value, __fmul_rn(e, s)), dw, s);
+}
+
+// ---------------------------------------------------------------------------- what a warp does with a token's 128 features
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* p, const float* v, int left, int wide)
+{
+    if (wide && left >= 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) p[j] = __float2bfloat16_rn(v[j]);
+    }
+}
+
+// Lane l has the sums g, u of features n0 + 4 l .. + 3 of token m.
+__device__ __forceinline__ void finish(const FfnOut& a, int m, int n0, float4 g4, float4 u4)
+{
+    const int lane = threadIdx.x & 31, n = n0 + lane * 4, left = a.N - n;
+    const float g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+    if (a.gu) {
+        __nv_bfloat16* const p = a.gu + m * a.ldgu + n;
+        store_bf16(p, g, left, a.wide_gu);
+        store_bf16(p + a.N, u, left, a.wide_gu);
+    }
+    float z[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = j < left ? __fmul_rn(activation(g[j], a.act), u[j]) : 0.f;
+    if (a.z) {
+        if (a.z_bf16) store_bf16(static_cast<__nv_bfloat16*>(a.z) + m * a.ldz + n, z, left, a.wide_z);
+        else {
+            float* const p = static_cast<float*>(a.z) + m * a.ldz + n;
+            if (a.wide_z && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(z[0], z[1], z[2], z[3]);
+            else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < left) p[j] = z[j];
+            }
+        }
+    }
+    if (!a.z8) return;
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(fabsf(z[j])));
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (top >= 0x7F800000u) {                         // values that are not finite do not count, and become NaN
+        top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (finite(z[j])) top = max(top, __float_as_uint(fabsf(z[j])));
+            else z[j] = __uint_as_float(0x7FC00000u);
+        }
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+    }
+    const int byte = scale_byte(__uint_as_float(top));
+    const float inv = scale_inverse(byte);
+    if (n < (a.N + 15) / 16 * 16)
+        *reinterpret_cast<uint32_t*>(a.z8 + m * a.ldz8 + n) = codes4(__fmul_rn(z[0], inv), __fmul_rn(z[1], inv), __fmul_rn(z[2], inv), __fmul_rn(z[3], inv));
+    if (lane == 0) {
+        const int b = n0 / kBlock;
+        uint8_t* const s = a.zs + scale_index(b, m, a.ldzs);
+        *s = (uint8_t)byte;
+        if (b == (a.N - 1) / kBlock)                  // zeros behind the row's last block
+            for (int k = 1; (b + k) & 3; ++k) s[k] = 0;
+    }
+}
+
+// ---------------------------------------------------------------------------- the kernel
+struct FfnUnit {
+    int n0, m0, k0, k1, split;
+};
+template <int BN>
+__device__ __forceinline__ FfnUnit ffn_unit(const FfnArgs& a, int u)
+{
+    FfnUnit x;
+    const int tile = u / a.splits;
+    x.split = u % a.splits;
+    x.n0 = tile % a.tiles_n * kLanes;
+    x.m0 = tile / a.tiles_n * BN;
+    x.k0 = x.split * a.per_split + min(x.split, a.longer);
+    x.k1 = x.k0 + a.per_split + (x.split < a.longer);
+    return x;
+}
+
+// JOIN: the blocks of a cluster have a tile's parts along k, one each, and add them out of each other's shared memory in their order.
+template <int BN, bool JOIN>
+__global__ void __launch_bounds__(kFfnThreads, 1)
+    gated_ffn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ FfnArgs a)
+{
+    using S = FfnShape<BN>;
+    extern __shared__ uint8_t raw[];
+    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* const scales = smem + S::kStages * S::kStageBytes;
+    float* const out = reinterpret_cast<float*>(scales + S::kPlaces * S::kBytesS);
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(scales + S::kPlaces * S::kBytesS + S::kBytesOut);
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int given_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int first = (int)blockIdx.x, stride = (int)gridDim.x;
+    const uint32_t full = smem_address(bars), empty = full + S::kStages * 8, acc_full = empty + S::kStages * 8, acc_empty = acc_full + S::kAccs * 8,
+                   scale_full = acc_empty + S::kAccs * 8, scale_empty = scale_full + S::kPlaces * 8, drained = scale_empty + S::kPlaces * 8;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            barrier_init(full + s * 8, 1);
+            barrier_init(empty + s * 8, 1);
+        }
+        for (int s = 0; s < S::kPlaces; ++s) {
+            barrier_init(scale_full + s * 8, 1);
+            barrier_init(scale_empty + s * 8, 1);
+        }
+        for (int s = 0; s < S::kAccs; ++s) {
+            barrier_init(acc_full + s * 8, 1);
+            barrier_init(acc_empty + s * 8, 8);          // the warps that read it
+        }
+        barrier_init(drained, 1);
+        given_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (JOIN) cluster_arrive();            // given_up is there to be written by the others; waited for at the end
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    after_previous();
+    const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * 2 * BN;
+    const int units = a.tiles * a.splits;
+
+    const auto wait_one = [&](uint32_t bar, uint32_t parity) { return barrier_wait(bar, parity, &given_up); };
+    const auto wait = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, &given_up)); };
+    if (warp == 0 && elected()) {
+        int s = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const FfnUnit x = ffn_unit<BN>(a, u);
+            for (int kb = x.k0; kb < x.k1; ++kb) {
+                if (!(ok = wait_one(empty + s * 8, phase))) break;
+                const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = full + s * 8;
+#ifdef HPSGD_DEBUG
+                const uint32_t stall = a.stall_odd && !(blockIdx.x & 1) ? 0u : a.stall;
+#else
+                constexpr uint32_t stall = 0;
+#endif
+                barrier_expect(bar, S::kStageBytes + stall);
+                // (rows of the gate's box behind its last feature are the other weights'; they come to nothing)
+                tma_load<false>(dst, &map_w, kb * kStageK, x.n0, bar);
+                tma_load<false>(dst + S::kBytesW, &map_w, kb * kStageK, a.out.N + x.n0, bar);
+                tma_load<false>(dst + 2 * S::kBytesW, &map_x, kb * kStageK, x.m0, bar);
+                if (++s == S::kStages) s = 0, phase ^= 1;
+            }
+        }
+        if (!ok) {                                   // giving up: the copies in flight still land
+            const uint64_t t = nanoseconds();
+            while (nanoseconds() - t < 10000000ull) {}
+        }
+    } else if (warp == 1 && elected()) {
+        const uint64_t desc = operand_descriptor(smem_address(smem)), desc_s = scale_descriptor(smem_address(scales));
+        int s = 0, place = 0, column = 0, acc = 0;
+        uint32_t phase = 0, place_phase = 0, acc_phase = 1;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const FfnUnit x = ffn_unit<BN>(a, u);
+            if (!(ok = wait_one(acc_empty + acc * 8, acc_phase))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t sc = 0;
+            for (int kb = x.k0; kb < x.k1; ++kb) {
+                if (!(ok = wait_one(full + s * 8, phase))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (kb == x.k0 || (kb & 3) == 0) {
+                    // the next group's scales, to columns that were used kPlaces + 1 groups ago: those products are done (see hpsgd_gemm.cu)
+                    if (!(ok = wait_one(scale_full + place * 8, place_phase))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    sc = tmem_scales + column * S::kScaleCols;
+                    const uint64_t src = desc_s + (uint32_t)(place * (S::kBytesS >> 4));
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) copy_scales<false>(sc + 4 * t, src + 32 * t);
+                    commit<false>(scale_empty + place * 8);
+                    if (++column == S::kPlaces + 1) column = 0;
+                    if (++place == S::kPlaces) place = 0, place_phase ^= 1;
+                }
+                const uint64_t dg = desc + (uint32_t)(s * (S::kStageBytes >> 4)), du = dg + (uint32_t)(S::kBytesW >> 4), dx = dg + (uint32_t)(2 * S::kBytesW >> 4);
+                const uint32_t id = instruction<BN, false>(kb & 3);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    mma<false>(tmem + acc * 2 * BN, dg + 2 * k, dx + 2 * k, id, sc, sc + 8, kb > x.k0 || k > 0);
+                    mma<false>(tmem + acc * 2 * BN + BN, du + 2 * k, dx + 2 * k, id, sc + 4, sc + 8, kb > x.k0 || k > 0);
+                }
+                commit<false>(empty + s * 8);
+                if (kb + 1 == x.k1) commit<false>(acc_full + acc * 8);
+                if (++s == S::kStages) s = 0, phase ^= 1;
+            }
+            if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
+        }
+        if (!ok) {                                  // products in flight read shared memory: let them end
+            commit<false>(drained);
+            const uint64_t t = nanoseconds();
+            while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
+        }
+    } else if (warp == 2) {
+        // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.
+        uint32_t w[3][4];
+        const auto fetch = [&](const FfnUnit& x, int kb) {
+            const int64_t g = kb >> 2;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = lane + 32 * j;
+                const bool in = x.n0 + r < a.out.N;
+                w[0][j] = in ? __ldg(a.sw + g * a.ldsw + x.n0 + r) : 0u;
+                w[1][j] = in ? __ldg(a.sw + g * a.ldsw + a.out.N + x.n0 + r) : 0u;
+                w[2][j] = r < BN && x.m0 + r < a.M ? __ldg(a.sx + g * a.ldsx + x.m0 + r) : 0u;
+            }
+        };
+        int place = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int u = first; u < units && ok; u += stride) {
+            const FfnUnit x = ffn_unit<BN>(a, u);
+            for (int kb = x.k0; kb < x.k1; kb = (kb | 3) + 1) {
+                fetch(x, kb);
+                if (!(ok = wait(scale_empty + place * 8, phase))) break;
+                uint4* const dst = reinterpret_cast<uint4*>(scales + place * S::kBytesS);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(scale_full + place * 8);
+                if (++place == S::kPlaces) place = 0, phase ^= 1;
+            }
+        }
+    } else if (warp >= 4) {
+        // Two warps for each quarter of the lanes, half of the columns each.
+        constexpr int kHalf = BN / 2;
+        const int part = warp & 3, half = (warp >> 2) - 1, c0 = half * kHalf;
+        const uint32_t mine = tmem + c0 + ((uint32_t)part << 21);
+        float* const staged = out + half * (2 * kChunk * kLanes);          // [sum][column][lane]
+        // the four warps of this half
+        const auto together = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(half + 1) : "memory"); };
+        const auto all_four = [&](bool yes) {
+            uint32_t all;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(all)
+                         : "r"((uint32_t)yes), "r"(half + 1)
+                         : "memory");
+            return all != 0;
+        };
+        const auto accumulator_read = [&](int acc) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) barrier_arrive(acc_empty + acc * 8);
+        };
+        int done = 0;
+        for (int u = first; u < units; u += stride, ++done) {
+            const FfnUnit x = ffn_unit<BN>(a, u);
+            const int acc = done % S::kAccs;
+            // the four warps of a half wait for one another below, so they go on together or not at all
+            if (!all_four(wait(acc_full + acc * 8, done / S::kAccs & 1))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t src = mine + acc * 2 * BN;
+#pragma unroll 1
+            for (int c = 0; c < kHalf; c += kChunk) {
+                float g[kChunk], v[kChunk];
+                load_columns<kChunk>(src + c, g);
+                load_columns<kChunk>(src + BN + c, v);
+                loads_done<kChunk>(g);
+                loads_done<kChunk>(v);
+                if (c + kChunk == kHalf) accumulator_read(acc);
+                // [column][lane]: a part's own place where this block's stages were (its only unit's products have read them), or the room for results
+                float* const to = (JOIN ? reinterpret_cast<float*>(smem) + (c0 + c) * kLanes : staged) + part * 32 + lane;
+                constexpr int kOther = JOIN ? BN * kLanes : kChunk * kLanes;
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    to[j * kLanes] = g[j];
+                    to[j * kLanes + kOther] = v[j];
+                }
+                if constexpr (!JOIN) {
+                    together();
+#pragma unroll
+                    for (int j = 0; j < kChunk / 4; ++j) {
+                        const int col = part * (kChunk / 4) + j, m = x.m0 + c0 + c + col;
+                        const float4* const p = reinterpret_cast<const float4*>(staged + col * kLanes) + lane;
+                        if (m < a.M) finish(a.out, m, x.n0, p[0], p[kChunk * kLanes / 4]);
+                    }
+                    together();                      // before the next columns take their place
+                }
+            }
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0 && given_up) atomicAdd(&g_ffn_timeouts, 1u);
+    if constexpr (JOIN) {
+        // A block that gave up has no part, and then none of the cluster's blocks writes anything of the tile.
+        cluster_wait();
+        if (given_up && threadIdx.x < a.splits) word_to_block(smem_address(const_cast<const int*>(&given_up)), threadIdx.x, 1u);
+        __syncwarp();
+        cluster_sync();
+        const FfnUnit x = ffn_unit<BN>(a, first);
+        const int cols = given_up ? 0 : min(BN, a.M - x.m0);
+        for (int c = warp * a.splits + x.split; c < cols; c += kFfnThreads / 32 * a.splits) {
+            const uint32_t at = smem_address(smem) + (c * kLanes + lane * 4) * 4;
+            float4 g = load_from_block(at, 0), v = load_from_block(at + BN * kLanes * 4, 0);
+            for (int k = 1; k < a.splits; ++k) {
+                const float4 g1 = load_from_block(at, k), v1 = load_from_block(at + BN * kLanes * 4, k);
+                g = make_float4(__fadd_rn(g.x, g1.x), __fadd_rn(g.y, g1.y), __fadd_rn(g.z, g1.z), __fadd_rn(g.w, g1.w));
+                v = make_float4(__fadd_rn(v.x, v1.x), __fadd_rn(v.y, v1.y), __fadd_rn(v.z, v1.z), __fadd_rn(v.w, v1.w));
+            }
+            finish(a.out, x.m0 + c, x.n0, g, v);
+        }
+        __syncwarp();
+        cluster_sync();                              // this block's memory stays until the others have read it
+    }
+    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+}
+
+// ---------------------------------------------------------------------------- backward
+// dg = dz u act'(g), du = dz act(g), side by side [M x 2 N], to the block format along rows and along columns and / or to bf16.  A block takes a
+// tile of 128 x 128 of the result, which is a whole block of each of its rows and columns.
+struct FfnBackward {
+    QuantOut out;
+    int N, act;
+    const __nv_bfloat16* gu;
+    const void* dz;
+    __nv_bfloat16* dgu;
+    int64_t ldgu, lddz, lddgu;
+    int wide, wide_out;                        // eight neighbours may be loaded, stored at once
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_kernel(const FfnBackward a)
+{
+    constexpr int kRows = kPatchRows;
+    __shared__ QuantRoom room;
+    const int lane = threadIdx.x & 15, patch = threadIdx.x >> 4;
+    const int tiles_c = (int)((a.out.cols + kTile - 1) / kTile);
+    const int br = (int)(blockIdx.x / (unsigned)tiles_c), bc = (int)(blockIdx.x % (unsigned)tiles_c);
+    const int row0 = br * kTile + patch * kRows, col0 = bc * kTile + lane * 8;
+    const int left = max(0, min(8, (int)a.out.cols - col0)), rows = (int)a.out.rows - row0;
+    const T* const dz = static_cast<const T*>(a.dz);
+    after_previous();
+    f8 x[kRows];
+    const auto gradient = [&](float g, float u, float d, bool of_gate) {
+        float value, slope;
+        activation(g, a.act, value, slope);
+        return of_gate ? __fmul_rn(__fmul_rn(d, u), slope) : __fmul_rn(d, value);
+    };
+    const bool of_gate = col0 < a.N;
+    const int n = of_gate ? col0 : col0 - a.N;
+    if (a.wide && left == 8 && (!of_gate || n + 8 <= a.N)) {
+        Raw8<__nv_bfloat16> g[kRows], u[kRows];
+        Raw8<T> d[kRows];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int here = k < rows ? 8 : 0;
+            const int64_t m = row0 + k;
+            g[k].load(a.gu + m * a.ldgu + n, here == 8, here);
+            u[k].load(a.gu + m * a.ldgu + a.N + n, here == 8 && of_gate, of_gate ? here : 0);
+            d[k].load(dz + m * a.lddz + n, here == 8, here);
+        }
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const f8 gk = g[k].values(), uk = u[k].values(), dk = d[k].values();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[k].v[j] = gradient(gk.v[j], uk.v[j], dk.v[j], of_gate);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[k].v[j] = 0.f;
+                if (k < rows && j < left) {
+                    const int64_t m = row0 + k;
+                    const bool gate = col0 + j < a.N;
+                    const int c = gate ? col0 + j : col0 + j - a.N;
+                    x[k].v[j] = gradient(load1(a.gu + m * a.ldgu + c), load1(a.gu + m * a.ldgu + a.N + c), load1(dz + m * a.lddz + c), gate);
+                }
+            }
+    }
+    if (a.dgu) {
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) store_some(a.dgu + (row0 + k) * a.lddgu + col0, x[k], a.wide_out && k < rows && left == 8, k < rows ? left : 0);
+    }
+    if (a.out.q || a.out.qt) quantize_tile<true>(a.out, room, x, br, bc);
+}
+
+// ---------------------------------------------------------------------------- host side
+struct FfnPlan {
+    int bn, tiles_n, tiles, splits, per_split, longer;
+};
+
+// The least power of two that holds all tokens, 128 at most.  Few tiles are split along k over the blocks of a cluster, as in hpsgd_gemm.cu.
+FfnPlan plan_of(int64_t M, int64_t N, int64_t K)
+{
+    const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    FfnPlan p{};
+    const int blocks = (int)up(K, kStageK);
+    p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    p.tiles_n = (int)up(N, kLanes);
+    p.tiles = (int)(p.tiles_n * up(M, p.bn));
+    p.splits = 1;
+    if (p.tiles <= kSms / 2 && blocks >= 8) p.splits = p.tiles > 32 ? 2 : p.tiles > 14 || blocks < 32 ? 4 : 8;
+    p.per_split = blocks / p.splits;
+    p.longer = blocks % p.splits;
+    return p;
+}
+
+template <int BN, bool JOIN>
+int forward_launch(const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
+{
+    using S = FfnShape<BN>;
+    static bool ready[64] = {};
+    int dev = 0;
+    OPS_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !ready[dev]) {
+        OPS_CUDA(cudaFuncSetAttribute(gated_ffn_kernel<BN, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        if (dev < 64) ready[dev] = true;
+    }
+    const int64_t units = (int64_t)a.tiles * a.splits;
+    return launch_clusters("hpsgd_gated_ffn_forward", gated_ffn_kernel<BN, JOIN>, dim3((unsigned)(JOIN ? units : std::min<int64_t>(units, sms))), kFfnThreads, S::kSmem,
+                           JOIN ? a.splits : 1, s, mx, mw, a);
+}
+
+template <bool JOIN>
+int forward_shape(const FfnPlan& p, const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
+{
+    switch (p.bn) {
+    case 16: return forward_launch<16, JOIN>(mx, mw, a, sms, s);
+    case 32: return forward_launch<32, JOIN>(mx, mw, a, sms, s);
+    case 64: return forward_launch<64, JOIN>(mx, mw, a, sms, s);
+    default: return forward_launch<128, JOIN>(mx, mw, a, sms, s);
+    }
+}
+
+int check_act(const char* what, int act)
+{
+    return act == HPSGD_SILU || act == HPSGD_GELU ? HPSGD_OK : report(HPSGD_E_BADARG, "%s: unknown activation %d", what, act);
+}
+
+// Rows of a plain matrix; *wide: `unit` elements may be taken at once.
+int check_plain(const char* what, const char* name, const void* p, int64_t* ld, int64_t cols, int64_t esz, int64_t unit, bool* wide)
+{
+    if (*ld == 0) *ld = cols;
+    if (!p) return HPSGD_OK;
+    if (*ld < cols) return report(HPSGD_E_BADARG, "%s: the stride of %s is below its row's length", what, name);
+    if (!aligned(p, esz)) return report(HPSGD_E_BADARG, "%s: %s is not aligned to its elements", what, name);
+    *wide = *wide && aligned(p, unit * esz) && *ld % unit == 0;
+    return HPSGD_OK;
+}
+
+}  // namespace
+
+// Time-outs of this file's kernels since the last report, which are taken off (the device is idle).
+HPSGD_HIDDEN int take_ffn_timeouts(unsigned int* n)
+{
+    OPS_CUDA(cudaMemcpyFromSymbol(n, g_ffn_timeouts, sizeof *n));
+    if (*n == 0) return HPSGD_OK;
+    const unsigned int zero = 0;
+    OPS_CUDA(cudaMemcpyToSymbol(g_ffn_timeouts, &zero, sizeof zero));
+    return HPSGD_OK;
+}
+
+}  // namespace ops
+}  // namespace hpsgd
+
+using namespace hpsgd;
+using namespace hpsgd::ops;
+
+extern "C" {
+
+int hpsgd_gated_ffn_forward(const hpsgd_gated_ffn_forward_args* args, void* stream)
+{
+    const char* what = "hpsgd_gated_ffn_forward";
+    if (!args) return report(HPSGD_E_BADARG, "%s: args is NULL", what);
+    hpsgd_gated_ffn_forward_args p = *args;
+    if (p.M < 0 || p.N < 0 || p.K < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
+    const int64_t most = 0x7FFFFFFF - 4096;
+    if (p.M > most || p.N > most / 2 || p.K > most || ((p.N + 127) / 128) * ((p.M + 15) / 16) > most / 8) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    OPS_TRY(check_act(what, p.act));
+    if (p.z_dtype != HPSGD_F32 && p.z_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown z_dtype %d", what, p.z_dtype);
+    if (p.M == 0 || p.N == 0) return HPSGD_OK;
+    if (p.K == 0) return report(HPSGD_E_BADARG, "%s: K is 0", what);
+    if (!p.x || !p.w) return report(HPSGD_E_BADARG, "%s: x or w is NULL", what);
+    if (!p.z8 && !p.z) return report(HPSGD_E_BADARG, "%s: no output is asked for", what);
+    OPS_TRY(check_fp8(what, "x", p.x, p.x_scale, &p.ldx, &p.ldsx, p.M, p.K));
+    OPS_TRY(check_fp8(what, "w", p.w, p.w_scale, &p.ldw, &p.ldsw, 2 * p.N, p.K));
+    OPS_TRY(check_fp8(what, "z8", p.z8, p.z_scale, &p.ldz8, &p.ldsz, p.M, p.N));
+    bool wide_z = true, wide_gu = p.N % 4 == 0;
+    OPS_TRY(check_plain(what, "z", p.z, &p.ldz, p.N, p.z_dtype == HPSGD_F32 ? 4 : 2, 4, &wide_z));
+    OPS_TRY(check_plain(what, "gu", p.gu, &p.ldgu, 2 * p.N, 2, 4, &wide_gu));
+    int sms = 0;
+    OPS_TRY(device_sms(&sms));
+    const FfnPlan plan = plan_of(p.M, p.N, p.K);
+    CUtensorMap mx, mw;
+    OPS_TRY(make_map(what, &mx, p.x, p.ldx, p.M, p.K, plan.bn));
+    OPS_TRY(make_map(what, &mw, p.w, p.ldw, 2 * p.N, p.K, kLanes));
+    FfnArgs a{};
+    a.out = FfnOut{(int)p.N, p.act, static_cast<uint8_t*>(p.z8), p.z_scale, p.z, static_cast<__nv_bfloat16*>(p.gu), p.ldz8, p.ldsz, p.ldz, p.ldgu,
+                   p.z_dtype == HPSGD_BF16, wide_z, wide_gu};
+    a.M = (int)p.M; a.K = (int)p.K;
+    a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split; a.longer = plan.longer;
+    a.sx = reinterpret_cast<const uint32_t*>(p.x_scale); a.sw = reinterpret_cast<const uint32_t*>(p.w_scale);
+    a.ldsx = p.ldsx; a.ldsw = p.ldsw;
+    a.stall = stall_mode() ? 16 : 0;
+    a.stall_odd = stall_mode() == 2;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return plan.splits > 1 ? forward_shape<true>(plan, mx, mw, a, sms, s) : forward_shape<false>(plan, mx, mw, a, sms, s);
+}
+
+int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* stream)
+{
+    const char* what = "hpsgd_gated_ffn_backward";
+    if (!args) return report(HPSGD_E_BADARG, "%s: args is NULL", what);
+    hpsgd_gated_ffn_backward_args p = *args;
+    if (p.M < 0 || p.N < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
+    const int64_t most = 0x7FFFFFFF - 4096;
+    if (p.M > most || p.N > most / 2 || ((p.M + 127) / 128) * ((2 * p.N + 127) / 128) > most) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    OPS_TRY(check_act(what, p.act));
+    if (p.dz_dtype != HPSGD_F32 && p.dz_dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown dz_dtype %d", what, p.dz_dtype);
+    if (p.M == 0 || p.N == 0) return HPSGD_OK;
+    if (!p.gu || !p.dz) return report(HPSGD_E_BADARG, "%s: gu or dz is NULL", what);
+    if (!p.dq && !p.dqt && !p.dgu) return report(HPSGD_E_BADARG, "%s: no output is asked for", what);
+    if (p.dgu == p.gu) return report(HPSGD_E_BADARG, "%s: dgu is gu's memory, which is read more than once", what);
+    bool wide = p.N % 8 == 0, wide_out = true;
+    OPS_TRY(check_plain(what, "gu", p.gu, &p.ldgu, 2 * p.N, 2, 8, &wide));
+    OPS_TRY(check_plain(what, "dz", p.dz, &p.lddz, p.N, p.dz_dtype == HPSGD_F32 ? 4 : 2, 8, &wide));
+    OPS_TRY(check_plain(what, "dgu", p.dgu, &p.lddgu, 2 * p.N, 2, 8, &wide_out));
+    OPS_TRY(check_fp8(what, "dq", p.dq, p.dq_scale, &p.lddq, &p.ldsdq, p.M, 2 * p.N));
+    OPS_TRY(check_fp8(what, "dqt", p.dqt, p.dqt_scale, &p.lddqt, &p.ldsdqt, 2 * p.N, p.M));
+    int sms = 0;
+    OPS_TRY(device_sms(&sms));
+    FfnBackward a{};
+    a.out = QuantOut{p.M, 2 * p.N, p.lddq, p.ldsdq, p.lddqt, p.ldsdqt, static_cast<uint8_t*>(p.dq), p.dq_scale, static_cast<uint8_t*>(p.dqt), p.dqt_scale};
+    a.N = (int)p.N; a.act = p.act; a.gu = static_cast<const __nv_bfloat16*>(p.gu); a.dz = p.dz; a.dgu = static_cast<__nv_bfloat16*>(p.dgu);
+    a.ldgu = p.ldgu; a.lddz = p.lddz; a.lddgu = p.lddgu; a.wide = wide; a.wide_out = wide_out;
+    const dim3 grid((unsigned)(((p.M + kTile - 1) / kTile) * ((2 * p.N + kTile - 1) / kTile)));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p.dz_dtype == HPSGD_F32) return launch_early(what, gated_ffn_backward_kernel<float>, grid, kQThreads, 0, s, a);
+    return launch_early(what, gated_ffn_backward_kernel<__nv_bfloat16>, grid, kQThreads, 0, s, a);
+}
+
+}  // extern "C"

@@ -23,11 +23,13 @@ __all__ = ["HPSGD_GRAD_NORM_WORKSPACE", "HPSGD_FP8", "hpsgd_adamw_tensor", "make
            "make_quantize_fp8", "hpsgd_quantize_fp8", "make_gemm_fp8", "hpsgd_gemm_fp8", "hpsgd_gemm_fp8_bytes",
            "make_gated_scan_forward", "hpsgd_gated_scan_forward", "make_gated_scan_backward", "hpsgd_gated_scan_backward", "hpsgd_gated_scan_saved_bytes",
            "make_distill_loss", "hpsgd_distill_loss", "hpsgd_distill_loss_backward",
+           "HPSGD_SILU", "HPSGD_GELU", "make_gated_ffn_forward", "hpsgd_gated_ffn_forward", "make_gated_ffn_backward", "hpsgd_gated_ffn_backward",
            "hpsgd_ops_check",
            "hpsgd_ops_debug_stall"]
 
 HPSGD_GRAD_NORM_WORKSPACE = 65536
 HPSGD_FP8 = 2
+HPSGD_SILU, HPSGD_GELU = 0, 1
 
 
 class hpsgd_adamw_tensor(ctypes.Structure):
@@ -77,7 +79,21 @@ class hpsgd_distill_loss_args(ctypes.Structure):
         [(n, _i64) for n in ("ldlogits", "ldteacher", "lddlogits")]
 
 
+class hpsgd_gated_ffn_forward_args(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("M", "N", "K")] + [("act", _ci), ("z_dtype", _ci)] + \
+        [(n, _vp) for n in ("x", "x_scale", "w", "w_scale", "z8", "z_scale", "z", "gu")] + \
+        [(n, _i64) for n in ("ldx", "ldsx", "ldw", "ldsw", "ldz8", "ldsz", "ldz", "ldgu")]
+
+
+class hpsgd_gated_ffn_backward_args(ctypes.Structure):
+    _fields_ = [(n, _i64) for n in ("M", "N")] + [("act", _ci), ("dz_dtype", _ci)] + \
+        [(n, _vp) for n in ("gu", "dz", "dq", "dq_scale", "dqt", "dqt_scale", "dgu")] + \
+        [(n, _i64) for n in ("ldgu", "lddz", "lddq", "ldsdq", "lddqt", "ldsdqt", "lddgu")]
+
+
 SIGNATURES = {
+    "hpsgd_gated_ffn_forward": (_ci, [_vp, _vp]),
+    "hpsgd_gated_ffn_backward": (_ci, [_vp, _vp]),
     "hpsgd_distill_loss": (_ci, [_vp, _vp]),
     "hpsgd_distill_loss_backward": (_ci, [_vp, _vp]),
     "hpsgd_gated_scan_saved_bytes": (ctypes.c_size_t, [_i64, _i64]),
@@ -403,6 +419,35 @@ def hpsgd_distill_loss(args, stream=None):
 
 def hpsgd_distill_loss_backward(args, stream=None):
     return _b._check(_b.load().hpsgd_distill_loss_backward(args.address, _on(stream)))
+
+
+# ---- the gated feed-forward layer ------------------------------------------------------
+def make_gated_ffn_forward(M, N, K, act, x, x_scale, w, w_scale, z8=None, z_scale=None, z=None, z_dtype=_b.HPSGD_BF16, gu=None, **strides):
+    pointers = dict(x=x, x_scale=x_scale, w=w, w_scale=w_scale, z8=z8, z_scale=z_scale, z=z, gu=gu)
+    ld = _strides(hpsgd_gated_ffn_forward_args, strides)
+    at = dict(x=_codes("x", x, M, K, ld["ldx"], K), x_scale=_scales("x_scale", x_scale, M, K, ld["ldsx"]), w=_codes("w", w, 2 * N, K, ld["ldw"], K),
+              w_scale=_scales("w_scale", w_scale, 2 * N, K, ld["ldsw"]), z8=_codes("z8", z8, M, N, ld["ldz8"], _up(N, 16)),
+              z_scale=_scales("z_scale", z_scale, M, N, ld["ldsz"]), z=_matrix("z", z, z_dtype, M, N, ld["ldz"] or N),
+              gu=_matrix("gu", gu, _b.HPSGD_BF16, M, 2 * N, ld["ldgu"] or 2 * N))
+    return Args(hpsgd_gated_ffn_forward_args, pointers, at, ld, M=M, N=N, K=K, act=act, z_dtype=z_dtype)
+
+
+def hpsgd_gated_ffn_forward(args, stream=None):
+    return _b._check(_b.load().hpsgd_gated_ffn_forward(args.address, _on(stream)))
+
+
+def make_gated_ffn_backward(M, N, act, gu, dz, dz_dtype, dq=None, dq_scale=None, dqt=None, dqt_scale=None, dgu=None, **strides):
+    pointers = dict(gu=gu, dz=dz, dq=dq, dq_scale=dq_scale, dqt=dqt, dqt_scale=dqt_scale, dgu=dgu)
+    ld = _strides(hpsgd_gated_ffn_backward_args, strides)
+    at = dict(gu=_matrix("gu", gu, _b.HPSGD_BF16, M, 2 * N, ld["ldgu"] or 2 * N), dz=_matrix("dz", dz, dz_dtype, M, N, ld["lddz"] or N),
+              dq=_codes("dq", dq, M, 2 * N, ld["lddq"], _up(2 * N, 16)), dq_scale=_scales("dq_scale", dq_scale, M, 2 * N, ld["ldsdq"]),
+              dqt=_codes("dqt", dqt, 2 * N, M, ld["lddqt"], _up(M, 16)), dqt_scale=_scales("dqt_scale", dqt_scale, 2 * N, M, ld["ldsdqt"]),
+              dgu=_matrix("dgu", dgu, _b.HPSGD_BF16, M, 2 * N, ld["lddgu"] or 2 * N))
+    return Args(hpsgd_gated_ffn_backward_args, pointers, at, ld, M=M, N=N, act=act, dz_dtype=dz_dtype)
+
+
+def hpsgd_gated_ffn_backward(args, stream=None):
+    return _b._check(_b.load().hpsgd_gated_ffn_backward(args.address, _on(stream)))
 
 
 def hpsgd_ops_check(stream=None):
