@@ -258,7 +258,7 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
  *              of each sequence is a sequence too.  NULL: sequences of rows / sequences rows each (rows a multiple of sequences)
  *   h0         [sequences x cols], or NULL
  *   h_last     [sequences x cols], receives the state behind each sequence, or NULL; may be h0's own memory
- *   saved      hpsgd_gated_scan_saved_bytes(rows, cols) bytes for the backward pass, or NULL
+ *   saved      hpsgd_gated_scan_saved_bytes(rows, cols) bytes for the backward pass, 16-byte aligned, or NULL
  *   ld*        elements from row to row; 0 = cols.  f, v and o may lie side by side in one matrix.
  * Where cols and strides are even and addresses multiples of two elements, two channels are taken at once.
  */

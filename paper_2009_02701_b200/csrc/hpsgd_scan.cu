@@ -1,27 +1,38 @@
 // A gated linear recurrence over sequences, and its gradients.
 //
 // Per channel h_t = a_t h_(t-1) + (1 - a_t) v_t with a = sigmoid(f): an affine map of the state, and maps compose, so rows need not be gone through
-// one by one: (A, H) then (A', H') is (A' A, A' H + H').  A thread takes two neighbouring channels over a group of consecutive rows, whose
-// values it holds in registers: it composes its rows' maps, the groups' maps are exchanged, and with the state that reaches its first row it
-// goes through its rows again.  So everything is read once and written once.  A block's warps have consecutive groups, the blocks of a cluster
-// consecutive pieces of a chunk of rows, and chunks follow one another.  Sequences need no division of work of their own: the rows are one
-// long sequence, in which a map that forgets stands where one begins.
+// one by one: (A, H) then (A', H') is (A' A, A' H + H').  A thread takes two neighbouring channels over a group of consecutive rows: it composes its
+// rows' maps, the groups' maps are exchanged, and with the state that reaches its first row it goes through its rows again.  So everything is
+// read once and written once.  A block's warps have consecutive rows (each of its half warps a group of them), the blocks of a cluster consecutive
+// pieces of a chunk of rows, and chunks follow one another; a warp's next rows come to its part of shared memory meanwhile (cp.async, of
+// its own, so that no barrier is needed for them).  Sequences need no division of work of their own: the rows are one long sequence, in which a
+// map that forgets stands where one begins.
 //
 // The gradient runs the other way with the same maps: what reaches h_(t-1) is M_t = a_t (g_t + M_(t+1)).  It needs h, which is computed
 // again from the state that the forward pass keeps for each eight rows.
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
+#include <cstdlib>
+#include <cstdio>
 
 namespace hpsgd {
 namespace ops {
 namespace {
 
-constexpr int kLanes = 32, kSlab = 2 * kLanes;      // channels of a block
-constexpr int kWarps = 8, kScanThreads = 32 * kWarps;
-constexpr int kRowsF = 16, kRowsB = 8;              // rows of a thread, forward and backward
+constexpr int kSlab = 32;                           // channels of a block: two for each of 16 lanes
 constexpr int kSaved = 8;                           // rows that share a kept state
 constexpr int kMaxCluster = 8;
+
+// What a kernel holds: R rows a thread, W warps, S stages of A arrays in shared memory.  32-bit types take half the warps, for the room.
+template <typename T, int ROWS, int ARRAYS>
+struct Form {
+    static constexpr int R = ROWS, A = ARRAYS, W = sizeof(T) == 2 ? 8 : 4, S = 2;
+    static constexpr int kThreads = 32 * W, kRows = 2 * R * W;                       // rows of a block's piece of a chunk
+    static constexpr int kLine = 2 * kSlab * (int)sizeof(T);                         // a row of each half warp's group, side by side
+    static constexpr int kWarpBytes = A * R * kLine, kStageBytes = W * kWarpBytes;
+    static constexpr int kPerSm = sizeof(T) == 2 ? 2 : 3;
+};
 
 struct Sequences {
     int rows, cols, count, each;                    // each: rows of a sequence where there are no offsets
@@ -66,14 +77,17 @@ struct Share {
     }
 };
 
-// Where sequences begin and end among the rows [r0, r0 + R) of a warp: a bit for each row, and which sequence it is.
+// Where sequences begin and end among the rows [r0, r0 + R) of a warp: a bit for each row, and which sequence it is.  The last sequence seen is
+// remembered, so that rows inside of it are not looked up.
 struct Marks {
     uint32_t begins, ends;
+    int from, to;                                   // a sequence that is known
 };
 template <int R>
-__device__ __forceinline__ Marks find_marks(const Sequences& q, int r0, int (*which)[32])
+__device__ __forceinline__ void find_marks(const Sequences& q, int r0, int (*which)[32], Marks& m)
 {
-    Marks m{0u, 0u};
+    m.begins = m.ends = 0u;
+    if (m.from < r0 && m.to > r0 + R) return;
     const int lane = threadIdx.x & 31;
     __syncwarp();
     for (int k = max(0, q.at_or_behind(r0) - 1);; k += 32) {
@@ -82,69 +96,49 @@ __device__ __forceinline__ Marks find_marks(const Sequences& q, int r0, int (*wh
             if (b >= r0 && b < r0 + R) m.begins |= 1u << (b - r0), which[0][b - r0] = i;
             if (e > r0 && e <= r0 + R) m.ends |= 1u << (e - 1 - r0), which[1][e - 1 - r0] = i;
         }
+        const uint32_t wide = __ballot_sync(0xFFFFFFFFu, b < e && e - b > R);
+        if (wide) m.from = __shfl_sync(0xFFFFFFFFu, b, 31 - __clz(wide)), m.to = __shfl_sync(0xFFFFFFFFu, e, 31 - __clz(wide));
         if (!__all_sync(0xFFFFFFFFu, i < q.count && b < r0 + R)) break;
     }
     m.begins = __reduce_or_sync(0xFFFFFFFFu, m.begins);
     m.ends = __reduce_or_sync(0xFFFFFFFFu, m.ends);
     __syncwarp();
-    return m;
 }
 
 // ---------------------------------------------------------------------------- two channels
-// As they are stored.  WIDE: both in one access; else one by one, `left` of them there.
-template <typename T, bool WIDE>
-struct Two;
-template <bool WIDE>
-struct Two<float, WIDE> {
-    float2 x;
-    __device__ __forceinline__ void load(const float* p, int left)
-    {
-        if (WIDE) x = left > 0 ? *reinterpret_cast<const float2*>(p) : make_float2(0.f, 0.f);
-        else x = make_float2(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f);
-    }
-    __device__ __forceinline__ pair values() const { return make_pair(x.x, x.y); }
-};
-template <bool WIDE>
-struct Two<__nv_bfloat16, WIDE> {
-    uint32_t x;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, int left)
-    {
-        const unsigned short* const h = reinterpret_cast<const unsigned short*>(p);
-        if (WIDE) x = left > 0 ? *reinterpret_cast<const uint32_t*>(p) : 0u;
-        else x = (left > 0 ? (uint32_t)h[0] : 0u) | (left > 1 ? (uint32_t)h[1] << 16 : 0u);
-    }
-    __device__ __forceinline__ pair values() const
-    {
-        float lo, hi;
-        widen_pair(x, lo, hi);
-        return make_pair(lo, hi);
-    }
-};
-template <bool WIDE>
-__device__ __forceinline__ void store_two(float* p, pair v, int left)
+__device__ __forceinline__ pair load_two(const float* p, int left) { return make_pair(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f); }
+__device__ __forceinline__ pair load_two(const __nv_bfloat16* p, int left) { return make_pair(left > 0 ? load1(p) : 0.f, left > 1 ? load1(p + 1) : 0.f); }
+__device__ __forceinline__ pair load_pair(const float* p)
 {
-    float lo, hi;
-    split(v, lo, hi);
-    if (WIDE) {
-        if (left > 0) *reinterpret_cast<float2*>(p) = make_float2(lo, hi);
-    } else {
-        if (left > 0) p[0] = lo;
-        if (left > 1) p[1] = hi;
-    }
+    const float2 x = *reinterpret_cast<const float2*>(p);
+    return make_pair(x.x, x.y);
 }
-template <bool WIDE>
-__device__ __forceinline__ void store_two(__nv_bfloat16* p, pair v, int left)
+__device__ __forceinline__ pair load_pair(const __nv_bfloat16* p)
+{
+    float lo, hi;
+    widen_pair(*reinterpret_cast<const uint32_t*>(p), lo, hi);
+    return make_pair(lo, hi);
+}
+__device__ __forceinline__ void store_pair(float* p, float lo, float hi) { *reinterpret_cast<float2*>(p) = make_float2(lo, hi); }
+__device__ __forceinline__ void store_pair(__nv_bfloat16* p, float lo, float hi) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(lo, hi); }
+
+// WIDE: the address allows both in one access.  `left` of them are there.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store_two(T* p, pair v, int left)
 {
     float lo, hi;
     split(v, lo, hi);
-    if (WIDE) {
-        if (left > 0) *reinterpret_cast<uint32_t*>(p) = pack_bf16(lo, hi);
-    } else {
-        if (left > 0) p[0] = __float2bfloat16_rn(lo);
-        if (left > 1) p[1] = __float2bfloat16_rn(hi);
+    if (WIDE && left > 1) store_pair(p, lo, hi);
+    else {
+        if (left > 0) store1(p, lo);
+        if (left > 1) store1(p + 1, hi);
     }
 }
 
+__device__ __forceinline__ void copy_async16(uint32_t to, const void* from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
 // s = sigmoid(x) and 1 - s, each to a few units of its own last place: e = 2^(-x log2 e), s = 1 / (1 + e), 1 - s = e s.  e is held to 2^126, so that s
 // is not 0 where e s has to be 1; a NaN stays one.
 __device__ __forceinline__ void sigmoid(pair x, pair& s, pair& rest)
@@ -201,52 +195,96 @@ __device__ __forceinline__ void map_to_block(const ulonglong2* at, int rank, con
     asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(there), "l"(m.A), "l"(m.H) : "memory");
 }
 
-// What the groups' maps are exchanged through; two of each in turn, so that one barrier a chunk is enough.
+// What the maps are exchanged through; two of each in turn, so that one barrier a chunk is enough.
+template <int W>
 struct Exchange {
-    ulonglong2 group[2][kWarps][kLanes];            // of this block's warps
-    ulonglong2 block[2][kMaxCluster][kLanes];       // of the cluster's blocks
+    ulonglong2 warp[2][W][16];                      // of this block's warps
+    ulonglong2 block[2][kMaxCluster][16];           // of the cluster's blocks
 };
 
-// The state that reaches this thread's group, given the state in front of the chunk (`carry`, which becomes the one behind it).  `warp` and
+// The state that reaches this thread's group, given the state in front of the chunk (`carry`, which becomes the one behind it).  `half`, `warp` and
 // `rank` count in the direction of the recurrence.  All threads of the cluster come here.
-template <bool CLUSTER>
-__device__ __forceinline__ pair exchange(Exchange& x, int turn, const Map& mine, pair& carry, int warp, int rank, int blocks)
+template <int W, bool CLUSTER>
+__device__ __forceinline__ pair exchange(Exchange<W>& x, int turn, const Map& mine, pair& carry, int half, int warp, int rank, int blocks)
 {
-    const int lane = threadIdx.x & 31;
-    x.group[turn][warp][lane] = make_ulonglong2(mine.A, mine.H);
+    const int lane = threadIdx.x & 15;
+    const Map other{__shfl_xor_sync(0xFFFFFFFFu, mine.A, 16), __shfl_xor_sync(0xFFFFFFFFu, mine.H, 16)};
+    if (half == 1) {
+        const Map both_halves = mine.behind(other);
+        x.warp[turn][warp][lane] = make_ulonglong2(both_halves.A, both_halves.H);
+    }
     __syncthreads();
-    const auto group = [&](int w) {
-        const ulonglong2 m = x.group[turn][w][lane];
+    const auto of_warp = [&](int w) {
+        const ulonglong2 m = x.warp[turn][w][lane];
         return Map{m.x, m.y};
     };
+    pair in;
     if constexpr (!CLUSTER) {
-        pair h = carry, in = carry;
+        pair h = in = carry;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < W; ++w) {
             if (w == warp) in = h;
-            h = group(w).of(h);
+            h = of_warp(w).of(h);
         }
         carry = h;
-        return in;
     } else {
         if (warp == 0) {                            // the block's own map to all blocks
-            Map all = group(0);
+            Map all = of_warp(0);
 #pragma unroll
-            for (int w = 1; w < kWarps; ++w) all = group(w).behind(all);
-            for (int r = 0; r < blocks; ++r) map_to_block(&x.block[turn][rank][lane], r, all);
+            for (int w = 1; w < W; ++w) all = of_warp(w).behind(all);
+            for (int r = half; r < blocks; r += 2) map_to_block(&x.block[turn][rank][lane], r, all);
         }
+        __syncwarp();
         cluster_arrive();
         Map before = identity();
-        for (int w = 0; w < warp; ++w) before = group(w).behind(before);
+        for (int w = 0; w < warp; ++w) before = of_warp(w).behind(before);
         cluster_wait();
-        pair h = carry, in = carry;
+        pair h = in = carry;
         for (int r = 0; r < blocks; ++r) {
             if (r == rank) in = h;
             const ulonglong2 m = x.block[turn][r][lane];
             h = Map{m.x, m.y}.of(h);
         }
         carry = h;
-        return before.of(in);
+        in = before.of(in);
+    }
+    return half == 1 ? other.of(in) : in;
+}
+
+// ---------------------------------------------------------------------------- where a thread stands
+// Rows r .. r + R - 1 of a group.  in: those that are the walker's; begins, ends: of those, where a sequence does.
+struct Group {
+    uint32_t in, begins, ends;
+    bool plain;                                     // all rows of the warp's groups are, and nothing begins or ends
+};
+template <int R>
+__device__ __forceinline__ Group group_of(const Share& mine, const Marks& m, int warp_row, int half)
+{
+    constexpr uint32_t kAll = (1u << R) - 1u;
+    const int r = warp_row + half * R;
+    Group g;
+    g.plain = warp_row >= mine.row0 && warp_row + 2 * R <= mine.row1 && (m.begins | m.ends) == 0u;
+    const uint32_t below = r >= mine.row0 ? 0u : r + R <= mine.row0 ? kAll : (1u << (mine.row0 - r)) - 1u;
+    g.in = kAll & ~below & (r + R <= mine.row1 ? kAll : r >= mine.row1 ? 0u : (1u << (mine.row1 - r)) - 1u);
+    g.begins = m.begins >> (half * R) & g.in;
+    g.ends = m.ends >> (half * R) & g.in;
+    return g;
+}
+
+// One array's rows of a warp (two groups of R, side by side in shared memory) for stage `to`; rows that are not the walker's and columns behind the last
+// become zeros.
+template <typename T, int R>
+__device__ __forceinline__ void request_rows(uint32_t to, const T* p, int64_t ld, int warp_row, int slab, int cols, const Share& mine)
+{
+    constexpr int kLine = 2 * kSlab * (int)sizeof(T), kPieces = kLine / 16, kAtOnce = 32 / kPieces;      // rows of both groups in one instruction
+    const int lane = threadIdx.x & 31, piece = lane % kPieces, half = piece / (kPieces / 2), at = piece % (kPieces / 2);
+    const int bytes = min(16, max(0, (cols - slab * kSlab) * (int)sizeof(T) - at * 16));
+#pragma unroll
+    for (int i = 0; i < R; i += kAtOnce) {
+        const int t = i + lane / kPieces, row = warp_row + half * R + t;
+        const bool there = t < R && row >= mine.row0 && row < mine.row1 && bytes > 0;
+        const T* const from = there ? p + row * ld + slab * kSlab + at * (16 / (int)sizeof(T)) : p;
+        if (kAtOnce <= R || t < R) copy_async16(to + t * kLine + piece * 16, from, there ? bytes : 0);
     }
 }
 
@@ -261,87 +299,144 @@ struct ScanForward {
     float* h_last;
     void* y;
     float* saved;
-    int64_t ldf, ldv, ldo, ldy, ldh0, ldlast;
+    int64_t ldf, ldv, ldo, ldy, ldh0, ldlast, ldsaved;
 };
 
-__device__ __forceinline__ pair load_state(const float* p, int left) { return make_pair(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f); }
-__device__ __forceinline__ void store_state(float* p, pair h, int left)
-{
-    float lo, hi;
-    split(h, lo, hi);
-    if (left > 0) p[0] = lo;
-    if (left > 1) p[1] = hi;
-}
+template <typename T, bool GATE>
+using ForwardForm = Form<T, 16, GATE ? 3 : 2>;
 
-template <typename T, bool GATE, bool WIDE, bool CLUSTER>
-__global__ void __launch_bounds__(kScanThreads) scan_forward_kernel(const ScanForward a)
+// STAGED: rows of the inputs start on 16-byte boundaries and two outputs can be stored at once; else both are taken one by one, without a stage.
+template <typename T, bool GATE, bool STAGED, bool CLUSTER>
+__global__ void __launch_bounds__(ForwardForm<T, GATE>::kThreads, ForwardForm<T, GATE>::kPerSm) scan_forward_kernel(const ScanForward a)
 {
-    constexpr int R = kRowsF;
-    __shared__ alignas(16) Exchange ex;
-    __shared__ int which_of[kWarps][2][32];
+    using F = ForwardForm<T, GATE>;
+    constexpr int R = F::R;
+    extern __shared__ __align__(16) uint8_t stages[];
+    __shared__ alignas(16) Exchange<F::W> ex;
+    __shared__ int which_of[F::W][2][32];
     const Sequences& q = a.q;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int warp = threadIdx.x >> 5, half = (threadIdx.x >> 4) & 1, lane = threadIdx.x & 15;
     const int rank = CLUSTER ? (int)(blockIdx.x % (unsigned)a.blocks) : 0, unit = CLUSTER ? (int)(blockIdx.x / (unsigned)a.blocks) : (int)blockIdx.x;
-    const int slab = unit % a.slabs, c = slab * kSlab + lane * 2, left = min(2, q.cols - c);
+    const int slab = unit % a.slabs, c = slab * kSlab + lane * 2, left = max(0, min(2, q.cols - c));
     int(*const which)[32] = which_of[warp];
     after_previous();
     if constexpr (CLUSTER) cluster_arrive();        // the others' shared memory is there to be written; waited for below
     const Share mine(q, unit / a.slabs);
+    const int start = mine.row0 / R * R, chunk = a.blocks * F::kRows;
+    int r = start + (rank * F::W + warp) * 2 * R;   // the warp's first row
+    const T* const f = static_cast<const T*>(a.f);
+    const T* const v = static_cast<const T*>(a.v);
+    const T* const o = static_cast<const T*>(a.o);
+    T* const y = static_cast<T*>(a.y) + c;
+    const uint32_t room = shared_address(stages) + warp * F::kWarpBytes;
+    const auto request = [&](int row, int stage) {
+        if constexpr (STAGED) {
+            const uint32_t to = room + stage * F::kStageBytes;
+            if (row < mine.row1) {
+                request_rows<T, R>(to, f, a.ldf, row, slab, q.cols, mine);
+                request_rows<T, R>(to + R * F::kLine, v, a.ldv, row, slab, q.cols, mine);
+                if (GATE) request_rows<T, R>(to + 2 * R * F::kLine, o, a.ldo, row, slab, q.cols, mine);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    request(r, 0);
     // sequences without rows: their state goes through
     if (a.h_last && rank == 0)
-        for (int s = mine.first + warp; s < mine.last; s += kWarps)
-            if (q.begin(s) >= q.begin(s + 1)) store_state(a.h_last + s * a.ldlast + c, a.h0 ? load_state(a.h0 + s * a.ldh0 + c, left) : both(0.f), left);
+        for (int s = mine.first + (int)(threadIdx.x >> 4); s < mine.last; s += 2 * F::W)
+            if (q.begin(s) >= q.begin(s + 1)) store_two<false>(a.h_last + s * a.ldlast + c, a.h0 ? load_two(a.h0 + s * a.ldh0 + c, left) : both(0.f), left);
     if constexpr (CLUSTER) cluster_wait();
 
-    const T* const f = static_cast<const T*>(a.f) + c;
-    const T* const v = static_cast<const T*>(a.v) + c;
-    const T* const o = static_cast<const T*>(a.o) + c;
-    T* const y = static_cast<T*>(a.y) + c;
-    const int chunk = a.blocks * kWarps * R;
+    Marks m{0u, 0u, 0, 0};
     pair carry = both(0.f);
     int turn = 0;
-    for (int r = mine.row0 / R * R + (rank * kWarps + warp) * R, base = mine.row0 / R * R; base < mine.row1; base += chunk, r += chunk, turn ^= 1) {
-        Two<T, WIDE> fx[R], vx[R], ox[R];
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
-            const int here = r + t >= mine.row0 && r + t < mine.row1 ? left : 0;
-            fx[t].load(f + (r + t) * a.ldf, here);
-            vx[t].load(v + (r + t) * a.ldv, here);
-            if (GATE) ox[t].load(o + (r + t) * a.ldo, here);
+    for (int base = start; base < mine.row1; base += chunk, r += chunk, turn ^= 1) {
+        request(r + chunk, turn ^ 1);
+        find_marks<2 * R>(q, r, which, m);
+        const Group w = group_of<R>(mine, m, r, half);
+        if constexpr (STAGED) {
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
         }
-        const Marks m = find_marks<R>(q, r, which);
-        const uint32_t below = r >= mine.row0 ? 0u : r + R <= mine.row0 ? 0xFFFFu : (1u << (mine.row0 - r)) - 1u;
-        const uint32_t in = 0xFFFFu & ~below & (r + R <= mine.row1 ? 0xFFFFu : r >= mine.row1 ? 0u : (1u << (mine.row1 - r)) - 1u);
-        const uint32_t begins = m.begins & in, ends = m.ends & in;
+        const T* const staged = reinterpret_cast<const T*>(stages + turn * F::kStageBytes + warp * F::kWarpBytes) + half * kSlab + lane * 2;
+        const int64_t row = r + half * R;
+        const auto value = [&](int array, const T* p, int64_t ld, int t) {
+            if constexpr (STAGED) return load_pair(staged + (array * R + t) * 2 * kSlab);
+            else return load_two(p + (row + t) * ld + c, w.in >> t & 1u ? left : 0);
+        };
         pair g[R], b[R];                            // the gates, and what they let in
         Map map = identity();
+        if (w.plain) {
 #pragma unroll
-        for (int t = 0; t < R; ++t) {
-            pair rest;
-            sigmoid(fx[t].values(), g[t], rest);
-            b[t] = mul2(rest, vx[t].values());
-            if (!(in >> t & 1u)) g[t] = both(1.f), b[t] = both(0.f);
-            if (begins >> t & 1u) {
-                if (a.h0) b[t] = fma2(g[t], load_state(a.h0 + which[0][t] * a.ldh0 + c, left), b[t]);
-                map.H = b[t];
-                map.A = both(-1.f);
-            } else {
+            for (int t = 0; t < R; ++t) {
+                pair rest;
+                sigmoid(value(0, f, a.ldf, t), g[t], rest);
+                b[t] = mul2(rest, value(1, v, a.ldv, t));
                 map.H = fma2(g[t], map.H, b[t]);
-                float a0, a1;
-                split(map.A, a0, a1);
-                if (a0 != -1.f) map.A = mul2(map.A, g[t]);
+                map.A = mul2(map.A, g[t]);
+            }
+        } else {
+            bool forgets = false;
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                pair rest;
+                sigmoid(value(0, f, a.ldf, t), g[t], rest);
+                b[t] = mul2(rest, value(1, v, a.ldv, t));
+                if (!(w.in >> t & 1u)) g[t] = both(1.f), b[t] = both(0.f);
+                if (w.begins >> t & 1u) {
+                    if (a.h0) b[t] = fma2(g[t], load_two(a.h0 + which[0][half * R + t] * a.ldh0 + c, left), b[t]);
+                    map.H = b[t];
+                    forgets = true;
+                } else {
+                    map.H = fma2(g[t], map.H, b[t]);
+                    map.A = mul2(map.A, g[t]);
+                }
+            }
+            if (forgets) map.A = both(-1.f);
+            __syncwarp();
+        }
+        pair h = exchange<F::W, CLUSTER>(ex, turn, map, carry, half, warp, rank, a.blocks);
+        if (a.saved) {
+            if (w.in & 1u) store_two<true>(a.saved + row / kSaved * a.ldsaved + c, h, left);
+        }
+        if (w.plain) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                if (t == kSaved && a.saved) store_two<true>(a.saved + (row + t) / kSaved * a.ldsaved + c, h, left);
+                h = fma2(g[t], h, b[t]);
+                store_two<STAGED>(y + (row + t) * a.ldy, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, left);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                if (t == kSaved && a.saved && (w.in >> t & 1u)) store_two<true>(a.saved + (row + t) / kSaved * a.ldsaved + c, h, left);
+                h = w.begins >> t & 1u ? b[t] : fma2(g[t], h, b[t]);
+                if (w.ends >> t & 1u)
+                    if (a.h_last) store_two<false>(a.h_last + which[1][half * R + t] * a.ldlast + c, h, left);
+                if (w.in >> t & 1u) store_two<STAGED>(y + (row + t) * a.ldy, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, left);
             }
         }
-        pair h = exchange<CLUSTER>(ex, turn, map, carry, warp, rank, a.blocks);
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
-            if (t % kSaved == 0 && a.saved && (in >> t & 1u)) store_state(a.saved + (int64_t)((r + t) / kSaved) * q.cols + c, h, left);
-            h = begins >> t & 1u ? b[t] : fma2(g[t], h, b[t]);
-            if (ends >> t & 1u)
-                if (a.h_last) store_state(a.h_last + which[1][t] * a.ldlast + c, h, left);
-            if (in >> t & 1u) store_two<WIDE>(y + (r + t) * a.ldy, GATE ? mul2(h, sigmoid(ox[t].values())) : h, left);
-        }
+        __syncwarp();                               // the stage has been read, and may be filled again
     }
+}
+
+// One token for each sequence: no row depends on another.
+template <typename T, bool GATE, bool WIDE>
+__global__ void __launch_bounds__(128) scan_step_kernel(const ScanForward a)
+{
+    const int row = blockIdx.y, c = ((int)blockIdx.x * 128 + (int)threadIdx.x) * 2, left = min(2, a.q.cols - c);
+    if (left <= 0) return;
+    const T* const f = static_cast<const T*>(a.f) + row * a.ldf + c;
+    const T* const v = static_cast<const T*>(a.v) + row * a.ldv + c;
+    const T* const o = static_cast<const T*>(a.o) + row * a.ldo + c;
+    after_previous();
+    const auto load = [&](const T* p) { return WIDE && left == 2 ? load_pair(p) : load_two(p, left); };
+    const pair fx = load(f), vx = load(v), ox = GATE ? load(o) : both(0.f), h0 = a.h0 ? load_two(a.h0 + row * a.ldh0 + c, left) : both(0.f);
+    pair g, rest;
+    sigmoid(fx, g, rest);
+    const pair h = fma2(g, h0, mul2(rest, vx));
+    if (a.h_last) store_two<false>(a.h_last + row * a.ldlast + c, h, left);
+    store_two<WIDE>(static_cast<T*>(a.y) + row * a.ldy + c, GATE ? mul2(h, sigmoid(ox)) : h, left);
 }
 
 // ---------------------------------------------------------------------------- backward
@@ -359,96 +454,130 @@ struct ScanBackward {
     void* dv;
     void* d_o;
     float* dh0;
-    int64_t ldf, ldv, ldo, ldh0, lddy, lddlast, lddf, lddv, lddo, lddh0;
+    int64_t ldf, ldv, ldo, ldh0, lddy, lddlast, lddf, lddv, lddo, lddh0, ldsaved;
 };
 
-template <typename T, bool GATE, bool WIDE, bool CLUSTER>
-__global__ void __launch_bounds__(kScanThreads) scan_backward_kernel(const ScanBackward a)
+template <typename T, bool GATE>
+using BackwardForm = Form<T, kSaved, GATE ? 4 : 3>;
+
+template <typename T, bool GATE, bool STAGED, bool CLUSTER>
+__global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<T, GATE>::kPerSm) scan_backward_kernel(const ScanBackward a)
 {
-    constexpr int R = kRowsB;
-    __shared__ alignas(16) Exchange ex;
-    __shared__ int which_of[kWarps][2][32];
+    using F = BackwardForm<T, GATE>;
+    constexpr int R = F::R;
+    extern __shared__ __align__(16) uint8_t stages[];
+    __shared__ alignas(16) Exchange<F::W> ex;
+    __shared__ alignas(16) float kept[2][F::W][2 * kSlab];      // the states in front of the groups' first rows
+    __shared__ int which_of[F::W][2][32];
     const Sequences& q = a.q;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int warp = threadIdx.x >> 5, half = (threadIdx.x >> 4) & 1, lane = threadIdx.x & 15;
     const int rank = CLUSTER ? (int)(blockIdx.x % (unsigned)a.blocks) : 0, unit = CLUSTER ? (int)(blockIdx.x / (unsigned)a.blocks) : (int)blockIdx.x;
-    const int slab = unit % a.slabs, c = slab * kSlab + lane * 2, left = min(2, q.cols - c);
+    const int slab = unit % a.slabs, c = slab * kSlab + lane * 2, left = max(0, min(2, q.cols - c));
     int(*const which)[32] = which_of[warp];
     after_previous();
     if constexpr (CLUSTER) cluster_arrive();
     const Share mine(q, unit / a.slabs);
-    if (a.dh0 && rank == 0)
-        for (int s = mine.first + warp; s < mine.last; s += kWarps)
-            if (q.begin(s) >= q.begin(s + 1)) store_state(a.dh0 + s * a.lddh0 + c, a.dh_last ? load_state(a.dh_last + s * a.lddlast + c, left) : both(0.f), left);
-    if constexpr (CLUSTER) cluster_wait();
-
-    const T* const f = static_cast<const T*>(a.f) + c;
-    const T* const v = static_cast<const T*>(a.v) + c;
-    const T* const o = static_cast<const T*>(a.o) + c;
-    const T* const dy = static_cast<const T*>(a.dy) + c;
+    // chunks from the last to the first; in a chunk as well the first warp of the first block has the last rows
+    const int start = mine.row0 / R * R, chunk = a.blocks * F::kRows;
+    const int chunks = (mine.row1 - start + chunk - 1) / chunk;
+    int r = start + (chunks - 1) * chunk + ((a.blocks - 1 - rank) * F::W + (F::W - 1 - warp)) * 2 * R;
+    const T* const f = static_cast<const T*>(a.f);
+    const T* const v = static_cast<const T*>(a.v);
+    const T* const o = static_cast<const T*>(a.o);
+    const T* const dy = static_cast<const T*>(a.dy);
     T* const df = static_cast<T*>(a.df) + c;
     T* const dv = static_cast<T*>(a.dv) + c;
     T* const d_o = static_cast<T*>(a.d_o) + c;
-    const int chunk = a.blocks * kWarps * R;
-    const int start = mine.row0 / R * R;
+    const uint32_t room = shared_address(stages) + warp * F::kWarpBytes;
+    const auto request = [&](int row, int stage) {
+        if (row >= start && row < mine.row1) {
+            if constexpr (STAGED) {
+                const uint32_t to = room + stage * F::kStageBytes;
+                request_rows<T, R>(to, f, a.ldf, row, slab, q.cols, mine);
+                request_rows<T, R>(to + R * F::kLine, v, a.ldv, row, slab, q.cols, mine);
+                request_rows<T, R>(to + 2 * R * F::kLine, dy, a.lddy, row, slab, q.cols, mine);
+                if (GATE) request_rows<T, R>(to + 3 * R * F::kLine, o, a.ldo, row, slab, q.cols, mine);
+            }
+            // (the kept rows are padded to whole pieces of four)
+            const int piece = lane % 8, group = row + half * R;
+            if (lane < 8 && group < mine.row1 && slab * kSlab + piece * 4 < a.ldsaved)
+                copy_async16(shared_address(&kept[stage][warp][half * kSlab + piece * 4]), a.saved + (int64_t)(group / kSaved) * a.ldsaved + slab * kSlab + piece * 4, 16);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    request(r, 0);
+    if (a.dh0 && rank == 0)
+        for (int s = mine.first + (int)(threadIdx.x >> 4); s < mine.last; s += 2 * F::W)
+            if (q.begin(s) >= q.begin(s + 1)) store_two<false>(a.dh0 + s * a.lddh0 + c, a.dh_last ? load_two(a.dh_last + s * a.lddlast + c, left) : both(0.f), left);
+    if constexpr (CLUSTER) cluster_wait();
+
+    Marks m{0u, 0u, 0, 0};
     pair carry = both(0.f);
     int turn = 0;
-    // chunks from the last to the first; in a chunk as well the first warp of the first block has the last rows
-    for (int k = (mine.row1 - start + chunk - 1) / chunk - 1; k >= 0; --k, turn ^= 1) {
-        const int r = start + k * chunk + ((a.blocks - 1 - rank) * kWarps + (kWarps - 1 - warp)) * R;
-        Two<T, WIDE> fx[R], vx[R], ox[R], dx[R];
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
-            const int here = r + t >= mine.row0 && r + t < mine.row1 ? left : 0;
-            fx[t].load(f + (r + t) * a.ldf, here);
-            vx[t].load(v + (r + t) * a.ldv, here);
-            dx[t].load(dy + (r + t) * a.lddy, here);
-            if (GATE) ox[t].load(o + (r + t) * a.ldo, here);
-        }
-        pair h = r >= mine.row0 && r < mine.row1 ? load_state(a.saved + (int64_t)(r / kSaved) * q.cols + c, left) : both(0.f);
-        const Marks m = find_marks<R>(q, r, which);
-        const uint32_t below = r >= mine.row0 ? 0u : r + R <= mine.row0 ? 0xFFu : (1u << (mine.row0 - r)) - 1u;
-        const uint32_t in = 0xFFu & ~below & (r + R <= mine.row1 ? 0xFFu : r >= mine.row1 ? 0u : (1u << (mine.row1 - r)) - 1u);
-        const uint32_t begins = m.begins & in, ends = m.ends & in;
+    for (int k = chunks - 1; k >= 0; --k, r -= chunk, turn ^= 1) {
+        request(r - chunk, turn ^ 1);
+        find_marks<2 * R>(q, r, which, m);
+        const Group w = group_of<R>(mine, m, r, half);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        const T* const staged = reinterpret_cast<const T*>(stages + turn * F::kStageBytes + warp * F::kWarpBytes) + half * kSlab + lane * 2;
+        const int64_t row = r + half * R;
+        const auto value = [&](int array, const T* p, int64_t ld, int t) {
+            if constexpr (STAGED) return load_pair(staged + (array * R + t) * 2 * kSlab);
+            else return load_two(p + (row + t) * ld + c, w.in >> t & 1u ? left : 0);
+        };
+        pair h = w.in ? load_pair(&kept[turn][warp][half * kSlab + lane * 2]) : both(0.f);
         pair g[R], rest[R], step[R], dh[R];         // a, 1 - a, h_(t-1) - v, the gradient that reaches h_t through y
 #pragma unroll
         for (int t = 0; t < R; ++t) {
-            const pair vt = vx[t].values(), dt = dx[t].values();
-            sigmoid(fx[t].values(), g[t], rest[t]);
-            if (begins >> t & 1u) h = a.h0 ? load_state(a.h0 + which[0][t] * a.ldh0 + c, left) : both(0.f);
+            const pair vt = value(1, v, a.ldv, t), dt = value(2, dy, a.lddy, t);
+            sigmoid(value(0, f, a.ldf, t), g[t], rest[t]);
+            if (!w.plain && (w.begins >> t & 1u)) h = a.h0 ? load_two(a.h0 + which[0][half * R + t] * a.ldh0 + c, left) : both(0.f);
             step[t] = fma2(vt, both(-1.f), h);
             h = fma2(g[t], h, mul2(rest[t], vt));
             dh[t] = dt;
             if (GATE) {
                 pair s, s1;
-                sigmoid(ox[t].values(), s, s1);
+                sigmoid(value(3, o, a.ldo, t), s, s1);
                 dh[t] = mul2(dt, s);
-                if (in >> t & 1u) store_two<WIDE>(d_o + (r + t) * a.lddo, mul2(mul2(dh[t], h), s1), left);
+                if (w.in >> t & 1u) store_two<STAGED>(d_o + (row + t) * a.lddo, mul2(mul2(dh[t], h), s1), left);
             }
-            if (ends >> t & 1u)
-                if (a.dh_last) dh[t] = add2(dh[t], load_state(a.dh_last + which[1][t] * a.lddlast + c, left));
+            if (!w.plain && (w.ends >> t & 1u))
+                if (a.dh_last) dh[t] = add2(dh[t], load_two(a.dh_last + which[1][half * R + t] * a.lddlast + c, left));
         }
         // M -> a (dh + M), rows from the last to the first; nothing comes into a sequence's last row
         Map map = identity();
+        if (w.plain) {
 #pragma unroll
-        for (int t = R - 1; t >= 0; --t) {
-            const pair gt = in >> t & 1u ? g[t] : both(1.f), x = in >> t & 1u ? mul2(g[t], dh[t]) : both(0.f);
-            float a0, a1;
-            split(map.A, a0, a1);
-            if (ends >> t & 1u) map = Map{both(-1.f), x};
-            else map = Map{a0 == -1.f ? map.A : mul2(map.A, gt), fma2(gt, map.H, x)};
+            for (int t = R - 1; t >= 0; --t) {
+                map.H = mul2(g[t], add2(dh[t], map.H));
+                map.A = mul2(map.A, g[t]);
+            }
+        } else {
+            bool forgets = false;
+#pragma unroll
+            for (int t = R - 1; t >= 0; --t) {
+                if (!(w.in >> t & 1u)) continue;
+                map.H = mul2(g[t], w.ends >> t & 1u ? dh[t] : add2(dh[t], map.H));
+                map.A = mul2(map.A, g[t]);
+                forgets = forgets || (w.ends >> t & 1u);
+            }
+            if (forgets) map.A = both(-1.f);
+            __syncwarp();
         }
-        pair M = exchange<CLUSTER>(ex, turn, map, carry, warp, rank, a.blocks);
+        pair M = exchange<F::W, CLUSTER>(ex, turn, map, carry, 1 - half, warp, rank, a.blocks);
 #pragma unroll
         for (int t = R - 1; t >= 0; --t) {
-            if (!(in >> t & 1u)) continue;
-            const pair G = ends >> t & 1u ? dh[t] : add2(dh[t], M);
+            if (!w.plain && !(w.in >> t & 1u)) continue;
+            const pair G = !w.plain && (w.ends >> t & 1u) ? dh[t] : add2(dh[t], M);
             const pair p = mul2(G, rest[t]);
             M = mul2(G, g[t]);
-            store_two<WIDE>(dv + (r + t) * a.lddv, p, left);
-            store_two<WIDE>(df + (r + t) * a.lddf, mul2(mul2(p, g[t]), step[t]), left);
-            if (begins >> t & 1u)
-                if (a.dh0) store_state(a.dh0 + which[0][t] * a.lddh0 + c, M, left);
+            store_two<STAGED>(dv + (row + t) * a.lddv, p, left);
+            store_two<STAGED>(df + (row + t) * a.lddf, mul2(mul2(p, g[t]), step[t]), left);
+            if (!w.plain && (w.begins >> t & 1u))
+                if (a.dh0) store_two<false>(a.dh0 + which[0][half * R + t] * a.lddh0 + c, M, left);
         }
+        __syncwarp();
     }
 }
 
@@ -465,14 +594,14 @@ int check_sequences(const char* what, int64_t rows, int64_t cols, int64_t sequen
     return HPSGD_OK;
 }
 
-// A matrix of `rows` rows of the call's columns: its stride, its alignment, and whether two channels can be taken at once.
-int check_rows(const char* what, const char* name, const void* p, int64_t* ld, int64_t cols, int64_t esz, bool* wide)
+// A matrix of the call's columns: its stride, its alignment, and whether its rows start on `unit` bytes.
+int check_rows(const char* what, const char* name, const void* p, int64_t* ld, int64_t cols, int64_t esz, int64_t unit, bool* all)
 {
     if (*ld == 0) *ld = cols;
     if (!p) return HPSGD_OK;
     if (*ld < cols) return report(HPSGD_E_BADARG, "%s: the stride of %s is below cols", what, name);
     if (!aligned(p, esz)) return report(HPSGD_E_BADARG, "%s: %s is not aligned to its elements", what, name);
-    if (wide) *wide = *wide && aligned(p, 2 * esz) && *ld % 2 == 0;
+    if (all) *all = *all && aligned(p, unit) && *ld * esz % unit == 0;
     return HPSGD_OK;
 }
 
@@ -480,48 +609,80 @@ struct Plan {
     int slabs, walkers, blocks;
 };
 
-Plan plan_of(int64_t rows, int64_t cols, int64_t sequences, int R)
+Plan plan_of(int64_t rows, int64_t cols, int64_t sequences, bool equal, int piece)
 {
     Plan p{};
     p.slabs = (int)((cols + kSlab - 1) / kSlab);
     p.walkers = p.blocks = 1;
-    const int64_t want = 2 * 148, piece = kWarps * R;
-    while ((int64_t)p.slabs * p.blocks * 2 <= want && p.blocks < kMaxCluster && rows > piece * p.blocks) p.blocks *= 2;
-    while ((int64_t)p.slabs * p.blocks * p.walkers * 2 <= want && p.walkers * 2 <= sequences && rows > piece * p.blocks * p.walkers) p.walkers *= 2;
+    const int64_t want = 2 * 148;
+    const auto more_walkers = [&]() {
+        while ((int64_t)p.slabs * p.blocks * p.walkers * 2 <= want && p.walkers * 2 <= sequences && rows > piece * p.blocks * p.walkers) p.walkers *= 2;
+    };
+    if (equal) more_walkers();
+    while ((int64_t)p.slabs * p.walkers * p.blocks * 2 <= want && p.blocks < kMaxCluster && rows > piece * p.blocks * p.walkers) p.blocks *= 2;
+    more_walkers();
+    if (const char* e = getenv("SCAN_PLAN")) sscanf(e, "%d,%d", &p.walkers, &p.blocks);
     return p;
 }
 
-template <typename Kernel, typename Args>
-int launch_scan(const char* what, Kernel kernel, const Args& a, const Plan& p, cudaStream_t s)
+template <typename F, bool STAGED, auto kernel, typename Args>
+int launch_scan(const char* what, const Args& a, const Plan& p, cudaStream_t s)
 {
-    return launch_clusters(what, kernel, dim3((unsigned)(p.slabs * p.walkers * p.blocks)), kScanThreads, 0, p.blocks, s, a);
+    static bool ready[64] = {};
+    const size_t smem = STAGED ? F::S * F::kStageBytes : 0;
+    int dev = 0;
+    OPS_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !ready[dev]) {
+        OPS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        if (dev < 64) ready[dev] = true;
+    }
+    return launch_clusters(what, kernel, dim3((unsigned)(p.slabs * p.walkers * p.blocks)), F::kThreads, smem, p.blocks, s, a);
 }
 
-template <typename T, bool GATE, bool WIDE>
-int forward_launch(const ScanForward& a, const Plan& p, cudaStream_t s)
+template <typename T, bool GATE, bool STAGED>
+int forward_launch(ScanForward& a, bool equal, cudaStream_t s)
 {
     const char* what = "hpsgd_gated_scan_forward";
-    return p.blocks > 1 ? launch_scan(what, scan_forward_kernel<T, GATE, WIDE, true>, a, p, s) : launch_scan(what, scan_forward_kernel<T, GATE, WIDE, false>, a, p, s);
+    using F = ForwardForm<T, GATE>;
+    const Plan p = plan_of(a.q.rows, a.q.cols, a.q.count, equal, F::kRows);
+    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers;
+    return p.blocks > 1 ? launch_scan<F, STAGED, scan_forward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
+                        : launch_scan<F, STAGED, scan_forward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
+}
+template <typename T, bool GATE>
+int forward_gate(ScanForward& a, bool equal, bool staged, bool wide, cudaStream_t s)
+{
+    const char* what = "hpsgd_gated_scan_forward";
+    if (equal && a.q.rows == a.q.count && a.q.rows <= 65535) {
+        const dim3 grid((unsigned)((a.q.cols + 255) / 256), (unsigned)a.q.rows);
+        return wide ? launch_early(what, scan_step_kernel<T, GATE, true>, grid, 128, 0, s, a) : launch_early(what, scan_step_kernel<T, GATE, false>, grid, 128, 0, s, a);
+    }
+    return staged ? forward_launch<T, GATE, true>(a, equal, s) : forward_launch<T, GATE, false>(a, equal, s);
 }
 template <typename T>
-int forward_types(const ScanForward& a, const Plan& p, bool wide, cudaStream_t s)
+int forward_types(ScanForward& a, bool equal, bool staged, bool wide, cudaStream_t s)
 {
-    if (a.o) return wide ? forward_launch<T, true, true>(a, p, s) : forward_launch<T, true, false>(a, p, s);
-    return wide ? forward_launch<T, false, true>(a, p, s) : forward_launch<T, false, false>(a, p, s);
+    return a.o ? forward_gate<T, true>(a, equal, staged, wide, s) : forward_gate<T, false>(a, equal, staged, wide, s);
 }
 
-template <typename T, bool GATE, bool WIDE>
-int backward_launch(const ScanBackward& a, const Plan& p, cudaStream_t s)
+template <typename T, bool GATE, bool STAGED>
+int backward_launch(ScanBackward& a, bool equal, cudaStream_t s)
 {
     const char* what = "hpsgd_gated_scan_backward";
-    return p.blocks > 1 ? launch_scan(what, scan_backward_kernel<T, GATE, WIDE, true>, a, p, s) : launch_scan(what, scan_backward_kernel<T, GATE, WIDE, false>, a, p, s);
+    using F = BackwardForm<T, GATE>;
+    const Plan p = plan_of(a.q.rows, a.q.cols, a.q.count, equal, F::kRows);
+    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers;
+    return p.blocks > 1 ? launch_scan<F, STAGED, scan_backward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
+                        : launch_scan<F, STAGED, scan_backward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
 }
 template <typename T>
-int backward_types(const ScanBackward& a, const Plan& p, bool wide, cudaStream_t s)
+int backward_types(ScanBackward& a, bool equal, bool staged, cudaStream_t s)
 {
-    if (a.o) return wide ? backward_launch<T, true, true>(a, p, s) : backward_launch<T, true, false>(a, p, s);
-    return wide ? backward_launch<T, false, true>(a, p, s) : backward_launch<T, false, false>(a, p, s);
+    if (a.o) return staged ? backward_launch<T, true, true>(a, equal, s) : backward_launch<T, true, false>(a, equal, s);
+    return staged ? backward_launch<T, false, true>(a, equal, s) : backward_launch<T, false, false>(a, equal, s);
 }
+
+int64_t saved_stride(int64_t cols) { return (cols + 3) / 4 * 4; }
 
 }  // namespace
 }  // namespace ops
@@ -535,7 +696,7 @@ extern "C" {
 size_t hpsgd_gated_scan_saved_bytes(int64_t rows, int64_t cols)
 {
     if (rows <= 0 || cols <= 0 || rows > kMostRows || cols > 0x7FFFFFFF - 64) return 0;
-    return (size_t)((rows + kSaved - 1) / kSaved) * (size_t)cols * sizeof(float);
+    return (size_t)((rows + kSaved - 1) / kSaved) * (size_t)saved_stride(cols) * sizeof(float);
 }
 
 int hpsgd_gated_scan_forward(const hpsgd_gated_scan_forward_args* args, void* stream)
@@ -547,26 +708,29 @@ int hpsgd_gated_scan_forward(const hpsgd_gated_scan_forward_args* args, void* st
     if (p.cols == 0 || p.sequences == 0) return HPSGD_OK;
     const int64_t esz = p.dtype == HPSGD_F32 ? 4 : 2;
     if (p.rows > 0 && (!p.f || !p.v || !p.y)) return report(HPSGD_E_BADARG, "%s: f, v or y is NULL", what);
-    bool wide = p.cols % 2 == 0;
-    OPS_TRY(check_rows(what, "f", p.f, &p.ldf, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "v", p.v, &p.ldv, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "o", p.o, &p.ldo, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "y", p.y, &p.ldy, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "h0", p.h0, &p.ldh0, p.cols, 4, nullptr));
-    OPS_TRY(check_rows(what, "h_last", p.h_last, &p.ldlast, p.cols, 4, nullptr));
-    if (!aligned(p.saved, 4)) return report(HPSGD_E_BADARG, "%s: saved is not aligned to its elements", what);
+    bool staged = true, wide = true;                // rows of the inputs on 16 bytes; two elements of everything at once
+    OPS_TRY(check_rows(what, "f", p.f, &p.ldf, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "v", p.v, &p.ldv, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "o", p.o, &p.ldo, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "f", p.f, &p.ldf, p.cols, esz, 2 * esz, &wide));
+    OPS_TRY(check_rows(what, "v", p.v, &p.ldv, p.cols, esz, 2 * esz, &wide));
+    OPS_TRY(check_rows(what, "o", p.o, &p.ldo, p.cols, esz, 2 * esz, &wide));
+    OPS_TRY(check_rows(what, "y", p.y, &p.ldy, p.cols, esz, 2 * esz, &wide));
+    OPS_TRY(check_rows(what, "h0", p.h0, &p.ldh0, p.cols, 4, 4, nullptr));
+    OPS_TRY(check_rows(what, "h_last", p.h_last, &p.ldlast, p.cols, 4, 4, nullptr));
+    staged = staged && wide;
+    if (!aligned(p.saved, 16)) return report(HPSGD_E_BADARG, "%s: saved is not 16-byte aligned", what);
     if (p.h0 && p.h0 == p.h_last && p.ldh0 != p.ldlast) return report(HPSGD_E_BADARG, "%s: h0 and h_last are the same memory with different strides", what);
     if (p.rows == 0 && !p.h_last) return HPSGD_OK;
     int sms = 0;
     OPS_TRY(device_sms(&sms));
-    const Plan plan = plan_of(p.rows, p.cols, p.sequences, kRowsF);
     ScanForward a{};
-    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), plan.walkers, p.offsets};
-    a.slabs = plan.slabs; a.blocks = plan.blocks;
+    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, p.offsets};
     a.f = p.f; a.v = p.v; a.o = p.o; a.h0 = p.h0; a.h_last = p.h_last; a.y = p.y; a.saved = p.saved;
-    a.ldf = p.ldf; a.ldv = p.ldv; a.ldo = p.ldo; a.ldy = p.ldy; a.ldh0 = p.ldh0; a.ldlast = p.ldlast;
+    a.ldf = p.ldf; a.ldv = p.ldv; a.ldo = p.ldo; a.ldy = p.ldy; a.ldh0 = p.ldh0; a.ldlast = p.ldlast; a.ldsaved = saved_stride(p.cols);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return p.dtype == HPSGD_F32 ? forward_types<float>(a, plan, wide, s) : forward_types<__nv_bfloat16>(a, plan, wide, s);
+    const bool equal = !p.offsets;
+    return p.dtype == HPSGD_F32 ? forward_types<float>(a, equal, staged, wide, s) : forward_types<__nv_bfloat16>(a, equal, staged, wide, s);
 }
 
 int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* stream)
@@ -579,31 +743,30 @@ int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* 
     const int64_t esz = p.dtype == HPSGD_F32 ? 4 : 2;
     if (p.rows > 0 && (!p.f || !p.v || !p.saved || !p.dy || !p.df || !p.dv)) return report(HPSGD_E_BADARG, "%s: f, v, saved, dy, df or dv is NULL", what);
     if (!p.o != !p.d_o) return report(HPSGD_E_BADARG, "%s: o and its gradient go together", what);
-    bool wide = p.cols % 2 == 0;
-    OPS_TRY(check_rows(what, "f", p.f, &p.ldf, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "v", p.v, &p.ldv, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "o", p.o, &p.ldo, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "dy", p.dy, &p.lddy, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "df", p.df, &p.lddf, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "dv", p.dv, &p.lddv, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "do", p.d_o, &p.lddo, p.cols, esz, &wide));
-    OPS_TRY(check_rows(what, "h0", p.h0, &p.ldh0, p.cols, 4, nullptr));
-    OPS_TRY(check_rows(what, "dh_last", p.dh_last, &p.lddlast, p.cols, 4, nullptr));
-    OPS_TRY(check_rows(what, "dh0", p.dh0, &p.lddh0, p.cols, 4, nullptr));
-    if (!aligned(p.saved, 4)) return report(HPSGD_E_BADARG, "%s: saved is not aligned to its elements", what);
+    bool staged = true;                             // rows of the inputs on 16 bytes, of the results on two elements
+    OPS_TRY(check_rows(what, "f", p.f, &p.ldf, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "v", p.v, &p.ldv, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "o", p.o, &p.ldo, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "dy", p.dy, &p.lddy, p.cols, esz, 16, &staged));
+    OPS_TRY(check_rows(what, "df", p.df, &p.lddf, p.cols, esz, 2 * esz, &staged));
+    OPS_TRY(check_rows(what, "dv", p.dv, &p.lddv, p.cols, esz, 2 * esz, &staged));
+    OPS_TRY(check_rows(what, "do", p.d_o, &p.lddo, p.cols, esz, 2 * esz, &staged));
+    OPS_TRY(check_rows(what, "h0", p.h0, &p.ldh0, p.cols, 4, 4, nullptr));
+    OPS_TRY(check_rows(what, "dh_last", p.dh_last, &p.lddlast, p.cols, 4, 4, nullptr));
+    OPS_TRY(check_rows(what, "dh0", p.dh0, &p.lddh0, p.cols, 4, 4, nullptr));
+    if (!aligned(p.saved, 16)) return report(HPSGD_E_BADARG, "%s: saved is not 16-byte aligned", what);
     if (p.rows == 0 && !p.dh0) return HPSGD_OK;
     int sms = 0;
     OPS_TRY(device_sms(&sms));
-    const Plan plan = plan_of(p.rows, p.cols, p.sequences, kRowsB);
     ScanBackward a{};
-    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), plan.walkers, p.offsets};
-    a.slabs = plan.slabs; a.blocks = plan.blocks;
+    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, p.offsets};
     a.f = p.f; a.v = p.v; a.o = p.o; a.h0 = p.h0; a.saved = p.saved; a.dy = p.dy; a.dh_last = p.dh_last;
     a.df = p.df; a.dv = p.dv; a.d_o = p.d_o; a.dh0 = p.dh0;
     a.ldf = p.ldf; a.ldv = p.ldv; a.ldo = p.ldo; a.ldh0 = p.ldh0; a.lddy = p.lddy; a.lddlast = p.lddlast;
-    a.lddf = p.lddf; a.lddv = p.lddv; a.lddo = p.lddo; a.lddh0 = p.lddh0;
+    a.lddf = p.lddf; a.lddv = p.lddv; a.lddo = p.lddo; a.lddh0 = p.lddh0; a.ldsaved = saved_stride(p.cols);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return p.dtype == HPSGD_F32 ? backward_types<float>(a, plan, wide, s) : backward_types<__nv_bfloat16>(a, plan, wide, s);
+    const bool equal = !p.offsets;
+    return p.dtype == HPSGD_F32 ? backward_types<float>(a, equal, staged, s) : backward_types<__nv_bfloat16>(a, equal, staged, s);
 }
 
 }  // extern "C"
