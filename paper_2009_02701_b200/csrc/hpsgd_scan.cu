@@ -13,6 +13,7 @@
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
+#include <type_traits>
 #include <cstdlib>
 #include <cstdio>
 
@@ -122,13 +123,13 @@ __device__ __forceinline__ pair load_pair(const __nv_bfloat16* p)
 __device__ __forceinline__ void store_pair(float* p, float lo, float hi) { *reinterpret_cast<float2*>(p) = make_float2(lo, hi); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float lo, float hi) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(lo, hi); }
 
-// WIDE: the address allows both in one access.  `left` of them are there.
-template <bool WIDE, typename T>
+// WIDE: the address allows both in one access.  `left` of them are there; ALL: both are.
+template <bool WIDE, bool ALL = false, typename T>
 __device__ __forceinline__ void store_two(T* p, pair v, int left)
 {
     float lo, hi;
     split(v, lo, hi);
-    if (WIDE && left > 1) store_pair(p, lo, hi);
+    if (WIDE && (ALL || left > 1)) store_pair(p, lo, hi);
     else {
         if (left > 0) store1(p, lo);
         if (left > 1) store1(p + 1, hi);
@@ -255,15 +256,15 @@ __device__ __forceinline__ pair exchange(Exchange<W>& x, int turn, const Map& mi
 // Rows r .. r + R - 1 of a group.  in: those that are the walker's; begins, ends: of those, where a sequence does.
 struct Group {
     uint32_t in, begins, ends;
-    bool plain;                                     // all rows of the warp's groups are, and nothing begins or ends
+    bool plain;                                     // all rows of the warp's groups are, nothing begins or ends, and all of the slab's columns are there
 };
 template <int R>
-__device__ __forceinline__ Group group_of(const Share& mine, const Marks& m, int warp_row, int half)
+__device__ __forceinline__ Group group_of(const Share& mine, const Marks& m, int warp_row, int half, bool whole)
 {
     constexpr uint32_t kAll = (1u << R) - 1u;
     const int r = warp_row + half * R;
     Group g;
-    g.plain = warp_row >= mine.row0 && warp_row + 2 * R <= mine.row1 && (m.begins | m.ends) == 0u;
+    g.plain = whole && warp_row >= mine.row0 && warp_row + 2 * R <= mine.row1 && (m.begins | m.ends) == 0u;
     const uint32_t below = r >= mine.row0 ? 0u : r + R <= mine.row0 ? kAll : (1u << (mine.row0 - r)) - 1u;
     g.in = kAll & ~below & (r + R <= mine.row1 ? kAll : r >= mine.row1 ? 0u : (1u << (mine.row1 - r)) - 1u);
     g.begins = m.begins >> (half * R) & g.in;
@@ -271,22 +272,48 @@ __device__ __forceinline__ Group group_of(const Share& mine, const Marks& m, int
     return g;
 }
 
-// One array's rows of a warp (two groups of R, side by side in shared memory) for stage `to`; rows that are not the walker's and columns behind the last
-// become zeros.
+// The rows of one array that a warp requests (two groups of R, side by side in shared memory), chunk after chunk: a lane has 16 bytes of every
+// kAtOnce-th row.
 template <typename T, int R>
-__device__ __forceinline__ void request_rows(uint32_t to, const T* p, int64_t ld, int warp_row, int slab, int cols, const Share& mine)
-{
-    constexpr int kLine = 2 * kSlab * (int)sizeof(T), kPieces = kLine / 16, kAtOnce = 32 / kPieces;      // rows of both groups in one instruction
-    const int lane = threadIdx.x & 31, piece = lane % kPieces, half = piece / (kPieces / 2), at = piece % (kPieces / 2);
-    const int bytes = min(16, max(0, (cols - slab * kSlab) * (int)sizeof(T) - at * 16));
-#pragma unroll
-    for (int i = 0; i < R; i += kAtOnce) {
-        const int t = i + lane / kPieces, row = warp_row + half * R + t;
-        const bool there = t < R && row >= mine.row0 && row < mine.row1 && bytes > 0;
-        const T* const from = there ? p + row * ld + slab * kSlab + at * (16 / (int)sizeof(T)) : p;
-        if (kAtOnce <= R || t < R) copy_async16(to + t * kLine + piece * 16, from, there ? bytes : 0);
+struct Requests {
+    static constexpr int kLine = 2 * kSlab * (int)sizeof(T), kPieces = kLine / 16, kAtOnce = 32 / kPieces;      // rows of both groups in one instruction
+    const char* at;                                 // of the rows that come next
+    const void* base;
+    int64_t step, next;                             // bytes: kAtOnce rows, a chunk
+
+    __device__ __forceinline__ Requests(const T* p, int64_t ld, int warp_row, int slab, int64_t chunk)
+    {
+        const int lane = threadIdx.x & 31, piece = lane % kPieces, half = piece / (kPieces / 2);
+        base = p;
+        at = reinterpret_cast<const char*>(p) + ((warp_row + half * R + lane / kPieces) * ld + slab * kSlab) * (int)sizeof(T) + piece % (kPieces / 2) * 16;
+        step = kAtOnce * ld * (int)sizeof(T);
+        next = chunk * ld * (int)sizeof(T);
     }
-}
+    __device__ __forceinline__ void skip() { at += next; }
+    // all rows and columns are there
+    __device__ __forceinline__ void all(uint32_t to)
+    {
+        const uint32_t mine = to + (threadIdx.x & 31) * 16;
+        const char* from = at;
+#pragma unroll
+        for (int i = 0; i < R; i += kAtOnce, from += step) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + i * kLine), "l"(from) : "memory");
+        at += next;
+    }
+    // rows that are not the walker's and columns behind the last become zeros
+    __device__ __forceinline__ void some(uint32_t to, int warp_row, int slab, int cols, const Share& mine)
+    {
+        const int lane = threadIdx.x & 31, piece = lane % kPieces, half = piece / (kPieces / 2);
+        const int bytes = min(16, max(0, (cols - slab * kSlab) * (int)sizeof(T) - piece % (kPieces / 2) * 16));
+        const char* from = at;
+#pragma unroll
+        for (int i = 0; i < R; i += kAtOnce, from += step) {
+            const int row = warp_row + half * R + i + lane / kPieces;
+            const bool there = row >= mine.row0 && row < mine.row1 && bytes > 0;
+            copy_async16(to + i * kLine + lane * 16, there ? from : base, there ? bytes : 0);
+        }
+        at += next;
+    }
+};
 
 // ---------------------------------------------------------------------------- forward
 struct ScanForward {
@@ -329,13 +356,19 @@ __global__ void __launch_bounds__(ForwardForm<T, GATE>::kThreads, ForwardForm<T,
     const T* const o = static_cast<const T*>(a.o);
     T* const y = static_cast<T*>(a.y) + c;
     const uint32_t room = shared_address(stages) + warp * F::kWarpBytes;
-    const auto request = [&](int row, int stage) {
+    const bool whole = q.cols - slab * kSlab >= kSlab;
+    Requests<T, R> rf(f, a.ldf, r, slab, chunk), rv(v, a.ldv, r, slab, chunk), ro(o, a.ldo, r, slab, chunk);
+    const auto request = [&](int row, int stage) {  // (rows one chunk behind those of the last call)
         if constexpr (STAGED) {
             const uint32_t to = room + stage * F::kStageBytes;
-            if (row < mine.row1) {
-                request_rows<T, R>(to, f, a.ldf, row, slab, q.cols, mine);
-                request_rows<T, R>(to + R * F::kLine, v, a.ldv, row, slab, q.cols, mine);
-                if (GATE) request_rows<T, R>(to + 2 * R * F::kLine, o, a.ldo, row, slab, q.cols, mine);
+            if (whole && row >= mine.row0 && row + 2 * R <= mine.row1) {
+                rf.all(to);
+                rv.all(to + R * F::kLine);
+                if (GATE) ro.all(to + 2 * R * F::kLine);
+            } else if (row < mine.row1) {
+                rf.some(to, row, slab, q.cols, mine);
+                rv.some(to + R * F::kLine, row, slab, q.cols, mine);
+                if (GATE) ro.some(to + 2 * R * F::kLine, row, slab, q.cols, mine);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
@@ -353,7 +386,7 @@ __global__ void __launch_bounds__(ForwardForm<T, GATE>::kThreads, ForwardForm<T,
     for (int base = start; base < mine.row1; base += chunk, r += chunk, turn ^= 1) {
         request(r + chunk, turn ^ 1);
         find_marks<2 * R>(q, r, which, m);
-        const Group w = group_of<R>(mine, m, r, half);
+        const Group w = group_of<R>(mine, m, r, half, whole);
         if constexpr (STAGED) {
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
@@ -396,24 +429,23 @@ __global__ void __launch_bounds__(ForwardForm<T, GATE>::kThreads, ForwardForm<T,
             __syncwarp();
         }
         pair h = exchange<F::W, CLUSTER>(ex, turn, map, carry, half, warp, rank, a.blocks);
-        if (a.saved) {
-            if (w.in & 1u) store_two<true>(a.saved + row / kSaved * a.ldsaved + c, h, left);
-        }
+        float* const keep = a.saved ? a.saved + row / kSaved * a.ldsaved + c : nullptr;
+        T* to = y + row * a.ldy;
         if (w.plain) {
 #pragma unroll
-            for (int t = 0; t < R; ++t) {
-                if (t == kSaved && a.saved) store_two<true>(a.saved + (row + t) / kSaved * a.ldsaved + c, h, left);
+            for (int t = 0; t < R; ++t, to += a.ldy) {
+                if (t % kSaved == 0 && keep) store_two<true, true>(keep + t / kSaved * a.ldsaved, h, left);
                 h = fma2(g[t], h, b[t]);
-                store_two<STAGED>(y + (row + t) * a.ldy, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, left);
+                store_two<STAGED, true>(to, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, 2);
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < R; ++t) {
-                if (t == kSaved && a.saved && (w.in >> t & 1u)) store_two<true>(a.saved + (row + t) / kSaved * a.ldsaved + c, h, left);
+            for (int t = 0; t < R; ++t, to += a.ldy) {
+                if (t % kSaved == 0 && keep && (w.in >> t & 1u)) store_two<true>(keep + t / kSaved * a.ldsaved, h, left);
                 h = w.begins >> t & 1u ? b[t] : fma2(g[t], h, b[t]);
                 if (w.ends >> t & 1u)
                     if (a.h_last) store_two<false>(a.h_last + which[1][half * R + t] * a.ldlast + c, h, left);
-                if (w.in >> t & 1u) store_two<STAGED>(y + (row + t) * a.ldy, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, left);
+                if (w.in >> t & 1u) store_two<STAGED>(to, GATE ? mul2(h, sigmoid(value(2, o, a.ldo, t))) : h, left);
             }
         }
         __syncwarp();                               // the stage has been read, and may be filled again
@@ -489,20 +521,32 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<
     T* const dv = static_cast<T*>(a.dv) + c;
     T* const d_o = static_cast<T*>(a.d_o) + c;
     const uint32_t room = shared_address(stages) + warp * F::kWarpBytes;
+    const bool whole = q.cols - slab * kSlab >= kSlab;
+    Requests<T, R> rf(f, a.ldf, r, slab, -chunk), rv(v, a.ldv, r, slab, -chunk), rd(dy, a.lddy, r, slab, -chunk), ro(o, a.ldo, r, slab, -chunk);
     const auto request = [&](int row, int stage) {
-        if (row >= start && row < mine.row1) {
-            if constexpr (STAGED) {
-                const uint32_t to = room + stage * F::kStageBytes;
-                request_rows<T, R>(to, f, a.ldf, row, slab, q.cols, mine);
-                request_rows<T, R>(to + R * F::kLine, v, a.ldv, row, slab, q.cols, mine);
-                request_rows<T, R>(to + 2 * R * F::kLine, dy, a.lddy, row, slab, q.cols, mine);
-                if (GATE) request_rows<T, R>(to + 3 * R * F::kLine, o, a.ldo, row, slab, q.cols, mine);
+        if constexpr (STAGED) {
+            const uint32_t to = room + stage * F::kStageBytes;
+            if (whole && row >= mine.row0 && row + 2 * R <= mine.row1) {
+                rf.all(to);
+                rv.all(to + R * F::kLine);
+                rd.all(to + 2 * R * F::kLine);
+                if (GATE) ro.all(to + 3 * R * F::kLine);
+            } else if (row >= start && row < mine.row1) {
+                rf.some(to, row, slab, q.cols, mine);
+                rv.some(to + R * F::kLine, row, slab, q.cols, mine);
+                rd.some(to + 2 * R * F::kLine, row, slab, q.cols, mine);
+                if (GATE) ro.some(to + 3 * R * F::kLine, row, slab, q.cols, mine);
+            } else {                                // behind the last row, in the last chunk, which comes first
+                rf.skip();
+                rv.skip();
+                rd.skip();
+                ro.skip();
             }
-            // (the kept rows are padded to whole pieces of four)
-            const int piece = lane % 8, group = row + half * R;
-            if (lane < 8 && group < mine.row1 && slab * kSlab + piece * 4 < a.ldsaved)
-                copy_async16(shared_address(&kept[stage][warp][half * kSlab + piece * 4]), a.saved + (int64_t)(group / kSaved) * a.ldsaved + slab * kSlab + piece * 4, 16);
         }
+        // (the kept rows are padded to whole pieces of four)
+        const int piece = lane % 8, group = row + half * R;
+        if (lane < 8 && row >= start && group < mine.row1 && slab * kSlab + piece * 4 < a.ldsaved)
+            copy_async16(shared_address(&kept[stage][warp][half * kSlab + piece * 4]), a.saved + (int64_t)(group / kSaved) * a.ldsaved + slab * kSlab + piece * 4, 16);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     request(r, 0);
@@ -517,7 +561,7 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<
     for (int k = chunks - 1; k >= 0; --k, r -= chunk, turn ^= 1) {
         request(r - chunk, turn ^ 1);
         find_marks<2 * R>(q, r, which, m);
-        const Group w = group_of<R>(mine, m, r, half);
+        const Group w = group_of<R>(mine, m, r, half, whole);
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
         const T* const staged = reinterpret_cast<const T*>(stages + turn * F::kStageBytes + warp * F::kWarpBytes) + half * kSlab + lane * 2;
@@ -528,32 +572,40 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<
         };
         pair h = w.in ? load_pair(&kept[turn][warp][half * kSlab + lane * 2]) : both(0.f);
         pair g[R], rest[R], step[R], dh[R];         // a, 1 - a, h_(t-1) - v, the gradient that reaches h_t through y
+        const auto gather = [&](auto tag) {
+            constexpr bool plain = decltype(tag)::value;
+            T* to = d_o + row * a.lddo;
 #pragma unroll
-        for (int t = 0; t < R; ++t) {
-            const pair vt = value(1, v, a.ldv, t), dt = value(2, dy, a.lddy, t);
-            sigmoid(value(0, f, a.ldf, t), g[t], rest[t]);
-            if (!w.plain && (w.begins >> t & 1u)) h = a.h0 ? load_two(a.h0 + which[0][half * R + t] * a.ldh0 + c, left) : both(0.f);
-            step[t] = fma2(vt, both(-1.f), h);
-            h = fma2(g[t], h, mul2(rest[t], vt));
-            dh[t] = dt;
-            if (GATE) {
-                pair s, s1;
-                sigmoid(value(3, o, a.ldo, t), s, s1);
-                dh[t] = mul2(dt, s);
-                if (w.in >> t & 1u) store_two<STAGED>(d_o + (row + t) * a.lddo, mul2(mul2(dh[t], h), s1), left);
+            for (int t = 0; t < R; ++t, to += a.lddo) {
+                const pair vt = value(1, v, a.ldv, t), dt = value(2, dy, a.lddy, t);
+                sigmoid(value(0, f, a.ldf, t), g[t], rest[t]);
+                if constexpr (!plain)
+                    if (w.begins >> t & 1u) h = a.h0 ? load_two(a.h0 + which[0][half * R + t] * a.ldh0 + c, left) : both(0.f);
+                step[t] = fma2(vt, both(-1.f), h);
+                h = fma2(g[t], h, mul2(rest[t], vt));
+                dh[t] = dt;
+                if (GATE) {
+                    pair s, s1;
+                    sigmoid(value(3, o, a.ldo, t), s, s1);
+                    dh[t] = mul2(dt, s);
+                    if (plain || (w.in >> t & 1u)) store_two<STAGED, plain>(to, mul2(mul2(dh[t], h), s1), left);
+                }
+                if constexpr (!plain)
+                    if (w.ends >> t & 1u)
+                        if (a.dh_last) dh[t] = add2(dh[t], load_two(a.dh_last + which[1][half * R + t] * a.lddlast + c, left));
             }
-            if (!w.plain && (w.ends >> t & 1u))
-                if (a.dh_last) dh[t] = add2(dh[t], load_two(a.dh_last + which[1][half * R + t] * a.lddlast + c, left));
-        }
+        };
         // M -> a (dh + M), rows from the last to the first; nothing comes into a sequence's last row
         Map map = identity();
         if (w.plain) {
+            gather(std::true_type{});
 #pragma unroll
             for (int t = R - 1; t >= 0; --t) {
                 map.H = mul2(g[t], add2(dh[t], map.H));
                 map.A = mul2(map.A, g[t]);
             }
         } else {
+            gather(std::false_type{});
             bool forgets = false;
 #pragma unroll
             for (int t = R - 1; t >= 0; --t) {
@@ -566,16 +618,27 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<
             __syncwarp();
         }
         pair M = exchange<F::W, CLUSTER>(ex, turn, map, carry, 1 - half, warp, rank, a.blocks);
+        T* to_v = dv + (row + R - 1) * a.lddv;
+        T* to_f = df + (row + R - 1) * a.lddf;
+        if (w.plain) {
 #pragma unroll
-        for (int t = R - 1; t >= 0; --t) {
-            if (!w.plain && !(w.in >> t & 1u)) continue;
-            const pair G = !w.plain && (w.ends >> t & 1u) ? dh[t] : add2(dh[t], M);
-            const pair p = mul2(G, rest[t]);
-            M = mul2(G, g[t]);
-            store_two<STAGED>(dv + (row + t) * a.lddv, p, left);
-            store_two<STAGED>(df + (row + t) * a.lddf, mul2(mul2(p, g[t]), step[t]), left);
-            if (!w.plain && (w.begins >> t & 1u))
-                if (a.dh0) store_two<false>(a.dh0 + which[0][half * R + t] * a.lddh0 + c, M, left);
+            for (int t = R - 1; t >= 0; --t, to_v -= a.lddv, to_f -= a.lddf) {
+                const pair G = add2(dh[t], M), p = mul2(G, rest[t]);
+                M = mul2(G, g[t]);
+                store_two<STAGED, true>(to_v, p, 2);
+                store_two<STAGED, true>(to_f, mul2(mul2(p, g[t]), step[t]), 2);
+            }
+        } else {
+#pragma unroll
+            for (int t = R - 1; t >= 0; --t, to_v -= a.lddv, to_f -= a.lddf) {
+                if (!(w.in >> t & 1u)) continue;
+                const pair G = w.ends >> t & 1u ? dh[t] : add2(dh[t], M), p = mul2(G, rest[t]);
+                M = mul2(G, g[t]);
+                store_two<STAGED>(to_v, p, left);
+                store_two<STAGED>(to_f, mul2(mul2(p, g[t]), step[t]), left);
+                if (w.begins >> t & 1u)
+                    if (a.dh0) store_two<false>(a.dh0 + which[0][half * R + t] * a.lddh0 + c, M, left);
+            }
         }
         __syncwarp();
     }
