@@ -1,13 +1,17 @@
 // The loss over a label and a teacher's top logits, and its gradient.
 //
 // Bound by HBM: a row of logits is read once and a row of gradients written once.  A row is held in the registers of one block, or of the
-// blocks of a cluster where it is longer than 16384 (8192 in fp32): all of it is requested at once, its sums of exponentials are joined over warps
-// and blocks, and what is in the registers then becomes the gradient.  Only rows beyond eight times that are read a second time, out of L2.
+// blocks of a cluster where it is longer: all of it is requested at once, its sums of exponentials are joined over warps and blocks, and what is in
+// the registers then becomes the gradient.  Only rows longer than eight blocks hold are read a second time, out of L2.
 //
 // Sums of exponentials: s = sum 2^(x c - k) with c = log2(e) / temperature and k the largest x c rounded up to a whole number, so that joining two
 // sums multiplies by an exact power of two, and x c - k is rounded once; the softmax is then 2^(x c - k) / s without any error of k's.
+//
+// Powers of two are what the SM does least of (16 a clock; two for each element are three quarters of the time that its bytes take).  With a label and a
+// teacher there are two temperatures, and four of them; where the teacher's is 2, 3 or 4, e^z is that power of e^(z / T), by multiplying.
 #include "hpsgd_ops_common.cuh"
 
+#include <algorithm>
 #include <cfloat>
 
 namespace hpsgd {
@@ -16,9 +20,11 @@ namespace {
 
 constexpr int kMaxTeacher = 1024;
 constexpr int kMaxLossCluster = 8;
+constexpr int kLossSms = 148;
 
 struct LossArgs {
     int rows, vocab, k, pieces, piece;              // pieces: blocks that share a row; piece: columns of each
+    int ahead;                                      // rows between a block's and the one that takes its place
     const void* z;
     const int64_t* labels;
     const int32_t* index;
@@ -29,10 +35,9 @@ struct LossArgs {
     const float* dloss;
     const void* z_end;
     int64_t ldz, ldt, lddz;
-    float c1, c2;                                   // log2(e) over the temperatures; c2 is only used where there are two
+    float c1, c2;                                   // log2(e) over the temperatures; c2, the teacher's, is only used where there are two
     float ct, wl, wt, temperature, scale;           // wt: with the square of the temperature
     int teacher_bf16;
-    int later;                                      // the gradient alone, from lse
     int main_is_teacher;                            // c1 is the teacher's temperature
 };
 
@@ -49,16 +54,22 @@ __device__ __forceinline__ Sum nothing() { return Sum{-FLT_MAX, 0.f}; }
 __device__ __forceinline__ float log2_of(const Sum& x) { return __fadd_rn(x.k, log2f(x.s)); }
 
 // Over the lanes of a warp; every lane has the result.
+__device__ __forceinline__ float top_of_lanes(float x)
+{
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float sum_of_lanes(float x)
+{
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) x = __fadd_rn(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
+    return x;
+}
 __device__ __forceinline__ Sum join_lanes(Sum x)
 {
-    float top = x.k;
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    x.s = __fmul_rn(x.s, exp2_of(x.k - top));
-    x.k = top;
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) x.s = __fadd_rn(x.s, __shfl_xor_sync(0xFFFFFFFFu, x.s, d));
-    return x;
+    const float top = top_of_lanes(x.k);
+    return Sum{top, sum_of_lanes(__fmul_rn(x.s, exp2_of(x.k - top)))};
 }
 
 struct Stats {
@@ -70,44 +81,90 @@ __device__ __forceinline__ float teacher_logit(const LossArgs& a, int64_t at)
     return a.teacher_bf16 ? load1(static_cast<const __nv_bfloat16*>(a.teacher) + at) : load1(static_cast<const float*>(a.teacher) + at);
 }
 
-// THREADS threads with NV groups of eight columns each (a tile); TWO: two temperatures; WIDE: rows allow the wide accesses.
-template <typename T, int THREADS, int NV, bool TWO, bool WIDE, bool CLUSTER>
+__device__ __forceinline__ pair exp2_pair(pair x)
+{
+    float lo, hi;
+    split(x, lo, hi);
+    return make_pair(exp2_of(lo), exp2_of(hi));
+}
+template <int N>
+__device__ __forceinline__ pair power(pair e)
+{
+    const pair e2 = mul2(e, e);
+    return N == 2 ? e2 : N == 3 ? mul2(e2, e) : mul2(e2, e2);
+}
+
+// How many temperatures there are: one; two, each with its own powers; or two of which the first's are the N-th powers of the second's.
+constexpr int kOne = 0, kTwo = 1;
+
+// The gradient before what is taken off at the label and the teacher's entries: A softmax(z) + B softmax(z / T), with the sums in A and B.
+template <int MODE>
+struct Softmax {
+    float c1, k1, c2, k2, A, B;
+    __device__ __forceinline__ pair operator()(pair x) const
+    {
+        if constexpr (MODE == kOne) return mul2(both(A), exp2_pair(fma2(x, both(c1), both(-k1))));
+        else {
+            const pair e = exp2_pair(fma2(x, both(c2), both(-k2)));
+            const pair f = MODE == kTwo ? exp2_pair(fma2(x, both(c1), both(-k1))) : power<MODE>(e);
+            return fma2(both(A), f, mul2(both(B), e));
+        }
+    }
+};
+
+// THREADS threads with NV groups of eight columns each (a tile).  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
+// are counted from the boundary in front of the row; else groups begin at column 0 and are taken piece by piece.  LATER: the gradient alone, from lse.
+template <typename T, int THREADS, int NV, int MODE, bool SHIFT, bool CLUSTER, bool LATER>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const LossArgs a)
 {
     constexpr int kWarpsHere = THREADS / 32, kTileCols = THREADS * NV * 8;
-    extern __shared__ float room[];                 // of each teacher entry, and of the label behind them: index, probability, its logit, the student's
+    constexpr bool kSecond = MODE != kOne;
+    extern __shared__ __align__(16) float room[];   // of each teacher entry, and of the label behind them: index, probability, its logit, the student's, seen twice
     __shared__ Stats of_warp[kWarpsHere];
     __shared__ alignas(8) Stats of_block[kMaxLossCluster];
     __shared__ float part[kWarpsHere];
-    const int k = a.k;
+    const int k = a.k, stride = (k + 4) / 4 * 4;
     int* const index = reinterpret_cast<int*>(room);
-    float* const p = room + (k + 1);
-    float* const t_of = p + (k + 1);
-    float* const z_of = t_of + (k + 1);
+    float* const p = room + stride;
+    float* const t_of = p + stride;
+    float* const z_of = t_of + stride;
+    uint8_t* const twice = reinterpret_cast<uint8_t*>(z_of + stride);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rank = CLUSTER ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
-    const int64_t row = CLUSTER ? blockIdx.x / (unsigned)a.pieces : blockIdx.x;
+    const int rank = CLUSTER || LATER ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
+    const int64_t row = CLUSTER || LATER ? blockIdx.x / (unsigned)a.pieces : blockIdx.x;
     const T* const z = static_cast<const T*>(a.z) + row * a.ldz;
-    const int first = rank * a.piece, cols = min(a.piece, a.vocab - first);      // this block's columns
-    if constexpr (CLUSTER) cluster_arrive();        // the others' memory is there to be written; waited for below
+    const int shift = SHIFT ? (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T) % 8) : 0;
+    const int first = rank * a.piece - shift, last = min(a.vocab, first + a.piece);      // this block's columns, from max(0, first)
+    if constexpr (CLUSTER && !LATER) cluster_arrive();      // the others' memory is there to be written; waited for below
     after_previous();
 
     Raw8<T> x[NV];
+    const auto column = [&](int tile, int v) { return first + tile + (v * THREADS + (int)threadIdx.x) * 8; };
     const auto request = [&](int tile) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = tile + (v * THREADS + (int)threadIdx.x) * 8, left = max(0, min(8, cols - c));
-            if constexpr (WIDE) x[v].load(z + first + c, left == 8, left);
-            else x[v].load(z + first + c, left, a.z, a.z_end);
+            const int c = column(tile, v), left = max(0, min(8, last - c));
+            // what is not a column is -infinity, and adds nothing
+            if (SHIFT ? c >= 0 && left == 8 : left == 8) {
+                if constexpr (SHIFT) x[v].load(z + c, true, 8);
+                else x[v].load(z + c, 8, a.z, a.z_end);
+            } else x[v].load_part(z + c, max(0, -c), left);
         }
     };
     request(0);
+    if (row + a.ahead < a.rows) {                   // the row that comes next here, to L2
+        const char* const next = reinterpret_cast<const char*>(z + a.ahead * a.ldz + max(0, first));
+        const int bytes = (last - max(0, first)) * (int)sizeof(T);
+#pragma unroll 1
+        for (int i = threadIdx.x * 128; i < bytes; i += THREADS * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(next + i));
+    }
     // the label and the teacher's entries meanwhile; an index outside the vocabulary makes the row NaN
     const int64_t label64 = a.labels ? a.labels[row] : -1;
     const bool has_label = label64 >= 0;
     const int label = has_label ? (int)min(label64, (int64_t)0x7FFFFFFF) : -1;
     bool wrong = label >= a.vocab;
     Stats mine{nothing(), nothing(), nothing()};
+#pragma unroll 1
     for (int j = threadIdx.x; j <= k; j += THREADS) {
         int i = j < k ? a.index[row * a.ldt + j] : label;
         float t = -INFINITY;
@@ -121,173 +178,228 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
             mine.teacher.add(kt, exp2_of(__fmaf_rn(t, a.ct, -kt)));
         }
     }
+    if (k > 0) {                                    // entries that share their index with another are rare, and known before they are needed
+        __syncthreads();
+#pragma unroll 1
+        for (int j = threadIdx.x; j <= k; j += THREADS) {
+            int same = 0;
+            const int i = index[j];
+#pragma unroll 1
+            for (int m = 0; m < k; m += 4) {
+                const int4 four = *reinterpret_cast<const int4*>(index + m);
+                same += (four.x == i) + (m + 1 < k && four.y == i) + (m + 2 < k && four.z == i) + (m + 3 < k && four.w == i);
+            }
+            twice[j] = same > (j < k ? 1 : 0);
+        }
+    }
 
-    if (!a.later) {
-        for (int tile = 0; tile < cols; tile += kTileCols) {
+    if constexpr (!LATER) {
+#pragma unroll 1
+        for (int tile = 0; tile < last - first; tile += kTileCols) {
             if (tile > 0) request(tile);
-            float top = -INFINITY;
-            f8 y[NV];
+            float top = x[0].top();
+#pragma unroll
+            for (int v = 1; v < NV; ++v) top = fmaxf(top, x[v].top());
+            top = top_of_lanes(top);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) x[v].keep();
+            // sums with a whole warp's k
+            const float kb = fmaxf(kSecond ? mine.two.k : mine.one.k, ceilf(__fmul_rn(top, kSecond ? a.c2 : a.c1)));
+            const float kf = MODE == kTwo ? fmaxf(mine.one.k, ceilf(__fmul_rn(top, a.c1))) : MODE == kOne ? kb : fmaxf(kb * MODE, -FLT_MAX);
+            const pair cb = both(kSecond ? a.c2 : a.c1), minus_kb = both(-kb), cf = both(a.c1), minus_kf = both(-kf);
+            pair sb = both(0.f), sf = both(0.f);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int left = cols - tile - (v * THREADS + (int)threadIdx.x) * 8;
-                y[v] = x[v].values();
+                const p4 y = to_pairs(x[v].values());
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (q >= left) y[v].v[q] = -INFINITY;
-                    top = fmaxf(top, y[v].v[q]);
+                for (int q = 0; q < 4; ++q) {
+                    const pair e = exp2_pair(fma2(y.v[q], cb, minus_kb));
+                    sb = add2(sb, e);
+                    if constexpr (MODE == kTwo) sf = add2(sf, exp2_pair(fma2(y.v[q], cf, minus_kf)));
+                    if constexpr (MODE > kTwo) sf = add2(sf, power<MODE>(e));
                 }
             }
-            const auto sum = [&](Sum& into, float c) {
-                const float kk = fmaxf(into.k, ceilf(__fmul_rn(top, c)));
-                float s = __fmul_rn(into.s, exp2_of(into.k - kk));
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) s = __fadd_rn(s, exp2_of(__fmaf_rn(y[v].v[q], c, -kk)));
-                into = Sum{kk, s};
-            };
-            sum(mine.one, a.c1);
-            if (TWO) sum(mine.two, a.c2);
+            float lo, hi;
+            split(sb, lo, hi);
+            Sum& base = kSecond ? mine.two : mine.one;
+            base = Sum{kb, __fmaf_rn(base.s, exp2_of(base.k - kb), __fadd_rn(lo, hi))};
+            if (kSecond) {
+                split(sf, lo, hi);
+                mine.one = Sum{kf, __fmaf_rn(mine.one.s, exp2_of(mine.one.k - kf), __fadd_rn(lo, hi))};
+            }
         }
     }
     if (wrong) mine.one.s = mine.two.s = mine.teacher.s = __uint_as_float(0x7FC00000u);
-    Stats all{join_lanes(mine.one), TWO ? join_lanes(mine.two) : nothing(), k > 0 ? join_lanes(mine.teacher) : nothing()};
+    Stats all;
+    all.one = Sum{LATER ? 0.f : mine.one.k, sum_of_lanes(mine.one.s)};      // (a warp has one k)
+    all.two = kSecond ? Sum{mine.two.k, sum_of_lanes(mine.two.s)} : nothing();
+    all.teacher = warp * 32 <= k ? join_lanes(mine.teacher) : nothing();
     if (lane == 0) of_warp[warp] = all;
     __syncthreads();
-    if (!CLUSTER || warp == 0) {
+    if (!CLUSTER || LATER || warp == 0) {
         const bool has = lane < kWarpsHere;
         const Stats w = of_warp[has ? lane : 0];
-        all = Stats{join_lanes(has ? w.one : nothing()), TWO ? join_lanes(has ? w.two : nothing()) : nothing(), join_lanes(has ? w.teacher : nothing())};
+        all.one = join_lanes(has ? w.one : nothing());
+        if (kSecond) all.two = join_lanes(has ? w.two : nothing());
+        all.teacher = join_lanes(has ? w.teacher : nothing());
     }
-    if constexpr (CLUSTER) {
+    if constexpr (CLUSTER && !LATER) {
         cluster_wait();
-        if (warp == 0 && lane < a.pieces) {
-            uint32_t there;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(shared_address(&of_block[rank])), "r"(lane));
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(all.one.k), "f"(all.one.s) : "memory");
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 8), "f"(all.two.k), "f"(all.two.s) : "memory");
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 16), "f"(all.teacher.k), "f"(all.teacher.s) : "memory");
+        if (warp == 0) {
+            if (lane < a.pieces) {
+                uint32_t there;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(shared_address(&of_block[rank])), "r"(lane));
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(all.one.k), "f"(all.one.s) : "memory");
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 8), "f"(all.two.k), "f"(all.two.s) : "memory");
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 16), "f"(all.teacher.k), "f"(all.teacher.s) : "memory");
+            }
+            asm volatile("fence.acq_rel.cluster;" ::: "memory");      // (only this warp has something to publish)
         }
         __syncwarp();
-        cluster_arrive();
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         cluster_wait();
         all = of_block[0];                          // (every block has the whole teacher)
+#pragma unroll 1
         for (int r = 1; r < a.pieces; ++r) {
             const Stats s = of_block[r];
             all.one.add(s.one.k, s.one.s);
-            if (TWO) all.two.add(s.two.k, s.two.s);
-            if (s.teacher.s != s.teacher.s) all.teacher.s = s.teacher.s;
+            if (kSecond) all.two.add(s.two.k, s.two.s);
         }
     }
 
     const bool has_teacher = k > 0 && !(all.teacher.s == 0.f);
-    if (a.later) {                                  // (no sums so far, but NaN where an index is wrong)
+    if constexpr (LATER) {                          // (no sums so far, but NaN where an index is wrong)
         const float l0 = a.lse[2 * row], l1 = a.lse[2 * row + 1], one = all.one.s != all.one.s ? all.one.s : 1.f;
         all.one = Sum{__fmul_rn(a.main_is_teacher ? l1 : l0, kLog2e), one};
-        if (TWO) all.two = Sum{__fmul_rn(l1, kLog2e), one};
+        if (kSecond) all.two = Sum{__fmul_rn(l1, kLog2e), one};
     }
-    const Sum& of_teacher = TWO ? all.two : all.one;      // the student's sum at the teacher's temperature
-    const float c_teacher = TWO ? a.c2 : a.c1;
+    const Sum& of_teacher = kSecond ? all.two : all.one;      // the student's sum at the teacher's temperature
+    const float c_teacher = kSecond ? a.c2 : a.c1;
 
     // the teacher's probabilities, and the loss
-    float sum = 0.f;
-    if (has_teacher || has_label) {
-        const float log_t = has_teacher ? log2f(all.teacher.s) : 0.f, log_s = log2f(of_teacher.s);
+    if (warp * 32 <= k) {
+        float sum = 0.f;
+        const float log_t = has_teacher ? log2f(all.teacher.s) : 0.f, log_s = LATER ? 0.f : log2f(of_teacher.s);
+#pragma unroll 1
         for (int j = threadIdx.x; j <= k; j += THREADS) {
             float pj = 0.f;
             if (j < k && t_of[j] != -INFINITY) {
                 const float u = __fmaf_rn(t_of[j], a.ct, -all.teacher.k);
                 pj = __fdividef(exp2_of(u), all.teacher.s);
-                const float kl = __fadd_rn(u - log_t, -(__fmaf_rn(z_of[j], c_teacher, -of_teacher.k) - log_s));
-                if (pj != 0.f) sum = __fmaf_rn(__fmul_rn(pj, a.wt), kl, sum);
-            } else if (j == k && has_label) {
+                if constexpr (!LATER) {
+                    const float kl = __fadd_rn(u - log_t, -(__fmaf_rn(z_of[j], c_teacher, -of_teacher.k) - log_s));
+                    if (pj != 0.f) sum = __fmaf_rn(__fmul_rn(pj, a.wt), kl, sum);
+                }
+            } else if (!LATER && j == k && has_label) {
                 sum = __fmaf_rn(a.wl, log2f(all.one.s) - __fmaf_rn(z_of[k], a.c1, -all.one.k), sum);
             }
             p[j] = pj;
         }
-        if (wrong) sum = __uint_as_float(0x7FC00000u);
+        if constexpr (!LATER) {
+            if (wrong) sum = __uint_as_float(0x7FC00000u);
+            if (a.loss) {
+                sum = sum_of_lanes(sum);
+                if (lane == 0) part[warp] = sum;
+            }
+        }
     }
-    if (a.loss && !a.later) {
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, d));
-        if (lane == 0) part[warp] = sum;
-    }
-    if (a.lse && !a.later && rank == 0 && threadIdx.x == 0) {
-        const float one = __fmul_rn(log2_of(all.one), 0.69314718f), two = TWO ? __fmul_rn(log2_of(all.two), 0.69314718f) : one;
+    if (!LATER && a.lse && rank == 0 && threadIdx.x == 0) {
+        const float one = __fmul_rn(log2_of(all.one), 0.69314718f), two = kSecond ? __fmul_rn(log2_of(all.two), 0.69314718f) : one;
         a.lse[2 * row] = one;
         a.lse[2 * row + 1] = two;
     }
-    __syncthreads();
-    if (a.loss && !a.later && rank == 0 && threadIdx.x == 0) {
-        float s = part[0];
-        for (int w = 1; w < kWarpsHere; ++w) s = __fadd_rn(s, part[w]);
-        a.loss[row] = __fmul_rn(s, 0.69314718f);
-    }
-    if (!a.dz) return;
 
     // the gradient
-    const float g = __fmul_rn(a.dloss ? a.dloss[row] : 1.f, a.scale);
-    const float on_label = has_label ? __fmul_rn(g, a.wl) : 0.f, on_teacher = has_teacher ? __fmul_rn(g, __fdividef(a.wt, a.temperature)) : 0.f;
-    const float A = on_label == 0.f && (TWO || on_teacher == 0.f) ? 0.f : __fdividef(TWO ? on_label : __fadd_rn(on_label, on_teacher), all.one.s);
-    const float B = TWO && on_teacher != 0.f ? __fdividef(on_teacher, all.two.s) : 0.f;
-    const bool none = on_label == 0.f && on_teacher == 0.f;
-    const auto softmax = [&](float y) {
-        float d = __fmul_rn(A, exp2_of(__fmaf_rn(y, a.c1, -all.one.k)));
-        if (TWO) d = __fmaf_rn(B, exp2_of(__fmaf_rn(y, a.c2, -all.two.k)), d);
-        return none ? 0.f : d;
-    };
-    T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
-    for (int tile = 0; tile < cols; tile += kTileCols) {
-        if (cols > kTileCols) request(tile);
+    float on_label = 0.f, on_teacher = 0.f;
+    Softmax<MODE> softmax;
+    bool none = true;
+    if (a.dz) {
+        const float g = __fmul_rn(a.dloss ? a.dloss[row] : 1.f, a.scale);
+        on_label = has_label ? __fmul_rn(g, a.wl) : 0.f;
+        on_teacher = has_teacher ? __fmul_rn(g, __fdividef(a.wt, a.temperature)) : 0.f;
+        const float main = kSecond ? on_label : __fadd_rn(on_label, on_teacher);
+        softmax = Softmax<MODE>{a.c1, all.one.k, a.c2, all.two.k, main != 0.f ? __fdividef(main, all.one.s) : 0.f, kSecond && on_teacher != 0.f ? __fdividef(on_teacher, all.two.s) : 0.f};
+        none = on_label == 0.f && on_teacher == 0.f;
+        T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
+#pragma unroll 1
+        for (int tile = 0; tile < last - first; tile += kTileCols) {
+            if (last - first > kTileCols) request(tile);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = tile + (v * THREADS + (int)threadIdx.x) * 8, left = max(0, min(8, cols - c));
-            f8 d = x[v].values();
+            for (int v = 0; v < NV; ++v) x[v].keep();
 #pragma unroll
-            for (int q = 0; q < 8; ++q) d.v[q] = softmax(d.v[q]);
-            if constexpr (WIDE) store_some(dz + first + c, d, left == 8, left);
-            else if (left > 0) store_unaligned(dz + first + c, d, left);
+            for (int v = 0; v < NV; ++v) {
+                const int c = column(tile, v), left = max(0, min(8, last - c));
+                p4 y = to_pairs(x[v].values());
+#pragma unroll
+                for (int q = 0; q < 4; ++q) y.v[q] = none ? both(0.f) : softmax(y.v[q]);
+                const f8 d = to_values(y);
+                if constexpr (SHIFT) {
+                    if (c >= 0 && left == 8) store8(dz + c, d);
+                    else store_part(dz + c, d, max(0, -c), left);
+                } else if (left > 0) store_unaligned(dz + c, d, left);
+            }
         }
     }
     // and what is taken off at the label and the teacher's entries; the same index twice is one element, written with the same value
     __syncthreads();
+    if (!LATER && a.loss && rank == 0 && threadIdx.x == 0) {
+        float s = part[0];
+#pragma unroll 1
+        for (int w = 1; w < kWarpsHere && w * 32 <= k; ++w) s = __fadd_rn(s, part[w]);
+        a.loss[row] = __fmul_rn(s, 0.69314718f);
+    }
     if (none) return;
+    T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
+#pragma unroll 1
     for (int j = threadIdx.x; j <= k; j += THREADS) {
         const int i = index[j];
-        if (i < first || i >= first + cols) continue;
-        float off = i == label ? on_label : 0.f, sum_p = 0.f;
-        for (int m = 0; m < k; ++m)
-            if (index[m] == i) sum_p = __fadd_rn(sum_p, p[m]);
-        store1(dz + i, __fadd_rn(softmax(z_of[j]), -__fmaf_rn(on_teacher, sum_p, off)));
+        if (i < max(0, first) || i >= last) continue;
+        float off = i == label ? on_label : 0.f, sum_p = p[j];
+        if (k > 0 && twice[j]) {
+            sum_p = 0.f;
+#pragma unroll 1
+            for (int m = 0; m < k; ++m)
+                if (index[m] == i) sum_p = __fadd_rn(sum_p, p[m]);
+        }
+        float lo, hi;
+        split(softmax(both(z_of[j])), lo, hi);
+        store1(dz + i, __fadd_rn(lo, -__fmaf_rn(on_teacher, sum_p, off)));
     }
 }
 
-template <typename T, int THREADS, int NV, bool CLUSTER>
-int loss_launch(const char* what, const LossArgs& a, bool two, bool wide, cudaStream_t s)
+template <typename T, int THREADS, int NV, bool CLUSTER, bool LATER>
+int loss_launch(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t s)
 {
     const dim3 grid((unsigned)((int64_t)a.rows * a.pieces));
-    const size_t smem = (size_t)(a.k + 1) * 16;
-    const auto go = [&](auto kernel) { return launch_clusters(what, kernel, grid, THREADS, smem, a.pieces, s, a); };
-    if (two) return wide ? go(loss_kernel<T, THREADS, NV, true, true, CLUSTER>) : go(loss_kernel<T, THREADS, NV, true, false, CLUSTER>);
-    return wide ? go(loss_kernel<T, THREADS, NV, false, true, CLUSTER>) : go(loss_kernel<T, THREADS, NV, false, false, CLUSTER>);
+    const size_t smem = (size_t)((a.k + 4) / 4 * 4) * 17;
+    a.ahead = std::max(1, kLossSms * (1024 / THREADS) / a.pieces);
+    const auto go = [&](auto kernel) { return launch_clusters(what, kernel, grid, THREADS, smem, CLUSTER && !LATER ? a.pieces : 1, s, a); };
+    if (mode == kOne) return shift ? go(loss_kernel<T, THREADS, NV, kOne, true, CLUSTER, LATER>) : go(loss_kernel<T, THREADS, NV, kOne, false, CLUSTER, LATER>);
+    if constexpr (!LATER) {
+        if (shift && mode == 2) return go(loss_kernel<T, THREADS, NV, 2, true, CLUSTER, LATER>);
+        if (shift && mode == 3) return go(loss_kernel<T, THREADS, NV, 3, true, CLUSTER, LATER>);
+        if (shift && mode == 4) return go(loss_kernel<T, THREADS, NV, 4, true, CLUSTER, LATER>);
+    }
+    return shift ? go(loss_kernel<T, THREADS, NV, kTwo, true, CLUSTER, LATER>) : go(loss_kernel<T, THREADS, NV, kTwo, false, CLUSTER, LATER>);
 }
 
-template <typename T>
-int loss_types(const char* what, LossArgs& a, bool two, bool wide, cudaStream_t s)
+template <typename T, bool LATER>
+int loss_types(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t s)
 {
-    const auto up8 = [](int64_t x) { return (int)((x + 7) / 8 * 8); };
-    a.pieces = 1;
-    a.piece = up8(a.vocab);
     constexpr int kMost = sizeof(T) == 4 ? 2 : 4;    // groups of eight that a thread holds
-    if (a.vocab <= 1024) return loss_launch<T, 128, 1, false>(what, a, two, wide, s);
-    if (a.vocab <= 4096) return loss_launch<T, 512, 1, false>(what, a, two, wide, s);
-    if (a.vocab <= 8192) return loss_launch<T, 512, 2, false>(what, a, two, wide, s);
-    if (kMost == 4 && a.vocab <= 16384) return loss_launch<T, 512, kMost, false>(what, a, two, wide, s);
+    const auto up8 = [](int64_t x) { return (int)((x + 7) / 8 * 8); };
+    const int64_t cols = (int64_t)a.vocab + (shift ? 7 : 0);      // counted from the boundary in front of the row
+    a.pieces = 1;
+    a.piece = up8(cols);
+    if (cols <= 1024) return loss_launch<T, 128, 1, false, LATER>(what, a, mode, shift, s);
+    if (cols <= 4096) return loss_launch<T, 512, 1, false, LATER>(what, a, mode, shift, s);
+    if (cols <= 8192) return loss_launch<T, 512, 2, false, LATER>(what, a, mode, shift, s);
+    if (kMost == 4 && cols <= 16384) return loss_launch<T, 512, kMost, false, LATER>(what, a, mode, shift, s);
     while (a.pieces < kMaxLossCluster && a.piece > kMost * 4096) {
         a.pieces *= 2;
-        a.piece = up8((a.vocab + a.pieces - 1) / a.pieces);
+        a.piece = up8((cols + a.pieces - 1) / a.pieces);
     }
-    return loss_launch<T, 512, kMost, true>(what, a, two, wide, s);
+    return loss_launch<T, 512, kMost, true, LATER>(what, a, mode, shift, s);
 }
 
 int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, void* stream)
@@ -336,11 +448,13 @@ int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, 
     a.wl = (float)p.label_weight; a.wt = (float)(p.teacher_weight * p.temperature * p.temperature);
     a.temperature = (float)p.temperature; a.scale = (float)p.grad_scale;
     a.teacher_bf16 = p.teacher_dtype == HPSGD_BF16;
-    a.later = later;
-    bool wide = aligned(p.logits, unit) && p.ldlogits * esz % unit == 0;
-    if (p.dlogits) wide = wide && aligned(p.dlogits, unit) && p.lddlogits * esz % unit == 0;
+    // rows of both lie alike to the wide boundaries
+    const bool shift = !p.dlogits || ((reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % unit == 0 && (p.ldlogits - p.lddlogits) * esz % unit == 0);
+    const bool whole = p.temperature == 2.0 || p.temperature == 3.0 || p.temperature == 4.0;
+    const int mode = !two ? kOne : whole && !later ? (int)p.temperature : kTwo;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return p.dtype == HPSGD_F32 ? loss_types<float>(what, a, two, wide, s) : loss_types<__nv_bfloat16>(what, a, two, wide, s);
+    if (later) return p.dtype == HPSGD_F32 ? loss_types<float, true>(what, a, mode, shift, s) : loss_types<__nv_bfloat16, true>(what, a, mode, shift, s);
+    return p.dtype == HPSGD_F32 ? loss_types<float, false>(what, a, mode, shift, s) : loss_types<__nv_bfloat16, false>(what, a, mode, shift, s);
 }
 
 }  // namespace

@@ -205,6 +205,19 @@ __device__ __forceinline__ void store_some(T* p, const f8& x, bool wide, int lef
         if (q < left) store1(p + q, x.v[q]);
 }
 
+// Elements from..to - 1 of eight, value by value, in short code: for the few groups that a row begins or ends in.
+template <typename T>
+__device__ __forceinline__ void store_part(T* p, const f8& x, int from, int to)
+{
+#pragma unroll 1
+    for (int q = from; q < to; ++q) {
+        float y = x.v[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) y = i == q ? x.v[i] : y;
+        store1(p + q, y);
+    }
+}
+
 // And for rows that do not allow the wide access: in the widest units that the address does.
 __device__ __forceinline__ void store_unaligned(float* p, const f8& x, int left)
 {
@@ -342,7 +355,7 @@ struct Raw8;
 template <>
 struct Raw8<float> {
     f8 x;
-    __device__ __forceinline__ void load(const float* p, bool wide, int left) { x = load_some(p, wide, left); }
+    __device__ __forceinline__ void load(const float* p, bool wide, int left) { x = ops::load_some(p, wide, left); }
     __device__ __forceinline__ void load(const float* p, int left, const void* lo, const void* hi)
     {
         uint32_t w[8];
@@ -350,9 +363,30 @@ struct Raw8<float> {
 #pragma unroll
             for (int q = 0; q < 8; ++q) x.v[q] = q < left ? __uint_as_float(w[q]) : 0.f;
         } else {
-            x = load_some(p, false, left);
+            x = ops::load_some(p, false, left);
         }
     }
+    // the elements from..to - 1 of the eight, value by value; the others are -infinity
+    __device__ __forceinline__ void load_part(const float* p, int from, int to)
+    {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x.v[q] = -INFINITY;
+#pragma unroll 1
+        for (int q = from; q < to; ++q) {             // (rare: short code, few registers)
+            const float y = p[q];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.v[i] = i == q ? y : x.v[i];
+        }
+    }
+    __device__ __forceinline__ float top() const
+    {
+        float t;
+        asm("max.f32 %0, %1, %2, %3;" : "=f"(t) : "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]));
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x.v[3]), "f"(x.v[4]));
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(t) : "f"(x.v[5]), "f"(x.v[6]));
+        return fmaxf(t, x.v[7]);
+    }
+    __device__ __forceinline__ void keep() {}
     __device__ __forceinline__ f8 values() const { return x; }
 };
 template <>
@@ -384,6 +418,31 @@ struct Raw8<__nv_bfloat16> {
             load(p, false, left);
         }
     }
+    __device__ __forceinline__ void load_part(const __nv_bfloat16* p, int from, int to)
+    {
+        const unsigned short* const h = reinterpret_cast<const unsigned short*>(p);
+        uint32_t w[4] = {0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};
+#pragma unroll 1
+        for (int q = from; q < to; ++q) {
+            const uint32_t y = h[q];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i == q >> 1) w[i] = q & 1 ? (w[i] & 0xFFFFu) | y << 16 : (w[i] & 0xFFFF0000u) | y;
+        }
+        u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ float top() const
+    {
+        uint32_t t, v;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(t) : "r"(u.x), "r"(u.y));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(u.z), "r"(u.w));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(t) : "r"(v));
+        float lo, hi;
+        widen_pair(t, lo, hi);
+        return fmaxf(lo, hi);
+    }
+    // The values are to be widened again behind this, rather than kept as such.
+    __device__ __forceinline__ void keep() { asm volatile("" : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w)); }
     __device__ __forceinline__ f8 values() const
     {
         f8 x;
