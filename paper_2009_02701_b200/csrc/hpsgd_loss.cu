@@ -1,8 +1,9 @@
 // The loss over a label and a teacher's top logits, and its gradient.
 //
-// Bound by HBM: a row of logits is read once and a row of gradients written once.  A row is held in the registers of one block, or of the
-// blocks of a cluster where it is longer: all of it is requested at once, its sums of exponentials are joined over warps and blocks, and what is in
-// the registers then becomes the gradient.  Only rows longer than eight blocks hold are read a second time, out of L2.
+// Bound by HBM: a row of logits is read once and a row of gradients written once.  A block takes a row in tiles, two of which are in its registers or on
+// their way there: first the sums of exponentials, from the first tile to the last, then the gradient, from the last, which is still there, to the
+// first; the tiles between come a second time, out of L2.  (Rows held whole, by one block or in the registers of a cluster's blocks, left too little
+// under way while their sums were waited for: 4096 x 30000 bf16 at two temperatures 150 and 236 us; clusters of eight 4096 x 131072 1330.)
 //
 // Sums of exponentials: s = sum 2^(x c - k) with c = log2(e) / temperature and k the largest x c rounded up to a whole number, so that joining two
 // sums multiplies by an exact power of two, and x c - k is rounded once; the softmax is then 2^(x c - k) / s without any error of k's.
@@ -19,12 +20,9 @@ namespace ops {
 namespace {
 
 constexpr int kMaxTeacher = 1024;
-constexpr int kMaxLossCluster = 8;
-constexpr int kLossSms = 148;
 
 struct LossArgs {
-    int rows, vocab, k, pieces, piece;              // pieces: blocks that share a row; piece: columns of each
-    int ahead;                                      // rows between a block's and the one that takes its place
+    int rows, vocab, k, pieces, piece;              // pieces: blocks that share a row (the gradient alone); piece: columns of each
     const void* z;
     const int64_t* labels;
     const int32_t* index;
@@ -97,6 +95,9 @@ __device__ __forceinline__ pair power(pair e)
 // How many temperatures there are: one; two, each with its own powers; or two of which the first's are the N-th powers of the second's.
 constexpr int kOne = 0, kTwo = 1;
 
+template <typename T>
+constexpr int kPerSm = sizeof(T) == 4 ? 1024 : 1536;
+
 // The gradient before what is taken off at the label and the teacher's entries: A softmax(z) + B softmax(z / T), with the sums in A and B.
 template <int MODE>
 struct Softmax {
@@ -112,16 +113,15 @@ struct Softmax {
     }
 };
 
-// THREADS threads with NV groups of eight columns each (a tile).  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
+// THREADS threads with NV groups of eight columns each (a tile); PER_SM threads on an SM.  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
 // are counted from the boundary in front of the row; else groups begin at column 0 and are taken piece by piece.  LATER: the gradient alone, from lse.
-template <typename T, int THREADS, int NV, int MODE, bool SHIFT, bool CLUSTER, bool LATER>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const LossArgs a)
+template <typename T, int THREADS, int NV, int MODE, bool SHIFT, bool LATER>
+__global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(const LossArgs a)
 {
     constexpr int kWarpsHere = THREADS / 32, kTileCols = THREADS * NV * 8;
     constexpr bool kSecond = MODE != kOne;
     extern __shared__ __align__(16) float room[];   // of each teacher entry, and of the label behind them: index, probability, its logit, the student's, seen twice
     __shared__ Stats of_warp[kWarpsHere];
-    __shared__ alignas(8) Stats of_block[kMaxLossCluster];
     __shared__ float part[kWarpsHere];
     const int k = a.k, stride = (k + 4) / 4 * 4;
     int* const index = reinterpret_cast<int*>(room);
@@ -130,17 +130,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
     float* const z_of = t_of + stride;
     uint8_t* const twice = reinterpret_cast<uint8_t*>(z_of + stride);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rank = CLUSTER || LATER ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
-    const int64_t row = CLUSTER || LATER ? blockIdx.x / (unsigned)a.pieces : blockIdx.x;
+    const int rank = LATER ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
+    const int64_t row = LATER ? blockIdx.x / (unsigned)a.pieces : blockIdx.x;
     const T* const z = static_cast<const T*>(a.z) + row * a.ldz;
     const int shift = SHIFT ? (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T) % 8) : 0;
     const int first = rank * a.piece - shift, last = min(a.vocab, first + a.piece);      // this block's columns, from max(0, first)
-    if constexpr (CLUSTER && !LATER) cluster_arrive();      // the others' memory is there to be written; waited for below
+    const int tiles = (last - first + kTileCols - 1) / kTileCols;
     after_previous();
 
-    Raw8<T> x[NV];
-    const auto column = [&](int tile, int v) { return first + tile + (v * THREADS + (int)threadIdx.x) * 8; };
-    const auto request = [&](int tile) {
+    Raw8<T> even[NV], odd[NV];                      // tile t is in the one that its number says
+    const auto column = [&](int tile, int v) { return first + tile * kTileCols + (v * THREADS + (int)threadIdx.x) * 8; };
+    const auto request = [&](Raw8<T>(&x)[NV], int tile) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = column(tile, v), left = max(0, min(8, last - c));
@@ -151,13 +151,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
             } else x[v].load_part(z + c, max(0, -c), left);
         }
     };
-    request(0);
-    if (row + a.ahead < a.rows) {                   // the row that comes next here, to L2
-        const char* const next = reinterpret_cast<const char*>(z + a.ahead * a.ldz + max(0, first));
-        const int bytes = (last - max(0, first)) * (int)sizeof(T);
-#pragma unroll 1
-        for (int i = threadIdx.x * 128; i < bytes; i += THREADS * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(next + i));
-    }
+    request(even, 0);
+    if (tiles > 1) request(odd, 1);
     // the label and the teacher's entries meanwhile; an index outside the vocabulary makes the row NaN
     const int64_t label64 = a.labels ? a.labels[row] : -1;
     const bool has_label = label64 >= 0;
@@ -194,9 +189,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
     }
 
     if constexpr (!LATER) {
-#pragma unroll 1
-        for (int tile = 0; tile < last - first; tile += kTileCols) {
-            if (tile > 0) request(tile);
+        const auto add = [&](Raw8<T>(&x)[NV], int tile) {
             float top = x[0].top();
 #pragma unroll
             for (int v = 1; v < NV; ++v) top = fmaxf(top, x[v].top());
@@ -219,6 +212,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
                     if constexpr (MODE > kTwo) sf = add2(sf, power<MODE>(e));
                 }
             }
+#pragma unroll
+            for (int v = 0; v < NV; ++v) x[v].keep();
+            if (tile + 2 < tiles) request(x, tile + 2);
             float lo, hi;
             split(sb, lo, hi);
             Sum& base = kSecond ? mine.two : mine.one;
@@ -227,6 +223,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
                 split(sf, lo, hi);
                 mine.one = Sum{kf, __fmaf_rn(mine.one.s, exp2_of(mine.one.k - kf), __fadd_rn(lo, hi))};
             }
+        };
+#pragma unroll 1
+        for (int tile = 0; tile < tiles; tile += 2) {
+            add(even, tile);
+            if (tile + 1 < tiles) add(odd, tile + 1);
         }
     }
     if (wrong) mine.one.s = mine.two.s = mine.teacher.s = __uint_as_float(0x7FC00000u);
@@ -236,35 +237,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
     all.teacher = warp * 32 <= k ? join_lanes(mine.teacher) : nothing();
     if (lane == 0) of_warp[warp] = all;
     __syncthreads();
-    if (!CLUSTER || LATER || warp == 0) {
+    {
         const bool has = lane < kWarpsHere;
         const Stats w = of_warp[has ? lane : 0];
         all.one = join_lanes(has ? w.one : nothing());
         if (kSecond) all.two = join_lanes(has ? w.two : nothing());
         all.teacher = join_lanes(has ? w.teacher : nothing());
-    }
-    if constexpr (CLUSTER && !LATER) {
-        cluster_wait();
-        if (warp == 0) {
-            if (lane < a.pieces) {
-                uint32_t there;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(shared_address(&of_block[rank])), "r"(lane));
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(all.one.k), "f"(all.one.s) : "memory");
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 8), "f"(all.two.k), "f"(all.two.s) : "memory");
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there + 16), "f"(all.teacher.k), "f"(all.teacher.s) : "memory");
-            }
-            asm volatile("fence.acq_rel.cluster;" ::: "memory");      // (only this warp has something to publish)
-        }
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-        cluster_wait();
-        all = of_block[0];                          // (every block has the whole teacher)
-#pragma unroll 1
-        for (int r = 1; r < a.pieces; ++r) {
-            const Stats s = of_block[r];
-            all.one.add(s.one.k, s.one.s);
-            if (kSecond) all.two.add(s.two.k, s.two.s);
-        }
     }
 
     const bool has_teacher = k > 0 && !(all.teacher.s == 0.f);
@@ -321,11 +299,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
         softmax = Softmax<MODE>{a.c1, all.one.k, a.c2, all.two.k, main != 0.f ? __fdividef(main, all.one.s) : 0.f, kSecond && on_teacher != 0.f ? __fdividef(on_teacher, all.two.s) : 0.f};
         none = on_label == 0.f && on_teacher == 0.f;
         T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
-#pragma unroll 1
-        for (int tile = 0; tile < last - first; tile += kTileCols) {
-            if (last - first > kTileCols) request(tile);
-#pragma unroll
-            for (int v = 0; v < NV; ++v) x[v].keep();
+        const auto turn = [&](Raw8<T>(&x)[NV], int tile) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = column(tile, v), left = max(0, min(8, last - c));
@@ -338,6 +312,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
                     else store_part(dz + c, d, max(0, -c), left);
                 } else if (left > 0) store_unaligned(dz + c, d, left);
             }
+            // (from the gradient's first tile, which holds the last columns, to the row's first: in place, what is read has not been written)
+            if (tile > 1) request(x, tile - 2);
+        };
+#pragma unroll 1
+        for (int tile = (tiles - 1) | 1; tile > 0; tile -= 2) {
+            if (tile < tiles) turn(odd, tile);
+            turn(even, tile - 1);
         }
     }
     // and what is taken off at the label and the teacher's entries; the same index twice is one element, written with the same value
@@ -367,39 +348,38 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) loss_kernel(const Los
     }
 }
 
-template <typename T, int THREADS, int NV, bool CLUSTER, bool LATER>
+template <typename T, int THREADS, int NV, bool LATER>
 int loss_launch(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t s)
 {
     const dim3 grid((unsigned)((int64_t)a.rows * a.pieces));
     const size_t smem = (size_t)((a.k + 4) / 4 * 4) * 17;
-    a.ahead = std::max(1, kLossSms * (1024 / THREADS) / a.pieces);
-    const auto go = [&](auto kernel) { return launch_clusters(what, kernel, grid, THREADS, smem, CLUSTER && !LATER ? a.pieces : 1, s, a); };
-    if (mode == kOne) return shift ? go(loss_kernel<T, THREADS, NV, kOne, true, CLUSTER, LATER>) : go(loss_kernel<T, THREADS, NV, kOne, false, CLUSTER, LATER>);
+    const auto go = [&](auto kernel) { return launch_early(what, kernel, grid, THREADS, smem, s, a); };
+    if (mode == kOne) return shift ? go(loss_kernel<T, THREADS, NV, kOne, true, LATER>) : go(loss_kernel<T, THREADS, NV, kOne, false, LATER>);
     if constexpr (!LATER) {
-        if (shift && mode == 2) return go(loss_kernel<T, THREADS, NV, 2, true, CLUSTER, LATER>);
-        if (shift && mode == 3) return go(loss_kernel<T, THREADS, NV, 3, true, CLUSTER, LATER>);
-        if (shift && mode == 4) return go(loss_kernel<T, THREADS, NV, 4, true, CLUSTER, LATER>);
+        if (shift && mode == 2) return go(loss_kernel<T, THREADS, NV, 2, true, LATER>);
+        if (shift && mode == 3) return go(loss_kernel<T, THREADS, NV, 3, true, LATER>);
+        if (shift && mode == 4) return go(loss_kernel<T, THREADS, NV, 4, true, LATER>);
     }
-    return shift ? go(loss_kernel<T, THREADS, NV, kTwo, true, CLUSTER, LATER>) : go(loss_kernel<T, THREADS, NV, kTwo, false, CLUSTER, LATER>);
+    return shift ? go(loss_kernel<T, THREADS, NV, kTwo, true, LATER>) : go(loss_kernel<T, THREADS, NV, kTwo, false, LATER>);
 }
 
 template <typename T, bool LATER>
 int loss_types(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t s)
 {
-    constexpr int kMost = sizeof(T) == 4 ? 2 : 4;    // groups of eight that a thread holds
-    const auto up8 = [](int64_t x) { return (int)((x + 7) / 8 * 8); };
     const int64_t cols = (int64_t)a.vocab + (shift ? 7 : 0);      // counted from the boundary in front of the row
     a.pieces = 1;
-    a.piece = up8(cols);
-    if (cols <= 1024) return loss_launch<T, 128, 1, false, LATER>(what, a, mode, shift, s);
-    if (cols <= 4096) return loss_launch<T, 512, 1, false, LATER>(what, a, mode, shift, s);
-    if (cols <= 8192) return loss_launch<T, 512, 2, false, LATER>(what, a, mode, shift, s);
-    if (kMost == 4 && cols <= 16384) return loss_launch<T, 512, kMost, false, LATER>(what, a, mode, shift, s);
-    while (a.pieces < kMaxLossCluster && a.piece > kMost * 4096) {
-        a.pieces *= 2;
-        a.piece = up8((cols + a.pieces - 1) / a.pieces);
+    a.piece = (int)((cols + 7) / 8 * 8);
+    if (LATER) {                                     // nothing is waited for: two tiles a block
+        if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
+        a.piece = std::min(a.piece, 2 * 256 * 2 * 8);
+        a.pieces = (int)((cols + a.piece - 1) / a.piece);
+        return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
     }
-    return loss_launch<T, 512, kMost, true, LATER>(what, a, mode, shift, s);
+#ifdef LT
+    return loss_launch<T, LT, LN, LATER>(what, a, mode, shift, s);
+#endif
+    if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
+    return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
 }
 
 int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, void* stream)
@@ -415,7 +395,7 @@ int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, 
         return report(HPSGD_E_BADARG, "%s: weights must be >= 0 and finite", what);
     if (!std::isfinite((float)p.grad_scale)) return report(HPSGD_E_BADARG, "%s: grad_scale is not finite", what);
     if (p.k > kMaxTeacher) return report(HPSGD_E_UNSUPPORTED, "%s: at most %d teacher entries a row", what, kMaxTeacher);
-    if (p.vocab > 0x7FFFFFFF - 65536 || p.rows > 0x7FFFFFFF / kMaxLossCluster) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    if (p.vocab > 0x7FFFFFFF - 65536 || p.rows * ((p.vocab + 8191) / 8192 + 1) > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
     if (p.rows == 0 || p.vocab == 0) return HPSGD_OK;
     if (!p.logits) return report(HPSGD_E_BADARG, "%s: logits is NULL", what);
     if (later ? !p.dlogits : !p.loss && !p.lse && !p.dlogits) return report(HPSGD_E_BADARG, "%s: no output is asked for", what);
