@@ -140,7 +140,14 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
 
     Raw8<T> even[NV], odd[NV];                      // tile t is in the one that its number says
     const auto column = [&](int tile, int v) { return first + tile * kTileCols + (v * THREADS + (int)threadIdx.x) * 8; };
+    const T* const mine_z = z + first + (int)threadIdx.x * 8;
+    // tiles that are neither the first nor the last are whole, and lie on the wide boundary where rows do (or can be made to)
     const auto request = [&](Raw8<T>(&x)[NV], int tile) {
+        if (SHIFT && tile > 0 && tile + 1 < tiles) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) x[v].load(mine_z + (int64_t)tile * kTileCols + v * THREADS * 8, true, 8);
+            return;
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = column(tile, v), left = max(0, min(8, last - c));
@@ -193,12 +200,19 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             float top = x[0].top();
 #pragma unroll
             for (int v = 1; v < NV; ++v) top = fmaxf(top, x[v].top());
-            top = top_of_lanes(top);
 #pragma unroll
             for (int v = 0; v < NV; ++v) x[v].keep();
-            // sums with a whole warp's k
-            const float kb = fmaxf(kSecond ? mine.two.k : mine.one.k, ceilf(__fmul_rn(top, kSecond ? a.c2 : a.c1)));
-            const float kf = MODE == kTwo ? fmaxf(mine.one.k, ceilf(__fmul_rn(top, a.c1))) : MODE == kOne ? kb : fmaxf(kb * MODE, -FLT_MAX);
+            Sum& base = kSecond ? mine.two : mine.one;
+            const float kt = __fmul_rn(top, kSecond ? a.c2 : a.c1);
+            if (__any_sync(0xFFFFFFFFu, !(kt <= base.k))) {      // a larger value than so far: the whole warp's k moves
+                const float kb = fmaxf(base.k, ceilf(top_of_lanes(kt)));
+                base = Sum{kb, __fmul_rn(base.s, exp2_of(base.k - kb))};
+                if (kSecond) {
+                    const float kf = MODE == kTwo ? fmaxf(mine.one.k, ceilf(__fmul_rn(top_of_lanes(top), a.c1))) : fmaxf(kb * MODE, -FLT_MAX);
+                    mine.one = Sum{kf, __fmul_rn(mine.one.s, exp2_of(mine.one.k - kf))};
+                }
+            }
+            const float kb = base.k, kf = mine.one.k;
             const pair cb = both(kSecond ? a.c2 : a.c1), minus_kb = both(-kb), cf = both(a.c1), minus_kf = both(-kf);
             pair sb = both(0.f), sf = both(0.f);
 #pragma unroll
@@ -217,11 +231,10 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             if (tile + 2 < tiles) request(x, tile + 2);
             float lo, hi;
             split(sb, lo, hi);
-            Sum& base = kSecond ? mine.two : mine.one;
-            base = Sum{kb, __fmaf_rn(base.s, exp2_of(base.k - kb), __fadd_rn(lo, hi))};
+            base.s = __fadd_rn(base.s, __fadd_rn(lo, hi));
             if (kSecond) {
                 split(sf, lo, hi);
-                mine.one = Sum{kf, __fmaf_rn(mine.one.s, exp2_of(mine.one.k - kf), __fadd_rn(lo, hi))};
+                mine.one.s = __fadd_rn(mine.one.s, __fadd_rn(lo, hi));
             }
         };
 #pragma unroll 1
@@ -299,14 +312,23 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
         softmax = Softmax<MODE>{a.c1, all.one.k, a.c2, all.two.k, main != 0.f ? __fdividef(main, all.one.s) : 0.f, kSecond && on_teacher != 0.f ? __fdividef(on_teacher, all.two.s) : 0.f};
         none = on_label == 0.f && on_teacher == 0.f;
         T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
+        T* const mine_dz = dz + first + (int)threadIdx.x * 8;
         const auto turn = [&](Raw8<T>(&x)[NV], int tile) {
+            const bool whole = SHIFT && tile > 0 && tile + 1 < tiles;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c = column(tile, v), left = max(0, min(8, last - c));
                 p4 y = to_pairs(x[v].values());
+                if (none) y = p4{};
+                else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) y.v[q] = none ? both(0.f) : softmax(y.v[q]);
+                    for (int q = 0; q < 4; ++q) y.v[q] = softmax(y.v[q]);
+                }
                 const f8 d = to_values(y);
+                if (whole) {
+                    store8(mine_dz + (int64_t)tile * kTileCols + v * THREADS * 8, d);
+                    continue;
+                }
+                const int c = column(tile, v), left = max(0, min(8, last - c));
                 if constexpr (SHIFT) {
                     if (c >= 0 && left == 8) store8(dz + c, d);
                     else store_part(dz + c, d, max(0, -c), left);
