@@ -39,6 +39,43 @@ struct LossArgs {
     int main_is_teacher;                            // c1 is the teacher's temperature
 };
 
+// How long a line is wanted in L2: what is read again until it has been, and nothing that has been written.
+__device__ __forceinline__ uint64_t keep_long()
+{
+    uint64_t x;
+    asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(x));
+    return x;
+}
+__device__ __forceinline__ uint64_t drop_first()
+{
+    uint64_t x;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(x));
+    return x;
+}
+__device__ __forceinline__ void load8(Raw8<float>& y, const float* p, uint64_t policy)
+{
+    f8& x = y.x;
+    asm volatile("ld.global.L2::cache_hint.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8], %9;"
+                 : "=f"(x.v[0]), "=f"(x.v[1]), "=f"(x.v[2]), "=f"(x.v[3]), "=f"(x.v[4]), "=f"(x.v[5]), "=f"(x.v[6]), "=f"(x.v[7])
+                 : "l"(p), "l"(policy));
+}
+__device__ __forceinline__ void load8(Raw8<__nv_bfloat16>& x, const __nv_bfloat16* p, uint64_t policy)
+{
+    asm volatile("ld.global.L2::cache_hint.v4.b32 {%0,%1,%2,%3}, [%4], %5;" : "=r"(x.u.x), "=r"(x.u.y), "=r"(x.u.z), "=r"(x.u.w) : "l"(p), "l"(policy));
+}
+__device__ __forceinline__ void store8(float* p, const f8& x, uint64_t policy)
+{
+    asm volatile("st.global.L2::cache_hint.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8}, %9;" ::"l"(p), "f"(x.v[0]), "f"(x.v[1]), "f"(x.v[2]), "f"(x.v[3]), "f"(x.v[4]),
+                 "f"(x.v[5]), "f"(x.v[6]), "f"(x.v[7]), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const f8& x, uint64_t policy)
+{
+    asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(p), "r"(pack_bf16(x.v[0], x.v[1])), "r"(pack_bf16(x.v[2], x.v[3])),
+                 "r"(pack_bf16(x.v[4], x.v[5])), "r"(pack_bf16(x.v[6], x.v[7])), "l"(policy)
+                 : "memory");
+}
+
 struct Sum {
     float k, s;                                     // s 2^k
     __device__ __forceinline__ void add(float k2, float s2)
@@ -142,10 +179,16 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
     const auto column = [&](int tile, int v) { return first + tile * kTileCols + (v * THREADS + (int)threadIdx.x) * 8; };
     const T* const mine_z = z + first + (int)threadIdx.x * 8;
     // tiles that are neither the first nor the last are whole, and lie on the wide boundary where rows do (or can be made to)
-    const auto request = [&](Raw8<T>(&x)[NV], int tile) {
+    constexpr bool kHints = THREADS == 512;          // long rows: what is under way at a time comes near L2's size
+    const uint64_t again = keep_long(), done = drop_first();
+    const auto request = [&](Raw8<T>(&x)[NV], int tile, bool last_time) {
         if (SHIFT && tile > 0 && tile + 1 < tiles) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) x[v].load(mine_z + (int64_t)tile * kTileCols + v * THREADS * 8, true, 8);
+            for (int v = 0; v < NV; ++v) {
+                const T* const from = mine_z + (int64_t)tile * kTileCols + v * THREADS * 8;
+                if constexpr (kHints) load8(x[v], from, last_time ? done : again);
+                else x[v].load(from, true, 8);
+            }
             return;
         }
 #pragma unroll
@@ -158,8 +201,8 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             } else x[v].load_part(z + c, max(0, -c), left);
         }
     };
-    request(even, 0);
-    if (tiles > 1) request(odd, 1);
+    request(even, 0, false);
+    if (tiles > 1) request(odd, 1, false);
     // the label and the teacher's entries meanwhile; an index outside the vocabulary makes the row NaN
     const int64_t label64 = a.labels ? a.labels[row] : -1;
     const bool has_label = label64 >= 0;
@@ -228,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             }
 #pragma unroll
             for (int v = 0; v < NV; ++v) x[v].keep();
-            if (tile + 2 < tiles) request(x, tile + 2);
+            if (tile + 2 < tiles) request(x, tile + 2, false);
             float lo, hi;
             split(sb, lo, hi);
             base.s = __fadd_rn(base.s, __fadd_rn(lo, hi));
@@ -325,17 +368,19 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
                 }
                 const f8 d = to_values(y);
                 if (whole) {
-                    store8(mine_dz + (int64_t)tile * kTileCols + v * THREADS * 8, d);
+                    T* const to = mine_dz + (int64_t)tile * kTileCols + v * THREADS * 8;
+                    if constexpr (kHints) store8(to, d, done);
+                    else ops::store8(to, d);
                     continue;
                 }
                 const int c = column(tile, v), left = max(0, min(8, last - c));
                 if constexpr (SHIFT) {
-                    if (c >= 0 && left == 8) store8(dz + c, d);
+                    if (c >= 0 && left == 8) ops::store8(dz + c, d);
                     else store_part(dz + c, d, max(0, -c), left);
                 } else if (left > 0) store_unaligned(dz + c, d, left);
             }
             // (from the gradient's first tile, which holds the last columns, to the row's first: in place, what is read has not been written)
-            if (tile > 1) request(x, tile - 2);
+            if (tile > 1) request(x, tile - 2, true);
         };
 #pragma unroll 1
         for (int tile = (tiles - 1) | 1; tile > 0; tile -= 2) {
@@ -397,9 +442,10 @@ int loss_types(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t
         a.pieces = (int)((cols + a.piece - 1) / a.piece);
         return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
     }
-#ifdef LT
-    return loss_launch<T, LT, LN, LATER>(what, a, mode, shift, s);
-#endif
+    // Rows of which six an SM, as blocks of 256 threads are held, do not fit L2 with room for what is written: three blocks of 512 an SM, and L2 is told
+    // what will be read again (4096 x 131072 bf16: 428 us; 450 without the hints; 490 with blocks of 256; one block of 1024 an SM 557).  Shorter ones: blocks of
+    // 256 (4096 x 30000: 125 us; of 512 139).
+    if (cols * (int64_t)sizeof(T) * 148 * 6 > (96 << 20)) return loss_launch<T, 512, 2, LATER>(what, a, mode, shift, s);
     if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
     return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
 }
