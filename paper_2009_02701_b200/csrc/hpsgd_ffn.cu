@@ -10,6 +10,7 @@
 #include "hpsgd_tensor_core.cuh"
 
 #include <algorithm>
+#include <cstdlib>
 
 namespace hpsgd {
 namespace ops {
@@ -25,16 +26,19 @@ constexpr int kChunk = 8;                  // columns that go through shared mem
 
 __device__ unsigned int g_ffn_timeouts;    // blocks whose wait ran out since the last report
 
-// BN: tokens of a tile.
-template <int BN>
+// BN: tokens of a tile.  PAIR: two blocks (a cluster) share a tile of 256 features, each with 128 of them and half of the tokens.
+template <int BN, bool PAIR>
 struct FfnShape {
     static constexpr int kStages = BN <= 64 ? 5 : 4;
-    static constexpr int kBytesW = kLanes * kStageK, kBytesX = BN * kStageK;      // of one of the weights, and of the tokens
+    static constexpr int kAtoms = BN <= 128 ? 1 : 2;                     // groups of 128 tokens' scales
+    static constexpr int kRowsX = PAIR ? BN / 2 : BN;                    // tokens in this block's shared memory
+    static constexpr int kBytesW = kLanes * kStageK, kBytesX = kRowsX * kStageK;      // of one of the weights, and of the tokens
     static constexpr int kStageBytes = 2 * kBytesW + kBytesX;
     static constexpr int kAccs = BN <= 64 ? 2 : 1;
-    static constexpr int kPlaces = 4;                                    // groups of scales (four k blocks) in shared memory
-    static constexpr int kBytesS = 512 * 3;                              // of one group: gate, gated, tokens
-    static constexpr int kScaleCols = 4 * 3;
+    static constexpr int kPlaces = PAIR ? 3 : 4;                         // groups of scales (four k blocks) in shared memory
+    static constexpr int kParts = 2 + kAtoms;                            // of one group: gate, gated, tokens
+    static constexpr int kBytesS = 512 * kParts;
+    static constexpr int kScaleCols = 4 * kParts;
     static constexpr int kCols = kAccs * 2 * BN + (kPlaces + 1) * kScaleCols;
     static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
     static constexpr int kBytesOut = 2 * 2 * kChunk * kLanes * 4;        // two halves, two sums
@@ -150,28 +154,29 @@ __device__ __forceinline__ void finish(const FfnOut& a, int m, int n0, float4 g4
 }
 
 // ---------------------------------------------------------------------------- the kernel
+// Unit u of a block's (or pair's) work; n0: this block's first feature.  Pairs' sums are not split.
 struct FfnUnit {
     int n0, m0, k0, k1, split;
 };
-template <int BN>
-__device__ __forceinline__ FfnUnit ffn_unit(const FfnArgs& a, int u)
+template <int BN, bool PAIR>
+__device__ __forceinline__ FfnUnit ffn_unit(const FfnArgs& a, int u, int rank)
 {
     FfnUnit x;
-    const int tile = u / a.splits;
-    x.split = u % a.splits;
-    x.n0 = tile % a.tiles_n * kLanes;
+    const int tile = PAIR ? u : u / a.splits;
+    x.split = PAIR ? 0 : u % a.splits;
+    x.n0 = tile % a.tiles_n * (PAIR ? 2 * kLanes : kLanes) + rank * kLanes;
     x.m0 = tile / a.tiles_n * BN;
-    x.k0 = x.split * a.per_split + min(x.split, a.longer);
-    x.k1 = x.k0 + a.per_split + (x.split < a.longer);
+    x.k0 = PAIR ? 0 : x.split * a.per_split + min(x.split, a.longer);
+    x.k1 = PAIR ? a.per_split : x.k0 + a.per_split + (x.split < a.longer);
     return x;
 }
 
 // JOIN: the blocks of a cluster have a tile's parts along k, one each, and add them out of each other's shared memory in their order.
-template <int BN, bool JOIN>
+template <int BN, bool PAIR, bool JOIN>
 __global__ void __launch_bounds__(kFfnThreads, 1)
     gated_ffn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ FfnArgs a)
 {
-    using S = FfnShape<BN>;
+    using S = FfnShape<BN, PAIR>;
     extern __shared__ uint8_t raw[];
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const scales = smem + S::kStages * S::kStageBytes;
@@ -180,7 +185,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int given_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int first = (int)blockIdx.x, stride = (int)gridDim.x;
+    const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, first = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x,
+              stride = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;      // the first block of a pair issues the products of both
     const uint32_t full = smem_address(bars), empty = full + S::kStages * 8, acc_full = empty + S::kStages * 8, acc_empty = acc_full + S::kAccs * 8,
                    scale_full = acc_empty + S::kAccs * 8, scale_empty = scale_full + S::kPlaces * 8, drained = scale_empty + S::kPlaces * 8;
     if (threadIdx.x == 0) {
@@ -189,28 +195,34 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
             barrier_init(empty + s * 8, 1);
         }
         for (int s = 0; s < S::kPlaces; ++s) {
-            barrier_init(scale_full + s * 8, 1);
+            barrier_init(scale_full + s * 8, PAIR ? 2 : 1);          // the scales of each block
             barrier_init(scale_empty + s * 8, 1);
         }
         for (int s = 0; s < S::kAccs; ++s) {
             barrier_init(acc_full + s * 8, 1);
-            barrier_init(acc_empty + s * 8, 8);          // the warps that read it
+            barrier_init(acc_empty + s * 8, PAIR ? 16 : 8);          // the warps that read it
         }
         barrier_init(drained, 1);
         given_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 3) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_slot)), "n"(S::kAlloc) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if constexpr (PAIR) cluster_sync();
     if constexpr (JOIN) cluster_arrive();            // given_up is there to be written by the others; waited for at the end
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     after_previous();
     const uint32_t tmem = tmem_slot, tmem_scales = tmem + S::kAccs * 2 * BN;
-    const int units = a.tiles * a.splits;
+    const int units = PAIR ? a.tiles : a.tiles * a.splits;
 
     const auto wait_one = [&](uint32_t bar, uint32_t parity) { return barrier_wait(bar, parity, &given_up); };
     const auto wait = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xFFFFFFFFu, barrier_wait(bar, parity, &given_up)); };
@@ -219,20 +231,21 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         uint32_t phase = 1;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
-            const FfnUnit x = ffn_unit<BN>(a, u);
+            const FfnUnit x = ffn_unit<BN, PAIR>(a, u, rank);
             for (int kb = x.k0; kb < x.k1; ++kb) {
                 if (!(ok = wait_one(empty + s * 8, phase))) break;
-                const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = full + s * 8;
+                // Both blocks' boxes count at the first block's barrier, which expects the bytes of both.
+                const uint32_t dst = smem_address(smem) + s * S::kStageBytes, bar = PAIR ? first_block_address(full + s * 8) : full + s * 8;
 #ifdef HPSGD_DEBUG
                 const uint32_t stall = a.stall_odd && !(blockIdx.x & 1) ? 0u : a.stall;
 #else
                 constexpr uint32_t stall = 0;
 #endif
-                barrier_expect(bar, S::kStageBytes + stall);
+                if (rank == 0) barrier_expect(full + s * 8, (PAIR ? 2 : 1) * S::kStageBytes + stall);
                 // (rows of the gate's box behind its last feature are the other weights'; they come to nothing)
-                tma_load<false>(dst, &map_w, kb * kStageK, x.n0, bar);
-                tma_load<false>(dst + S::kBytesW, &map_w, kb * kStageK, a.out.N + x.n0, bar);
-                tma_load<false>(dst + 2 * S::kBytesW, &map_x, kb * kStageK, x.m0, bar);
+                tma_load<PAIR>(dst, &map_w, kb * kStageK, x.n0, bar);
+                tma_load<PAIR>(dst + S::kBytesW, &map_w, kb * kStageK, a.out.N + x.n0, bar);
+                tma_load<PAIR>(dst + 2 * S::kBytesW, &map_x, kb * kStageK, x.m0 + rank * S::kRowsX, bar);
                 if (++s == S::kStages) s = 0, phase ^= 1;
             }
         }
@@ -240,13 +253,13 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
             const uint64_t t = nanoseconds();
             while (nanoseconds() - t < 10000000ull) {}
         }
-    } else if (warp == 1 && elected()) {
+    } else if (warp == 1 && rank == 0 && elected()) {
         const uint64_t desc = operand_descriptor(smem_address(smem)), desc_s = scale_descriptor(smem_address(scales));
         int s = 0, place = 0, column = 0, acc = 0;
         uint32_t phase = 0, place_phase = 0, acc_phase = 1;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
-            const FfnUnit x = ffn_unit<BN>(a, u);
+            const FfnUnit x = ffn_unit<BN, PAIR>(a, u, rank);
             if (!(ok = wait_one(acc_empty + acc * 8, acc_phase))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             uint32_t sc = 0;
@@ -260,32 +273,32 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
                     sc = tmem_scales + column * S::kScaleCols;
                     const uint64_t src = desc_s + (uint32_t)(place * (S::kBytesS >> 4));
 #pragma unroll
-                    for (int t = 0; t < 3; ++t) copy_scales<false>(sc + 4 * t, src + 32 * t);
-                    commit<false>(scale_empty + place * 8);
+                    for (int t = 0; t < S::kParts; ++t) copy_scales<PAIR>(sc + 4 * t, src + 32 * t);
+                    commit<PAIR>(scale_empty + place * 8);
                     if (++column == S::kPlaces + 1) column = 0;
                     if (++place == S::kPlaces) place = 0, place_phase ^= 1;
                 }
                 const uint64_t dg = desc + (uint32_t)(s * (S::kStageBytes >> 4)), du = dg + (uint32_t)(S::kBytesW >> 4), dx = dg + (uint32_t)(2 * S::kBytesW >> 4);
-                const uint32_t id = instruction<BN, false>(kb & 3);
+                const uint32_t id = instruction<BN, PAIR>(kb & 3);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    mma<false>(tmem + acc * 2 * BN, dg + 2 * k, dx + 2 * k, id, sc, sc + 8, kb > x.k0 || k > 0);
-                    mma<false>(tmem + acc * 2 * BN + BN, du + 2 * k, dx + 2 * k, id, sc + 4, sc + 8, kb > x.k0 || k > 0);
+                    mma<PAIR>(tmem + acc * 2 * BN, dg + 2 * k, dx + 2 * k, id, sc, sc + 8, kb > x.k0 || k > 0);
+                    mma<PAIR>(tmem + acc * 2 * BN + BN, du + 2 * k, dx + 2 * k, id, sc + 4, sc + 8, kb > x.k0 || k > 0);
                 }
-                commit<false>(empty + s * 8);
-                if (kb + 1 == x.k1) commit<false>(acc_full + acc * 8);
+                commit<PAIR>(empty + s * 8);
+                if (kb + 1 == x.k1) commit<PAIR>(acc_full + acc * 8);
                 if (++s == S::kStages) s = 0, phase ^= 1;
             }
             if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
         }
         if (!ok) {                                  // products in flight read shared memory: let them end
-            commit<false>(drained);
+            commit<PAIR>(drained);
             const uint64_t t = nanoseconds();
             while (!barrier_try(drained, 0) && nanoseconds() - t < 1000000000ull) {}
         }
     } else if (warp == 2) {
         // Lane l brings the words of rows l, l + 32, l + 64, l + 96: one 16-byte row of what the copy to tensor memory reads.
-        uint32_t w[3][4];
+        uint32_t w[S::kParts][4];
         const auto fetch = [&](const FfnUnit& x, int kb) {
             const int64_t g = kb >> 2;
 #pragma unroll
@@ -294,23 +307,27 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
                 const bool in = x.n0 + r < a.out.N;
                 w[0][j] = in ? __ldg(a.sw + g * a.ldsw + x.n0 + r) : 0u;
                 w[1][j] = in ? __ldg(a.sw + g * a.ldsw + a.out.N + x.n0 + r) : 0u;
-                w[2][j] = r < BN && x.m0 + r < a.M ? __ldg(a.sx + g * a.ldsx + x.m0 + r) : 0u;
+#pragma unroll
+                for (int t = 0; t < S::kAtoms; ++t) w[2 + t][j] = 128 * t + r < BN && x.m0 + 128 * t + r < a.M ? __ldg(a.sx + g * a.ldsx + x.m0 + 128 * t + r) : 0u;
             }
         };
         int place = 0;
         uint32_t phase = 1;
         bool ok = true;
         for (int u = first; u < units && ok; u += stride) {
-            const FfnUnit x = ffn_unit<BN>(a, u);
+            const FfnUnit x = ffn_unit<BN, PAIR>(a, u, rank);
             for (int kb = x.k0; kb < x.k1; kb = (kb | 3) + 1) {
                 fetch(x, kb);
                 if (!(ok = wait(scale_empty + place * 8, phase))) break;
                 uint4* const dst = reinterpret_cast<uint4*>(scales + place * S::kBytesS);
 #pragma unroll
-                for (int t = 0; t < 3; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+                for (int t = 0; t < S::kParts; ++t) dst[32 * t + lane] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) barrier_arrive(scale_full + place * 8);
+                if (lane == 0) {
+                    if constexpr (PAIR) barrier_arrive_cluster(first_block_address(scale_full + place * 8));
+                    else barrier_arrive(scale_full + place * 8);
+                }
                 if (++place == S::kPlaces) place = 0, phase ^= 1;
             }
         }
@@ -333,11 +350,14 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         const auto accumulator_read = [&](int acc) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) barrier_arrive(acc_empty + acc * 8);
+            if (lane == 0) {
+                if constexpr (PAIR) barrier_arrive_cluster(first_block_address(acc_empty + acc * 8));
+                else barrier_arrive(acc_empty + acc * 8);
+            }
         };
         int done = 0;
         for (int u = first; u < units; u += stride, ++done) {
-            const FfnUnit x = ffn_unit<BN>(a, u);
+            const FfnUnit x = ffn_unit<BN, PAIR>(a, u, rank);
             const int acc = done % S::kAccs;
             // the four warps of a half wait for one another below, so they go on together or not at all
             if (!all_four(wait(acc_full + acc * 8, done / S::kAccs & 1))) break;
@@ -383,7 +403,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         if (given_up && threadIdx.x < a.splits) word_to_block(smem_address(const_cast<const int*>(&given_up)), threadIdx.x, 1u);
         __syncwarp();
         cluster_sync();
-        const FfnUnit x = ffn_unit<BN>(a, first);
+        const FfnUnit x = ffn_unit<BN, PAIR>(a, first, 0);
         const int cols = given_up ? 0 : min(BN, a.M - x.m0);
         for (int c = warp * a.splits + x.split; c < cols; c += kFfnThreads / 32 * a.splits) {
             const uint32_t at = smem_address(smem) + (c * kLanes + lane * 4) * 4;
@@ -398,7 +418,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         __syncwarp();
         cluster_sync();                              // this block's memory stays until the others have read it
     }
-    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+    if constexpr (PAIR) cluster_sync();              // the other block's arrivals and products reach into this one
+    if (warp == 3) {
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kAlloc));
+    }
 }
 
 // ---------------------------------------------------------------------------- backward
@@ -474,49 +498,81 @@ __global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_kernel(const 
 
 // ---------------------------------------------------------------------------- host side
 struct FfnPlan {
-    int bn, tiles_n, tiles, splits, per_split, longer;
+    int bn, pair, tiles_n, tiles, splits, per_split, longer;
 };
 
-// The least power of two that holds all tokens, 128 at most.  Few tiles are split along k over the blocks of a cluster, as in hpsgd_gemm.cu.
+constexpr int kPairTokens = 224;           // 2 x 224 accumulator columns and four groups' scales are the 512 columns of tensor memory
+
+// The least power of two that holds all tokens, 128 at most, or 224 on pairs of SMs, whichever takes fewer rounds of work.  Few tiles are split
+// along k over the blocks of a cluster, as in hpsgd_gemm.cu.
 FfnPlan plan_of(int64_t M, int64_t N, int64_t K)
 {
     const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     FfnPlan p{};
     const int blocks = (int)up(K, kStageK);
     p.bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    p.tiles_n = (int)up(N, kLanes);
-    p.tiles = (int)(p.tiles_n * up(M, p.bn));
+    int64_t tiles_n = up(N, kLanes), tiles = tiles_n * up(M, p.bn);
+    if (M > 128) {
+        const int64_t pairs_n = up(N, 2 * kLanes), pairs = pairs_n * up(M, kPairTokens);
+        const char* e = getenv("FFN_PAIR");
+        if (e ? atoi(e) : (double)up(pairs, kSms / 2) * 1.4 < (double)up(tiles, kSms)) {
+            p.pair = 1;
+            p.bn = kPairTokens;
+            tiles_n = pairs_n;
+            tiles = pairs;
+        }
+    }
+    p.tiles_n = (int)tiles_n;
+    p.tiles = (int)tiles;
     p.splits = 1;
-    if (p.tiles <= kSms / 2 && blocks >= 8) p.splits = p.tiles > 32 ? 2 : p.tiles > 14 || blocks < 32 ? 4 : 8;
+    if (!p.pair && p.tiles <= kSms / 2 && blocks >= 8) p.splits = p.tiles > 32 ? 2 : p.tiles > 14 || blocks < 32 ? 4 : 8;
     p.per_split = blocks / p.splits;
     p.longer = blocks % p.splits;
     return p;
 }
 
-template <int BN, bool JOIN>
+template <int BN, bool PAIR, bool JOIN>
 int forward_launch(const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
 {
-    using S = FfnShape<BN>;
-    static bool ready[64] = {};
+    using S = FfnShape<BN, PAIR>;
+    const auto kernel = gated_ffn_kernel<BN, PAIR, JOIN>;
+    // Per device: the blocks (or pairs) that it holds at a time; pairs need both their SMs in one GPU cluster, so there may be fewer than half the SMs.
+    static int workers[64] = {};
     int dev = 0;
     OPS_CUDA(cudaGetDevice(&dev));
-    if (dev >= 64 || !ready[dev]) {
-        OPS_CUDA(cudaFuncSetAttribute(gated_ffn_kernel<BN, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
-        if (dev < 64) ready[dev] = true;
+    int at_once = dev < 64 ? workers[dev] : 0;
+    if (at_once == 0) {
+        OPS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        at_once = sms;
+        if (PAIR) {
+            cudaLaunchConfig_t cfg{};
+            cudaLaunchAttribute attr{};
+            cfg.gridDim = dim3(2);
+            cfg.blockDim = dim3(kFfnThreads);
+            cfg.dynamicSmemBytes = S::kSmem;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 2;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            OPS_CUDA(cudaOccupancyMaxActiveClusters(&at_once, kernel, &cfg));
+        }
+        at_once = std::max(1, at_once);
+        if (dev < 64) workers[dev] = at_once;
     }
-    const int64_t units = (int64_t)a.tiles * a.splits;
-    return launch_clusters("hpsgd_gated_ffn_forward", gated_ffn_kernel<BN, JOIN>, dim3((unsigned)(JOIN ? units : std::min<int64_t>(units, sms))), kFfnThreads, S::kSmem,
-                           JOIN ? a.splits : 1, s, mx, mw, a);
+    const int64_t units = (int64_t)a.tiles * a.splits, blocks = JOIN ? units : std::min<int64_t>(units, at_once);
+    return launch_clusters("hpsgd_gated_ffn_forward", kernel, dim3((unsigned)((PAIR ? 2 : 1) * blocks)), kFfnThreads, S::kSmem, PAIR ? 2 : JOIN ? a.splits : 1, s, mx, mw, a);
 }
 
 template <bool JOIN>
 int forward_shape(const FfnPlan& p, const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
 {
     switch (p.bn) {
-    case 16: return forward_launch<16, JOIN>(mx, mw, a, sms, s);
-    case 32: return forward_launch<32, JOIN>(mx, mw, a, sms, s);
-    case 64: return forward_launch<64, JOIN>(mx, mw, a, sms, s);
-    default: return forward_launch<128, JOIN>(mx, mw, a, sms, s);
+    case 16: return forward_launch<16, false, JOIN>(mx, mw, a, sms, s);
+    case 32: return forward_launch<32, false, JOIN>(mx, mw, a, sms, s);
+    case 64: return forward_launch<64, false, JOIN>(mx, mw, a, sms, s);
+    case 128: return forward_launch<128, false, JOIN>(mx, mw, a, sms, s);
+    default: return forward_launch<kPairTokens, true, false>(mx, mw, a, sms, s);
     }
 }
 
@@ -580,7 +636,7 @@ int hpsgd_gated_ffn_forward(const hpsgd_gated_ffn_forward_args* args, void* stre
     OPS_TRY(device_sms(&sms));
     const FfnPlan plan = plan_of(p.M, p.N, p.K);
     CUtensorMap mx, mw;
-    OPS_TRY(make_map(what, &mx, p.x, p.ldx, p.M, p.K, plan.bn));
+    OPS_TRY(make_map(what, &mx, p.x, p.ldx, p.M, p.K, plan.pair ? plan.bn / 2 : plan.bn));
     OPS_TRY(make_map(what, &mw, p.w, p.ldw, 2 * p.N, p.K, kLanes));
     FfnArgs a{};
     a.out = FfnOut{(int)p.N, p.act, static_cast<uint8_t*>(p.z8), p.z_scale, p.z, static_cast<__nv_bfloat16*>(p.gu), p.ldz8, p.ldsz, p.ldz, p.ldgu,
