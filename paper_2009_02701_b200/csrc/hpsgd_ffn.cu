@@ -21,8 +21,8 @@ HPSGD_HIDDEN int stall_mode();
 namespace {
 
 constexpr int kSms = 148;
-constexpr int kFfnThreads = 384;           // copies, products, scales, one idle warp; eight warps for results
-constexpr int kChunk = 8;                  // columns that go through shared memory at a time, for each half of the eight warps
+constexpr int kGroups = 4;                 // of warps for results: each has a quarter of the tokens, and its four warps the 128 features of them
+constexpr int kFfnThreads = 128 + 128 * kGroups;      // copies, products, scales, one idle warp; and those
 
 __device__ unsigned int g_ffn_timeouts;    // blocks whose wait ran out since the last report
 
@@ -41,7 +41,8 @@ struct FfnShape {
     static constexpr int kScaleCols = 4 * kParts;
     static constexpr int kCols = kAccs * 2 * BN + (kPlaces + 1) * kScaleCols;
     static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static constexpr int kBytesOut = 2 * 2 * kChunk * kLanes * 4;        // two halves, two sums
+    static constexpr int kMine = BN / kGroups;                           // tokens of a group of warps
+    static constexpr int kBytesOut = 2 * 2 * kGroups * 4 * kMine * 4;    // largest magnitudes by warp: of two tiles in turn, of all and of the finite
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kPlaces * kBytesS + kBytesOut + 256;
 };
 
@@ -180,7 +181,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
     extern __shared__ uint8_t raw[];
     uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* const scales = smem + S::kStages * S::kStageBytes;
-    float* const out = reinterpret_cast<float*>(scales + S::kPlaces * S::kBytesS);
+    uint32_t* const tops = reinterpret_cast<uint32_t*>(scales + S::kPlaces * S::kBytesS);
     uint64_t* const bars = reinterpret_cast<uint64_t*>(scales + S::kPlaces * S::kBytesS + S::kBytesOut);
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int given_up;
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         }
         for (int s = 0; s < S::kAccs; ++s) {
             barrier_init(acc_full + s * 8, 1);
-            barrier_init(acc_empty + s * 8, PAIR ? 16 : 8);          // the warps that read it
+            barrier_init(acc_empty + s * 8, (PAIR ? 2 : 1) * 4 * kGroups);      // the warps that read it
         }
         barrier_init(drained, 1);
         given_up = 0;
@@ -332,18 +333,17 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
             }
         }
     } else if (warp >= 4) {
-        // Two warps for each quarter of the lanes, half of the columns each.
-        constexpr int kHalf = BN / 2;
-        const int part = warp & 3, half = (warp >> 2) - 1, c0 = half * kHalf;
+        // A warp has 32 features and a group's tokens.  First all of them go through the activation, to registers, so that the accumulator is free for the next
+        // tile's products; then, with the largest magnitudes of the group's four warps, which make a block, through the rounding.
+        constexpr int kMine = S::kMine, kC = kMine < 8 ? kMine : 8, kWords = (kMine + 31) / 32;
+        const int part = warp & 3, group = __shfl_sync(0xFFFFFFFFu, (warp >> 2) - 1, 0), c0 = group * kMine;
         const uint32_t mine = tmem + c0 + ((uint32_t)part << 21);
-        float* const staged = out + half * (2 * kChunk * kLanes);          // [sum][column][lane]
-        // the four warps of this half
-        const auto together = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(half + 1) : "memory"); };
+        // the four warps of this group
         const auto all_four = [&](bool yes) {
             uint32_t all;
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                          : "=r"(all)
-                         : "r"((uint32_t)yes), "r"(half + 1)
+                         : "r"((uint32_t)yes), "r"(group + 1)
                          : "memory");
             return all != 0;
         };
@@ -359,38 +359,119 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
         for (int u = first; u < units; u += stride, ++done) {
             const FfnUnit x = ffn_unit<BN, PAIR>(a, u, rank);
             const int acc = done % S::kAccs;
-            // the four warps of a half wait for one another below, so they go on together or not at all
+            // the four warps of a group wait for one another below, so they go on together or not at all
             if (!all_four(wait(acc_full + acc * 8, done / S::kAccs & 1))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t src = mine + acc * 2 * BN;
-#pragma unroll 1
-            for (int c = 0; c < kHalf; c += kChunk) {
-                float g[kChunk], v[kChunk];
-                load_columns<kChunk>(src + c, g);
-                load_columns<kChunk>(src + BN + c, v);
-                loads_done<kChunk>(g);
-                loads_done<kChunk>(v);
-                if (c + kChunk == kHalf) accumulator_read(acc);
-                // [column][lane]: a part's own place where this block's stages were (its only unit's products have read them), or the room for results
-                float* const to = (JOIN ? reinterpret_cast<float*>(smem) + (c0 + c) * kLanes : staged) + part * 32 + lane;
-                constexpr int kOther = JOIN ? BN * kLanes : kChunk * kLanes;
+            if constexpr (JOIN) {                    // [sum][column][lane], where this block's stages were (its only unit's products have read them)
+                float* const to = reinterpret_cast<float*>(smem) + c0 * kLanes + part * 32 + lane;
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) {
-                    to[j * kLanes] = g[j];
-                    to[j * kLanes + kOther] = v[j];
-                }
-                if constexpr (!JOIN) {
-                    together();
+                for (int c = 0; c < kMine; c += kC) {
+                    float g[kC], v[kC];
+                    load_columns<kC>(src + c, g);
+                    load_columns<kC>(src + BN + c, v);
+                    loads_done<kC>(g);
+                    loads_done<kC>(v);
 #pragma unroll
-                    for (int j = 0; j < kChunk / 4; ++j) {
-                        const int col = part * (kChunk / 4) + j, m = x.m0 + c0 + c + col;
-                        const float4* const p = reinterpret_cast<const float4*>(staged + col * kLanes) + lane;
-                        if (m < a.M) finish(a.out, m, x.n0, p[0], p[kChunk * kLanes / 4]);
+                    for (int j = 0; j < kC; ++j) {
+                        to[(c + j) * kLanes] = g[j];
+                        to[(c + j) * kLanes + BN * kLanes] = v[j];
                     }
-                    together();                      // before the next columns take their place
+                }
+                accumulator_read(acc);
+            } else {
+                const FfnOut& o = a.out;
+                const int n = x.n0 + part * 32 + lane, m0 = x.m0 + c0, cols = a.M - m0;
+                const bool in = n < o.N;
+                float z[kMine];
+                uint32_t top[kWords];                // lane l's: of columns l, l + 32
+#pragma unroll
+                for (int c = 0; c < kMine; c += kC) {
+                    float g[kC], v[kC];
+                    load_columns<kC>(src + c, g);
+                    load_columns<kC>(src + BN + c, v);
+                    loads_done<kC>(g);
+                    loads_done<kC>(v);
+                    if (c + kC == kMine) accumulator_read(acc);
+                    if (o.gu) {
+#pragma unroll
+                        for (int j = 0; j < kC; ++j) {
+                            __nv_bfloat16* const row = o.gu + (m0 + c + j) * o.ldgu;
+                            if (in && c + j < cols) {
+                                row[n] = __float2bfloat16_rn(g[j]);
+                                row[o.N + n] = __float2bfloat16_rn(v[j]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kC; ++j) {
+                        const float y = in ? __fmul_rn(activation(g[j], o.act), v[j]) : 0.f;
+                        z[c + j] = y;
+                        const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fabsf(y)));
+                        if (lane == ((c + j) & 31)) top[(c + j) >> 5] = t;
+                    }
+                }
+                if (o.z) {
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j)
+                        if (in && j < cols) {
+                            if (o.z_bf16) static_cast<__nv_bfloat16*>(o.z)[(m0 + j) * o.ldz + n] = __float2bfloat16_rn(z[j]);
+                            else static_cast<float*>(o.z)[(m0 + j) * o.ldz + n] = z[j];
+                        }
+                }
+                if (!o.z8) continue;
+                // [turn][finite][group][warp][column]
+                uint32_t* const place = tops + (done & 1) * (2 * kGroups * 4 * kMine) + group * (4 * kMine);
+                const auto exchange = [&](uint32_t* at) {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i)
+                        if (i * 32 + lane < kMine) at[part * kMine + i * 32 + lane] = top[i];
+                    all_four(true);
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        const int col = min(i * 32 + lane, kMine - 1);
+                        top[i] = max(max(at[col], at[kMine + col]), max(at[2 * kMine + col], at[3 * kMine + col]));
+                    }
+                };
+                exchange(place);
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) odd = odd || top[i] >= 0x7F800000u;
+                if (__any_sync(0xFFFFFFFFu, odd)) {  // (alike in the four warps) values that are not finite do not count, and become NaN
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) {
+                        const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(finite_magnitude(z[j])));
+                        if (lane == (j & 31)) top[j >> 5] = t;
+                        if (!finite(z[j])) z[j] = __uint_as_float(0x7FC00000u);
+                    }
+                    exchange(place + kGroups * 4 * kMine);
+                }
+                float inverse[kWords];
+                const int b = x.n0 / kBlock;
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) {
+                    const int byte = scale_byte(__uint_as_float(top[i])), col = i * 32 + lane;
+                    inverse[i] = scale_inverse(byte);
+                    if (part == 0 && col < kMine && col < cols && x.n0 < o.N) {
+                        uint8_t* const s = o.zs + scale_index(b, m0 + col, o.ldzs);
+                        *s = (uint8_t)byte;
+                        if (b == (o.N - 1) / kBlock)      // zeros behind the row's last block
+                            for (int k = 1; (b + k) & 3; ++k) s[k] = 0;
+                    }
+                }
+                const bool stored = n < (o.N + 15) / 16 * 16;
+#pragma unroll
+                for (int j = 0; j < kMine; j += 2) {
+                    unsigned short two;
+                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;"
+                        : "=h"(two)
+                        : "f"(__fmul_rn(z[j + 1], __shfl_sync(0xFFFFFFFFu, inverse[(j + 1) >> 5], (j + 1) & 31))),
+                          "f"(__fmul_rn(z[j], __shfl_sync(0xFFFFFFFFu, inverse[j >> 5], j & 31))));
+                    uint8_t* const row = o.z8 + (m0 + j) * o.ldz8;
+                    if (stored && j < cols) row[n] = (uint8_t)two;
+                    if (stored && j + 1 < cols) row[o.ldz8 + n] = (uint8_t)(two >> 8);
                 }
             }
-            __syncwarp();
         }
     }
     __syncwarp();

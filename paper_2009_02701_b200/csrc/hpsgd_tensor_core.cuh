@@ -163,7 +163,9 @@ template <int C>
 __device__ __forceinline__ void load_columns(uint32_t tmem, float* x)
 {
     uint32_t* r = reinterpret_cast<uint32_t*>(x);
-    if constexpr (C == 8)
+    if constexpr (C == 4)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(tmem));
+    else if constexpr (C == 8)
         asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                      : "r"(tmem));
