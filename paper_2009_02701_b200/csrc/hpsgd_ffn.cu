@@ -3,14 +3,18 @@
 //
 // Forward, z = act(x Wg^T) * (x Wu^T): the product of hpsgd_gemm.cu with two accumulators, whose lanes are the same 128 features: the gate's rows
 // of the weights on one, those of what it gates on the other, tokens on the columns of both.  A stage of shared memory has 128 k of both weights and of
-// the tokens, so the tokens are read once for the two.  What leaves: eight columns of both accumulators go through shared memory, so that a warp has
-// the 128 features of one token, which are a block of the result: their activation, the block's largest magnitude and its codes stay in the warp, and
-// 128 bytes of codes are written at once; the sums themselves, which the backward pass needs, in bf16.
+// the tokens, so the tokens are read once for the two.  With many tokens two SMs work on one tile of 256 features x 224 tokens (cta_group::2), whose two times 224
+// accumulator columns and scales are the whole of tensor memory.
+//
+// Bound by what feeds the tensor cores out of L2 and by the power cap with long sums (8192 x 8192 x 2048: 219 us, 2.5 PFLOP/s), and with short ones by what the sums go
+// through: activation, product, the block's largest magnitude, rounding, 33 instructions for each.  Sixteen warps do that, from tensor memory to registers in one
+// go, so that the accumulator is free for the next products before anything is rounded.  (Eight warps that took eight columns at a time through
+// shared memory, for 128 features of a token to a warp, took 443 us.)
 #include "hpsgd_quantize.cuh"
 #include "hpsgd_tensor_core.cuh"
 
 #include <algorithm>
-#include <cstdlib>
+#include <type_traits>
 
 namespace hpsgd {
 namespace ops {
@@ -49,7 +53,6 @@ struct FfnShape {
 // Where a token's results go.
 struct FfnOut {
     int N;
-    int act;
     uint8_t* z8;
     uint8_t* zs;
     void* z;
@@ -74,21 +77,23 @@ constexpr float kGelu1 = 1.59576912f, kGelu3 = 0.044715f;      // 2 sqrt(2 / pi)
 
 __device__ __forceinline__ float sigmoid(float x) { return reciprocal(__fadd_rn(1.f, exp2_of(__fmul_rn(x, -kLog2e)))); }
 
-__device__ __forceinline__ float activation(float g, int act)
+template <int ACT>
+__device__ __forceinline__ float activation(float g)
 {
-    const float w = act == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, __fmul_rn(g, g)), g, g));
+    const float w = ACT == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, __fmul_rn(g, g)), g, g));
     return __fmul_rn(g, sigmoid(w));
 }
 
 // act(g) and its derivative: with s = sigmoid(w), s + g s (1 - s) w'.
-__device__ __forceinline__ void activation(float g, int act, float& value, float& slope)
+template <int ACT>
+__device__ __forceinline__ void activation(float g, float& value, float& slope)
 {
     const float g2 = __fmul_rn(g, g);
-    const float w = act == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, g2), g, g));
-    const float dw = act == HPSGD_SILU ? 1.f : __fmul_rn(kGelu1, __fmaf_rn(3.f * kGelu3, g2, 1.f));
+    const float w = ACT == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, g2), g, g));
     const float e = exp2_of(fminf(__fmul_rn(w, -kLog2e), 126.f)), s = reciprocal(__fadd_rn(1.f, e));
     value = __fmul_rn(g, s);
-    slope = __fmaf_rn(__fmul_rn(value, __fmul_rn(e, s)), dw, s);
+    const float t = __fmul_rn(value, __fmul_rn(e, s));
+    slope = ACT == HPSGD_SILU ? __fadd_rn(t, s) : __fmaf_rn(t, __fmul_rn(kGelu1, __fmaf_rn(3.f * kGelu3, g2, 1.f)), s);
 }
 
 // ---------------------------------------------------------------------------- what a warp does with a token's 128 features
@@ -103,6 +108,7 @@ __device__ __forceinline__ void store_bf16(__nv_bfloat16* p, const float* v, int
 }
 
 // Lane l has the sums g, u of features n0 + 4 l .. + 3 of token m.
+template <int ACT>
 __device__ __forceinline__ void finish(const FfnOut& a, int m, int n0, float4 g4, float4 u4)
 {
     const int lane = threadIdx.x & 31, n = n0 + lane * 4, left = a.N - n;
@@ -114,7 +120,7 @@ __device__ __forceinline__ void finish(const FfnOut& a, int m, int n0, float4 g4
     }
     float z[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] = j < left ? __fmul_rn(activation(g[j], a.act), u[j]) : 0.f;
+    for (int j = 0; j < 4; ++j) z[j] = j < left ? __fmul_rn(activation<ACT>(g[j]), u[j]) : 0.f;
     if (a.z) {
         if (a.z_bf16) store_bf16(static_cast<__nv_bfloat16*>(a.z) + m * a.ldz + n, z, left, a.wide_z);
         else {
@@ -173,7 +179,7 @@ __device__ __forceinline__ FfnUnit ffn_unit(const FfnArgs& a, int u, int rank)
 }
 
 // JOIN: the blocks of a cluster have a tile's parts along k, one each, and add them out of each other's shared memory in their order.
-template <int BN, bool PAIR, bool JOIN>
+template <int BN, bool PAIR, bool JOIN, int ACT>
 __global__ void __launch_bounds__(kFfnThreads, 1)
     gated_ffn_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ FfnArgs a)
 {
@@ -385,32 +391,43 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
                 const bool in = n < o.N;
                 float z[kMine];
                 uint32_t top[kWords];                // lane l's: of columns l, l + 32
+                // ALL: every token and feature of the tile is there; KEEP: the sums are kept.  (A column's offset is the same in all threads, so it is added on
+                // the way to memory.)
+                const auto through = [&](auto all, auto keep) {
+                    constexpr bool ALL = decltype(all)::value, KEEP = decltype(keep)::value;
+                    uint16_t* const to_g = reinterpret_cast<uint16_t*>(o.gu) + m0 * o.ldgu + n;
+                    uint16_t* const to_u = to_g + o.N;
 #pragma unroll
-                for (int c = 0; c < kMine; c += kC) {
-                    float g[kC], v[kC];
-                    load_columns<kC>(src + c, g);
-                    load_columns<kC>(src + BN + c, v);
-                    loads_done<kC>(g);
-                    loads_done<kC>(v);
-                    if (c + kC == kMine) accumulator_read(acc);
-                    if (o.gu) {
+                    for (int c = 0; c < kMine; c += kC) {
+                        float g[kC], v[kC];
+                        load_columns<kC>(src + c, g);
+                        load_columns<kC>(src + BN + c, v);
+                        loads_done<kC>(g);
+                        loads_done<kC>(v);
+                        if (c + kC == kMine) accumulator_read(acc);
 #pragma unroll
-                        for (int j = 0; j < kC; ++j) {
-                            __nv_bfloat16* const row = o.gu + (m0 + c + j) * o.ldgu;
-                            if (in && c + j < cols) {
-                                row[n] = __float2bfloat16_rn(g[j]);
-                                row[o.N + n] = __float2bfloat16_rn(v[j]);
+                        for (int j = 0; j < kC; j += 2) {
+                            if constexpr (KEEP) {
+                                const uint32_t gg = pack_bf16(g[j], g[j + 1]), uu = pack_bf16(v[j], v[j + 1]);
+                                const int64_t at = (c + j) * o.ldgu, next = (c + j + 1) * o.ldgu;
+                                if (ALL || (in && c + j < cols)) to_g[at] = (uint16_t)gg, to_u[at] = (uint16_t)uu;
+                                if (ALL || (in && c + j + 1 < cols)) to_g[next] = (uint16_t)(gg >> 16), to_u[next] = (uint16_t)(uu >> 16);
                             }
                         }
-                    }
 #pragma unroll
-                    for (int j = 0; j < kC; ++j) {
-                        const float y = in ? __fmul_rn(activation(g[j], o.act), v[j]) : 0.f;
-                        z[c + j] = y;
-                        const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fabsf(y)));
-                        if (lane == ((c + j) & 31)) top[(c + j) >> 5] = t;
+                        for (int j = 0; j < kC; ++j) {
+                            const float y = __fmul_rn(activation<ACT>(g[j]), v[j]);
+                            z[c + j] = ALL || in ? y : 0.f;
+                            const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fabsf(z[c + j])));
+                            if (lane == ((c + j) & 31)) top[(c + j) >> 5] = t;
+                        }
                     }
-                }
+                };
+                const bool all = x.m0 + BN <= a.M && x.n0 + kLanes <= o.N;
+                using Yes = std::true_type;
+                using No = std::false_type;
+                if (all) o.gu ? through(Yes{}, Yes{}) : through(Yes{}, No{});
+                else o.gu ? through(No{}, Yes{}) : through(No{}, No{});
                 if (o.z) {
 #pragma unroll
                     for (int j = 0; j < kMine; ++j)
@@ -459,17 +476,21 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
                             for (int k = 1; (b + k) & 3; ++k) s[k] = 0;
                     }
                 }
-                const bool stored = n < (o.N + 15) / 16 * 16;
-#pragma unroll
-                for (int j = 0; j < kMine; j += 2) {
+                const auto two_codes = [&](int j) {  // of columns j, j + 1
                     unsigned short two;
                     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;"
                         : "=h"(two)
                         : "f"(__fmul_rn(z[j + 1], __shfl_sync(0xFFFFFFFFu, inverse[(j + 1) >> 5], (j + 1) & 31))),
                           "f"(__fmul_rn(z[j], __shfl_sync(0xFFFFFFFFu, inverse[j >> 5], j & 31))));
-                    uint8_t* const row = o.z8 + (m0 + j) * o.ldz8;
-                    if (stored && j < cols) row[n] = (uint8_t)two;
-                    if (stored && j + 1 < cols) row[o.ldz8 + n] = (uint8_t)(two >> 8);
+                    return two;
+                };
+                uint8_t* const to = o.z8 + m0 * o.ldz8 + n;
+                const bool stored = n < (o.N + 15) / 16 * 16;
+#pragma unroll
+                for (int j = 0; j < kMine; j += 2) {
+                    const unsigned short two = two_codes(j);
+                    if (all || (stored && j < cols)) to[j * o.ldz8] = (uint8_t)two;
+                    if (all || (stored && j + 1 < cols)) to[(j + 1) * o.ldz8] = (uint8_t)(two >> 8);
                 }
             }
         }
@@ -494,7 +515,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
                 g = make_float4(__fadd_rn(g.x, g1.x), __fadd_rn(g.y, g1.y), __fadd_rn(g.z, g1.z), __fadd_rn(g.w, g1.w));
                 v = make_float4(__fadd_rn(v.x, v1.x), __fadd_rn(v.y, v1.y), __fadd_rn(v.z, v1.z), __fadd_rn(v.w, v1.w));
             }
-            finish(a.out, x.m0 + c, x.n0, g, v);
+            finish<ACT>(a.out, x.m0 + c, x.n0, g, v);
         }
         __syncwarp();
         cluster_sync();                              // this block's memory stays until the others have read it
@@ -511,7 +532,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
 // tile of 128 x 128 of the result, which is a whole block of each of its rows and columns.
 struct FfnBackward {
     QuantOut out;
-    int N, act;
+    int N;
     const __nv_bfloat16* gu;
     const void* dz;
     __nv_bfloat16* dgu;
@@ -519,8 +540,64 @@ struct FfnBackward {
     int wide, wide_out;                        // eight neighbours may be loaded, stored at once
 };
 
-template <typename T>
+// Where N is a multiple of the block, a block of threads takes a tile of dg and the one of du that comes from the same sums: these are read, and the activation
+// is computed, once; du waits in shared memory, each thread's own, while dg is written (4096 x 4096 from bf16: 53 us; tile by tile 64).
+template <typename T, int ACT>
 __global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_kernel(const FfnBackward a)
+{
+    constexpr int kRows = kPatchRows;
+    extern __shared__ __align__(16) float4 waiting[];      // [half a row][thread]
+    __shared__ QuantRoom room;
+    const int lane = threadIdx.x & 15, patch = threadIdx.x >> 4;
+    const int tiles_c = a.N / kTile;
+    const int br = (int)(blockIdx.x / (unsigned)tiles_c), bc = (int)(blockIdx.x % (unsigned)tiles_c);
+    const int row0 = br * kTile + patch * kRows, col0 = bc * kTile + lane * 8, rows = (int)a.out.rows - row0;
+    const T* const dz = static_cast<const T*>(a.dz);
+    after_previous();
+    f8 x[kRows];
+    Raw8<__nv_bfloat16> g[kRows], u[kRows];
+    Raw8<T> d[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        const int here = k < rows ? 8 : 0;
+        const int64_t m = row0 + k;
+        g[k].load(a.gu + m * a.ldgu + col0, a.wide && here == 8, here);
+        u[k].load(a.gu + m * a.ldgu + a.N + col0, a.wide && here == 8, here);
+        d[k].load(dz + m * a.lddz + col0, a.wide && here == 8, here);
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        const f8 gk = g[k].values(), uk = u[k].values(), dk = d[k].values();
+        f8 y;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float value, slope;
+            activation<ACT>(gk.v[j], value, slope);
+            x[k].v[j] = __fmul_rn(__fmul_rn(dk.v[j], uk.v[j]), slope);
+            y.v[j] = __fmul_rn(dk.v[j], value);
+        }
+        waiting[2 * k * kQThreads + threadIdx.x] = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
+        waiting[(2 * k + 1) * kQThreads + threadIdx.x] = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
+    }
+    const auto write = [&](int col, int tile) {
+        if (a.dgu) {
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) store_some(a.dgu + (row0 + k) * a.lddgu + col, x[k], a.wide_out && k < rows, k < rows ? 8 : 0);
+        }
+        if (a.out.q || a.out.qt) quantize_tile<true>(a.out, room, x, br, tile);
+    };
+    write(col0, bc);
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        const float4 lo = waiting[2 * k * kQThreads + threadIdx.x], hi = waiting[(2 * k + 1) * kQThreads + threadIdx.x];
+        x[k] = f8{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
+    }
+    write(a.N + col0, tiles_c + bc);
+}
+
+// Any N: a tile of the result by itself, which may have columns of both.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_any_kernel(const FfnBackward a)
 {
     constexpr int kRows = kPatchRows;
     __shared__ QuantRoom room;
@@ -534,7 +611,7 @@ __global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_kernel(const 
     f8 x[kRows];
     const auto gradient = [&](float g, float u, float d, bool of_gate) {
         float value, slope;
-        activation(g, a.act, value, slope);
+        activation<ACT>(g, value, slope);
         return of_gate ? __fmul_rn(__fmul_rn(d, u), slope) : __fmul_rn(d, value);
     };
     const bool of_gate = col0 < a.N;
@@ -577,6 +654,23 @@ __global__ void __launch_bounds__(kQThreads, 2) gated_ffn_backward_kernel(const 
     if (a.out.q || a.out.qt) quantize_tile<true>(a.out, room, x, br, bc);
 }
 
+template <typename T, int ACT>
+int backward_launch(const FfnBackward& a, cudaStream_t s)
+{
+    const char* what = "hpsgd_gated_ffn_backward";
+    const int64_t tiles_r = (a.out.rows + kTile - 1) / kTile;
+    if (a.N % kTile != 0) return launch_early(what, gated_ffn_backward_any_kernel<T, ACT>, dim3((unsigned)(tiles_r * ((a.out.cols + kTile - 1) / kTile))), kQThreads, 0, s, a);
+    constexpr int kSmem = kTile * kTile * 4;
+    static bool ready[64] = {};
+    int dev = 0;
+    OPS_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !ready[dev]) {
+        OPS_CUDA(cudaFuncSetAttribute(gated_ffn_backward_kernel<T, ACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        if (dev < 64) ready[dev] = true;
+    }
+    return launch_early(what, gated_ffn_backward_kernel<T, ACT>, dim3((unsigned)(tiles_r * (a.N / kTile))), kQThreads, kSmem, s, a);
+}
+
 // ---------------------------------------------------------------------------- host side
 struct FfnPlan {
     int bn, pair, tiles_n, tiles, splits, per_split, longer;
@@ -584,9 +678,13 @@ struct FfnPlan {
 
 constexpr int kPairTokens = 224;           // 2 x 224 accumulator columns and four groups' scales are the 512 columns of tensor memory
 
-// The least power of two that holds all tokens, 128 at most, or 224 on pairs of SMs, whichever takes fewer rounds of work.  Few tiles are split
-// along k over the blocks of a cluster, as in hpsgd_gemm.cu.
-FfnPlan plan_of(int64_t M, int64_t N, int64_t K)
+// The least power of two that holds all tokens, 128 at most; or 224 on pairs of SMs, which takes fewer bytes out of L2 for a product, but keeps both SMs from the
+// next tile's products while the sums go through the activation.  In a round of tiles an SM spent 0.47 us for each k block and 1.2 us more (3.4 where the
+// sums are kept) on 128 tokens, and 0.78 and 1.2 (6.3) on its half of a pair's: 8192 x 8192 x 2048 242 us on single SMs, 219 on pairs; 4096 x 4096 x 1024 with
+// the sums kept 53 and 66.  The fewer of these, rounds counted whole.
+//
+// Few tiles are split along k over the blocks of a cluster, as in hpsgd_gemm.cu.
+FfnPlan plan_of(int64_t M, int64_t N, int64_t K, bool keep)
 {
     const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     FfnPlan p{};
@@ -595,8 +693,7 @@ FfnPlan plan_of(int64_t M, int64_t N, int64_t K)
     int64_t tiles_n = up(N, kLanes), tiles = tiles_n * up(M, p.bn);
     if (M > 128) {
         const int64_t pairs_n = up(N, 2 * kLanes), pairs = pairs_n * up(M, kPairTokens);
-        const char* e = getenv("FFN_PAIR");
-        if (e ? atoi(e) : (double)up(pairs, kSms / 2) * 1.4 < (double)up(tiles, kSms)) {
+        if ((double)up(pairs, kSms / 2) * (78.0 * blocks + (keep ? 630.0 : 120.0)) < (double)up(tiles, kSms) * (47.0 * blocks + (keep ? 340.0 : 120.0))) {
             p.pair = 1;
             p.bn = kPairTokens;
             tiles_n = pairs_n;
@@ -612,11 +709,11 @@ FfnPlan plan_of(int64_t M, int64_t N, int64_t K)
     return p;
 }
 
-template <int BN, bool PAIR, bool JOIN>
-int forward_launch(const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
+template <int BN, bool PAIR, bool JOIN, int ACT>
+int forward_act(const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
 {
     using S = FfnShape<BN, PAIR>;
-    const auto kernel = gated_ffn_kernel<BN, PAIR, JOIN>;
+    const auto kernel = gated_ffn_kernel<BN, PAIR, JOIN, ACT>;
     // Per device: the blocks (or pairs) that it holds at a time; pairs need both their SMs in one GPU cluster, so there may be fewer than half the SMs.
     static int workers[64] = {};
     int dev = 0;
@@ -645,15 +742,21 @@ int forward_launch(const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& 
     return launch_clusters("hpsgd_gated_ffn_forward", kernel, dim3((unsigned)((PAIR ? 2 : 1) * blocks)), kFfnThreads, S::kSmem, PAIR ? 2 : JOIN ? a.splits : 1, s, mx, mw, a);
 }
 
+template <int BN, bool PAIR, bool JOIN>
+int forward_launch(int act, const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
+{
+    return act == HPSGD_SILU ? forward_act<BN, PAIR, JOIN, HPSGD_SILU>(mx, mw, a, sms, s) : forward_act<BN, PAIR, JOIN, HPSGD_GELU>(mx, mw, a, sms, s);
+}
+
 template <bool JOIN>
-int forward_shape(const FfnPlan& p, const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
+int forward_shape(const FfnPlan& p, int act, const CUtensorMap& mx, const CUtensorMap& mw, const FfnArgs& a, int sms, cudaStream_t s)
 {
     switch (p.bn) {
-    case 16: return forward_launch<16, false, JOIN>(mx, mw, a, sms, s);
-    case 32: return forward_launch<32, false, JOIN>(mx, mw, a, sms, s);
-    case 64: return forward_launch<64, false, JOIN>(mx, mw, a, sms, s);
-    case 128: return forward_launch<128, false, JOIN>(mx, mw, a, sms, s);
-    default: return forward_launch<kPairTokens, true, false>(mx, mw, a, sms, s);
+    case 16: return forward_launch<16, false, JOIN>(act, mx, mw, a, sms, s);
+    case 32: return forward_launch<32, false, JOIN>(act, mx, mw, a, sms, s);
+    case 64: return forward_launch<64, false, JOIN>(act, mx, mw, a, sms, s);
+    case 128: return forward_launch<128, false, JOIN>(act, mx, mw, a, sms, s);
+    default: return forward_launch<kPairTokens, true, false>(act, mx, mw, a, sms, s);
     }
 }
 
@@ -715,12 +818,12 @@ int hpsgd_gated_ffn_forward(const hpsgd_gated_ffn_forward_args* args, void* stre
     OPS_TRY(check_plain(what, "gu", p.gu, &p.ldgu, 2 * p.N, 2, 4, &wide_gu));
     int sms = 0;
     OPS_TRY(device_sms(&sms));
-    const FfnPlan plan = plan_of(p.M, p.N, p.K);
+    const FfnPlan plan = plan_of(p.M, p.N, p.K, p.gu != nullptr);
     CUtensorMap mx, mw;
     OPS_TRY(make_map(what, &mx, p.x, p.ldx, p.M, p.K, plan.pair ? plan.bn / 2 : plan.bn));
     OPS_TRY(make_map(what, &mw, p.w, p.ldw, 2 * p.N, p.K, kLanes));
     FfnArgs a{};
-    a.out = FfnOut{(int)p.N, p.act, static_cast<uint8_t*>(p.z8), p.z_scale, p.z, static_cast<__nv_bfloat16*>(p.gu), p.ldz8, p.ldsz, p.ldz, p.ldgu,
+    a.out = FfnOut{(int)p.N, static_cast<uint8_t*>(p.z8), p.z_scale, p.z, static_cast<__nv_bfloat16*>(p.gu), p.ldz8, p.ldsz, p.ldz, p.ldgu,
                    p.z_dtype == HPSGD_BF16, wide_z, wide_gu};
     a.M = (int)p.M; a.K = (int)p.K;
     a.tiles_n = plan.tiles_n; a.tiles = plan.tiles; a.splits = plan.splits; a.per_split = plan.per_split; a.longer = plan.longer;
@@ -729,7 +832,7 @@ int hpsgd_gated_ffn_forward(const hpsgd_gated_ffn_forward_args* args, void* stre
     a.stall = stall_mode() ? 16 : 0;
     a.stall_odd = stall_mode() == 2;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return plan.splits > 1 ? forward_shape<true>(plan, mx, mw, a, sms, s) : forward_shape<false>(plan, mx, mw, a, sms, s);
+    return plan.splits > 1 ? forward_shape<true>(plan, p.act, mx, mw, a, sms, s) : forward_shape<false>(plan, p.act, mx, mw, a, sms, s);
 }
 
 int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* stream)
@@ -756,12 +859,11 @@ int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* st
     OPS_TRY(device_sms(&sms));
     FfnBackward a{};
     a.out = QuantOut{p.M, 2 * p.N, p.lddq, p.ldsdq, p.lddqt, p.ldsdqt, static_cast<uint8_t*>(p.dq), p.dq_scale, static_cast<uint8_t*>(p.dqt), p.dqt_scale};
-    a.N = (int)p.N; a.act = p.act; a.gu = static_cast<const __nv_bfloat16*>(p.gu); a.dz = p.dz; a.dgu = static_cast<__nv_bfloat16*>(p.dgu);
+    a.N = (int)p.N; a.gu = static_cast<const __nv_bfloat16*>(p.gu); a.dz = p.dz; a.dgu = static_cast<__nv_bfloat16*>(p.dgu);
     a.ldgu = p.ldgu; a.lddz = p.lddz; a.lddgu = p.lddgu; a.wide = wide; a.wide_out = wide_out;
-    const dim3 grid((unsigned)(((p.M + kTile - 1) / kTile) * ((2 * p.N + kTile - 1) / kTile)));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (p.dz_dtype == HPSGD_F32) return launch_early(what, gated_ffn_backward_kernel<float>, grid, kQThreads, 0, s, a);
-    return launch_early(what, gated_ffn_backward_kernel<__nv_bfloat16>, grid, kQThreads, 0, s, a);
+    if (p.dz_dtype == HPSGD_F32) return p.act == HPSGD_SILU ? backward_launch<float, HPSGD_SILU>(a, s) : backward_launch<float, HPSGD_GELU>(a, s);
+    return p.act == HPSGD_SILU ? backward_launch<__nv_bfloat16, HPSGD_SILU>(a, s) : backward_launch<__nv_bfloat16, HPSGD_GELU>(a, s);
 }
 
 }  // extern "C"
