@@ -14,8 +14,6 @@
 
 #include <algorithm>
 #include <type_traits>
-#include <cstdlib>
-#include <cstdio>
 
 namespace hpsgd {
 namespace ops {
@@ -25,19 +23,19 @@ constexpr int kSlab = 32;                           // channels of a block: two 
 constexpr int kSaved = 8;                           // rows that share a kept state
 constexpr int kMaxCluster = 8;
 
-// What a kernel holds: R rows a thread, W warps, S stages of A arrays in shared memory.  32-bit types take half the warps, for the room.
-template <typename T, int ROWS, int ARRAYS>
+// What a kernel holds: R rows a thread, W warps, S stages of A arrays in shared memory; PER_SM warps on an SM.
+template <typename T, int ROWS, int ARRAYS, int WARPS, int PER_SM>
 struct Form {
-    static constexpr int R = ROWS, A = ARRAYS, W = sizeof(T) == 2 ? 8 : 4, S = 2;
+    static constexpr int R = ROWS, A = ARRAYS, W = WARPS, S = 2;
     static constexpr int kThreads = 32 * W, kRows = 2 * R * W;                       // rows of a block's piece of a chunk
     static constexpr int kLine = 2 * kSlab * (int)sizeof(T);                         // a row of each half warp's group, side by side
     static constexpr int kWarpBytes = A * R * kLine, kStageBytes = W * kWarpBytes;
-    static constexpr int kPerSm = sizeof(T) == 2 ? 2 : 3;
+    static constexpr int kPerSm = PER_SM / W;
 };
 
 struct Sequences {
     int rows, cols, count, each;                    // each: rows of a sequence where there are no offsets
-    int walkers;
+    int walkers, share;                             // rows of a walker's share
     const int64_t* offsets;
 
     // First row of sequence s; s = count gives the end of the last one.
@@ -69,7 +67,7 @@ struct Share {
     int first, last, row0, row1;                    // sequences [first, last), rows [row0, row1)
     __device__ __forceinline__ Share(const Sequences& q, int walker)
     {
-        const auto border = [&](int w) { return (int)((int64_t)q.rows * w / q.walkers); };
+        const auto border = [&](int w) { return min(q.rows, w * q.share); };
         first = walker == 0 ? 0 : q.at_or_behind(border(walker));
         last = walker + 1 == q.walkers ? q.count : q.at_or_behind(border(walker + 1));
         last = max(first, last);
@@ -120,8 +118,9 @@ __device__ __forceinline__ pair load_pair(const __nv_bfloat16* p)
     widen_pair(*reinterpret_cast<const uint32_t*>(p), lo, hi);
     return make_pair(lo, hi);
 }
-__device__ __forceinline__ void store_pair(float* p, float lo, float hi) { *reinterpret_cast<float2*>(p) = make_float2(lo, hi); }
-__device__ __forceinline__ void store_pair(__nv_bfloat16* p, float lo, float hi) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(lo, hi); }
+// (written so that what is read from shared memory behind a store may be requested in front of it)
+__device__ __forceinline__ void store_pair(float* p, float lo, float hi) { asm volatile("st.global.v2.f32 [%0], {%1, %2};" ::"l"(p), "f"(lo), "f"(hi)); }
+__device__ __forceinline__ void store_pair(__nv_bfloat16* p, float lo, float hi) { asm volatile("st.global.b32 [%0], %1;" ::"l"(p), "r"(pack_bf16(lo, hi))); }
 
 // WIDE: the address allows both in one access.  `left` of them are there; ALL: both are.
 template <bool WIDE, bool ALL = false, typename T>
@@ -145,8 +144,7 @@ __device__ __forceinline__ void copy_async16(uint32_t to, const void* from, int 
 __device__ __forceinline__ void sigmoid(pair x, pair& s, pair& rest)
 {
     float lo, hi;
-    split(x, lo, hi);
-    lo = __fmul_rn(lo, -kLog2e), hi = __fmul_rn(hi, -kLog2e);
+    split(mul2(x, both(-kLog2e)), lo, hi);
     asm("min.NaN.f32 %0, %0, %1;" : "+f"(lo) : "f"(126.f));
     asm("min.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(126.f));
     const pair e = make_pair(exp2_of(lo), exp2_of(hi));
@@ -158,9 +156,9 @@ __device__ __forceinline__ void sigmoid(pair x, pair& s, pair& rest)
 __device__ __forceinline__ pair sigmoid(pair x)
 {
     float lo, hi;
-    split(x, lo, hi);
+    split(mul2(x, both(-kLog2e)), lo, hi);
     float d0, d1;
-    split(add2(make_pair(exp2_of(__fmul_rn(lo, -kLog2e)), exp2_of(__fmul_rn(hi, -kLog2e))), both(1.f)), d0, d1);
+    split(add2(make_pair(exp2_of(lo), exp2_of(hi)), both(1.f)), d0, d1);
     return make_pair(reciprocal(d0), reciprocal(d1));
 }
 
@@ -234,9 +232,11 @@ __device__ __forceinline__ pair exchange(Exchange<W>& x, int turn, const Map& mi
 #pragma unroll
             for (int w = 1; w < W; ++w) all = of_warp(w).behind(all);
             for (int r = half; r < blocks; r += 2) map_to_block(&x.block[turn][rank][lane], r, all);
+            // Only this warp has something to publish; a release by all of them waits for every store of theirs to device memory as well.
+            asm volatile("fence.acq_rel.cluster;" ::: "memory");
         }
         __syncwarp();
-        cluster_arrive();
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         Map before = identity();
         for (int w = 0; w < warp; ++w) before = of_warp(w).behind(before);
         cluster_wait();
@@ -329,14 +329,16 @@ struct ScanForward {
     int64_t ldf, ldv, ldo, ldy, ldh0, ldlast, ldsaved;
 };
 
-template <typename T, bool GATE>
-using ForwardForm = Form<T, 16, GATE ? 3 : 2>;
+// Blocks of a cluster wait for one another, and longest for the cluster's barrier: there a chunk is 16 rows a thread (8 in fp32) of eight warps.  By
+// themselves they are many, and small: eight rows a thread of four warps, so that there are twice as many warps to wait with.
+template <typename T, bool GATE, bool CLUSTER>
+using ForwardForm = Form<T, CLUSTER && sizeof(T) == 2 ? 16 : 8, GATE ? 3 : 2, CLUSTER ? 8 : 4, !CLUSTER && sizeof(T) == 2 ? 32 : 16>;
 
 // STAGED: rows of the inputs start on 16-byte boundaries and two outputs can be stored at once; else both are taken one by one, without a stage.
 template <typename T, bool GATE, bool STAGED, bool CLUSTER>
-__global__ void __launch_bounds__(ForwardForm<T, GATE>::kThreads, ForwardForm<T, GATE>::kPerSm) scan_forward_kernel(const ScanForward a)
+__global__ void __launch_bounds__(ForwardForm<T, GATE, CLUSTER>::kThreads, ForwardForm<T, GATE, CLUSTER>::kPerSm) scan_forward_kernel(const ScanForward a)
 {
-    using F = ForwardForm<T, GATE>;
+    using F = ForwardForm<T, GATE, CLUSTER>;
     constexpr int R = F::R;
     extern __shared__ __align__(16) uint8_t stages[];
     __shared__ alignas(16) Exchange<F::W> ex;
@@ -489,13 +491,13 @@ struct ScanBackward {
     int64_t ldf, ldv, ldo, ldh0, lddy, lddlast, lddf, lddv, lddo, lddh0, ldsaved;
 };
 
-template <typename T, bool GATE>
-using BackwardForm = Form<T, kSaved, GATE ? 4 : 3>;
+template <typename T, bool GATE, bool CLUSTER>
+using BackwardForm = Form<T, kSaved, GATE ? 4 : 3, CLUSTER ? 8 : 4, sizeof(T) == 2 ? 16 : CLUSTER ? 8 : 12>;
 
 template <typename T, bool GATE, bool STAGED, bool CLUSTER>
-__global__ void __launch_bounds__(BackwardForm<T, GATE>::kThreads, BackwardForm<T, GATE>::kPerSm) scan_backward_kernel(const ScanBackward a)
+__global__ void __launch_bounds__(BackwardForm<T, GATE, CLUSTER>::kThreads, BackwardForm<T, GATE, CLUSTER>::kPerSm) scan_backward_kernel(const ScanBackward a)
 {
-    using F = BackwardForm<T, GATE>;
+    using F = BackwardForm<T, GATE, CLUSTER>;
     constexpr int R = F::R;
     extern __shared__ __align__(16) uint8_t stages[];
     __shared__ alignas(16) Exchange<F::W> ex;
@@ -672,19 +674,23 @@ struct Plan {
     int slabs, walkers, blocks;
 };
 
-Plan plan_of(int64_t rows, int64_t cols, int64_t sequences, bool equal, int piece)
+// Walkers first: they wait for nobody (16384 x 2048 bf16 of 16 sequences: 66 and 107 us with 16 walkers; clusters of eight 117 and 170), but what a sequence
+// that is longer than a walker's share has more is waited for at the end, so without equal sequences each has two on the average.  Where they do not
+// fill half of the SMs' places, clusters, whose blocks share rows whatever the sequences are, as many as the device holds at once (65536 x 1024
+// of one sequence: 150 us with clusters of eight, 195 with four, 445 with two).
+template <int ALONE, int TOGETHER>
+Plan plan_of(int64_t rows, int64_t cols, int64_t sequences, bool equal)
 {
+    constexpr int64_t kAlone = 148 * 8, kTogether = 148 * 2;
     Plan p{};
     p.slabs = (int)((cols + kSlab - 1) / kSlab);
     p.walkers = p.blocks = 1;
-    const int64_t want = 2 * 148;
-    const auto more_walkers = [&]() {
-        while ((int64_t)p.slabs * p.blocks * p.walkers * 2 <= want && p.walkers * 2 <= sequences && rows > piece * p.blocks * p.walkers) p.walkers *= 2;
-    };
-    if (equal) more_walkers();
-    while ((int64_t)p.slabs * p.walkers * p.blocks * 2 <= want && p.blocks < kMaxCluster && rows > piece * p.blocks * p.walkers) p.blocks *= 2;
-    more_walkers();
-    if (const char* e = getenv("SCAN_PLAN")) sscanf(e, "%d,%d", &p.walkers, &p.blocks);
+    const int64_t most = equal ? sequences : (sequences + 1) / 2;
+    while ((int64_t)p.slabs * p.walkers * 2 <= kAlone && p.walkers * 2 <= most && rows > ALONE * p.walkers) p.walkers *= 2;
+    if ((int64_t)p.slabs * p.walkers * 2 > kAlone / 2 || rows <= ALONE * p.walkers * 2) return p;
+    p.walkers = 1;
+    while ((int64_t)p.slabs * p.blocks * 2 <= kTogether && p.blocks < kMaxCluster && rows > TOGETHER * p.blocks) p.blocks *= 2;
+    while ((int64_t)p.slabs * p.blocks * p.walkers * 2 <= kTogether && p.walkers * 2 <= most && rows > TOGETHER * p.blocks * p.walkers) p.walkers *= 2;
     return p;
 }
 
@@ -706,11 +712,12 @@ template <typename T, bool GATE, bool STAGED>
 int forward_launch(ScanForward& a, bool equal, cudaStream_t s)
 {
     const char* what = "hpsgd_gated_scan_forward";
-    using F = ForwardForm<T, GATE>;
-    const Plan p = plan_of(a.q.rows, a.q.cols, a.q.count, equal, F::kRows);
-    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers;
-    return p.blocks > 1 ? launch_scan<F, STAGED, scan_forward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
-                        : launch_scan<F, STAGED, scan_forward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
+    using Alone = ForwardForm<T, GATE, false>;
+    using Together = ForwardForm<T, GATE, true>;
+    const Plan p = plan_of<Alone::kRows, Together::kRows>(a.q.rows, a.q.cols, a.q.count, equal);
+    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers; a.q.share = (a.q.rows + p.walkers - 1) / p.walkers;
+    return p.blocks > 1 ? launch_scan<Together, STAGED, scan_forward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
+                        : launch_scan<Alone, STAGED, scan_forward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
 }
 template <typename T, bool GATE>
 int forward_gate(ScanForward& a, bool equal, bool staged, bool wide, cudaStream_t s)
@@ -732,17 +739,22 @@ template <typename T, bool GATE, bool STAGED>
 int backward_launch(ScanBackward& a, bool equal, cudaStream_t s)
 {
     const char* what = "hpsgd_gated_scan_backward";
-    using F = BackwardForm<T, GATE>;
-    const Plan p = plan_of(a.q.rows, a.q.cols, a.q.count, equal, F::kRows);
-    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers;
-    return p.blocks > 1 ? launch_scan<F, STAGED, scan_backward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
-                        : launch_scan<F, STAGED, scan_backward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
+    using Alone = BackwardForm<T, GATE, false>;
+    using Together = BackwardForm<T, GATE, true>;
+    const Plan p = plan_of<Alone::kRows, Together::kRows>(a.q.rows, a.q.cols, a.q.count, equal);
+    a.slabs = p.slabs; a.blocks = p.blocks; a.q.walkers = p.walkers; a.q.share = (a.q.rows + p.walkers - 1) / p.walkers;
+    return p.blocks > 1 ? launch_scan<Together, STAGED, scan_backward_kernel<T, GATE, STAGED, true>>(what, a, p, s)
+                        : launch_scan<Alone, STAGED, scan_backward_kernel<T, GATE, STAGED, false>>(what, a, p, s);
+}
+template <typename T, bool GATE>
+int backward_gate(ScanBackward& a, bool equal, bool staged, cudaStream_t s)
+{
+    return staged ? backward_launch<T, GATE, true>(a, equal, s) : backward_launch<T, GATE, false>(a, equal, s);
 }
 template <typename T>
 int backward_types(ScanBackward& a, bool equal, bool staged, cudaStream_t s)
 {
-    if (a.o) return staged ? backward_launch<T, true, true>(a, equal, s) : backward_launch<T, true, false>(a, equal, s);
-    return staged ? backward_launch<T, false, true>(a, equal, s) : backward_launch<T, false, false>(a, equal, s);
+    return a.o ? backward_gate<T, true>(a, equal, staged, s) : backward_gate<T, false>(a, equal, staged, s);
 }
 
 int64_t saved_stride(int64_t cols) { return (cols + 3) / 4 * 4; }
@@ -788,7 +800,7 @@ int hpsgd_gated_scan_forward(const hpsgd_gated_scan_forward_args* args, void* st
     int sms = 0;
     OPS_TRY(device_sms(&sms));
     ScanForward a{};
-    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, p.offsets};
+    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, 0, p.offsets};
     a.f = p.f; a.v = p.v; a.o = p.o; a.h0 = p.h0; a.h_last = p.h_last; a.y = p.y; a.saved = p.saved;
     a.ldf = p.ldf; a.ldv = p.ldv; a.ldo = p.ldo; a.ldy = p.ldy; a.ldh0 = p.ldh0; a.ldlast = p.ldlast; a.ldsaved = saved_stride(p.cols);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -822,7 +834,7 @@ int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* 
     int sms = 0;
     OPS_TRY(device_sms(&sms));
     ScanBackward a{};
-    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, p.offsets};
+    a.q = Sequences{(int)p.rows, (int)p.cols, (int)p.sequences, (int)(p.rows / p.sequences), 1, 0, p.offsets};
     a.f = p.f; a.v = p.v; a.o = p.o; a.h0 = p.h0; a.saved = p.saved; a.dy = p.dy; a.dh_last = p.dh_last;
     a.df = p.df; a.dv = p.dv; a.d_o = p.d_o; a.dh0 = p.dh0;
     a.ldf = p.ldf; a.ldv = p.ldv; a.ldo = p.ldo; a.ldh0 = p.ldh0; a.lddy = p.lddy; a.lddlast = p.lddlast;
