@@ -1,7 +1,8 @@
 /*
  * libhpsgd, operators: what a program that trains or runs a language model needs beside the
- * replica update and the merge of hpsgd.h: the optimizer step over many tensors, and the layer in 8-bit
- * floating point that its gradients come from (norm, quantisation, matrix product).
+ * replica update and the merge of hpsgd.h: the optimizer step over many tensors, the layer in 8-bit
+ * floating point that its gradients come from (norm, quantisation, matrix product, gated feed-forward
+ * layer), a gated recurrence over sequences, and the loss.
  * (The HPSGD paper has no counterpart for any of them.)
  *
  * Conventions (in addition to those of hpsgd.h)

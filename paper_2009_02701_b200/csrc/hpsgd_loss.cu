@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             } else x[v].load_part(z + c, max(0, -c), left);
         }
     };
-    request(even, 0, false);
-    if (tiles > 1) request(odd, 1, false);
+    request(even, 0, tiles < 3);
+    if (tiles > 1) request(odd, 1, tiles < 4);
     // the label and the teacher's entries meanwhile; an index outside the vocabulary makes the row NaN
     const int64_t label64 = a.labels ? a.labels[row] : -1;
     const bool has_label = label64 >= 0;
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             }
 #pragma unroll
             for (int v = 0; v < NV; ++v) x[v].keep();
-            if (tile + 2 < tiles) request(x, tile + 2, false);
+            if (tile + 2 < tiles) request(x, tile + 2, tile + 4 >= tiles);      // (the last two stay in registers)
             float lo, hi;
             split(sb, lo, hi);
             base.s = __fadd_rn(base.s, __fadd_rn(lo, hi));

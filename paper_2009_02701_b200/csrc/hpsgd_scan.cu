@@ -10,6 +10,12 @@
 //
 // The gradient runs the other way with the same maps: what reaches h_(t-1) is M_t = a_t (g_t + M_(t+1)).  It needs h, which is computed
 // again from the state that the forward pass keeps for each eight rows.
+//
+// Bytes: 8 an element forward and 14 backward in bf16 with output gates, and half a byte each for the kept states.  What bounds it now is the chain of a
+// warp's instructions (an instruction every 6.5 cycles of a warp, 60 % of what the unit for powers and quotients can do, four an element):
+// 16384 x 2048 of 16 sequences 64 us forward, 104 backward (HBM would allow 43 and 75); 65536 x 1024 of one sequence 150 us (82).  Measured and
+// not kept: a chunk's second pass interleaved with the next one's first in the same registers (64 -> 84 us), three and four stages (fewer blocks:
+// 82), maps that say in one flag for a block that none forgets (no change).
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
@@ -332,7 +338,7 @@ struct ScanForward {
 // Blocks of a cluster wait for one another, and longest for the cluster's barrier: there a chunk is 16 rows a thread (8 in fp32) of eight warps.  By
 // themselves they are many, and small: eight rows a thread of four warps, so that there are twice as many warps to wait with.
 template <typename T, bool GATE, bool CLUSTER>
-using ForwardForm = Form<T, CLUSTER && sizeof(T) == 2 ? 16 : 8, GATE ? 3 : 2, CLUSTER ? 8 : 4, !CLUSTER && sizeof(T) == 2 ? 32 : 16>;
+using ForwardForm = Form<T, CLUSTER && sizeof(T) == 2 ? 16 : 8, GATE ? 3 : 2, CLUSTER || sizeof(T) == 4 ? 8 : 4, !CLUSTER && sizeof(T) == 2 ? 32 : 16>;
 
 // STAGED: rows of the inputs start on 16-byte boundaries and two outputs can be stored at once; else both are taken one by one, without a stage.
 template <typename T, bool GATE, bool STAGED, bool CLUSTER>
