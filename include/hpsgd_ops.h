@@ -412,9 +412,9 @@ int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* st
 int hpsgd_ops_check(void* stream);
 
 /*
- * Checked build only; HPSGD_E_UNSUPPORTED otherwise.  1: the barriers of hpsgd_gemm_fp8 are told to expect 16 bytes more than its copies
- * bring, so that its waits run out after two seconds: the way to see the time-out path (no results, HPSGD_E_TIMEOUT from
- * hpsgd_ops_check, the device usable as before) without a fault.  2: those of thread blocks with odd numbers only.
+ * Checked build only; HPSGD_E_UNSUPPORTED otherwise.  1: the barriers of hpsgd_gemm_fp8 and hpsgd_gated_ffn_forward are told to expect 16
+ * bytes more than their copies bring, so that their waits run out after two seconds: the way to see the time-out path (no results,
+ * HPSGD_E_TIMEOUT from hpsgd_ops_check, the device usable as before) without a fault.  2: those of thread blocks with odd numbers only.
  */
 int hpsgd_ops_debug_stall(int enable);
 

@@ -150,7 +150,7 @@ struct Softmax {
     }
 };
 
-// THREADS threads with NV groups of eight columns each (a tile); PER_SM threads on an SM.  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
+// THREADS threads with NV groups of eight columns each (a tile); kPerSm threads on an SM.  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
 // are counted from the boundary in front of the row; else groups begin at column 0 and are taken piece by piece.  LATER: the gradient alone, from lse.
 template <typename T, int THREADS, int NV, int MODE, bool SHIFT, bool LATER>
 __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(const LossArgs a)
