@@ -84,13 +84,15 @@ __device__ __forceinline__ float activation(float g)
     return __fmul_rn(g, sigmoid(w));
 }
 
-// act(g) and its derivative: with s = sigmoid(w), s + g s (1 - s) w'.
+// act(g) and its derivative: with s = sigmoid(w), s + g s (1 - s) w'.  A gate is held to where s is 2^-126: below, the products of s with g and w' would grow again,
+// since s is not smaller, while both results are 0 next to anything.  Above 10 gelu's slope is s, but a square that overflows would make 0 times infinity of the rest.
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float& value, float& slope)
 {
-    const float g2 = __fmul_rn(g, g);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(g) : "f"(ACT == HPSGD_SILU ? -87.33f : -10.001f));
+    const float g2 = fminf(__fmul_rn(g, g), 101.f);
     const float w = ACT == HPSGD_SILU ? g : __fmul_rn(kGelu1, __fmaf_rn(__fmul_rn(kGelu3, g2), g, g));
-    const float e = exp2_of(fminf(__fmul_rn(w, -kLog2e), 126.f)), s = reciprocal(__fadd_rn(1.f, e));
+    const float e = exp2_of(__fmul_rn(w, -kLog2e)), s = reciprocal(__fadd_rn(1.f, e));
     value = __fmul_rn(g, s);
     const float t = __fmul_rn(value, __fmul_rn(e, s));
     slope = ACT == HPSGD_SILU ? __fadd_rn(t, s) : __fmaf_rn(t, __fmul_rn(kGelu1, __fmaf_rn(3.f * kGelu3, g2, 1.f)), s);

@@ -221,6 +221,29 @@ def test_backward_far_out_and_with_fewer_results(act):
     assert ((q & 127 == 127) <= bad).all() and (c.dqt.codes()[0] == 0x7F).sum() <= 2
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("N", [128, 100])
+@pytest.mark.parametrize("dz_dtype", [F32, BF])
+def test_backward_of_the_largest_gates(act, N, dz_dtype):
+    """Where the sigmoid is 0 or 1 to binary32 the slope is too, whatever its other factors' sizes are: beside the bounds of the reference, 2^-112 (230 units, the most that
+    g w' is where the sigmoid is 2^-126, and what the gate is held to there)."""
+    sizes = np.array([0.0, 1.0, 9.0, 9.98, 10.06, 11.0, 50.0, 87.0, 88.5, 100.0, 1e4, 1e11, 1e15, 1.7e19, 1.9e19, 1e25, 1e30, 3e38])
+    g = np.resize(np.concatenate([sizes, -sizes]), (5, N))
+    gu = torch.ones(5, 2 * N, dtype=BF, device="cuda")
+    gu[:, :N] = torch.from_numpy(g).to(BF)
+    g = gu[:, :N].double().cpu().numpy()
+    dgu = torch.full((5, 2 * N), MARK, dtype=BF, device="cuda")
+    hp.hpsgd_gated_ffn_backward(hp.make_gated_ffn_backward(5, N, ACT[act], gu, torch.ones(5, N, dtype=dz_dtype, device="cuda"), KIND[dz_dtype], dgu=dgu))
+    got = dgu.double().cpu().numpy()
+    w, dw = ref.inner(g, act)
+    s, r = ref.sigmoid(w), ref.sigmoid(-w)
+    err = s * (r * (np.abs(w) * 2.0 ** -20.6 + 2.0 ** -22) + 2.0 ** -21) + np.abs(g * dw) * s * r * (np.abs(w) * 2.0 ** -19 + 2.0 ** -19.5) + 2.0 ** -112
+    want = ref.slope(g, act)
+    assert np.all(np.abs(got[:, :N] - want) <= err + E16 * (np.abs(want) + err))
+    want, err = ref.act(g, act), np.abs(g) * s * (r * (np.abs(w) * 2.0 ** -20.6 + 2.0 ** -22) + 2.0 ** -21) + 2.0 ** -112
+    assert np.all(np.abs(got[:, N:] - want) <= err + E16 * (np.abs(want) + err))
+
+
 def test_the_same_bits_every_time_and_from_a_graph():
     M, N, K = 300, 640, 1100
     c, d = Forward(M, N, K, "silu", *inputs(M, N, K, 3)), Backward(M, N, "silu", seed=1)
