@@ -463,7 +463,7 @@ int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, 
         return report(HPSGD_E_BADARG, "%s: weights must be >= 0 and finite", what);
     if (!std::isfinite((float)p.grad_scale)) return report(HPSGD_E_BADARG, "%s: grad_scale is not finite", what);
     if (p.k > kMaxTeacher) return report(HPSGD_E_UNSUPPORTED, "%s: at most %d teacher entries a row", what, kMaxTeacher);
-    if (p.vocab > 0x7FFFFFFF - 65536 || p.rows * ((p.vocab + 8191) / 8192 + 1) > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    if (p.rows > 0x7FFFFFFF || p.vocab > 0x7FFFFFFF - 65536 || p.rows * ((p.vocab + 8191) / 8192 + 1) > 0x7FFFFFFF) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
     if (p.rows == 0 || p.vocab == 0) return HPSGD_OK;
     if (!p.logits) return report(HPSGD_E_BADARG, "%s: logits is NULL", what);
     if (later ? !p.dlogits : !p.loss && !p.lse && !p.dlogits) return report(HPSGD_E_BADARG, "%s: no output is asked for", what);

@@ -40,6 +40,8 @@ def test_outputs_and_sizes():
     for call in (hp.hpsgd_distill_loss, hp.hpsgd_distill_loss_backward):
         for change in (dict(k=1025), dict(vocab=1 << 31), dict(rows=1 << 30)):
             refused(hp.HPSGD_E_UNSUPPORTED, lambda: call(make(**change)))
+        for change in (dict(rows=1 << 31), dict(rows=1 << 62), dict(rows=(1 << 62) + 5), dict(rows=(1 << 63) - 1, vocab=1)):
+            refused(hp.HPSGD_E_UNSUPPORTED, lambda: call(make(**change)))
         for change in (dict(rows=0), dict(vocab=0)):
             assert call(make(**change)) == 0
     with pytest.raises(TypeError):
