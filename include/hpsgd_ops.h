@@ -328,6 +328,8 @@ int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* 
  *   ld*             elements from row to row; 0 = vocab, for the teacher's two matrices k
  * Rows with neither label nor teacher have loss and gradient 0, whatever their logits are.  Logits of -infinity have probability 0 (a label or
  * a teacher's entry there makes the loss infinite); NaN and +infinity make their row NaN, and so does a label or an index that is not below vocab.
+ * Finite logits may be of any size, a mask of the type's lowest value among them, in a part of a row or all over it, the teacher's too; rows whose largest
+ * logit / T is beyond 2^20 log 2 take longer.
  * A term with weight 0 is left out: its arguments are not read.  Rows whose addresses and strides are multiples of 32 bytes (16 for bf16) take the wide
  * accesses.
  */
@@ -347,7 +349,10 @@ typedef struct hpsgd_distill_loss_args {
 } hpsgd_distill_loss_args;
 int hpsgd_distill_loss(const hpsgd_distill_loss_args* args, void* stream);
 
-/* dlogits alone, where dloss comes later: lse is what the first call wrote; loss is not touched. */
+/*
+ * dlogits alone, where dloss comes later: lse is what the first call wrote; loss is not touched.  An lse in binary32 carries half a unit of its last place into
+ * every probability; beyond 2^20 log 2 the sums are taken from the logits again.
+ */
 int hpsgd_distill_loss_backward(const hpsgd_distill_loss_args* args, void* stream);
 
 /* ------------------------------------------------------------------------------------

@@ -10,6 +10,10 @@
 //
 // Powers of two are what the SM does least of (16 a clock; two for each element are three quarters of the time that its bytes take).  With a label and a
 // teacher there are two temperatures, and four of them; where the teacher's is 2, 3 or 4, e^z is that power of e^(z / T), by multiplying.
+//
+// Large logits: x c - k is the product's rounding error where x c has no digits left behind the point, and that can be 2^100 either way.  k is held above
+// -kFar, so masked words that are far below add nothing wherever they are, and a row that is far out as a whole, or has its label or a teacher's entry
+// there, is done by far_row(): from differences to the largest logit, one element after another.
 #include "hpsgd_ops_common.cuh"
 
 #include <algorithm>
@@ -35,6 +39,7 @@ struct LossArgs {
     int64_t ldz, ldt, lddz;
     float c1, c2;                                   // log2(e) over the temperatures; c2, the teacher's, is only used where there are two
     float ct, wl, wt, temperature, scale;           // wt: with the square of the temperature
+    float inverse;                                  // 1 / temperature
     int teacher_bf16;
     int main_is_teacher;                            // c1 is the teacher's temperature
 };
@@ -86,6 +91,10 @@ struct Sum {
     }
 };
 __device__ __forceinline__ Sum nothing() { return Sum{-FLT_MAX, 0.f}; }
+
+// Exponents x c of this magnitude and more are far.  Below it a product's rounding is at most 2^-5, so x c - k of the largest is in (-1, 2^-5].
+constexpr float kFar = 1048576.f;
+__device__ __forceinline__ bool is_far(float k) { return k >= kFar || k == -kFar; }      // (k does not go below -kFar)
 __device__ __forceinline__ float log2_of(const Sum& x) { return __fadd_rn(x.k, log2f(x.s)); }
 
 // Over the lanes of a warp; every lane has the result.
@@ -150,6 +159,154 @@ struct Softmax {
     }
 };
 
+// What a block knows of the teacher's entries, and of the label behind them: index (-1: not there), probability, its logit, the student's, seen twice.
+struct Entries {
+    int stride;
+    int* index;
+    float* p;
+    float* t_of;
+    float* z_of;
+    uint8_t* twice;
+    __device__ __forceinline__ Entries(float* room, int k)
+        : stride((k + 4) / 4 * 4), index(reinterpret_cast<int*>(room)), p(room + stride), t_of(p + stride), z_of(t_of + stride), twice(reinterpret_cast<uint8_t*>(z_of + stride))
+    {
+    }
+};
+
+// What is taken off the gradient at the label and the teacher's entries among the columns [first, last); the same index twice is one element, written with the
+// same value.  softmax(x): the gradient before that, of a logit x.
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ void take_off(const Entries& e, int k, T* dz, int first, int last, float on_label, float on_teacher, const F& softmax)
+{
+    const int label = e.index[k];
+#pragma unroll 1
+    for (int j = threadIdx.x; j <= k; j += THREADS) {
+        const int i = e.index[j];
+        if (i < first || i >= last) continue;
+        const float off = i == label ? on_label : 0.f;
+        float sum_p = e.p[j];
+        if (k > 0 && e.twice[j]) {
+            sum_p = 0.f;
+#pragma unroll 1
+            for (int m = 0; m < k; ++m)
+                if (e.index[m] == i) sum_p = __fadd_rn(sum_p, e.p[m]);
+        }
+        const float y = softmax(e.z_of[j]);
+        store1(dz + i, __fadd_rn(y, -__fmaf_rn(on_teacher, sum_p, off)));
+    }
+}
+
+// A row that is far out, by the whole block: everything from differences to the largest logit (the largest entry, for the teacher).  Rare, so it is short: one
+// element after another.  (As a function that is called it took registers from the kernel even where it was not: 4096 x 30000 125 -> 135 us.)  LATER: the
+// gradient from the logits, since an lse in binary32 of that magnitude no longer holds the logarithm of the sum; the row's first block does all of it (the row
+// may be written in place).
+template <typename T, int THREADS, bool LATER>
+__device__ __forceinline__ void far_row(const LossArgs& a, const Entries& e, int64_t row, float* of_warp)
+{
+    const int k = a.k, vocab = a.vocab;
+    const T* const z = static_cast<const T*>(a.z) + row * a.ldz;
+    const auto over_block = [&](float x, bool largest) {
+        x = largest ? top_of_lanes(x) : sum_of_lanes(x);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) of_warp[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = of_warp[0];
+#pragma unroll 1
+        for (int w = 1; w < THREADS / 32; ++w) x = largest ? fmaxf(x, of_warp[w]) : __fadd_rn(x, of_warp[w]);
+        return x;
+    };
+    const auto power_of = [](float far, float c) { return exp2_of(__fmul_rn(far, c)); };
+    const float c1 = kLog2e, c2 = a.ct;
+    const int64_t label = a.labels ? a.labels[row] : -1;
+    bool wrong = label >= vocab;
+#pragma unroll 1
+    for (int j = threadIdx.x; j < k; j += THREADS) wrong = wrong || a.index[row * a.ldt + j] >= vocab;
+
+    // the student's sums
+    float top = -INFINITY, s1 = 0.f, s2 = 0.f;
+    bool nan = wrong;
+#pragma unroll 1
+    for (int c = threadIdx.x; c < vocab; c += THREADS) {
+        const float x = load1(z + c);
+        nan = nan || x != x;
+        top = fmaxf(top, x);
+    }
+    wrong = __syncthreads_or(wrong);
+    nan = __syncthreads_or(nan);
+    top = over_block(top, true);
+#pragma unroll 1
+    for (int c0 = threadIdx.x; c0 < vocab; c0 += 32 * THREADS) {
+        float part1 = 0.f, part2 = 0.f;              // (32 at a time: few roundings one upon another)
+#pragma unroll 1
+        for (int c = c0; c < min(vocab, c0 + 32 * THREADS); c += THREADS) {
+            const float x = __fadd_rn(load1(z + c), -top);
+            part1 = __fadd_rn(part1, power_of(x, c1));
+            part2 = __fadd_rn(part2, power_of(x, c2));
+        }
+        s1 = __fadd_rn(s1, part1);
+        s2 = __fadd_rn(s2, part2);
+    }
+    s1 = over_block(s1, false);
+    s2 = over_block(s2, false);
+    if (top == -INFINITY) s1 = s2 = 0.f;            // nothing is there: its differences to itself are no numbers
+    if (nan) s1 = s2 = __uint_as_float(0x7FC00000u);
+
+    // the teacher's probabilities
+    float top_t = -INFINITY, st = 0.f;
+    bool entry = false;
+#pragma unroll 1
+    for (int j = threadIdx.x; j < k; j += THREADS) {
+        entry = entry || e.t_of[j] != -INFINITY;
+        top_t = fmaxf(top_t, e.t_of[j]);
+    }
+    const bool has_teacher = __syncthreads_or(entry);
+    top_t = over_block(top_t, true);
+#pragma unroll 1
+    for (int j = threadIdx.x; j < k; j += THREADS)
+        if (e.t_of[j] != -INFINITY) st = __fadd_rn(st, power_of(__fadd_rn(e.t_of[j], -top_t), c2));
+    st = over_block(st, false);
+    constexpr float kLn2 = 0.69314718f;
+    const float log_1 = __fmul_rn(kLn2, log2f(s1)), log_2 = __fmul_rn(kLn2, log2f(s2)), log_t = __fmul_rn(kLn2, log2f(st));
+    const auto half_of = [](float x, float y) { return __fmaf_rn(0.5f, x, __fmul_rn(-0.5f, y)); };      // of x - y, which may be more than there is
+    float loss = 0.f;
+#pragma unroll 1
+    for (int j = threadIdx.x; j <= k; j += THREADS) {
+        float p = 0.f;
+        if (j < k && e.t_of[j] != -INFINITY) {
+            p = __fdividef(power_of(__fadd_rn(e.t_of[j], -top_t), c2), st);
+            if (!LATER && p != 0.f) {                // p wt ((t - top_t - z + top) / T - log_t + log_2)
+                const float w = __fmul_rn(p, a.wt), y = __fadd_rn(half_of(e.t_of[j], top_t), -half_of(e.z_of[j], top));
+                loss = __fmaf_rn(__fmul_rn(2.f, __fmul_rn(w, a.inverse)), y, __fmaf_rn(w, __fadd_rn(log_2, -log_t), loss));
+            }
+        } else if (!LATER && j == k && label >= 0) loss = __fmaf_rn(__fmul_rn(-2.f, a.wl), half_of(e.z_of[k], top), __fmaf_rn(a.wl, log_1, loss));
+        e.p[j] = p;
+    }
+    if constexpr (!LATER) {
+        loss = over_block(loss, false);
+        if (threadIdx.x == 0 && a.loss) a.loss[row] = wrong ? __uint_as_float(0x7FC00000u) : loss;
+        if (threadIdx.x == 0 && a.lse) {
+            a.lse[2 * row] = __fadd_rn(top, log_1);
+            a.lse[2 * row + 1] = __fmaf_rn(top, a.inverse, log_2);
+        }
+        if (!a.dz) return;
+    }
+
+    T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
+    const float g = __fmul_rn(a.dloss ? a.dloss[row] : 1.f, a.scale), on_label = label >= 0 ? __fmul_rn(g, a.wl) : 0.f,
+                on_teacher = has_teacher ? __fmul_rn(g, __fmul_rn(a.wt, a.inverse)) : 0.f;
+    const bool none = on_label == 0.f && on_teacher == 0.f;
+    const auto softmax = [&](float x) {
+        const float far = __fadd_rn(x, -top);
+        float y = on_label != 0.f ? __fmul_rn(on_label, __fdividef(power_of(far, c1), s1)) : 0.f;
+        if (on_teacher != 0.f) y = __fmaf_rn(on_teacher, __fdividef(power_of(far, c2), s2), y);
+        return y;
+    };
+#pragma unroll 1
+    for (int c = threadIdx.x; c < vocab; c += THREADS) store1(dz + c, none ? 0.f : softmax(load1(z + c)));
+    __syncthreads();
+    if (!none) take_off<THREADS>(e, k, dz, 0, vocab, on_label, on_teacher, softmax);
+}
+
 // THREADS threads with NV groups of eight columns each (a tile); kPerSm threads on an SM.  SHIFT: rows of logits and of the gradient lie alike to the wide boundaries, and columns
 // are counted from the boundary in front of the row; else groups begin at column 0 and are taken piece by piece.  LATER: the gradient alone, from lse.
 template <typename T, int THREADS, int NV, int MODE, bool SHIFT, bool LATER>
@@ -157,15 +314,11 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
 {
     constexpr int kWarpsHere = THREADS / 32, kTileCols = THREADS * NV * 8;
     constexpr bool kSecond = MODE != kOne;
-    extern __shared__ __align__(16) float room[];   // of each teacher entry, and of the label behind them: index, probability, its logit, the student's, seen twice
+    extern __shared__ __align__(16) float room[];
     __shared__ Stats of_warp[kWarpsHere];
     __shared__ float part[kWarpsHere];
-    const int k = a.k, stride = (k + 4) / 4 * 4;
-    int* const index = reinterpret_cast<int*>(room);
-    float* const p = room + stride;
-    float* const t_of = p + stride;
-    float* const z_of = t_of + stride;
-    uint8_t* const twice = reinterpret_cast<uint8_t*>(z_of + stride);
+    const int k = a.k;
+    const Entries e(room, k);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = LATER ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
     const int64_t row = LATER ? blockIdx.x / (unsigned)a.pieces : blockIdx.x;
@@ -208,33 +361,37 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
     const bool has_label = label64 >= 0;
     const int label = has_label ? (int)min(label64, (int64_t)0x7FFFFFFF) : -1;
     bool wrong = label >= a.vocab;
-    Stats mine{nothing(), nothing(), nothing()};
+    Stats mine{Sum{MODE > kTwo ? -kFar * MODE : -kFar, 0.f}, Sum{-kFar, 0.f}, nothing()};
+    const float c_most = kSecond ? fmaxf(a.c1, a.c2) : a.c1;
 #pragma unroll 1
     for (int j = threadIdx.x; j <= k; j += THREADS) {
         int i = j < k ? a.index[row * a.ldt + j] : label;
         float t = -INFINITY;
         if (j < k && i >= 0) t = teacher_logit(a, row * a.ldt + j);
         if (i >= a.vocab) wrong = true, i = -1;
-        index[j] = i < 0 ? -1 : i;
-        t_of[j] = t;
-        z_of[j] = i >= 0 ? load1(z + i) : 0.f;
+        const float x = i >= 0 ? load1(z + i) : 0.f, tc = __fmul_rn(t, a.ct);
+        e.index[j] = i < 0 ? -1 : i;
+        e.t_of[j] = t;
+        e.z_of[j] = x;
         if (t != -INFINITY) {
-            const float kt = ceilf(__fmul_rn(t, a.ct));
+            const float kt = fmaxf(ceilf(tc), -kFar);
             mine.teacher.add(kt, exp2_of(__fmaf_rn(t, a.ct, -kt)));
         }
+        // a far logit of the student's at the label, or where the teacher's probability is not sure to be 0, makes the row far
+        if (!LATER && fabsf(x) * c_most >= kFar && (j == k || tc > -2.f * kFar)) mine.teacher.add(kFar, 0.f);
     }
     if (k > 0) {                                    // entries that share their index with another are rare, and known before they are needed
         __syncthreads();
 #pragma unroll 1
         for (int j = threadIdx.x; j <= k; j += THREADS) {
             int same = 0;
-            const int i = index[j];
+            const int i = e.index[j];
 #pragma unroll 1
             for (int m = 0; m < k; m += 4) {
-                const int4 four = *reinterpret_cast<const int4*>(index + m);
+                const int4 four = *reinterpret_cast<const int4*>(e.index + m);
                 same += (four.x == i) + (m + 1 < k && four.y == i) + (m + 2 < k && four.z == i) + (m + 3 < k && four.w == i);
             }
-            twice[j] = same > (j < k ? 1 : 0);
+            e.twice[j] = same > (j < k ? 1 : 0);
         }
     }
 
@@ -251,7 +408,7 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
                 const float kb = fmaxf(base.k, ceilf(top_of_lanes(kt)));
                 base = Sum{kb, __fmul_rn(base.s, exp2_of(base.k - kb))};
                 if (kSecond) {
-                    const float kf = MODE == kTwo ? fmaxf(mine.one.k, ceilf(__fmul_rn(top_of_lanes(top), a.c1))) : fmaxf(kb * MODE, -FLT_MAX);
+                    const float kf = MODE == kTwo ? fmaxf(mine.one.k, ceilf(__fmul_rn(top_of_lanes(top), a.c1))) : kb * MODE;
                     mine.one = Sum{kf, __fmul_rn(mine.one.s, exp2_of(mine.one.k - kf))};
                 }
             }
@@ -307,6 +464,12 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
         all.one = Sum{__fmul_rn(a.main_is_teacher ? l1 : l0, kLog2e), one};
         if (kSecond) all.two = Sum{__fmul_rn(l1, kLog2e), one};
     }
+    // (all threads of the block are of one mind)
+    if (__builtin_expect((LATER ? fabsf(all.one.k) >= kFar || (kSecond && fabsf(all.two.k) >= kFar) || is_far(all.teacher.k)
+              : is_far(kSecond ? all.two.k : all.one.k) || (MODE == kTwo && is_far(all.one.k)) || is_far(all.teacher.k)), 0)) {
+        if (rank == 0) far_row<T, THREADS, LATER>(a, e, row, part);
+        return;
+    }
     const Sum& of_teacher = kSecond ? all.two : all.one;      // the student's sum at the teacher's temperature
     const float c_teacher = kSecond ? a.c2 : a.c1;
 
@@ -317,17 +480,17 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
 #pragma unroll 1
         for (int j = threadIdx.x; j <= k; j += THREADS) {
             float pj = 0.f;
-            if (j < k && t_of[j] != -INFINITY) {
-                const float u = __fmaf_rn(t_of[j], a.ct, -all.teacher.k);
+            if (j < k && e.t_of[j] != -INFINITY) {
+                const float u = __fmaf_rn(e.t_of[j], a.ct, -all.teacher.k);
                 pj = __fdividef(exp2_of(u), all.teacher.s);
                 if constexpr (!LATER) {
-                    const float kl = __fadd_rn(u - log_t, -(__fmaf_rn(z_of[j], c_teacher, -of_teacher.k) - log_s));
+                    const float kl = __fadd_rn(u - log_t, -(__fmaf_rn(e.z_of[j], c_teacher, -of_teacher.k) - log_s));
                     if (pj != 0.f) sum = __fmaf_rn(__fmul_rn(pj, a.wt), kl, sum);
                 }
             } else if (!LATER && j == k && has_label) {
-                sum = __fmaf_rn(a.wl, log2f(all.one.s) - __fmaf_rn(z_of[k], a.c1, -all.one.k), sum);
+                sum = __fmaf_rn(a.wl, log2f(all.one.s) - __fmaf_rn(e.z_of[k], a.c1, -all.one.k), sum);
             }
-            p[j] = pj;
+            e.p[j] = pj;
         }
         if constexpr (!LATER) {
             if (wrong) sum = __uint_as_float(0x7FC00000u);
@@ -388,7 +551,6 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             turn(even, tile - 1);
         }
     }
-    // and what is taken off at the label and the teacher's entries; the same index twice is one element, written with the same value
     __syncthreads();
     if (!LATER && a.loss && rank == 0 && threadIdx.x == 0) {
         float s = part[0];
@@ -397,22 +559,11 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
         a.loss[row] = __fmul_rn(s, 0.69314718f);
     }
     if (none) return;
-    T* const dz = static_cast<T*>(a.dz) + row * a.lddz;
-#pragma unroll 1
-    for (int j = threadIdx.x; j <= k; j += THREADS) {
-        const int i = index[j];
-        if (i < max(0, first) || i >= last) continue;
-        float off = i == label ? on_label : 0.f, sum_p = p[j];
-        if (k > 0 && twice[j]) {
-            sum_p = 0.f;
-#pragma unroll 1
-            for (int m = 0; m < k; ++m)
-                if (index[m] == i) sum_p = __fadd_rn(sum_p, p[m]);
-        }
+    take_off<THREADS>(e, k, static_cast<T*>(a.dz) + row * a.lddz, max(0, first), last, on_label, on_teacher, [&](float x) {
         float lo, hi;
-        split(softmax(both(z_of[j])), lo, hi);
-        store1(dz + i, __fadd_rn(lo, -__fmaf_rn(on_teacher, sum_p, off)));
-    }
+        split(softmax(both(x)), lo, hi);
+        return lo;
+    });
 }
 
 template <typename T, int THREADS, int NV, bool LATER>
@@ -494,7 +645,7 @@ int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, 
     a.c1 = (float)(a.main_is_teacher ? log2e / p.temperature : log2e);
     a.c2 = a.ct = (float)(log2e / p.temperature);
     a.wl = (float)p.label_weight; a.wt = (float)(p.teacher_weight * p.temperature * p.temperature);
-    a.temperature = (float)p.temperature; a.scale = (float)p.grad_scale;
+    a.temperature = (float)p.temperature; a.inverse = (float)(1.0 / p.temperature); a.scale = (float)p.grad_scale;
     a.teacher_bf16 = p.teacher_dtype == HPSGD_BF16;
     // rows of both lie alike to the wide boundaries
     const bool shift = !p.dlogits || ((reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % unit == 0 && (p.ldlogits - p.lddlogits) * esz % unit == 0);
