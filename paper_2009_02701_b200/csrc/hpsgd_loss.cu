@@ -404,7 +404,9 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
             for (int v = 0; v < NV; ++v) x[v].keep();
             Sum& base = kSecond ? mine.two : mine.one;
             const float kt = __fmul_rn(top, kSecond ? a.c2 : a.c1);
-            if (__any_sync(0xFFFFFFFFu, !(kt <= base.k))) {      // a larger value than so far: the whole warp's k moves
+            // a larger value than so far: the whole warp's k moves.  (Of two temperatures each has a step of its own: at a high one logits that differ by
+            // hundreds are within one step, at a low one the other's.)
+            if (__any_sync(0xFFFFFFFFu, !(kt <= base.k) || (MODE == kTwo && !(__fmul_rn(top, a.c1) <= mine.one.k)))) {
                 const float kb = fmaxf(base.k, ceilf(top_of_lanes(kt)));
                 base = Sum{kb, __fmul_rn(base.s, exp2_of(base.k - kb))};
                 if (kSecond) {
