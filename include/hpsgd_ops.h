@@ -321,7 +321,7 @@ int hpsgd_gated_scan_backward(const hpsgd_gated_scan_backward_args* args, void* 
  *   dtype, teacher_dtype   HPSGD_F32 or HPSGD_BF16, of logits and dlogits and of teacher_logits
  *   labels          rows numbers, or NULL; a negative one: the row has no label and no CE
  *   teacher_index, teacher_logits   [rows x k], k <= 1024 (else HPSGD_E_UNSUPPORTED); an entry whose index is negative or whose logit is
- *                   -infinity is not there, and a row without any has no KL.  Indices may repeat.
+ *                   -infinity is not there, whatever stands in the other place, and a row without any has no KL.  Indices may repeat.
  *   loss            rows floats, or NULL;   lse: rows x 2 floats, lse(z) and lse(z / T), for the second call, or NULL
  *   dlogits         the gradient in the same pass, or NULL; may be the logits' own memory
  *   dloss           rows floats, the gradients of the rows' losses, or NULL (1).  Where c is 0, dlogits is 0 whatever the logits are.

@@ -220,7 +220,7 @@ __device__ __forceinline__ void far_row(const LossArgs& a, const Entries& e, int
     const int64_t label = a.labels ? a.labels[row] : -1;
     bool wrong = label >= vocab;
 #pragma unroll 1
-    for (int j = threadIdx.x; j < k; j += THREADS) wrong = wrong || a.index[row * a.ldt + j] >= vocab;
+    for (int j = threadIdx.x; j < k; j += THREADS) wrong = wrong || (e.t_of[j] != -INFINITY && a.index[row * a.ldt + j] >= vocab);
 
     // the student's sums
     float top = -INFINITY, s1 = 0.f, s2 = 0.f;
@@ -368,8 +368,9 @@ __global__ void __launch_bounds__(THREADS, kPerSm<T> / THREADS) loss_kernel(cons
         int i = j < k ? a.index[row * a.ldt + j] : label;
         float t = -INFINITY;
         if (j < k && i >= 0) t = teacher_logit(a, row * a.ldt + j);
+        const float x = i >= 0 && i < a.vocab ? load1(z + i) : 0.f, tc = __fmul_rn(t, a.ct);
+        if (j < k && t == -INFINITY) i = -1;         // not there, whatever the index is
         if (i >= a.vocab) wrong = true, i = -1;
-        const float x = i >= 0 ? load1(z + i) : 0.f, tc = __fmul_rn(t, a.ct);
         e.index[j] = i < 0 ? -1 : i;
         e.t_of[j] = t;
         e.z_of[j] = x;
