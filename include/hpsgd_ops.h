@@ -410,9 +410,10 @@ int hpsgd_gated_ffn_backward(const hpsgd_gated_ffn_backward_args* args, void* st
 
 /*
  * Wait for `stream` and report what only the device can know: HPSGD_E_TIMEOUT if a wait inside hpsgd_gemm_fp8 or hpsgd_gated_ffn_forward ran out on this device
- * since the last call, HPSGD_E_CUDA if the work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts
+ * since the last call (on whatever stream: where there is one to report, the whole device is waited for, and both operators are named), HPSGD_E_CUDA if the
+ * work failed.  A tile of D (up to 256 rows and columns) whose waits ran out, in whichever of its parts
  * along k, is left as it was, and nothing is added to it; other tiles may have been written.  Products whose parts go through the workspace
- * write nothing from such a time-out on until it has been reported here (the whole device is waited for then).
+ * write nothing from such a time-out on until it has been reported here.
  */
 int hpsgd_ops_check(void* stream);
 

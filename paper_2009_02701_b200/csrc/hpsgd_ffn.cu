@@ -780,11 +780,14 @@ int check_plain(const char* what, const char* name, const void* p, int64_t* ld, 
 
 }  // namespace
 
-// Time-outs of this file's kernels since the last report, which are taken off (the device is idle).
-HPSGD_HIDDEN int take_ffn_timeouts(unsigned int* n)
+// Time-outs of this file's kernels since the last report; and the count set to 0, for which the device has to be idle.
+HPSGD_HIDDEN int ffn_timeouts(unsigned int* n)
 {
     OPS_CUDA(cudaMemcpyFromSymbol(n, g_ffn_timeouts, sizeof *n));
-    if (*n == 0) return HPSGD_OK;
+    return HPSGD_OK;
+}
+HPSGD_HIDDEN int clear_ffn_timeouts()
+{
     const unsigned int zero = 0;
     OPS_CUDA(cudaMemcpyToSymbol(g_ffn_timeouts, &zero, sizeof zero));
     return HPSGD_OK;

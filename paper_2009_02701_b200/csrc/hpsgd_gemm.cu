@@ -21,7 +21,8 @@ namespace hpsgd {
 namespace ops {
 
 HPSGD_HIDDEN int check_fp8(const char* what, const char* name, const void* q, const void* s, int64_t* ld, int64_t* lds, int64_t rows, int64_t cols);
-HPSGD_HIDDEN int take_ffn_timeouts(unsigned int* n);
+HPSGD_HIDDEN int ffn_timeouts(unsigned int* n);
+HPSGD_HIDDEN int clear_ffn_timeouts();
 
 namespace {
 
@@ -697,15 +698,20 @@ int hpsgd_ops_check(void* stream)
     OPS_CUDA(cudaStreamSynchronize(s));
     unsigned int n = 0, ffn = 0;
     OPS_CUDA(cudaMemcpyFromSymbol(&n, g_gemm_timeouts, sizeof n));
-    OPS_TRY(take_ffn_timeouts(&ffn));
-    if (n != 0) {
+    OPS_TRY(ffn_timeouts(&ffn));
+    if (n != 0 || ffn != 0) {
+        // Blocks on other streams may be about to give up, and a sum of parts may still have to see the count: nothing is set to 0 before the device is idle.
         const unsigned int zero = 0;
-        OPS_CUDA(cudaDeviceSynchronize());             // a sum of parts on another stream may still have to see the count
+        OPS_CUDA(cudaDeviceSynchronize());
         OPS_CUDA(cudaMemcpyFromSymbol(&n, g_gemm_timeouts, sizeof n));
+        OPS_TRY(ffn_timeouts(&ffn));
         OPS_CUDA(cudaMemcpyToSymbol(g_gemm_timeouts, &zero, sizeof zero));
-        return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks gave up waiting for their own loads or products after two seconds; their tiles were not written", n);
+        OPS_TRY(clear_ffn_timeouts());
+        const char* why = "gave up waiting for their own loads or products after two seconds; their tiles were not written";
+        if (ffn == 0) return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks %s", n, why);
+        if (n == 0) return report(HPSGD_E_TIMEOUT, "hpsgd_gated_ffn_forward: %u blocks %s", ffn, why);
+        return report(HPSGD_E_TIMEOUT, "hpsgd_gemm_fp8: %u blocks, hpsgd_gated_ffn_forward: %u blocks %s", n, ffn, why);
     }
-    if (ffn != 0) return report(HPSGD_E_TIMEOUT, "hpsgd_gated_ffn_forward: %u blocks gave up waiting for their own loads or products after two seconds; their tiles were not written", ffn);
     return HPSGD_OK;
 }
 
