@@ -501,6 +501,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1)
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0 && given_up) atomicAdd(&g_ffn_timeouts, 1u);
+    if constexpr (JOIN || PAIR) __syncwarp();
     if constexpr (JOIN) {
         // A block that gave up has no part, and then none of the cluster's blocks writes anything of the tile.
         cluster_wait();

@@ -98,6 +98,7 @@ __device__ __forceinline__ float reciprocal(float x)
 
 // ---------------------------------------------------------------------------- blocks of a cluster
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// (.aligned: the whole warp comes as one.  Behind lanes that went ways of their own there is a __syncwarp() first.)
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 

@@ -386,7 +386,10 @@ __global__ void __launch_bounds__(ForwardForm<T, GATE, CLUSTER>::kThreads, Forwa
     if (a.h_last && rank == 0)
         for (int s = mine.first + (int)(threadIdx.x >> 4); s < mine.last; s += 2 * F::W)
             if (q.begin(s) >= q.begin(s + 1)) store_two<false>(a.h_last + s * a.ldlast + c, a.h0 ? load_two(a.h0 + s * a.ldh0 + c, left) : both(0.f), left);
-    if constexpr (CLUSTER) cluster_wait();
+    if constexpr (CLUSTER) {
+        __syncwarp();
+        cluster_wait();
+    }
 
     Marks m{0u, 0u, 0, 0};
     pair carry = both(0.f);
@@ -561,7 +564,10 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE, CLUSTER>::kThreads, Back
     if (a.dh0 && rank == 0)
         for (int s = mine.first + (int)(threadIdx.x >> 4); s < mine.last; s += 2 * F::W)
             if (q.begin(s) >= q.begin(s + 1)) store_two<false>(a.dh0 + s * a.lddh0 + c, a.dh_last ? load_two(a.dh_last + s * a.lddlast + c, left) : both(0.f), left);
-    if constexpr (CLUSTER) cluster_wait();
+    if constexpr (CLUSTER) {
+        __syncwarp();
+        cluster_wait();
+    }
 
     Marks m{0u, 0u, 0, 0};
     pair carry = both(0.f);
