@@ -659,13 +659,14 @@ __global__ void __launch_bounds__(BackwardForm<T, GATE, CLUSTER>::kThreads, Back
 }
 
 // ---------------------------------------------------------------------------- host side
-constexpr int64_t kMostRows = 0x7FFFFFFF - 65536;   // rows of a chunk that reaches past the end are counted too
+// rows of a chunk and columns of a block that reach past the end are counted too
+constexpr int64_t kMostRows = 0x7FFFFFFF - 65536, kMostCols = 0x7FFFFFFF - 512;
 
 int check_sequences(const char* what, int64_t rows, int64_t cols, int64_t sequences, int dtype, const int64_t* offsets)
 {
     if (rows < 0 || cols < 0 || sequences < 0) return report(HPSGD_E_BADARG, "%s: a size is negative", what);
     if (dtype != HPSGD_F32 && dtype != HPSGD_BF16) return report(HPSGD_E_BADARG, "%s: unknown dtype %d", what, dtype);
-    if (rows > kMostRows || cols > 0x7FFFFFFF - 64 || sequences > 0x7FFFFFFF - 64) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
+    if (rows > kMostRows || cols > kMostCols || sequences > 0x7FFFFFFF - 64) return report(HPSGD_E_UNSUPPORTED, "%s: a size is too large", what);
     if (!offsets && sequences > 0 && rows % sequences) return report(HPSGD_E_BADARG, "%s: without offsets rows must be a multiple of sequences", what);
     if (!aligned(offsets, 8)) return report(HPSGD_E_BADARG, "%s: offsets is not 8-byte aligned", what);
     return HPSGD_OK;
@@ -782,7 +783,7 @@ extern "C" {
 
 size_t hpsgd_gated_scan_saved_bytes(int64_t rows, int64_t cols)
 {
-    if (rows <= 0 || cols <= 0 || rows > kMostRows || cols > 0x7FFFFFFF - 64) return 0;
+    if (rows <= 0 || cols <= 0 || rows > kMostRows || cols > kMostCols) return 0;
     return (size_t)((rows + kSaved - 1) / kSaved) * (size_t)saved_stride(cols) * sizeof(float);
 }
 
