@@ -590,18 +590,19 @@ int loss_types(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t
     const int64_t cols = (int64_t)a.vocab + (shift ? 7 : 0);      // counted from the boundary in front of the row
     a.pieces = 1;
     a.piece = (int)((cols + 7) / 8 * 8);
-    if (LATER) {                                     // nothing is waited for: two tiles a block
+    if constexpr (LATER) {                           // nothing is waited for: two tiles a block
         if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
         a.piece = std::min(a.piece, 2 * 256 * 2 * 8);
         a.pieces = (int)((cols + a.piece - 1) / a.piece);
         return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
+    } else {
+        // Rows of which six an SM, as blocks of 256 threads are held, do not fit L2 with room for what is written: three blocks of 512 an SM, and L2 is told
+        // what will be read again (4096 x 131072 bf16: 428 us; 450 without the hints; 490 with blocks of 256; one block of 1024 an SM 557).  Shorter ones: blocks of
+        // 256 (4096 x 30000: 125 us; of 512 139).
+        if (cols * (int64_t)sizeof(T) * 148 * 6 > (96 << 20)) return loss_launch<T, 512, 2, LATER>(what, a, mode, shift, s);
+        if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
+        return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
     }
-    // Rows of which six an SM, as blocks of 256 threads are held, do not fit L2 with room for what is written: three blocks of 512 an SM, and L2 is told
-    // what will be read again (4096 x 131072 bf16: 428 us; 450 without the hints; 490 with blocks of 256; one block of 1024 an SM 557).  Shorter ones: blocks of
-    // 256 (4096 x 30000: 125 us; of 512 139).
-    if (cols * (int64_t)sizeof(T) * 148 * 6 > (96 << 20)) return loss_launch<T, 512, 2, LATER>(what, a, mode, shift, s);
-    if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
-    return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);
 }
 
 int run_loss(const char* what, const hpsgd_distill_loss_args* args, bool later, void* stream)
