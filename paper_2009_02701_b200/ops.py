@@ -3,7 +3,8 @@ marshalling only.  What a call needs every time (a table of tensors, an argument
 function and passed again and again; the buffers it names have to stay alive, which the returned object sees to.
 
 Tensors are checked when they are named: on a CUDA device, of the type that the call reads there, rows of consecutive elements as far apart
-as the call is told, and as much memory as it will touch (HPSGD_E_BADARG).  Plain addresses are taken as they are.
+as the call is told, and as much memory as it will touch (HPSGD_E_BADARG).  Those of one argument block are on one device, which has to be the current
+one when it is called with.  Plain addresses are taken as they are.
 
 A call goes to the ``stream`` it is given (0 is CUDA's legacy default stream); left out, to torch's current stream where the
 process uses torch on CUDA, so that it is ordered with the torch operations around it.
@@ -112,8 +113,14 @@ SIGNATURES = {
 }
 
 
-def _on(stream):
-    """The stream of a call: the one that is given, or torch's current one."""
+def _current_device():
+    return sys.modules["torch"]._C._cuda_getDevice()
+
+
+def _on(stream, device=None):
+    """The stream of a call: the one that is given, or torch's current one.  ``device``: where the call's tensors are, which has to be the current one."""
+    if device is not None and device != _current_device():
+        raise _b.HpsgdError(_b.HPSGD_E_BADARG, "the call's tensors are on device %d, the current one is %d" % (device, _current_device()))
     if stream is not None:
         return _stream(stream)
     torch = sys.modules.get("torch")
@@ -279,11 +286,25 @@ def hpsgd_grad_norm(table, max_norm, workspace, out, stream=None):
 
 
 # ---- argument blocks -------------------------------------------------------------------
+def _one_device(pointers):
+    """The device that all of the tensors are on, or None where there are addresses only."""
+    device = None
+    for name, x in pointers.items():
+        if x is None or x.__class__ is int:
+            continue
+        here = x.get_device()
+        if device is None:
+            device = here
+        elif here != device:
+            _refuse(name, "is on device %d, others on %d" % (here, device))
+    return device
+
+
 class Args:
     """A filled argument struct with its address, and what it points to (`pointers`, as given; `addresses`, as checked)."""
 
     def __init__(self, struct, pointers, addresses, strides, **plain):
-        self.struct, self.keep = struct(), pointers
+        self.struct, self.keep, self.device = struct(), pointers, _one_device(pointers)
         for name, value in {**addresses, **strides, **plain}.items():
             setattr(self.struct, name, value)
         self.address = ctypes.addressof(self.struct)
@@ -310,7 +331,7 @@ def make_rmsnorm_forward(rows, cols, eps, dtype, x, weight, residual=None, h=Non
 
 
 def hpsgd_rmsnorm_forward(args, stream=None):
-    return _b._check(_b.load().hpsgd_rmsnorm_forward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_rmsnorm_forward(args.address, _on(stream, args.device)))
 
 
 def hpsgd_rmsnorm_backward_bytes(rows, cols):
@@ -328,7 +349,7 @@ def make_rmsnorm_backward(rows, cols, dtype, h, weight, rstd, dy, dx, dweight, w
 
 
 def hpsgd_rmsnorm_backward(args, stream=None):
-    return _b._check(_b.load().hpsgd_rmsnorm_backward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_rmsnorm_backward(args.address, _on(stream, args.device)))
 
 
 def make_quantize_fp8(rows, cols, dtype, x, q=None, scale=None, qt=None, scale_t=None, x_scale=None, **strides):
@@ -342,7 +363,7 @@ def make_quantize_fp8(rows, cols, dtype, x, q=None, scale=None, qt=None, scale_t
 
 
 def hpsgd_quantize_fp8(args, stream=None):
-    return _b._check(_b.load().hpsgd_quantize_fp8(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_quantize_fp8(args.address, _on(stream, args.device)))
 
 
 def hpsgd_gemm_fp8_bytes(M, N, K):
@@ -362,7 +383,7 @@ def make_gemm_fp8(M, N, K, a, a_scale, b, b_scale, d, d_dtype, accumulate=False,
 
 
 def hpsgd_gemm_fp8(args, stream=None):
-    return _b._check(_b.load().hpsgd_gemm_fp8(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_gemm_fp8(args.address, _on(stream, args.device)))
 
 
 # ---- a gated linear recurrence ---------------------------------------------------------
@@ -380,7 +401,7 @@ def make_gated_scan_forward(rows, cols, sequences, dtype, f, v, y, o=None, offse
 
 
 def hpsgd_gated_scan_forward(args, stream=None):
-    return _b._check(_b.load().hpsgd_gated_scan_forward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_gated_scan_forward(args.address, _on(stream, args.device)))
 
 
 def make_gated_scan_backward(rows, cols, sequences, dtype, f, v, saved, dy, df, dv, o=None, do=None, offsets=None, h0=None, dh_last=None, dh0=None, **strides):
@@ -394,7 +415,7 @@ def make_gated_scan_backward(rows, cols, sequences, dtype, f, v, saved, dy, df, 
 
 
 def hpsgd_gated_scan_backward(args, stream=None):
-    return _b._check(_b.load().hpsgd_gated_scan_backward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_gated_scan_backward(args.address, _on(stream, args.device)))
 
 
 # ---- the loss --------------------------------------------------------------------------
@@ -414,11 +435,11 @@ def make_distill_loss(rows, vocab, k, dtype, logits, labels=None, teacher_index=
 
 
 def hpsgd_distill_loss(args, stream=None):
-    return _b._check(_b.load().hpsgd_distill_loss(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_distill_loss(args.address, _on(stream, args.device)))
 
 
 def hpsgd_distill_loss_backward(args, stream=None):
-    return _b._check(_b.load().hpsgd_distill_loss_backward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_distill_loss_backward(args.address, _on(stream, args.device)))
 
 
 # ---- the gated feed-forward layer ------------------------------------------------------
@@ -433,7 +454,7 @@ def make_gated_ffn_forward(M, N, K, act, x, x_scale, w, w_scale, z8=None, z_scal
 
 
 def hpsgd_gated_ffn_forward(args, stream=None):
-    return _b._check(_b.load().hpsgd_gated_ffn_forward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_gated_ffn_forward(args.address, _on(stream, args.device)))
 
 
 def make_gated_ffn_backward(M, N, act, gu, dz, dz_dtype, dq=None, dq_scale=None, dqt=None, dqt_scale=None, dgu=None, **strides):
@@ -447,7 +468,7 @@ def make_gated_ffn_backward(M, N, act, gu, dz, dz_dtype, dq=None, dq_scale=None,
 
 
 def hpsgd_gated_ffn_backward(args, stream=None):
-    return _b._check(_b.load().hpsgd_gated_ffn_backward(args.address, _on(stream)))
+    return _b._check(_b.load().hpsgd_gated_ffn_backward(args.address, _on(stream, args.device)))
 
 
 def hpsgd_ops_check(stream=None):
