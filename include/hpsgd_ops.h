@@ -261,7 +261,8 @@ int hpsgd_gemm_fp8(const hpsgd_gemm_fp8_args* args, void* stream);
  *   h_last     [sequences x cols], receives the state behind each sequence, or NULL; may be h0's own memory
  *   saved      hpsgd_gated_scan_saved_bytes(rows, cols) bytes for the backward pass, 16-byte aligned, or NULL
  *   ld*        elements from row to row; 0 = cols.  f, v and o may lie side by side in one matrix.
- * Where cols and strides are even and addresses multiples of two elements, two channels are taken at once.
+ * Rows whose addresses and strides are multiples of 16 bytes (of two elements for y, and for what the backward call writes) are copied ahead of their use;
+ * others are read value by value, which takes about four times as long.  A state that is updated in place is no longer there for the backward call's h0.
  */
 typedef struct hpsgd_gated_scan_forward_args {
     int64_t rows, cols, sequences;

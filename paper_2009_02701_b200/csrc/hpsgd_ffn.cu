@@ -6,8 +6,9 @@
 // the tokens, so the tokens are read once for the two.  With many tokens two SMs work on one tile of 256 features x 224 tokens (cta_group::2), whose two times 224
 // accumulator columns and scales are the whole of tensor memory.
 //
-// Bound by what feeds the tensor cores out of L2 and by the power cap with long sums (8192 x 8192 x 2048: 219 us, 2.5 PFLOP/s), and with short ones by what the sums go
-// through: activation, product, the block's largest magnitude, rounding, 33 instructions for each.  Sixteen warps do that, from tensor memory to registers in one
+// Bound by what feeds the tensor cores out of L2 and by the power cap with long sums (8192 x 8192 x 2048: 219 us, 2.5 PFLOP/s; 265 us when it is run for long and the
+// cap has settled), and with short ones by what the sums go through: activation, product, the block's largest magnitude, rounding, 35 instructions for a result and 50
+// where its sums are kept.  Sixteen warps do that, from tensor memory to registers in one
 // go, so that the accumulator is free for the next products before anything is rounded.  (Eight warps that took eight columns at a time through
 // shared memory, for 128 features of a token to a warp, took 443 us.)
 #include "hpsgd_quantize.cuh"
@@ -684,7 +685,8 @@ constexpr int kPairTokens = 224;           // 2 x 224 accumulator columns and fo
 // The least power of two that holds all tokens, 128 at most; or 224 on pairs of SMs, which takes fewer bytes out of L2 for a product, but keeps both SMs from the
 // next tile's products while the sums go through the activation.  In a round of tiles an SM spent 0.47 us for each k block and 1.2 us more (3.4 where the
 // sums are kept) on 128 tokens, and 0.78 and 1.2 (6.3) on its half of a pair's: 8192 x 8192 x 2048 242 us on single SMs, 219 on pairs; 4096 x 4096 x 1024 with
-// the sums kept 53 and 66.  The fewer of these, rounds counted whole.
+// the sums kept 53 and 66.  The fewer of these, rounds counted whole.  (Sizes that it was not made from: 1001 x 2744 x 1000 22.6 us either way and with the sums kept
+// 26.6 where single SMs take 24.6; 3000 x 5000 x 3000 90 and 94; from 256 to 2048 tokens x 4096 x 1024 single SMs, which are 6 to 12 us faster.)
 //
 // Few tiles are split along k over the blocks of a cluster, as in hpsgd_gemm.cu.
 FfnPlan plan_of(int64_t M, int64_t N, int64_t K, bool keep)

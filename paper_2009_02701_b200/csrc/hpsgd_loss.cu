@@ -197,7 +197,7 @@ __device__ __forceinline__ void take_off(const Entries& e, int k, T* dz, int fir
 }
 
 // A row that is far out, by the whole block: everything from differences to the largest logit (the largest entry, for the teacher).  Rare, so it is short: one
-// element after another.  (As a function that is called it took registers from the kernel even where it was not: 4096 x 30000 125 -> 135 us.)  LATER: the
+// element after another (4096 x 30000, all of them such rows: 491 us).  (As a function that is called it took registers from the kernel even where it was not: 4096 x 30000 125 -> 135 us.)  LATER: the
 // gradient from the logits, since an lse in binary32 of that magnitude no longer holds the logarithm of the sum; the row's first block does all of it (the row
 // may be written in place).
 template <typename T, int THREADS, bool LATER>
@@ -598,7 +598,7 @@ int loss_types(const char* what, LossArgs& a, int mode, bool shift, cudaStream_t
     } else {
         // Rows of which six an SM, as blocks of 256 threads are held, do not fit L2 with room for what is written: three blocks of 512 an SM, and L2 is told
         // what will be read again (4096 x 131072 bf16: 428 us; 450 without the hints; 490 with blocks of 256; one block of 1024 an SM 557).  Shorter ones: blocks of
-        // 256 (4096 x 30000: 125 us; of 512 139).
+        // 256 (4096 x 30000: 127 us; of 512 139).
         if (cols * (int64_t)sizeof(T) * 148 * 6 > (96 << 20)) return loss_launch<T, 512, 2, LATER>(what, a, mode, shift, s);
         if (cols <= 1024) return loss_launch<T, 128, 1, LATER>(what, a, mode, shift, s);
         return loss_launch<T, 256, 2, LATER>(what, a, mode, shift, s);

@@ -12,7 +12,7 @@
 // again from the state that the forward pass keeps for each eight rows.
 //
 // Bytes: 8 an element forward and 14 backward in bf16 with output gates, and half a byte each for the kept states.  What bounds it now is the chain of a
-// warp's instructions (an instruction every 6.5 cycles of a warp, 60 % of what the unit for powers and quotients can do, four an element):
+// warp's instructions (an instruction every 6.5 cycles of a warp; the unit for powers and quotients, four an element, is 55 % busy forward and 47 % backward):
 // 16384 x 2048 of 16 sequences 64 us forward, 104 backward (HBM would allow 43 and 75); 65536 x 1024 of one sequence 150 us (82).  Measured and
 // not kept: a chunk's second pass interleaved with the next one's first in the same registers (64 -> 84 us), three and four stages (fewer blocks:
 // 82), maps that say in one flag for a block that none forgets (no change).
@@ -145,8 +145,8 @@ __device__ __forceinline__ void copy_async16(uint32_t to, const void* from, int 
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
-// s = sigmoid(x) and 1 - s, each to a few units of its own last place: e = 2^(-x log2 e), s = 1 / (1 + e), 1 - s = e s.  e is held to 2^126, so that s
-// is not 0 where e s has to be 1; a NaN stays one.
+// s = sigmoid(x) and 1 - s: e = 2^(-x log2 e), s = 1 / (1 + e), 1 - s = e s.  The exponent is rounded with its product, so e is right to |x| 2^-23 + 2^-22 of
+// itself, and so is the smaller of the two; the one next to 1 to a few 2^-24.  e is held to 2^126, so that s is not 0 where e s has to be 1; a NaN stays one.
 __device__ __forceinline__ void sigmoid(pair x, pair& s, pair& rest)
 {
     float lo, hi;
