@@ -368,8 +368,8 @@ int hpsgd_distill_loss_backward(const hpsgd_distill_loss_args* args, void* strea
  *              At least one of z8, z.
  *   gu         [M x 2 N] bf16, receives g | u rounded, for the backward pass, or NULL
  *   ld*        as in hpsgd_quantize_fp8; ldz, ldgu: elements from row to row, 0 = N and 2 N
- * K >= 1.  With M = 1 (one token) it streams the weights.  Products are exact and added in binary32 in an order that depends on the sizes alone; values held as the NaN
- * code make the results they enter NaN.  The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).
+ * K >= 1.  With M = 1 (one token) it streams the weights.  Products are exact and added in binary32 on the tensor cores in an order that depends on the sizes alone
+ * (a sum is off by about 2^-24 of the sum of its products' magnitudes); values held as the NaN code make the results they enter NaN.  The kernel waits for its own copies and products only, for two seconds at most (see hpsgd_ops_check).
  */
 enum { HPSGD_SILU = 0, HPSGD_GELU = 1 };
 typedef struct hpsgd_gated_ffn_forward_args {

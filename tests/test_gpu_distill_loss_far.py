@@ -134,6 +134,26 @@ def test_logits_that_are_large_all_over(scale, T):
         c.check()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_in_place_is_the_same_and_from_a_graph(dtype):
+    for T, vocab in ((1.0, 40000), (2.5, 700), (2.0, 131075)):
+        c = masked(vocab, LOWEST[BF], T, dtype, seed=8)
+        hp.hpsgd_distill_loss(c.args())
+        want, loss, z = c.dz.clone(), c.loss.clone(), c.z.clone()
+        hp.hpsgd_distill_loss(c.args(dlogits=c.z))
+        torch.cuda.synchronize()
+        assert torch.equal(c.z, want) and torch.equal(c.loss, loss)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            hp.hpsgd_distill_loss(c.args())
+        c.z.copy_(z)
+        c.dz.zero_()
+        c.loss.fill_(ordinary.MARK)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.dz, want) and torch.equal(c.loss, loss)
+
+
 def test_in_place_later_is_the_same():
     """The gradient alone, over the logits, where it starts from the logits and not from lse: several blocks would share such a row."""
     for T in (1.0, 2.5):

@@ -1,4 +1,5 @@
 """hpsgd_ops_check where waits ran out in more than one operator and on more than one stream: all of it is reported, and once."""
+import gc
 import time
 
 import pytest
@@ -10,6 +11,14 @@ from tests.test_gpu_gemm import Operand
 from tests.test_gpu_ops_checked import checked_library  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def nothing_left():
+    """A caught time-out holds its frames, and they the operands: both are let go here, not whenever the collector comes by, so that they do not cut up the device
+    memory that later tests get."""
+    yield
+    gc.collect()
 
 
 class Product:
